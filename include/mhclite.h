@@ -65,7 +65,8 @@ typedef enum mhclite_status {
     MHCLITE_ERR_BAD_ARG = -1,      /* n not in [2,5], C % 8 != 0, T < 0, null / misaligned pointer, ... */
     MHCLITE_ERR_CUDA = -2,         /* a CUDA runtime call or launch failed; see mhclite_last_error */
     MHCLITE_ERR_WORKSPACE = -3,    /* workspace missing or smaller than mhclite_workspace_bytes */
-    MHCLITE_ERR_TIMEOUT = -4       /* a bounded device-side wait gave up (status word, never a trap) */
+    MHCLITE_ERR_TIMEOUT = -4,      /* a bounded device-side wait gave up (status word, never a trap) */
+    MHCLITE_ERR_INDEX = -5         /* a token index outside the table was met (status words, see mhclite_set_status_words) */
 } mhclite_status;
 
 /* ---- context -------------------------------------------------------------------------------- */
@@ -303,6 +304,88 @@ MHCLITE_API int mhclite_depth_product(mhclite_ctx* ctx, int64_t T, const float* 
 /* Relative range of paper Eq. (3), per token: nu[t] = (smallest positive entry) / (largest entry) of the
  * n x n matrix X[t] (0 when no entry is positive); 1/nu bounds the Sinkhorn-Knopp iteration count. */
 MHCLITE_API int mhclite_relative_range(mhclite_ctx* ctx, int64_t T, const float* X, float* nu, void* stream);
+
+/* ---- around the stack: lookup, block norms, dropout, loss -------------------------------------------
+ *
+ * What a model adds to a stack of mixing layers: the token rows that fill x_0, the norms that enclose a sublayer f, and
+ * the loss of the last hidden rows.  (Paper Section 4 trains such models; it takes these parts as given.)
+ *   - C and n are the context's, C at most 16384 for the block calls.
+ *   - Calls that need scratch take it as an argument (device, 256-byte aligned, at least the stated bytes, no contents
+ *     to keep between calls), not from the attached workspace: calls with scratch of their own may overlap on the GPU, and
+ *     each captured graph keeps its own.
+ *   - Token ids and targets are int64 (8-byte aligned); other pointers 16-byte aligned.
+ *   - T == 0 launches no kernel, but parameter gradients that are not accumulated are then set to zero.
+ *   - Results are the same bit for bit from run to run. */
+
+/* Attaches 8 device ints (caller-owned, cleared by this call, synchronous; NULL detaches) in which the calls below record
+ * the first token index outside its table, or a wait that gave up; mhclite_device_status reports it. */
+MHCLITE_API int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words);
+typedef enum mhclite_op {          /* the operator named in such a report */
+    MHCLITE_OP_EMBED = 20,
+    MHCLITE_OP_EMBED_BWD = 21,
+    MHCLITE_OP_LINEAR_CE = 22
+} mhclite_op;
+
+/* x0[t,j,:] = bf16(scale * E[ids[t],:]) for each of the n streams j.  E [V,C], fp32 when table_f32 != 0, else bf16;
+ * x0 [T,n,C] bf16.  A token whose id is outside [0, V) gets zero rows and is reported (MHCLITE_ERR_INDEX). */
+MHCLITE_API int mhclite_embed_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, const int64_t* ids, const void* E, int table_f32,
+                        float scale, mhclite_bf16* x0, void* stream);
+/* Gradient of embed_fwd from g = dL/dx0 [T,n,C] bf16:
+ *   dE[v,:] (+)= scale * sum over {t: ids[t] = v} and the streams of g[t,j,:]      [V,C] f32
+ * added to dE when accumulate != 0 (rows of other tokens stay untouched), else stored (their rows are zeroed).
+ * Tokens outside [0, V) are left out and reported. */
+MHCLITE_API size_t mhclite_embed_scratch_bytes(int C, int64_t T, int64_t V);
+MHCLITE_API int mhclite_embed_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const int64_t* ids, const mhclite_bf16* g, float scale,
+                        float* dE, int accumulate, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The norm that opens a sublayer: v[t,c] = u[t,c] rstd[t] w[c], rstd[t] = (mean_c u[t,c]^2 + eps)^-1/2.
+ * u, v [T,C] bf16; w [C], rstd [T] f32 (saved for the backward). */
+MHCLITE_API int mhclite_block_in_fwd(mhclite_ctx* ctx, int64_t T, const mhclite_bf16* u, const float* w, float eps,
+                        mhclite_bf16* v, float* rstd, void* stream);
+/* du [T,C] bf16 and dw [C] f32 (added when accumulate_params != 0) from dv [T,C] bf16. */
+MHCLITE_API size_t mhclite_block_scratch_bytes(int C, int64_t T);
+MHCLITE_API int mhclite_block_in_bwd(mhclite_ctx* ctx, int64_t T, const mhclite_bf16* u, const float* w, const float* rstd,
+                        const mhclite_bf16* dv, mhclite_bf16* du, float* dw, int accumulate_params,
+                        void* scratch, size_t scratch_bytes, void* stream);
+
+/* What closes a sublayer, its output o [T,C] bf16 normalised, gated, dropped out and scaled before the merge:
+ *   y[t,c] = s drop(sigmoid(gate[t,c]) o[t,c] rstd[t] w[c])
+ * gate [T,C] bf16 or NULL (no gate), s = *scale (f32, device) or 1 for NULL, drop as in mhclite_dropout with the element
+ * index t C + c (p_drop = 0: none, rng may be NULL).  rstd as in block_in_fwd. */
+MHCLITE_API int mhclite_block_out_fwd(mhclite_ctx* ctx, int64_t T, const mhclite_bf16* o, const mhclite_bf16* gate, const float* w,
+                        const float* scale, float eps, float p_drop, const uint64_t* rng, mhclite_bf16* y, float* rstd,
+                        void* stream);
+/* Its gradient from dy [T,C] bf16: d_o, dgate [T,C] bf16 (dgate is given if and only if gate is), dw [C], dscale [1] f32
+ * (dscale may be NULL; both added when accumulate_params != 0).  rng must hold the values of the forward call. */
+MHCLITE_API int mhclite_block_out_bwd(mhclite_ctx* ctx, int64_t T, const mhclite_bf16* o, const mhclite_bf16* gate, const float* w,
+                        const float* scale, const float* rstd, float p_drop, const uint64_t* rng, const mhclite_bf16* dy,
+                        mhclite_bf16* d_o, mhclite_bf16* dgate, float* dw, float* dscale, int accumulate_params,
+                        void* scratch, size_t scratch_bytes, void* stream);
+
+/* y[i] = x[i] / (1 - p) where element i stays, 0 where it is dropped, for any count of bf16 elements; the same call on dy
+ * is the gradient.  The mask is not stored: element i stays when its 16 bits of Philox4x32-10 (key: the seed; counter: the
+ * 64-bit group i / 8, then the 64-bit offset; half-word i % 8 of the four output words, low halves first) are at least
+ * round(65536 p), and p counts as rounded to that multiple of 2^-16.  0 <= p < 1 - 2^-17.
+ *   rng [2] device: (seed, offset), read when the kernel runs, so that a captured graph draws new masks when the caller
+ *   changes the offset between replays.  Dropped elements are 0 whatever x holds. */
+MHCLITE_API int mhclite_dropout(mhclite_ctx* ctx, int64_t count, const mhclite_bf16* x, float p, const uint64_t* rng,
+                        mhclite_bf16* y, void* stream);
+
+/* Softmax cross entropy of the logits l[t,v] = logit_scale <h[t,:], W[v,:]>, which are never stored:
+ *   lse[t] = log sum_v exp l[t,v],   loss[t] = lse[t] - l[t,target[t]]        [T] f32
+ * h [T,C], W [V,C] bf16.  Rows with a negative target have none: loss and lse are 0, h is not used.  A target of V or
+ * more counts as none and is reported.  T V < 2^46. */
+MHCLITE_API size_t mhclite_linear_ce_scratch_bytes(int C, int64_t T, int64_t V, int backward);
+MHCLITE_API int mhclite_linear_ce_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, const mhclite_bf16* h, const mhclite_bf16* W,
+                        const int64_t* target, float logit_scale, float* loss, float* lse,
+                        void* scratch, size_t scratch_bytes, void* stream);
+/* Gradient from dloss [T] f32 (dL/dloss; the reduction over tokens is the caller's) and the forward's lse:
+ *   dh[t,:] = dloss[t] logit_scale (sum_v softmax(l)[t,v] W[v,:] - W[target[t],:])    [T,C] bf16, 0 without a target
+ *   dW[v,:] = sum_t dloss[t] logit_scale (softmax(l)[t,v] - [v = target[t]]) h[t,:]   [V,C] bf16 (overwritten)
+ * The bracket enters the products rounded to bf16; sums are fp32. */
+MHCLITE_API int mhclite_linear_ce_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const mhclite_bf16* h, const mhclite_bf16* W,
+                        const int64_t* target, float logit_scale, const float* lse, const float* dloss,
+                        mhclite_bf16* dh, mhclite_bf16* dW, void* scratch, size_t scratch_bytes, void* stream);
 
 /* ---- whole step from host buffers -------------------------------------------------------------- */
 

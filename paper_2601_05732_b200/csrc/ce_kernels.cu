@@ -1,0 +1,473 @@
+// Softmax cross entropy of h W^T over a large vocabulary, without the logits in memory:
+//   l[t,v] = scale <h_t, W_v>,  lse_t = log sum_v exp l[t,v],  loss_t = lse_t - l[t,target_t],
+//   G[t,v] = scale dloss_t (exp(l[t,v] - lse_t) - [v = target_t]),  dh = G W,  dW = G^T h.
+//
+// Forward: one tcgen05 matrix product whose epilogue reduces each 128 x 256 tile of logits, still in tensor memory, to a
+// (maximum, sum) pair a row; ce_join_k joins a row's pairs.  Backward: the vocabulary in pieces.  A piece's logits are
+// computed again (2 T V C operations more, against T V values written and read back, and in fp32, where logits stored in
+// 16 bits would move exp(l - lse) by percents), turned into G in bf16, and G enters the two products.  A piece holds all
+// tokens, so its rows of dW are complete at once; dh adds up over the pieces in fp32.
+//
+// Rows without a target (padding, prompts) are left out before the products: ce_rows_k lists the others and copies their
+// h side by side, so such rows cost nothing, and what they hold (NaN included) reaches neither loss nor gradients.
+//
+// Tiles: 128 x 256 a CTA, K in steps of 64 (one 128-byte swizzle row of bf16) through a ring of TMA stages, accumulators
+// double buffered in tensor memory so that the epilogue of one tile overlaps the products of the next.
+#include "common.cuh"
+#include "kernels.h"
+#include "mma.cuh"
+#include "tc.cuh"
+
+namespace mhcl {
+
+constexpr int kCeM = 128, kCeN = 256, kCeK = 64;
+constexpr int kCeStages = 4;
+constexpr int kCeABytes = kCeM * kCeK * 2, kCeBBytes = kCeN * kCeK * 2, kCeStage = kCeABytes + kCeBBytes;
+constexpr int kCeThreads = 192;                       // warp 0: TMA, warp 1: MMA, warps 2..5: epilogue
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+enum CeMode { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
+
+struct CeArgs {
+    const int* live;            // number of rows with a target
+    const int* rows;            // [live] their token indices
+    int64_t T, V;
+    int C;
+    int v0, vn;                 // the piece: rows v0 .. v0 + vn of W (vn a multiple of 256 except for the last piece)
+    int m_tiles, n_tiles;       // at most; m_tiles of the row-wise modes is cut to `live` on the device
+    float scale;
+    // CE_STATS
+    float2* part;               // [n_tiles][Tpad] (maximum, sum) in base 2
+    float* tlogit;              // [Tpad] the target's logit
+    const int64_t* target;
+    int Tpad;
+    // CE_GRAD
+    const float* lse;
+    const float* dloss;
+    __nv_bfloat16* G;           // [Tpad][pitch]
+    int64_t pitch;
+    // CE_DH
+    float* dh_acc;              // [Tpad][C] sums over the pieces so far
+    __nv_bfloat16* dh;          // [T][C]
+    int first, last;
+    // CE_DW
+    __nv_bfloat16* dW;          // [V][C]
+    int* status;
+};
+
+struct CeCtl {
+    uint64_t full[kCeStages], empty[kCeStages], acc_full[2], acc_empty[2];
+    uint32_t tmem_base;
+    int abort[3];
+};
+
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// Tile order: groups of 16 row tiles, column tiles inside a group, so that the CTAs of a wave share operands in L2.
+__device__ __forceinline__ void ce_tile(int i, int mt, int nt, int& m, int& n) {
+    constexpr int kGroup = 16;
+    const int per = kGroup * nt, g = i / per, r = i - g * per, gm = min(kGroup, mt - g * kGroup);
+    n = r / gm;
+    m = g * kGroup + (r - n * gm);
+}
+
+template <int MODE>
+__global__ void __launch_bounds__(kCeThreads, 1)
+ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb, const CeArgs a) {
+    constexpr bool A_MN = MODE == CE_DW, B_MN = MODE == CE_DH || MODE == CE_DW;
+    extern __shared__ __align__(1024) unsigned char smem_raw[];
+    unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    CeCtl* ctl = reinterpret_cast<CeCtl*>(smem + kCeStages * kCeStage);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    volatile int* abort = ctl->abort;
+    const int live = *a.live;
+    const int mt = MODE == CE_DW ? a.m_tiles : (live + kCeM - 1) / kCeM, nt = a.n_tiles, tiles = mt * nt;
+    const int ksize = MODE == CE_DW ? live : MODE == CE_DH ? a.vn : a.C;
+    const int ksteps = (ksize + kCeK - 1) / kCeK;
+
+    if (tid == 0) {
+        for (int s = 0; s < kCeStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->acc_full[s]), 1); mbar_init(smem_u32(&ctl->acc_empty[s]), 4); }
+        abort[0] = abort[1] = abort[2] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = ctl->tmem_base;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int it = 0;
+            bool ok = true;
+            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+                int m, n;
+                ce_tile(i, mt, nt, m, n);
+                for (int k = 0; k < ksteps; ++k, ++it) {
+                    const int s = it % kCeStages;
+                    ok = mbar_wait(smem_u32(&ctl->empty[s]), ((it / kCeStages) & 1) ^ 1, abort, 1, it);
+                    if (!ok) break;
+                    const uint32_t full = smem_u32(&ctl->full[s]), sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
+                    mbar_expect_tx(full, kCeStage);
+                    if (A_MN) {
+                        for (int b = 0; b < kCeM / 64; ++b) tma_load_2d(sa + b * 8192, &tma, full, m * kCeM + b * 64, k * kCeK);
+                    } else {
+                        tma_load_2d(sa, &tma, full, k * kCeK, m * kCeM);
+                    }
+                    if (B_MN) {
+                        for (int b = 0; b < kCeN / 64; ++b)
+                            tma_load_2d(sb + b * 8192, &tmb, full, n * kCeN + b * 64, (MODE == CE_DH ? a.v0 : 0) + k * kCeK);
+                    } else {
+                        tma_load_2d(sb, &tmb, full, k * kCeK, a.v0 + n * kCeN);
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc_mn(kCeM, kCeN, A_MN, B_MN);
+            int it = 0, j = 0;
+            bool ok = true;
+            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x, ++j) {
+                const int buf = j & 1;
+                ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((j >> 1) & 1) ^ 1, abort, 2, j);
+                if (!ok) break;
+                tc_fence_after();
+                for (int k = 0; k < ksteps; ++k, ++it) {
+                    const int s = it % kCeStages;
+                    ok = mbar_wait(smem_u32(&ctl->full[s]), (it / kCeStages) & 1, abort, 3, it);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
+#pragma unroll
+                    for (int kk = 0; kk < kCeK / 16; ++kk) {
+                        const uint64_t ad = A_MN ? smem_desc(sa + kk * 2048, 8192, 1024, 2) : smem_desc(sa + kk * 32, 16, 1024, 2);
+                        const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, 8192, 1024, 2) : smem_desc(sb + kk * 32, 16, 1024, 2);
+                        tc_mma(tmem + buf * kCeN, ad, bd, idesc, (k > 0 || kk > 0) ? 1u : 0u);
+                    }
+                    tc_commit(smem_u32(&ctl->empty[s]));
+                }
+                if (ok) tc_commit(smem_u32(&ctl->acc_full[buf]));
+            }
+        }
+    } else {
+        const int quad = warp & 3, row = quad * 32 + lane;
+        bool ok = true;
+        int j = 0;
+        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x, ++j) {
+            const int buf = j & 1;
+            ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            int m, n;
+            ce_tile(i, mt, nt, m, n);
+            const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
+            const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN;
+            if (MODE == CE_STATS || MODE == CE_GRAD) {
+                const bool in = r < live;
+                const int t = in ? a.rows[r] : 0;
+                const int tgt = in ? (int)(a.target[t] - a.v0) - n * kCeN : -1;      // the target's column in this tile
+                const int cols = min(kCeN, (int)(a.V - a.v0) - n * kCeN);            // of the vocabulary (the rest is padding)
+                const float k2 = a.scale * kLog2e;
+                if (MODE == CE_STATS) {
+                    float mx = -INFINITY, sum = 0.f;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                        float v[32];
+                        tc_ld32(acc + c0, v);
+                        if (c0 >= cols) break;
+                        if (__any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (tgt == c0 + e) a.tlogit[r] = v[e] * a.scale;
+                        }
+                        float top = mx;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            v[e] = c0 + e < cols ? v[e] * k2 : -INFINITY;
+                            top = fmaxf(top, v[e]);
+                        }
+                        const float base = top == -INFINITY ? 0.f : top;
+                        sum *= ex2(mx - base);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) sum += ex2(v[e] - base);
+                        mx = top;
+                    }
+                    if (in) a.part[(int64_t)n * a.Tpad + r] = make_float2(mx, sum);
+                } else {
+                    const float lse2 = in ? a.lse[t] * kLog2e : 0.f, f = in ? a.dloss[t] * a.scale : 0.f;
+                    __nv_bfloat16* out = a.G + (int64_t)r * a.pitch + n * kCeN;
+#pragma unroll 1
+                    for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                        float v[32];
+                        tc_ld32(acc + c0, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            v[e] = ex2(fmaf(v[e], k2, -lse2));
+                            if (tgt == c0 + e) v[e] -= 1.f;
+                            v[e] = (in && c0 + e < cols) ? v[e] * f : 0.f;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4*>(out + c0 + e) = pack8(v + e);
+                    }
+                }
+            } else {
+                const bool in = MODE == CE_DH ? r < live : r < a.vn;
+                const int64_t orow = MODE == CE_DH ? (in ? a.rows[r] : 0) : a.v0 + r;
+#pragma unroll 1
+                for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                    float v[32];
+                    tc_ld32(acc + c0, v);
+                    const int c = n * kCeN + c0;
+                    if (!in) continue;
+                    if (MODE == CE_DW && ksteps == 0) {                 // no row has a target: nothing was accumulated
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        if (c + e >= a.C) continue;
+                        if (MODE == CE_DH) {
+                            float4* p = (float4*)(a.dh_acc + (int64_t)r * a.C + c + e);
+                            if (!a.first) {
+                                const float4 x = p[0], y = p[1];
+                                v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
+                                v[e + 4] += y.x; v[e + 5] += y.y; v[e + 6] += y.z; v[e + 7] += y.w;
+                            }
+                            if (a.last) {
+                                *reinterpret_cast<uint4*>(a.dh + orow * a.C + c + e) = pack8(v + e);
+                            } else {
+                                p[0] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                                p[1] = make_float4(v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
+                            }
+                        } else {
+                            *reinterpret_cast<uint4*>(a.dW + orow * a.C + c + e) = pack8(v + e);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[buf]));
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (ctl->abort[0]) {
+        for (int i = 0; i < 64; ++i) __nanosleep(2000);        // copies in flight land before the memory is given up
+        if (tid == 0 && a.status && atomicCAS(a.status, 0, MHCLITE_ERR_TIMEOUT) == 0) {
+            a.status[1] = MHCLITE_OP_LINEAR_CE + 100 * MODE; a.status[2] = ctl->abort[1]; a.status[3] = blockIdx.x;
+            a.status[4] = ctl->abort[2];
+        }
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// ---- rows with a target ----------------------------------------------------------------------------------------------
+// Block b handles `per` tokens: counts the targets before them, numbers its own rows, copies their h side by side, and
+// clears the outputs of the rows without a target (loss and lse, or dh).  The last block pads the list's h with zero rows
+// to the next multiple of 128, which the products read.
+__global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* __restrict__ target,
+                                                  const uint4* __restrict__ h, uint4* __restrict__ hl, int* __restrict__ rows,
+                                                  int* __restrict__ live, float* __restrict__ loss, float* __restrict__ lse,
+                                                  uint4* __restrict__ dh, int* __restrict__ status) {
+    __shared__ int wcnt[32], base_s;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = C >> 3;
+    const int64_t t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
+    int mine = 0;
+    for (int64_t t = tid; t < t0; t += 1024) { const int64_t y = target[t]; mine += y >= 0 && y < V; }
+    mine = __reduce_add_sync(0xffffffffu, mine);
+    if (lane == 0) wcnt[warp] = mine;
+    __syncthreads();
+    if (warp == 0) {
+        const int v = __reduce_add_sync(0xffffffffu, wcnt[lane]);
+        if (lane == 0) base_s = v;
+    }
+    __syncthreads();
+    int base = base_s;
+    for (int64_t b = t0; b < t1; b += 32) {                     // every warp numbers all of the block's rows: no exchange
+        const int64_t t = b + lane;
+        const int64_t y = t < t1 ? target[t] : -1;
+        const bool ok = y >= 0 && y < V;
+        const uint32_t m = __ballot_sync(0xffffffffu, ok);
+        if (warp == 0 && t < t1) {
+            if (ok) rows[base + __popc(m & ((1u << lane) - 1u))] = (int)t;
+            else {
+                if (loss) { loss[t] = 0.f; lse[t] = 0.f; }
+                if (y >= V && status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
+                    status[1] = MHCLITE_OP_LINEAR_CE; status[2] = (int)y; status[3] = (int)(t >> 31); status[4] = (int)(t & 0x7FFFFFFF);
+                }
+            }
+        }
+        for (int i = warp; i < 32 && b + i < t1; i += 32) {     // a warp a row
+            if (m >> i & 1u) {
+                uint4* to = hl + (int64_t)(base + __popc(m & ((1u << i) - 1u))) * nv;
+                const uint4* from = h + (b + i) * nv;
+                for (int v = lane; v < nv; v += 32) to[v] = ld_stream(from + v);
+            } else if (dh) {
+                for (int v = lane; v < nv; v += 32) dh[(b + i) * nv + v] = make_uint4(0, 0, 0, 0);
+            }
+        }
+        base += __popc(m);
+    }
+    if (t1 == T) {
+        if (tid == 0) *live = base;
+        const int pad = min(Tpad, (base + 127) / 128 * 128);
+        for (int64_t i = tid; i < (int64_t)(pad - base) * nv; i += 1024) hl[(int64_t)base * nv + i] = make_uint4(0, 0, 0, 0);
+    }
+}
+
+// Joins the (maximum, sum) pairs of a row: 32 rows a block, eight ranges of tiles side by side.
+__global__ void __launch_bounds__(256) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_tiles, int Tpad,
+                                                 const float2* __restrict__ part, const float* __restrict__ tlogit,
+                                                 float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ float2 red[8][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = *live;
+    float m = -INFINITY, s = 0.f;
+    if (r < n) {
+        const int per = (n_tiles + 7) / 8, n1 = min(n_tiles, (warp + 1) * per);
+#pragma unroll 4
+        for (int k = warp * per; k < n1; ++k) {
+            const float2 p = part[(int64_t)k * Tpad + r];
+            const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+            s = s * ex2(m - base) + p.y * ex2(p.x - base);
+            m = top;
+        }
+    }
+    red[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp != 0 || r >= n) return;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) top = fmaxf(top, red[w][lane].x);
+    const float base = top == -INFINITY ? 0.f : top;
+    s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
+    const float l = (top + lg2(s)) * kLn2;
+    const int t = rows[r];
+    lse[t] = l;
+    loss[t] = l - tlogit[r];
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------
+// Pieces of the vocabulary in the backward: G of a piece takes at most about 256 MB.
+struct CePlan {
+    int Tpad, n_tiles;
+    int pieces; int64_t piece;             // vocabulary rows a piece, a multiple of 256
+    int *live, *rows;
+    __nv_bfloat16* hl;
+    float2* part; float* tlogit;
+    __nv_bfloat16* G; float* dh_acc;
+    size_t bytes;
+};
+static CePlan plan_ce(int64_t T, int64_t V, int C, int grad, void* base) {
+    CePlan p;
+    char* b = (char*)base;
+    size_t off = 0;
+    auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
+    p.Tpad = (int)round_up64(T > 0 ? T : 1, 128);
+    p.n_tiles = (int)((V + kCeN - 1) / kCeN);
+    p.live = (int*)take(256);
+    p.rows = (int*)take((size_t)p.Tpad * 4);
+    p.hl = (__nv_bfloat16*)take((size_t)p.Tpad * C * 2);
+    p.part = nullptr; p.tlogit = nullptr; p.G = nullptr; p.dh_acc = nullptr;
+    p.pieces = 1; p.piece = 0;
+    if (!grad) {
+        p.part = (float2*)take((size_t)p.n_tiles * p.Tpad * 8);
+        p.tlogit = (float*)take((size_t)p.Tpad * 4);
+    } else {
+        int64_t most = ((int64_t)128 << 20) / p.Tpad / 256 * 256;
+        if (most < 256) most = 256;
+        p.pieces = (int)((V + most - 1) / most);
+        p.piece = round_up64((V + p.pieces - 1) / p.pieces, 256);
+        p.pieces = (int)((V + p.piece - 1) / p.piece);
+        p.G = (__nv_bfloat16*)take((size_t)p.Tpad * p.piece * 2);
+        p.dh_acc = (float*)take(p.pieces > 1 ? (size_t)p.Tpad * C * 4 : 0);
+    }
+    p.bytes = off;
+    return p;
+}
+size_t ce_scratch_bytes(int64_t T, int64_t V, int C, int grad) { return plan_ce(T, V, C, grad, nullptr).bytes; }
+
+static void launch_ce_rows(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const int64_t* target, const void* h,
+                           float* loss, float* lse, void* dh, cudaStream_t s) {
+    int64_t per = 32;
+    while ((T + per - 1) / per > 296) per += 32;
+    c->launches += 1;
+    ce_rows_k<<<(unsigned)((T + per - 1) / per), 1024, 0, s>>>(T, V, c->C, per, p.Tpad, target, (const uint4*)h, (uint4*)p.hl, p.rows,
+                                                               p.live, loss, lse, (uint4*)dh, c->op_status);
+}
+
+template <int MODE>
+static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const CeArgs& a, cudaStream_t s) {
+    constexpr int smem = kCeStages * kCeStage + (int)sizeof(CeCtl) + 1024;
+    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+    cudaFuncSetAttribute(ce_gemm_k<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    c->launches += 1;
+    ce_gemm_k<MODE><<<(unsigned)(tiles < c->sm_count ? tiles : c->sm_count), kCeThreads, smem, s>>>(ma, mb, a);
+}
+
+// Tensor maps: a K-major operand is copied in boxes of 64 k x `rows` rows, an MN-major one in boxes of 64 x 64 k.
+static bool map_k(CUtensorMap* m, const void* p, int64_t rows, int64_t k, int64_t pitch, int box_rows) {
+    return make_tensor_map_2d(m, p, (uint64_t)k, (uint64_t)rows, (uint64_t)pitch, kCeK, (uint32_t)box_rows, 128);
+}
+static bool map_mn(CUtensorMap* m, const void* p, int64_t k, int64_t mn, int64_t pitch) {
+    return make_tensor_map_2d(m, p, (uint64_t)mn, (uint64_t)k, (uint64_t)pitch, 64, kCeK, 128);
+}
+
+bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
+                          float* loss, float* lse, void* scratch, cudaStream_t s) {
+    const CePlan p = plan_ce(T, V, c->C, 0, scratch);
+    CUtensorMap mh, mw;
+    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, kCeM) || !map_k(&mw, W, V, c->C, c->C, kCeN)) return false;
+    launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, s);
+    CeArgs a = {};
+    a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
+    a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
+    a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
+    launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
+    c->launches += 1;
+    ce_join_k<<<(unsigned)(p.Tpad / 32), 256, 0, s>>>(p.live, p.rows, p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
+    return true;
+}
+
+bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
+                          const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s) {
+    const CePlan p = plan_ce(T, V, c->C, 1, scratch);
+    const int C = c->C;
+    CUtensorMap mh, mw, mg, mwn, mgt, mhn;
+    if (!map_k(&mh, p.hl, p.Tpad, C, C, kCeM) || !map_k(&mw, W, V, C, C, kCeN) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, kCeM) ||
+        !map_mn(&mwn, W, V, C, C) || !map_mn(&mgt, p.G, p.Tpad, p.piece, p.piece) || !map_mn(&mhn, p.hl, p.Tpad, C, C))
+        return false;
+    launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, s);
+    CeArgs a = {};
+    a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
+    a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
+    a.dW = (__nv_bfloat16*)dW; a.status = c->op_status;
+    for (int i = 0; i < p.pieces; ++i) {
+        a.v0 = (int)(i * p.piece);
+        a.vn = (int)(V - a.v0 < p.piece ? V - a.v0 : p.piece);
+        a.first = i == 0; a.last = i + 1 == p.pieces;
+        a.m_tiles = p.Tpad / kCeM; a.n_tiles = (a.vn + kCeN - 1) / kCeN;
+        launch_ce_gemm<CE_GRAD>(c, mh, mw, a, s);
+        a.m_tiles = (a.vn + kCeM - 1) / kCeM; a.n_tiles = (C + kCeN - 1) / kCeN;
+        launch_ce_gemm<CE_DW>(c, mgt, mhn, a, s);
+        a.m_tiles = p.Tpad / kCeM;
+        launch_ce_gemm<CE_DH>(c, mg, mwn, a, s);
+    }
+    return true;
+}
+
+}  // namespace mhcl

@@ -28,6 +28,7 @@ struct mhclite_ctx {
     size_t ws_bytes;
     mutable int64_t launches;     // kernels launched through this context
     int* status_word;             // device status word inside the attached workspace (null until first used)
+    int* op_status;               // caller-owned status words of the calls that take their own scratch (null: no report)
     bool timing;                  // record CUDA events around the main kernels (mhclite_set_kernel_timing)
     cudaEvent_t ev[MHCLITE_KERNEL_COUNT][2];
     mutable bool ev_recorded[MHCLITE_KERNEL_COUNT];   // the pair has bracketed at least one launch

@@ -1,0 +1,351 @@
+// The lookup that fills the residual streams and its gradient:
+//   x0[t,j,:] = bf16(scale E[id_t,:])  for every stream j,
+//   dE[v,:] (+)= scale sum_{t: id_t = v} sum_j g[t,j,:].
+//
+// The forward is bound by the n rows it writes a token.  The gradient is bound by the n rows it reads a token and the
+// table it writes; its sums must not depend on the order in which blocks run, so the tokens are sorted first
+// (embed_sort_k, stable: tokens of one id stay in ascending order), then embed_grad_k walks the sorted list in chunks,
+// one warp a chunk and 256 channels, and keeps the running sum of the current id in fp32 registers.  An id whose tokens
+// span several chunks leaves one partial row a chunk, which embed_join_k adds up in order: a token as frequent as the
+// commonest word does not serialise.  Rows that no token meets are zeroed by further blocks of embed_grad_k, from a bit
+// mask that the sort leaves, so each row of dE is written once.
+#include "common.cuh"
+#include "kernels.h"
+
+namespace mhcl {
+
+__device__ __forceinline__ void report_index(int* status, int kernel, int64_t where, int64_t value) {
+    if (status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
+        status[1] = kernel;
+        status[2] = (int)value;
+        status[3] = (int)(where >> 31);
+        status[4] = (int)(where & 0x7FFFFFFF);
+    }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, int n, int tpt, const int64_t* __restrict__ ids,
+                                                   const void* __restrict__ E, float scale, uint4* __restrict__ x0,
+                                                   int* __restrict__ status) {
+    const int nv = C >> 3, per = 256 / tpt, lt = threadIdx.x % tpt;
+    const int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / tpt;
+    if (t >= T) return;
+    const int64_t id = ids[t];
+    const bool ok = id >= 0 && id < V;
+    if (!ok && lt == 0) report_index(status, MHCLITE_OP_EMBED, t, id);
+    uint4* row = x0 + t * n * nv;
+    for (int v = lt; v < nv; v += tpt) {
+        float f[8];
+        if (!ok) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = 0.f;
+        } else if (F32) {
+            const float4* p = (const float4*)E + (id * nv + v) * 2;
+            const float4 a = __ldg(p), b = __ldg(p + 1);
+            f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+        } else {
+            unpack8(__ldg((const uint4*)E + id * nv + v), f);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= scale;
+        if (!ok)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = 0.f;
+        const uint4 o = pack8(f);
+        for (int j = 0; j < n; ++j) st_stream(row + j * nv + v, o);
+    }
+}
+
+// ---- stable sort of the tokens by id ---------------------------------------------------------------------------------
+// One cluster sorts (least significant digit first, 8 bits a pass): a warp owns a contiguous range of the list and counts
+// its digits without atomics, the blocks exchange their 256 totals through distributed shared memory, and each warp then
+// walks its range again and places the tokens.  A launch a pass would cost more than the pass.
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t ld_peer(const uint32_t* p, uint32_t rank) {   // 32 bits of another block's shared memory
+    uint32_t a = (uint32_t)__cvta_generic_to_shared(p), b, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(a), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(b) : "memory");
+    return v;
+}
+
+__global__ void __launch_bounds__(kSortThreads) embed_sort_k(int64_t T, int64_t V, int passes, const int64_t* __restrict__ ids,
+                                                             uint2* buf0, uint2* buf1, uint32_t* mask, int* __restrict__ status) {
+    __shared__ uint32_t cnt[kSortWarps][256];
+    __shared__ uint32_t tot[256], off[256], wsum[8];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t me = cluster_rank(), nb = cluster_size();
+    const int64_t per = ((T + (int64_t)nb * kSortWarps - 1) / ((int64_t)nb * kSortWarps) + 31) / 32 * 32;
+    const int64_t i0 = ((int64_t)me * kSortWarps + warp) * per, i1 = i0 + per < T ? i0 + per : T;
+    for (int64_t w = (int64_t)me * kSortThreads + tid; w < (V + 31) / 32; w += (int64_t)nb * kSortThreads) mask[w] = 0;
+    uint2 *src = buf0, *dst = buf1;
+    for (int p = 0; p < passes; ++p) {
+        for (int i = tid; i < kSortWarps * 256; i += kSortThreads) cnt[0][i] = 0;
+        __syncthreads();
+        for (int64_t b = i0; b < i1; b += 32) {
+            const bool in = b + lane < i1;
+            uint32_t key = 0;
+            if (in) {
+                if (p == 0) {
+                    const int64_t id = ids[b + lane];
+                    const bool ok = id >= 0 && id < V;
+                    if (!ok) report_index(status, MHCLITE_OP_EMBED_BWD, b + lane, id);
+                    key = ok ? (uint32_t)id : (uint32_t)V;     // tokens without a row go last
+                    src[b + lane] = make_uint2(key, (uint32_t)(b + lane));
+                } else {
+                    key = __ldcg(src + b + lane).x;
+                }
+            }
+            const uint32_t live = __ballot_sync(0xffffffffu, in);
+            if (in) {
+                const uint32_t d = (key >> (8 * p)) & 255u, peers = __match_any_sync(live, d);
+                if (lane == __ffs(peers) - 1) cnt[warp][d] += __popc(peers);
+            }
+            __syncwarp();
+        }
+        __syncthreads();
+        if (tid < 256) {                                       // the warps' counts become offsets within the block
+            uint32_t run = 0;
+            for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = cnt[w][tid]; cnt[w][tid] = run; run += c; }
+            tot[tid] = run;
+        }
+        cluster_sync_all();
+        uint32_t before = 0, all = 0;
+        if (tid < 256) {
+            for (uint32_t r = 0; r < nb; ++r) { const uint32_t c = ld_peer(&tot[tid], r); if (r < me) before += c; all += c; }
+            uint32_t inc = all;                                // inclusive scan over the digits
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
+            if (lane == 31) wsum[warp] = inc;
+            off[tid] = inc - all + before;
+        }
+        __syncthreads();
+        if (tid < 256) {
+            uint32_t add = 0;
+            for (int w = 0; w < warp; ++w) add += wsum[w];
+            off[tid] += add;
+        }
+        __syncthreads();
+        for (int64_t b = i0; b < i1; b += 32) {
+            const bool in = b + lane < i1;
+            const uint32_t live = __ballot_sync(0xffffffffu, in);
+            if (in) {
+                const uint2 kv = __ldcg(src + b + lane);
+                const uint32_t d = (kv.x >> (8 * p)) & 255u, peers = __match_any_sync(live, d);
+                const uint32_t rank = __popc(peers & ((1u << lane) - 1u)), base = off[d] + cnt[warp][d];
+                __syncwarp(live);
+                if (rank == 0) cnt[warp][d] += __popc(peers);
+                if (p == 0) {                                  // one lane an id marks its row
+                    const uint32_t same = __match_any_sync(live, kv.x);
+                    if (kv.x < V && lane == __ffs(same) - 1) atomicOr(mask + (kv.x >> 5), 1u << (kv.x & 31));
+                }
+                __stcg(dst + base + rank, kv);
+            }
+            __syncwarp();
+        }
+        uint2* h = src; src = dst; dst = h;
+        cluster_sync_all();
+    }
+}
+
+// ---- sums over the sorted list ---------------------------------------------------------------------------------------
+// Warp (chunk, slice) adds up `R` list entries for channels [256 slice, 256 slice + 256), 8 a lane.
+template <int N_>
+__global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int C, int R, int64_t sum_blocks, int slices,
+                                                    const uint2* __restrict__ list, const uint32_t* __restrict__ mask,
+                                                    const uint4* __restrict__ g, float scale, float* __restrict__ dE,
+                                                    float* __restrict__ own, float* __restrict__ cont, int accumulate) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
+    if (blockIdx.x >= sum_blocks) {                            // rows that no token meets
+        const int64_t zb = blockIdx.x - sum_blocks, nzb = gridDim.x - sum_blocks;
+        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int64_t v = zb * 8 + warp; v < V; v += nzb * 8) {
+            if (__ldg(mask + (v >> 5)) >> (v & 31) & 1u) continue;
+            float4* row = (float4*)(dE + v * C);
+            for (int c = lane; c < C / 4; c += 32) __stcs(row + c, zero);
+        }
+        return;
+    }
+    const int64_t unit = (int64_t)blockIdx.x * 8 + warp;
+    const int64_t chunk = unit / slices;
+    const int v = (int)(unit % slices) * 32 + lane;            // this lane's 16-byte vector of a row
+    const int64_t p0 = chunk * R;
+    if (p0 >= T) return;
+    const int cnt = (int)(T - p0 < R ? T - p0 : R);
+    const uint2 mine = lane < cnt ? __ldg(list + p0 + lane) : make_uint2(0xFFFFFFFFu, 0);
+    const uint32_t prev = p0 > 0 ? __ldg(&list[p0 - 1].x) : 0xFFFFFFFFu;
+    const uint32_t next = p0 + cnt < T ? __ldg(&list[p0 + cnt].x) : 0xFFFFFFFFu;
+    const bool act = v < nv;
+    float acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+    constexpr int U = 16 / N_ > 4 ? 4 : 16 / N_;               // tokens whose rows are in flight together
+    for (int i = 0; i < cnt; i += U) {
+        uint4 d[U][N_];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            const uint32_t t = __shfl_sync(0xffffffffu, mine.y, (i + k) & 31);
+            if (act && i + k < cnt) {
+#pragma unroll
+                for (int j = 0; j < N_; ++j) d[k][j] = ld_stream(g + ((int64_t)t * N_ + j) * nv + v);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (i + k >= cnt) break;
+            const uint32_t key = __shfl_sync(0xffffffffu, mine.x, i + k);
+            const uint32_t after = i + k + 1 < cnt ? __shfl_sync(0xffffffffu, mine.x, (i + k + 1) & 31) : next;
+            if (act) {
+#pragma unroll
+                for (int j = 0; j < N_; ++j) {
+                    float f[8];
+                    unpack8(d[k][j], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] += f[e];
+                }
+            }
+            const bool last = i + k + 1 == cnt;
+            if (key != after || last) {
+                const uint32_t first_key = __shfl_sync(0xffffffffu, mine.x, 0);
+                if (act && key < V) {
+                    const bool began_before = key == first_key && prev == key;
+                    float* to = began_before ? cont + chunk * C : (last && after == key) ? own + chunk * C : nullptr;
+                    if (to) {
+                        float4* o = (float4*)(to + v * 8);
+                        o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                        o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                    } else {
+                        float4* o = (float4*)(dE + (int64_t)key * C + v * 8);
+                        float4 a = accumulate ? o[0] : make_float4(0.f, 0.f, 0.f, 0.f), b = accumulate ? o[1] : a;
+                        a.x += scale * acc[0]; a.y += scale * acc[1]; a.z += scale * acc[2]; a.w += scale * acc[3];
+                        b.x += scale * acc[4]; b.y += scale * acc[5]; b.z += scale * acc[6]; b.w += scale * acc[7];
+                        o[0] = a; o[1] = b;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+            }
+        }
+    }
+}
+
+// The ids that span chunks: the block of the chunk in which such an id begins adds its partial rows, eight ranges of
+// them side by side and then in order.
+__global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C, int R, const uint2* __restrict__ list,
+                                                    const float* __restrict__ own, const float* __restrict__ cont, float scale,
+                                                    float* __restrict__ dE, int accumulate) {
+    __shared__ float4 red[8][32][2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
+    const int64_t chunk = blockIdx.x, p0 = chunk * R, p1 = p0 + R;
+    if (p1 >= T) return;
+    const uint32_t key = __ldg(&list[p1 - 1].x);
+    if (key >= V || __ldg(&list[p1].x) != key) return;                              // nothing goes on into the next chunk
+    if (p0 > 0 && __ldg(&list[p0].x) == key && __ldg(&list[p0 - 1].x) == key) return;   // it began in an earlier chunk
+    int64_t lo = p1, hi = T;                                                        // first entry behind the id
+    while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (__ldg(&list[mid].x) <= key) lo = mid + 1; else hi = mid;
+    }
+    const int64_t c1 = (lo - 1) / R, parts = c1 - chunk;                            // chunks chunk + 1 .. c1 hold the rest
+    const int64_t per = (parts + 7) / 8, a0 = chunk + 1 + warp * per, a1 = a0 + per < c1 + 1 ? a0 + per : c1 + 1;
+    const int v = blockIdx.y * 32 + lane;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+    if (v < nv) {
+#pragma unroll 4
+        for (int64_t c = a0; c < a1; ++c) {
+            const float4* q = (const float4*)(cont + c * C + v * 8);
+            const float4 x = __ldg(q), y = __ldg(q + 1);
+            a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+            b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+        }
+    }
+    red[warp][lane][0] = a;
+    red[warp][lane][1] = b;
+    __syncthreads();
+    if (warp != 0 || v >= nv) return;
+    const float4* q = (const float4*)(own + chunk * C + v * 8);
+    a = __ldg(q); b = __ldg(q + 1);
+    for (int w = 0; w < 8; ++w) {
+        const float4 x = red[w][lane][0], y = red[w][lane][1];
+        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+    }
+    float4* o = (float4*)(dE + (int64_t)key * C + v * 8);
+    float4 s0 = accumulate ? o[0] : make_float4(0.f, 0.f, 0.f, 0.f), s1 = accumulate ? o[1] : s0;
+    s0.x += scale * a.x; s0.y += scale * a.y; s0.z += scale * a.z; s0.w += scale * a.w;
+    s1.x += scale * b.x; s1.y += scale * b.y; s1.z += scale * b.z; s1.w += scale * b.w;
+    o[0] = s0; o[1] = s1;
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------
+void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* E, int table_f32, float scale,
+                      void* x0, cudaStream_t s) {
+    int tpt = 32;                                              // threads a token
+    while (tpt < 256 && tpt * 8 < c->C) tpt *= 2;
+    const unsigned grid = (unsigned)((T + 256 / tpt - 1) / (256 / tpt));
+    c->launches += 1;
+    auto k = table_f32 ? embed_fwd_k<true> : embed_fwd_k<false>;
+    k<<<grid, 256, 0, s>>>(T, V, c->C, c->n, tpt, ids, E, scale, (uint4*)x0, c->op_status);
+}
+
+// List entries a warp adds up: 32 where that leaves enough warps to fill the GPU, fewer for short lists.
+static int embed_chunk(int64_t T, int C) {
+    const int64_t slices = (C / 8 + 31) / 32;
+    int R = 32;
+    while (R > 4 && (T + R - 1) / R * slices < 148 * 24) R /= 2;
+    return R;
+}
+
+struct EmbedScratch { uint2 *buf0, *buf1; uint32_t* mask; float *own, *cont; size_t bytes; };
+static EmbedScratch plan_embed(int64_t T, int64_t V, int C, void* base) {
+    EmbedScratch p;
+    char* b = (char*)base;
+    size_t off = 0;
+    const int64_t chunks = (T + embed_chunk(T, C) - 1) / embed_chunk(T, C);
+    auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
+    p.buf0 = (uint2*)take((size_t)T * 8);
+    p.buf1 = (uint2*)take((size_t)T * 8);
+    p.mask = (uint32_t*)take((size_t)((V + 31) / 32) * 4);
+    p.own = (float*)take((size_t)chunks * C * 4);
+    p.cont = (float*)take((size_t)chunks * C * 4);
+    p.bytes = off;
+    return p;
+}
+size_t embed_scratch_bytes(int64_t T, int64_t V, int C) { return plan_embed(T, V, C, nullptr).bytes; }
+
+cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* g, float scale, float* dE,
+                             int accumulate, void* scratch, cudaStream_t s) {
+    const EmbedScratch p = plan_embed(T, V, c->C, scratch);
+    int bits = 1;
+    while ((V >> bits) != 0) ++bits;                           // keys run to V
+    const int passes = (bits + 7) / 8;
+    int nb = 1;                                                // blocks of the cluster: about 256 tokens a warp at most
+    while (nb < 8 && T > (int64_t)nb * kSortWarps * 64) nb *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(nb);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = nb; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    c->launches += 3;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, embed_sort_k, T, V, passes, ids, p.buf0, p.buf1, p.mask, c->op_status);
+    if (e != cudaSuccess) return e;
+    const uint2* list = (passes & 1) ? p.buf1 : p.buf0;
+    const int R = embed_chunk(T, c->C), slices = (c->C / 8 + 31) / 32;
+    const int64_t chunks = (T + R - 1) / R, sum_blocks = (chunks * slices + 7) / 8;
+    const int64_t zero_blocks = accumulate ? 0 : ((V + 7) / 8 < c->sm_count * 8 ? (V + 7) / 8 : c->sm_count * 8);
+    MHCL_DISPATCH_N(c->n, embed_grad_k<N_><<<(unsigned)(sum_blocks + zero_blocks), 256, 0, s>>>(
+        T, V, c->C, R, sum_blocks, slices, list, p.mask, (const uint4*)g, scale, dE, p.own, p.cont, accumulate))
+    embed_join_k<<<dim3((unsigned)chunks, (unsigned)slices), 256, 0, s>>>(T, V, c->C, R, list, p.own, p.cont, scale, dE, accumulate);
+    return cudaGetLastError();
+}
+
+}  // namespace mhcl

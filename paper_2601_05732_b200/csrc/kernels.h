@@ -115,4 +115,29 @@ void launch_tail_mma(const mhclite_ctx* c, int64_t T, int N, const TailPlan& p, 
                      const float* H_pre, const float* W, const float* gain, void* dx, int acc_dx, float* Gpart,
                      float* dW, float* dgain, int acc_params, cudaStream_t s);
 
+// block_kernels.cu : the norms around a sublayer, with gate, scale and dropout, and dropout alone
+constexpr int kMaxRowC = 16384;               // channels of a row that a team of warps holds in registers
+int block_parts(int64_t T, int C, int sm_count);
+void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
+                      float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s);
+// dw_part [block_parts][C], ds_part [block_parts] (used when dscale is given)
+void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
+                      const float* rstd, float p_drop, const uint64_t* rng, const void* dy, void* dx, void* dgate, float* dw,
+                      float* dscale, int accumulate, float* dw_part, double* ds_part, cudaStream_t s);
+void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p, const uint64_t* rng, void* y, cudaStream_t s);
+
+// embed_kernels.cu : token rows into the residual streams, and the table's gradient
+void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* E, int table_f32, float scale,
+                      void* x0, cudaStream_t s);
+size_t embed_scratch_bytes(int64_t T, int64_t V, int C);
+cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* g, float scale, float* dE,
+                             int accumulate, void* scratch, cudaStream_t s);
+
+// ce_kernels.cu : cross entropy of h W^T without the logits in memory; false when the tensor maps could not be built
+size_t ce_scratch_bytes(int64_t T, int64_t V, int C, int grad);
+bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
+                          float* loss, float* lse, void* scratch, cudaStream_t s);
+bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
+                          const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s);
+
 }  // namespace mhcl

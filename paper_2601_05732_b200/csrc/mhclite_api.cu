@@ -2,6 +2,7 @@
 #include <stdarg.h>
 #include <new>
 
+#include "api_checks.cuh"
 #include "common.cuh"
 #include "kernels.h"
 
@@ -52,45 +53,9 @@ Workspace plan_workspace(int n, int C, int64_t T, int N, void* base, int sm_coun
     return w;
 }
 
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
-// Makes the context's device current for the duration of a call.
-struct DeviceGuard {
-    int prev = -1;
-    bool switched = false;
-    cudaError_t err = cudaSuccess;
-    explicit DeviceGuard(int dev) {
-        err = cudaGetDevice(&prev);
-        if (err == cudaSuccess && prev != dev) { err = cudaSetDevice(dev); switched = (err == cudaSuccess); }
-    }
-    ~DeviceGuard() { if (switched) cudaSetDevice(prev); }
-};
-
 }  // namespace mhcl
 
 using namespace mhcl;
-
-#define MHCL_REQUIRE_CTX(ctx)  do { if (!(ctx)) return MHCLITE_ERR_BAD_ARG; (ctx)->err[0] = 0; } while (0)
-#define MHCL_REQUIRE_T(ctx, T) do { if ((T) < 0) return fail(ctx, MHCLITE_ERR_BAD_ARG, "T < 0"); } while (0)
-#define MHCL_PTR(ctx, p)                                                                            \
-    do {                                                                                            \
-        if (!(p)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "null pointer: %s", #p);                    \
-        if (!aligned16(p)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "pointer not 16-byte aligned: %s", #p); \
-    } while (0)
-#define MHCL_OPT_PTR(ctx, p)                                                                        \
-    do {                                                                                            \
-        if ((p) && !aligned16(p)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "pointer not 16-byte aligned: %s", #p); \
-    } while (0)
-// An output that aliases an input is refused: the kernels read activations through the read-only path and by TMA.
-#define MHCL_NO_ALIAS(ctx, out, in)                                                                 \
-    do {                                                                                            \
-        if ((const void*)(out) == (const void*)(in))                                                \
-            return fail(ctx, MHCLITE_ERR_BAD_ARG, "%s must not alias %s", #out, #in);               \
-    } while (0)
-#define MHCL_DEVICE(ctx)                                                                            \
-    DeviceGuard guard_((ctx)->device);                                                              \
-    if (guard_.err != cudaSuccess) return check_cuda(ctx, guard_.err, "cudaSetDevice")
-#define MHCL_LAUNCH_CHECK(ctx, what) do { int rc_ = check_cuda(ctx, cudaGetLastError(), what); if (rc_) return rc_; } while (0)
 
 static int need_workspace(mhclite_ctx* ctx, int64_t T, int kind, Workspace* w) {
     const size_t need = plan_workspace(ctx->n, ctx->C, T, ctx_cols(ctx, kind), nullptr, ctx->sm_count).bytes;
@@ -195,6 +160,7 @@ const char* mhclite_status_string(int status) {
         case MHCLITE_ERR_CUDA: return "CUDA error";
         case MHCLITE_ERR_WORKSPACE: return "workspace missing or too small";
         case MHCLITE_ERR_TIMEOUT: return "device-side wait timed out";
+        case MHCLITE_ERR_INDEX: return "token index outside the table";
         default: return "unknown status";
     }
 }
@@ -212,6 +178,7 @@ int mhclite_create(mhclite_ctx** out, int n, int C, int device) {
     ctx->n = n; ctx->C = C; ctx->device = device; ctx->nfact = ipow_fact(n); ctx->table_dev = nullptr;
     ctx->pending_T = -1; ctx->pending_x = nullptr;
     ctx->ws = nullptr; ctx->ws_bytes = 0; ctx->err[0] = 0; ctx->launches = 0; ctx->timing = false; ctx->status_word = nullptr;
+    ctx->op_status = nullptr;
     for (int k = 0; k < MHCLITE_KERNEL_COUNT; ++k) { ctx->ev[k][0] = ctx->ev[k][1] = nullptr; ctx->ev_recorded[k] = false; }
     ctx->copy_in = ctx->copy_out = nullptr; ctx->ev_fork = ctx->ev_join = nullptr;
     for (int k = 0; k < MHCLITE_STEP_CHUNKS; ++k) ctx->ev_in[k] = ctx->ev_cmp[k] = nullptr;
@@ -866,16 +833,34 @@ int mhclite_step_host(mhclite_ctx* ctx, int64_t T, const mhclite_bf16* x_host, c
 
 int64_t mhclite_kernel_launches(const mhclite_ctx* ctx) { return ctx ? ctx->launches : 0; }
 
+int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words) {
+    MHCL_REQUIRE_CTX(ctx);
+    MHCL_OPT_PTR(ctx, words);
+    if (words) {
+        MHCL_DEVICE(ctx);
+        int rc = check_cuda(ctx, cudaMemset(words, 0, 32), "clearing the status words");
+        if (rc) return rc;
+    }
+    ctx->op_status = words;
+    return MHCLITE_OK;
+}
+
 int mhclite_device_status(mhclite_ctx* ctx) {
     MHCL_REQUIRE_CTX(ctx);
-    if (!ctx->status_word) return MHCLITE_OK;
+    if (!ctx->status_word && !ctx->op_status) return MHCLITE_OK;
     MHCL_DEVICE(ctx);
-    int v[5] = {0, 0, 0, 0, 0};
-    int rc = check_cuda(ctx, cudaMemcpy(v, ctx->status_word, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
-    if (rc) return rc;
-    if (v[0] != 0)
-        return fail(ctx, v[0], "a kernel gave up on a bounded wait (kernel %d, wait %d, block %d, index %d)", v[1], v[2],
-                    v[3], v[4]);
+    for (const int* words : {ctx->status_word, ctx->op_status}) {
+        if (!words) continue;
+        int v[5] = {0, 0, 0, 0, 0};
+        int rc = check_cuda(ctx, cudaMemcpy(v, words, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
+        if (rc) return rc;
+        if (v[0] == MHCLITE_ERR_INDEX)
+            return fail(ctx, v[0], "operator %d met token index %d (low 32 bits) outside the table, at token %lld", v[1], v[2],
+                        (long long)(((int64_t)v[3] << 31) | v[4]));
+        if (v[0] != 0)
+            return fail(ctx, v[0], "a kernel gave up on a bounded wait (kernel %d, wait %d, block %d, index %d)", v[1], v[2],
+                        v[3], v[4]);
+    }
     return MHCLITE_OK;
 }
 

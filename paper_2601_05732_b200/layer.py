@@ -6,6 +6,9 @@ library's kernels.
 
 Forward (paper Eq. (1), (4), (5)):   pre  -> [sublayer f: the caller's] -> post
 Backward:                            post_bwd -> [f's backward]        -> tail
+
+A model (``model_fwd`` / ``model_bwd``) is a stack with its two ends, token lookup and loss, and with the norms, gate,
+scale and dropout around each sublayer (``block_sublayer``); what lies between the norms stays the caller's.
 """
 from __future__ import annotations
 
@@ -139,3 +142,90 @@ def stack_bwd(ctx: MhcLite, Ps, Bs, g_top, sublayer_bwd, eps=1e-6):
         tail_bwd(ctx, P, B, B.x_in, g, B.du, eps, True)
         g = B.dx
     return g
+
+
+class BlockParams:
+    """What encloses one sublayer: norm weights w_in, w_out [C] and the residual scale [1], fp32; p_drop of its output."""
+
+    def __init__(self, w_in, w_out, scale, device, p_drop=0.0):
+        f = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(device)
+        self.w_in, self.w_out, self.scale, self.p_drop = f(w_in), f(w_out), f(np.reshape(scale, (1,))), float(p_drop)
+
+
+class BlockBuffers:
+    """Outputs, saved tensors and gradients of one sublayer's enclosure for T tokens."""
+
+    def __init__(self, ctx: MhcLite, T: int, gated: bool):
+        C, dev = ctx.C, f"cuda:{ctx.device}"
+        f32 = lambda *s: torch.empty(*s, dtype=torch.float32, device=dev)
+        bf = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=dev)
+        self.v, self.y, self.r_in, self.r_out = bf(T, C), bf(T, C), f32(T), f32(T)
+        self.du, self.d_o, self.dgate = bf(T, C), bf(T, C), bf(T, C) if gated else None
+        self.dw_in, self.dw_out, self.dscale = f32(C), f32(C), f32(1)
+        self.o = self.gate = None              # what the caller's inner function returned
+
+
+def block_sublayer(ctx: MhcLite, Ks, KBs, inner, rng=None, eps=1e-6):
+    """The `sublayer` of stack_fwd: norm, the caller's `inner(l, v)` -> (o, gate or None), then norm, gate, dropout and
+    residual scale.  rng: int64 [layers, 2] on the device, (seed, offset) of each layer's dropout; the caller gives a layer
+    an offset of its own and moves the offsets on from step to step."""
+    def f(l, u):
+        K, B = Ks[l], KBs[l]
+        ctx.block_in_fwd(u, K.w_in, eps, B.v, B.r_in)
+        B.o, B.gate = inner(l, B.v)
+        ctx.block_out_fwd(B.o, B.gate, K.w_out, K.scale, eps, K.p_drop, None if rng is None else rng[l], B.y, B.r_out)
+        return B.y
+    return f
+
+
+def block_sublayer_bwd(ctx: MhcLite, Ks, KBs, inner_bwd, rng=None, accumulate_params=False):
+    """The `sublayer_bwd` of stack_bwd; `inner_bwd(l, v, d_o, dgate)` is the caller's backward of `inner` and returns dv.
+    rng holds what it held in the forward."""
+    def f(l, u, dy):
+        K, B = Ks[l], KBs[l]
+        ctx.block_out_bwd(B.o, B.gate, K.w_out, K.scale, B.r_out, K.p_drop, None if rng is None else rng[l], dy, B.d_o, B.dgate,
+                          B.dw_out, B.dscale, accumulate_params)
+        dv = inner_bwd(l, B.v, B.d_o, B.dgate)
+        ctx.block_in_bwd(u, K.w_in, B.r_in, dv, B.du, B.dw_in, accumulate_params)
+        return B.du
+    return f
+
+
+class ModelEnds:
+    """The two ends of a model for T tokens: the table E [V,C] (fp32 or bf16) with its scale, the last norm w [C], the
+    head W [V,C] bf16, and their buffers.  The last hidden row of a token is the mean over its streams."""
+
+    def __init__(self, ctx: MhcLite, T: int, E: torch.Tensor, embed_scale: float, w: torch.Tensor, W: torch.Tensor,
+                 logit_scale: float = 1.0):
+        n, C, dev = ctx.n, ctx.C, f"cuda:{ctx.device}"
+        f32 = lambda *s: torch.empty(*s, dtype=torch.float32, device=dev)
+        bf = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=dev)
+        self.E, self.embed_scale, self.w, self.W, self.logit_scale = E, float(embed_scale), w, W, float(logit_scale)
+        self.x0, self.top, self.h = bf(T, n, C), bf(T, C), bf(T, C)
+        self.mix, self.r = torch.full((T, n), 1.0 / n, device=dev), f32(T)
+        self.loss, self.lse = f32(T), f32(T)
+        self.dh, self.dtop, self.dx, self.dmix = bf(T, C), bf(T, C), bf(T, n, C), f32(T, n)
+        self.dE, self.dw, self.dW = f32(*E.shape), f32(C), bf(*W.shape)
+
+
+def model_fwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, sublayer, eps=1e-6, fuse_layers=True):
+    """Token ids [T] to the loss of each token [T] (0 where target is negative): lookup into the streams, the stack, the
+    mean of the streams, the last norm, cross entropy.  Everything the backward needs stays in M, Bs and the sublayer's
+    buffers."""
+    ctx.embed_fwd(ids, M.E, M.embed_scale, M.x0)
+    M.x_top = stack_fwd(ctx, Ps, Bs, M.x0, sublayer, eps, fuse_layers)
+    ctx.premix_fwd(M.x_top, M.mix, M.top)
+    ctx.block_in_fwd(M.top, M.w, eps, M.h, M.r)
+    ctx.linear_ce_fwd(M.h, M.W, target, M.logit_scale, M.loss, M.lse)
+    return M.loss
+
+
+def model_bwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, dloss, sublayer_bwd, eps=1e-6, accumulate_params=False):
+    """Backward of model_fwd from dloss [T] fp32: M.dW, M.dw, M.dE, and the layers' gradients in Bs.  accumulate_params
+    concerns the fp32 gradients M.dw and M.dE; M.dW is overwritten, and the layers' gradients are as stack_bwd leaves them."""
+    ctx.linear_ce_bwd(M.h, M.W, target, M.logit_scale, M.lse, dloss, M.dh, M.dW)
+    ctx.block_in_bwd(M.top, M.w, M.r, M.dh, M.dtop, M.dw, accumulate_params)
+    ctx.premix_bwd(M.x_top, M.mix, M.dtop, M.dmix, M.dx, False)
+    g0 = stack_bwd(ctx, Ps, Bs, M.dx, sublayer_bwd, eps)
+    ctx.embed_bwd(ids, g0, M.embed_scale, M.dE, accumulate_params)
+    return M.dE
