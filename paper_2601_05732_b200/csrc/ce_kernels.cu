@@ -11,7 +11,8 @@
 // Rows without a target (padding, prompts) are left out before the products: ce_rows_k lists the others and copies their
 // h side by side, so such rows cost nothing, and what they hold (NaN included) reaches neither loss nor gradients.
 //
-// Tiles: 128 x 256 a CTA, K in steps of 64 (one 128-byte swizzle row of bf16) through a ring of TMA stages, accumulators
+// Tiles: 256 x 256 a pair of CTAs (tcgen05 cta_group::2: each CTA stages 128 rows of A and 128 columns of B, and holds 128
+// rows of the accumulator), K in steps of 64 (one 128-byte swizzle row of bf16) through a ring of TMA stages, accumulators
 // double buffered in tensor memory so that the epilogue of one tile overlaps the products of the next.
 #include "common.cuh"
 #include "kernels.h"
@@ -20,10 +21,12 @@
 
 namespace mhcl {
 
-constexpr int kCeM = 128, kCeN = 256, kCeK = 64;
-constexpr int kCeStages = 4;
-constexpr int kCeABytes = kCeM * kCeK * 2, kCeBBytes = kCeN * kCeK * 2, kCeStage = kCeABytes + kCeBBytes;
-constexpr int kCeThreads = 192;                       // warp 0: TMA, warp 1: MMA, warps 2..5: epilogue
+constexpr int kCeM = 256, kCeN = 256, kCeK = 64;       // tile of a pair
+constexpr int kCeHalf = 128;                           // rows of A, columns of B and accumulator rows of one CTA
+constexpr int kCeStages = 6;
+constexpr int kCeABytes = kCeHalf * kCeK * 2, kCeStage = 2 * kCeABytes;
+constexpr int kCeEpiWarps = 8;                         // two per tensor-memory quadrant: columns 0..127 and 128..255
+constexpr int kCeThreads = 64 + 32 * kCeEpiWarps;      // warp 0: TMA, warp 1: MMA, the others: epilogue
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 enum CeMode { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
@@ -37,13 +40,14 @@ struct CeArgs {
     int m_tiles, n_tiles;       // at most; m_tiles of the row-wise modes is cut to `live` on the device
     float scale;
     // CE_STATS
-    float2* part;               // [n_tiles][Tpad] (maximum, sum) in base 2
+    float2* part;               // [2 n_tiles][Tpad] (maximum, sum) in base 2 of 128 columns each
     float* tlogit;              // [Tpad] the target's logit
     const int64_t* target;
     int Tpad;
     // CE_GRAD
     const float* lse;
     const float* dloss;
+    const uint32_t* ref;        // bits of the largest finite |dloss|
     __nv_bfloat16* G;           // [Tpad][pitch]
     int64_t pitch;
     // CE_DH
@@ -64,6 +68,61 @@ struct CeCtl {
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+// The bracket of a row is kept as (p - [v = target]) dloss / ref in bf16, with ref the largest |dloss|; the products'
+// epilogues multiply by scale ref in fp32.  Equal dloss (a mean over the tokens) then cost no rounding, where 1 / T rounded
+// to bf16 would put one common error of up to 2^-9 on every gradient.
+__device__ __forceinline__ float ce_ref(const uint32_t* ref) { const float r = __uint_as_float(*ref); return r > 0.f ? r : 1.f; }
+
+// 32 bytes to global memory in one instruction (a full sector a thread).
+__device__ __forceinline__ void st32(void* p, const uint4& a, const uint4& b) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x),
+                 "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+
+// ---- pairs of CTAs -----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cta_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t leader_addr(uint32_t a) {            // the same shared-memory offset in CTA 0 of the pair
+    uint32_t b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(b) : "r"(a));
+    return b;
+}
+__device__ __forceinline__ void pair_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// Into this CTA's shared memory; the bytes count on a barrier of the pair's leader.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tc_mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5, %5, %5, %5, %5}, p;\n\t}"
+                 ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u) : "memory");
+}
+// Arrives on the barrier at this offset in both CTAs when the MMAs issued so far are done.
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// A wait on a barrier that gives up after four seconds, or when another role of the CTA has.
+__device__ __forceinline__ bool ce_wait(uint32_t bar, uint32_t parity, volatile int* abort, int where, int index) {
+    if (mbar_try_wait(bar, parity)) return true;
+    uint64_t t0 = 0, t;
+    for (uint32_t i = 0;; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (abort[0]) return false;
+        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+        if (i == 0) t0 = t;
+        if (t - t0 > 4000000000ull) break;
+    }
+    if (abort[0] == 0) { abort[1] = where; abort[2] = index; }
+    abort[0] = 1;
+    return false;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // Tile order: groups of 16 row tiles, column tiles inside a group, so that the CTAs of a wave share operands in L2.
 __device__ __forceinline__ void ce_tile(int i, int mt, int nt, int& m, int& n) {
     constexpr int kGroup = 16;
@@ -73,13 +132,15 @@ __device__ __forceinline__ void ce_tile(int i, int mt, int nt, int& m, int& n) {
 }
 
 template <int MODE>
-__global__ void __launch_bounds__(kCeThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCeThreads, 1)
 ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb, const CeArgs a) {
     constexpr bool A_MN = MODE == CE_DW, B_MN = MODE == CE_DH || MODE == CE_DW;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     CeCtl* ctl = reinterpret_cast<CeCtl*>(smem + kCeStages * kCeStage);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t rank = cta_rank();
+    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     volatile int* abort = ctl->abort;
     const int live = *a.live;
     const int mt = MODE == CE_DW ? a.m_tiles : (live + kCeM - 1) / kCeM, nt = a.n_tiles, tiles = mt * nt;
@@ -88,17 +149,18 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 
     if (tid == 0) {
         for (int s = 0; s < kCeStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->acc_full[s]), 1); mbar_init(smem_u32(&ctl->acc_empty[s]), 4); }
+        for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->acc_full[s]), 1); mbar_init(smem_u32(&ctl->acc_empty[s]), 2 * kCeEpiWarps); }
         abort[0] = abort[1] = abort[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (warp == 1) {                                      // both CTAs of the pair take part
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
+    pair_sync();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
 
@@ -106,42 +168,47 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
         if (lane == 0) {
             int it = 0;
             bool ok = true;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x) {
+            for (int i = pair; i < tiles && ok; i += pairs) {
                 int m, n;
                 ce_tile(i, mt, nt, m, n);
+                const int am = m * kCeM + (int)rank * kCeHalf, bn = n * kCeN + (int)rank * kCeHalf;
                 for (int k = 0; k < ksteps; ++k, ++it) {
                     const int s = it % kCeStages;
-                    ok = mbar_wait(smem_u32(&ctl->empty[s]), ((it / kCeStages) & 1) ^ 1, abort, 1, it);
+                    ok = ce_wait(smem_u32(&ctl->empty[s]), ((it / kCeStages) & 1) ^ 1, abort, 1, it);
                     if (!ok) break;
-                    const uint32_t full = smem_u32(&ctl->full[s]), sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
-                    mbar_expect_tx(full, kCeStage);
+                    const uint32_t own = smem_u32(&ctl->full[s]), full = leader_addr(own);
+                    const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
+                    if (rank == 0) mbar_expect_tx(own, 2 * kCeStage);          // the bytes of both CTAs
                     if (A_MN) {
-                        for (int b = 0; b < kCeM / 64; ++b) tma_load_2d(sa + b * 8192, &tma, full, m * kCeM + b * 64, k * kCeK);
+                        for (int b = 0; b < kCeHalf / 64; ++b) tma_load_2d_pair(sa + b * 8192, &tma, full, am + b * 64, k * kCeK);
                     } else {
-                        tma_load_2d(sa, &tma, full, k * kCeK, m * kCeM);
+                        tma_load_2d_pair(sa, &tma, full, k * kCeK, am);
                     }
                     if (B_MN) {
-                        for (int b = 0; b < kCeN / 64; ++b)
-                            tma_load_2d(sb + b * 8192, &tmb, full, n * kCeN + b * 64, (MODE == CE_DH ? a.v0 : 0) + k * kCeK);
+                        for (int b = 0; b < kCeHalf / 64; ++b)
+                            tma_load_2d_pair(sb + b * 8192, &tmb, full, bn + b * 64, (MODE == CE_DH ? a.v0 : 0) + k * kCeK);
                     } else {
-                        tma_load_2d(sb, &tmb, full, k * kCeK, a.v0 + n * kCeN);
+                        tma_load_2d_pair(sb, &tmb, full, k * kCeK, a.v0 + bn);
                     }
                 }
             }
+            // the last products release their stages on both CTAs' barriers: neither CTA leaves before they have
+            for (int d = 0; d < kCeStages && ok; ++d, ++it)
+                if (it >= kCeStages) ok = ce_wait(smem_u32(&ctl->empty[it % kCeStages]), ((it / kCeStages) & 1) ^ 1, abort, 5, it);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             constexpr uint32_t idesc = umma_idesc_mn(kCeM, kCeN, A_MN, B_MN);
             int it = 0, j = 0;
             bool ok = true;
-            for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x, ++j) {
+            for (int i = pair; i < tiles && ok; i += pairs, ++j) {
                 const int buf = j & 1;
-                ok = mbar_wait(smem_u32(&ctl->acc_empty[buf]), ((j >> 1) & 1) ^ 1, abort, 2, j);
+                ok = ce_wait(smem_u32(&ctl->acc_empty[buf]), ((j >> 1) & 1) ^ 1, abort, 2, j);
                 if (!ok) break;
                 tc_fence_after();
                 for (int k = 0; k < ksteps; ++k, ++it) {
                     const int s = it % kCeStages;
-                    ok = mbar_wait(smem_u32(&ctl->full[s]), (it / kCeStages) & 1, abort, 3, it);
+                    ok = ce_wait(smem_u32(&ctl->full[s]), (it / kCeStages) & 1, abort, 3, it);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
@@ -149,40 +216,41 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                     for (int kk = 0; kk < kCeK / 16; ++kk) {
                         const uint64_t ad = A_MN ? smem_desc(sa + kk * 2048, 8192, 1024, 2) : smem_desc(sa + kk * 32, 16, 1024, 2);
                         const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, 8192, 1024, 2) : smem_desc(sb + kk * 32, 16, 1024, 2);
-                        tc_mma(tmem + buf * kCeN, ad, bd, idesc, (k > 0 || kk > 0) ? 1u : 0u);
+                        tc_mma_pair(tmem + buf * kCeN, ad, bd, idesc, (k > 0 || kk > 0) ? 1u : 0u);
                     }
-                    tc_commit(smem_u32(&ctl->empty[s]));
+                    tc_commit_pair(smem_u32(&ctl->empty[s]));
                 }
-                if (ok) tc_commit(smem_u32(&ctl->acc_full[buf]));
+                if (ok) tc_commit_pair(smem_u32(&ctl->acc_full[buf]));
             }
         }
     } else {
-        const int quad = warp & 3, row = quad * 32 + lane;
+        const int quad = warp & 3, half = (warp - 2) >> 2, row = (int)rank * kCeHalf + quad * 32 + lane;
         bool ok = true;
         int j = 0;
-        for (int i = blockIdx.x; i < tiles && ok; i += gridDim.x, ++j) {
+        for (int i = pair; i < tiles && ok; i += pairs, ++j) {
             const int buf = j & 1;
-            ok = mbar_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
+            ok = ce_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             int m, n;
             ce_tile(i, mt, nt, m, n);
             const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
-            const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN;
+            const int n0 = n * kCeN + half * kCeHalf;           // this warp's 128 columns
+            const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN + half * kCeHalf;
             if (MODE == CE_STATS || MODE == CE_GRAD) {
                 const bool in = r < live;
                 const int t = in ? a.rows[r] : 0;
-                const int tgt = in ? (int)(a.target[t] - a.v0) - n * kCeN : -1;      // the target's column in this tile
-                const int cols = min(kCeN, (int)(a.V - a.v0) - n * kCeN);            // of the vocabulary (the rest is padding)
+                const int tgt = in ? (int)(a.target[t] - a.v0) - n0 : -1;            // the target's column among them
+                const int cols = (int)(a.V - a.v0) - n0;                             // of the vocabulary (the rest is padding)
                 const float k2 = a.scale * kLog2e;
                 if (MODE == CE_STATS) {
                     float mx = -INFINITY, sum = 0.f;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                    for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
+                        if (c0 >= cols) break;
                         float v[32];
                         tc_ld32(acc + c0, v);
-                        if (c0 >= cols) break;
                         if (__any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
@@ -200,12 +268,12 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         for (int e = 0; e < 32; ++e) sum += ex2(v[e] - base);
                         mx = top;
                     }
-                    if (in) a.part[(int64_t)n * a.Tpad + r] = make_float2(mx, sum);
+                    if (in) a.part[(int64_t)(2 * n + half) * a.Tpad + r] = make_float2(mx, sum);
                 } else {
-                    const float lse2 = in ? a.lse[t] * kLog2e : 0.f, f = in ? a.dloss[t] * a.scale : 0.f;
-                    __nv_bfloat16* out = a.G + (int64_t)r * a.pitch + n * kCeN;
+                    const float lse2 = in ? a.lse[t] * kLog2e : 0.f, f = in ? a.dloss[t] / ce_ref(a.ref) : 0.f;
+                    __nv_bfloat16* out = a.G + (int64_t)r * a.pitch + n0;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                    for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                         float v[32];
                         tc_ld32(acc + c0, v);
 #pragma unroll
@@ -215,17 +283,18 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                             v[e] = (in && c0 + e < cols) ? v[e] * f : 0.f;
                         }
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) *reinterpret_cast<uint4*>(out + c0 + e) = pack8(v + e);
+                        for (int e = 0; e < 32; e += 16) st32(out + c0 + e, pack8(v + e), pack8(v + e + 8));
                     }
                 }
             } else {
                 const bool in = MODE == CE_DH ? r < live : r < a.vn;
                 const int64_t orow = MODE == CE_DH ? (in ? a.rows[r] : 0) : a.v0 + r;
+                const float f = a.scale * ce_ref(a.ref);
 #pragma unroll 1
-                for (int c0 = 0; c0 < kCeN; c0 += 32) {
+                for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                     float v[32];
                     tc_ld32(acc + c0, v);
-                    const int c = n * kCeN + c0;
+                    const int c = n0 + c0;
                     if (!in) continue;
                     if (MODE == CE_DW && ksteps == 0) {                 // no row has a target: nothing was accumulated
 #pragma unroll
@@ -241,21 +310,21 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                                 v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
                                 v[e + 4] += y.x; v[e + 5] += y.y; v[e + 6] += y.z; v[e + 7] += y.w;
                             }
-                            if (a.last) {
-                                *reinterpret_cast<uint4*>(a.dh + orow * a.C + c + e) = pack8(v + e);
-                            } else {
+                            if (!a.last) {
                                 p[0] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
                                 p[1] = make_float4(v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
+                                continue;
                             }
-                        } else {
-                            *reinterpret_cast<uint4*>(a.dW + orow * a.C + c + e) = pack8(v + e);
                         }
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) v[e + x] *= f;
+                        *reinterpret_cast<uint4*>((MODE == CE_DH ? a.dh : a.dW) + orow * a.C + c + e) = pack8(v + e);
                     }
                 }
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[buf]));
+            if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&ctl->acc_empty[buf])));
         }
     }
     tc_fence_before();
@@ -268,20 +337,23 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
         }
     }
     __syncthreads();
+    pair_sync();                                               // the other CTA's products may read this one's memory until here
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 
 // ---- rows with a target ----------------------------------------------------------------------------------------------
 // Block b handles `per` tokens: counts the targets before them, numbers its own rows, copies their h side by side, and
-// clears the outputs of the rows without a target (loss and lse, or dh).  The last block pads the list's h with zero rows
-// to the next multiple of 128, which the products read.
+// clears the outputs of the rows without a target (loss and lse, or dh).  In the backward it also joins the
+// largest finite |dloss| of its rows (as bits: a maximum does not depend on the order).  The last block pads the list's h
+// with zero rows to the next multiple of 256, which the products read.
 __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* __restrict__ target,
                                                   const uint4* __restrict__ h, uint4* __restrict__ hl, int* __restrict__ rows,
                                                   int* __restrict__ live, float* __restrict__ loss, float* __restrict__ lse,
-                                                  uint4* __restrict__ dh, int* __restrict__ status) {
+                                                  uint4* __restrict__ dh, const float* __restrict__ dloss, uint32_t* ref,
+                                                  int* __restrict__ status) {
     __shared__ int wcnt[32], base_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = C >> 3;
     const int64_t t0 = blockIdx.x * per, t1 = t0 + per < T ? t0 + per : T;
@@ -296,14 +368,20 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
     }
     __syncthreads();
     int base = base_s;
+    uint32_t top = 0;
     for (int64_t b = t0; b < t1; b += 32) {                     // every warp numbers all of the block's rows: no exchange
         const int64_t t = b + lane;
         const int64_t y = t < t1 ? target[t] : -1;
         const bool ok = y >= 0 && y < V;
         const uint32_t m = __ballot_sync(0xffffffffu, ok);
         if (warp == 0 && t < t1) {
-            if (ok) rows[base + __popc(m & ((1u << lane) - 1u))] = (int)t;
-            else {
+            if (ok) {
+                rows[base + __popc(m & ((1u << lane) - 1u))] = (int)t;
+                if (dloss) {
+                    const uint32_t d = __float_as_uint(dloss[t]) & 0x7FFFFFFFu;
+                    if (d < 0x7F800000u && d > top) top = d;
+                }
+            } else {
                 if (loss) { loss[t] = 0.f; lse[t] = 0.f; }
                 if (y >= V && status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
                     status[1] = MHCLITE_OP_LINEAR_CE; status[2] = (int)y; status[3] = (int)(t >> 31); status[4] = (int)(t & 0x7FFFFFFF);
@@ -321,22 +399,26 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
         }
         base += __popc(m);
     }
+    if (dloss && warp == 0) {
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) atomicMax(ref, top);
+    }
     if (t1 == T) {
         if (tid == 0) *live = base;
-        const int pad = min(Tpad, (base + 127) / 128 * 128);
+        const int pad = min(Tpad, (base + kCeM - 1) / kCeM * kCeM);
         for (int64_t i = tid; i < (int64_t)(pad - base) * nv; i += 1024) hl[(int64_t)base * nv + i] = make_uint4(0, 0, 0, 0);
     }
 }
 
 // Joins the (maximum, sum) pairs of a row: 32 rows a block, eight ranges of tiles side by side.
-__global__ void __launch_bounds__(256) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_tiles, int Tpad,
+__global__ void __launch_bounds__(256) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_parts, int Tpad,
                                                  const float2* __restrict__ part, const float* __restrict__ tlogit,
                                                  float* __restrict__ loss, float* __restrict__ lse) {
     __shared__ float2 red[8][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = *live;
     float m = -INFINITY, s = 0.f;
     if (r < n) {
-        const int per = (n_tiles + 7) / 8, n1 = min(n_tiles, (warp + 1) * per);
+        const int per = (n_parts + 7) / 8, n1 = min(n_parts, (warp + 1) * per);
 #pragma unroll 4
         for (int k = warp * per; k < n1; ++k) {
             const float2 p = part[(int64_t)k * Tpad + r];
@@ -367,6 +449,7 @@ struct CePlan {
     int Tpad, n_tiles;
     int pieces; int64_t piece;             // vocabulary rows a piece, a multiple of 256
     int *live, *rows;
+    uint32_t* ref;
     __nv_bfloat16* hl;
     float2* part; float* tlogit;
     __nv_bfloat16* G; float* dh_acc;
@@ -377,15 +460,16 @@ static CePlan plan_ce(int64_t T, int64_t V, int C, int grad, void* base) {
     char* b = (char*)base;
     size_t off = 0;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
-    p.Tpad = (int)round_up64(T > 0 ? T : 1, 128);
+    p.Tpad = (int)round_up64(T > 0 ? T : 1, kCeM);
     p.n_tiles = (int)((V + kCeN - 1) / kCeN);
     p.live = (int*)take(256);
+    p.ref = (uint32_t*)p.live + 1;
     p.rows = (int*)take((size_t)p.Tpad * 4);
     p.hl = (__nv_bfloat16*)take((size_t)p.Tpad * C * 2);
     p.part = nullptr; p.tlogit = nullptr; p.G = nullptr; p.dh_acc = nullptr;
     p.pieces = 1; p.piece = 0;
     if (!grad) {
-        p.part = (float2*)take((size_t)p.n_tiles * p.Tpad * 8);
+        p.part = (float2*)take((size_t)p.n_tiles * 2 * p.Tpad * 8);
         p.tlogit = (float*)take((size_t)p.Tpad * 4);
     } else {
         int64_t most = ((int64_t)128 << 20) / p.Tpad / 256 * 256;
@@ -402,12 +486,13 @@ static CePlan plan_ce(int64_t T, int64_t V, int C, int grad, void* base) {
 size_t ce_scratch_bytes(int64_t T, int64_t V, int C, int grad) { return plan_ce(T, V, C, grad, nullptr).bytes; }
 
 static void launch_ce_rows(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const int64_t* target, const void* h,
-                           float* loss, float* lse, void* dh, cudaStream_t s) {
+                           float* loss, float* lse, void* dh, const float* dloss, cudaStream_t s) {
+    if (dloss) cudaMemsetAsync(p.ref, 0, sizeof(uint32_t), s);
     int64_t per = 32;
     while ((T + per - 1) / per > 296) per += 32;
     c->launches += 1;
     ce_rows_k<<<(unsigned)((T + per - 1) / per), 1024, 0, s>>>(T, V, c->C, per, p.Tpad, target, (const uint4*)h, (uint4*)p.hl, p.rows,
-                                                               p.live, loss, lse, (uint4*)dh, c->op_status);
+                                                               p.live, loss, lse, (uint4*)dh, dloss, p.ref, c->op_status);
 }
 
 template <int MODE>
@@ -416,7 +501,8 @@ static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CU
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
     cudaFuncSetAttribute(ce_gemm_k<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     c->launches += 1;
-    ce_gemm_k<MODE><<<(unsigned)(tiles < c->sm_count ? tiles : c->sm_count), kCeThreads, smem, s>>>(ma, mb, a);
+    const int64_t pairs = tiles < c->sm_count / 2 ? tiles : c->sm_count / 2;
+    ce_gemm_k<MODE><<<(unsigned)(2 * pairs), kCeThreads, smem, s>>>(ma, mb, a);
 }
 
 // Tensor maps: a K-major operand is copied in boxes of 64 k x `rows` rows, an MN-major one in boxes of 64 x 64 k.
@@ -431,15 +517,15 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
                           float* loss, float* lse, void* scratch, cudaStream_t s) {
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);
     CUtensorMap mh, mw;
-    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, kCeM) || !map_k(&mw, W, V, c->C, c->C, kCeN)) return false;
-    launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, s);
+    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, kCeHalf) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
+    launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, nullptr, s);
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
     a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
     a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
     launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
     c->launches += 1;
-    ce_join_k<<<(unsigned)(p.Tpad / 32), 256, 0, s>>>(p.live, p.rows, p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
+    ce_join_k<<<(unsigned)(p.Tpad / 32), 256, 0, s>>>(p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
     return true;
 }
 
@@ -448,14 +534,14 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     const CePlan p = plan_ce(T, V, c->C, 1, scratch);
     const int C = c->C;
     CUtensorMap mh, mw, mg, mwn, mgt, mhn;
-    if (!map_k(&mh, p.hl, p.Tpad, C, C, kCeM) || !map_k(&mw, W, V, C, C, kCeN) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, kCeM) ||
+    if (!map_k(&mh, p.hl, p.Tpad, C, C, kCeHalf) || !map_k(&mw, W, V, C, C, kCeHalf) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, kCeHalf) ||
         !map_mn(&mwn, W, V, C, C) || !map_mn(&mgt, p.G, p.Tpad, p.piece, p.piece) || !map_mn(&mhn, p.hl, p.Tpad, C, C))
         return false;
-    launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, s);
+    launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, dloss, s);
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
-    a.dW = (__nv_bfloat16*)dW; a.status = c->op_status;
+    a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.status = c->op_status;
     for (int i = 0; i < p.pieces; ++i) {
         a.v0 = (int)(i * p.piece);
         a.vn = (int)(V - a.v0 < p.piece ? V - a.v0 : p.piece);
