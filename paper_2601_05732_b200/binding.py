@@ -132,6 +132,9 @@ class MhcLite:
         if not torch.cuda.is_available():
             raise RuntimeError("mHC-lite needs a CUDA device; there is no CPU path")
         self._torch = torch
+        # the handle itself where torch hands it out: building a Stream object costs a microsecond a call
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
         self.lib = load()
         self.n, self.C, self.device = n, C_, device
         self.nfact = math.factorial(n)          # residual weights per token (K once a subset is attached)
@@ -170,7 +173,7 @@ class MhcLite:
         return t.data_ptr()
 
     def _stream(self):
-        return self._torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self.device)
 
     def n_cols(self, kind: int = 0) -> int:
         return (self.nfact if kind == 0 else self.n * self.n) + 2 * self.n
@@ -412,11 +415,11 @@ class MhcLite:
     # -- around the stack: lookup, block norms, dropout, loss ------------------------------------------
     def _arg(self, name, t, dtype, *shape):
         """Device pointer of a contiguous tensor of exactly this type and shape on the context's device."""
+        if t.dtype is dtype and t.shape == shape and t.get_device() == self.device and t.is_contiguous():
+            return t.data_ptr()
         if t.dtype != dtype or tuple(t.shape) != shape:
             raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
-        if not t.is_cuda or t.device.index != self.device or not t.is_contiguous():
-            raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device}")
-        return t.data_ptr()
+        raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device}")
 
     def _scratch(self, kind, *sizes):
         """Scratch of one call: allocated with torch on the current stream, which returns it in stream order (and keeps

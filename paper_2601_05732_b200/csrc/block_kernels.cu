@@ -33,16 +33,34 @@ __device__ __forceinline__ float team_sum(float v, float* red, int& slot) {
     return s;
 }
 
-__device__ __forceinline__ float sigmoidf(float a) { return __fdividef(1.f, 1.f + __expf(-a)); }
+// sigmoid of a pair: 1 / (1 + 2^(-a log2 e)); 2^x overflows to infinity for a far below 0, whose reciprocal is 0.
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t a) {
+    float x, y;
+    unpack2f(mul2(a, pack2f(-1.4426950408889634f, -1.4426950408889634f)), x, y);
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x));
+    asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(y));
+    unpack2f(add2(pack2f(x, y), pack2f(1.f, 1.f)), x, y);
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x));
+    asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(y));
+    return pack2f(x, y);
+}
+__device__ __forceinline__ uint64_t both(float x) { return pack2f(x, x); }
+// the 8 weights of a vector, as packed pairs
+__device__ __forceinline__ void load_w(const float4* __restrict__ w, int v, uint64_t* o) {
+    const ulonglong2 a = __ldg((const ulonglong2*)w + 2 * v), b = __ldg((const ulonglong2*)w + 2 * v + 1);
+    o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+}
 
 struct DropArgs {
     const uint64_t* rng;      // device (seed, offset); null: no dropout
-    uint32_t threshold;
+    uint32_t threshold;       // in units of 2^-16
     float factor;
 };
 
+// The arithmetic runs on packed pairs (two fp32 operations an instruction): with gate and dropout a vector of 8 elements
+// takes some 170 instructions forward and 230 backward, and with scalar ones the issue slots, not HBM, bounded the kernels.
 template <int VPT, int WPR, bool GATE, bool DROP>
-__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads)
+__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads, WPR * 32 > kBlockThreads ? 1 : 3)
 block_fwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, float eps, DropArgs da, uint4* __restrict__ out, float* __restrict__ rstd) {
     __shared__ float red[2 * 16];
@@ -57,46 +75,47 @@ block_fwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restri
         xv[k] = v < nv ? ld_stream(x + t * nv + v) : make_uint4(0, 0, 0, 0);
         if (GATE) gv[k] = v < nv ? ld_stream(gate + t * nv + v) : make_uint4(0, 0, 0, 0);
     }
-    float ss = 0.f;
+    uint64_t ss2 = 0;
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-        float f[8];
-        unpack8(xv[k], f);
+        uint64_t f[4];
+        unpack8x2(xv[k], f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) ss = fmaf(f[e], f[e], ss);
+        for (int e = 0; e < 4; ++e) ss2 = fma2(f[e], f[e], ss2);
     }
-    ss = team_sum<WPR>(ss, red, slot);
-    const float r = rsqrtf(ss / (float)C + eps);
+    float s0, s1;
+    unpack2f(ss2, s0, s1);
+    const float r = rsqrtf(team_sum<WPR>(s0 + s1, red, slot) / (float)C + eps);
     if (lt == 0) rstd[t] = r;
     const float s = scale ? __ldg(scale) : 1.f;
-    uint64_t seed = 0, offset = 0;
-    if (DROP) { seed = __ldg((const unsigned long long*)da.rng); offset = __ldg((const unsigned long long*)da.rng + 1); }
+    const uint64_t r2 = both(r), s2 = both(s), fac2 = both(da.factor);
+    const Philox rng(DROP ? da.rng : nullptr, DROP);
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
         const int v = lt + k * WPR * 32;
         if (v >= nv) continue;
-        float f[8], g[8];
-        unpack8(xv[k], f);
-        if (GATE) unpack8(gv[k], g);
-        const float4 w0 = __ldg(w + 2 * v), w1 = __ldg(w + 2 * v + 1);
-        const float wf[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+        uint64_t f[4], g[4], wf[4];
+        unpack8x2(xv[k], f);
+        load_w(w, v, wf);
+        if (GATE) unpack8x2(gv[k], g);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            f[e] = f[e] * r * wf[e];
-            if (GATE) f[e] *= sigmoidf(g[e]);
+        for (int e = 0; e < 4; ++e) {
+            f[e] = mul2(mul2(f[e], r2), wf[e]);
+            if (GATE) f[e] = mul2(f[e], sigmoid2(g[e]));
         }
-        if (DROP) drop8(f, (uint64_t)(t * nv + v), seed, offset, da.threshold, da.factor);
+        if (DROP) drop8(f, rng((uint64_t)(t * nv + v)), da.threshold << 16, fac2);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= s;
-        st_stream(out + t * nv + v, pack8(f));
+        for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s2);
+        st_stream(out + t * nv + v, pack8x2(f));
     }
 }
 
-// With z = drop'(dy) s, oh = o r, e = z sigmoid(a) w:
-//   do = r (e - oh mean(e oh)),  da = z oh w sig (1 - sig),  dw = sum_t z sig oh,  ds = sum dy drop(sig oh w).
-// The scale's sum runs over all T C elements and may cancel: it is added up in 64 bits from the rows on.
+// With d = drop'(dy), z = d sig, oh = o r, e = s z w (the gradient with respect to oh):
+//   do = r (e - oh mean(e oh)),  da = e oh (1 - sig),  dw = s sum_t z oh,  ds = sum z w oh.
+// s is applied once to each result.  The scale's sum runs over all T C elements and may cancel: it is added up in 64 bits
+// from the rows on.
 template <int VPT, int WPR, bool GATE, bool DROP>
-__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads)
+__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads, WPR * 32 > kBlockThreads ? 1 : 2)
 block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, const float* __restrict__ rstd, DropArgs da, const uint4* __restrict__ dy,
             uint4* __restrict__ dx, uint4* __restrict__ dgate, float* __restrict__ dw_part, double* __restrict__ ds_part) {
@@ -106,20 +125,19 @@ block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restri
     const int nv = C >> 3, lt = threadIdx.x % (WPR * 32), teams = blockDim.x / (WPR * 32), team = threadIdx.x / (WPR * 32);
     int slot = 0;
     const float s = scale ? __ldg(scale) : 1.f;
-    uint64_t seed = 0, offset = 0;
-    if (DROP) { seed = __ldg((const unsigned long long*)da.rng); offset = __ldg((const unsigned long long*)da.rng + 1); }
-    float acc[VPT][8];
+    const uint64_t s2 = both(s), fac2 = both(da.factor), minus1 = both(-1.f);
+    const Philox rng(DROP ? da.rng : nullptr, DROP);
+    uint64_t acc[VPT][4];
 #pragma unroll
     for (int k = 0; k < VPT; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[k][e] = 0.f;
+        for (int e = 0; e < 4; ++e) acc[k][e] = 0;
     double dsum = 0.0;
     for (int64_t t = (int64_t)blockIdx.x * teams + team; t < T; t += (int64_t)gridDim.x * teams) {
         uint4 xv[VPT], gv[VPT], yv[VPT];
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
             const int v = lt + k * WPR * 32;
-            xv[k] = yv[k] = gv[k] = make_uint4(0, 0, 0, 0);
             if (v < nv) {
                 xv[k] = ld_stream(x + t * nv + v);
                 yv[k] = ld_stream(dy + t * nv + v);
@@ -127,48 +145,45 @@ block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restri
             }
         }
         const float r = __ldg(rstd + t);
-        float ds = 0.f;
-        float z[VPT][8];                                   // drop'(dy) s sig
+        const uint64_t r2 = both(r);
+        uint64_t ds2 = 0;
+        uint64_t zw[VPT][4];                               // z w
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
             const int v = lt + k * WPR * 32;
             if (v >= nv) continue;
-            float f[8], g[8];
-            unpack8(xv[k], f);
-            unpack8(yv[k], z[k]);
-            if (GATE) unpack8(gv[k], g);
-            if (DROP) drop8(z[k], (uint64_t)(t * nv + v), seed, offset, da.threshold, da.factor);
-            const float4 w0 = __ldg(w + 2 * v), w1 = __ldg(w + 2 * v + 1);
-            const float wf[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
-            float da8[8];
+            uint64_t f[4], g[4], wf[4], dg[4];
+            unpack8x2(xv[k], f);
+            unpack8x2(yv[k], zw[k]);
+            load_w(w, v, wf);
+            if (GATE) unpack8x2(gv[k], g);
+            if (DROP) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16, fac2);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float oh = f[e] * r;
-                if (GATE) {
-                    const float sg = sigmoidf(g[e]);
-                    z[k][e] *= sg;
-                    da8[e] = z[k][e] * s * oh * wf[e] * (1.f - sg);
-                }
-                const float c = z[k][e] * oh;              // without s: the factor of dw and ds
-                acc[k][e] = fmaf(c, s, acc[k][e]);
-                ds = fmaf(c, wf[e], ds);
+            for (int e = 0; e < 4; ++e) {
+                const uint64_t oh = mul2(f[e], r2);
+                if (GATE) { g[e] = sigmoid2(g[e]); zw[k][e] = mul2(zw[k][e], g[e]); }
+                acc[k][e] = fma2(zw[k][e], oh, acc[k][e]);
+                zw[k][e] = mul2(zw[k][e], wf[e]);
+                const uint64_t q = mul2(zw[k][e], oh);
+                ds2 = add2(ds2, q);
+                if (GATE) dg[e] = mul2(mul2(q, s2), fma2(g[e], minus1, both(1.f)));
             }
-            if (GATE) st_stream(dgate + t * nv + v, pack8(da8));
+            if (GATE) st_stream(dgate + t * nv + v, pack8x2(dg));
         }
-        float m = team_sum<WPR>(ds, red, slot);                // sum_c of e oh / s, and the row's part of ds
+        float m0, m1;
+        unpack2f(ds2, m0, m1);
+        const float m = team_sum<WPR>(m0 + m1, red, slot);         // sum_c of e oh / s: the row's part of ds
         if (lt == 0) dsum += (double)m;
-        m *= s / (float)C;
+        const uint64_t rs2 = both(r * s), c2 = both(-r * (m / (float)C));
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
             const int v = lt + k * WPR * 32;
             if (v >= nv) continue;
-            float f[8];
-            unpack8(xv[k], f);
-            const float4 w0 = __ldg(w + 2 * v), w1 = __ldg(w + 2 * v + 1);
-            const float wf[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+            uint64_t f[4];
+            unpack8x2(xv[k], f);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = r * (z[k][e] * s * wf[e] - f[e] * r * m);
-            st_stream(dx + t * nv + v, pack8(f));
+            for (int e = 0; e < 4; ++e) f[e] = mul2(fma2(f[e], c2, zw[k][e]), rs2);
+            st_stream(dx + t * nv + v, pack8x2(f));
         }
     }
     // column sums of the block: the teams' rows through shared memory, in a fixed order
@@ -177,14 +192,14 @@ block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restri
         const int v = lt + k * WPR * 32;
         if (v < nv)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sm[team * C + v * 8 + e] = acc[k][e];
+            for (int e = 0; e < 4; ++e) *(uint64_t*)(sm + team * C + v * 8 + 2 * e) = acc[k][e];
     }
     if (lt == 0) dred[team] = dsum;
     __syncthreads();
     for (int c = threadIdx.x; c < C; c += blockDim.x) {
         float a = 0.f;
         for (int i = 0; i < teams; ++i) a += sm[i * C + c];
-        dw_part[(int64_t)blockIdx.x * C + c] = a;
+        dw_part[(int64_t)blockIdx.x * C + c] = a * s;
     }
     if (ds_part && threadIdx.x == 0) {
         double a = 0.0;
@@ -227,46 +242,55 @@ __global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* _
     }
 }
 
+// A thread takes four groups of 8 elements 256 apart: their loads are in flight together, and the round keys are made
+// once for the four.
+constexpr int kDropGroups = 4;
 __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloat16* __restrict__ x, DropArgs da,
                                                  __nv_bfloat16* __restrict__ y) {
-    const uint64_t seed = __ldg((const unsigned long long*)da.rng), offset = __ldg((const unsigned long long*)da.rng + 1);
-    const int64_t full = count >> 3;
-    for (int64_t g = (int64_t)blockIdx.x * 256 + threadIdx.x; g * 8 < count; g += (int64_t)gridDim.x * 256) {
-        float f[8];
+    const Philox rng(da.rng, true);
+    const uint32_t thr = da.threshold << 16;
+    const uint64_t fac2 = both(da.factor);
+    const int64_t full = count >> 3, g0 = (int64_t)blockIdx.x * (256 * kDropGroups) + threadIdx.x;
+    uint4 v[kDropGroups];
+#pragma unroll
+    for (int k = 0; k < kDropGroups; ++k)
+        if (g0 + k * 256 < full) v[k] = ld_stream(x + (g0 + k * 256) * 8);
+#pragma unroll
+    for (int k = 0; k < kDropGroups; ++k) {
+        const int64_t g = g0 + k * 256;
+        uint64_t f[4];
         if (g < full) {
-            unpack8(ld_stream(x + g * 8), f);
-            drop8(f, (uint64_t)g, seed, offset, da.threshold, da.factor);
-            st_stream(y + g * 8, pack8(f));
-        } else {                                           // the last, partial group
+            unpack8x2(v[k], f);
+            drop8(f, rng((uint64_t)g), thr, fac2);
+            st_stream(y + g * 8, pack8x2(f));
+        } else if (g * 8 < count) {                        // the last, partial group
             const int m = (int)(count - g * 8);
-            for (int e = 0; e < 8; ++e) f[e] = e < m ? __bfloat162float(x[g * 8 + e]) : 0.f;
-            drop8(f, (uint64_t)g, seed, offset, da.threshold, da.factor);
-            for (int e = 0; e < m; ++e) y[g * 8 + e] = __float2bfloat16_rn(f[e]);
+            float s[8];
+            for (int e = 0; e < 8; ++e) s[e] = e < m ? __bfloat162float(x[g * 8 + e]) : 0.f;
+            for (int e = 0; e < 4; ++e) f[e] = pack2f(s[2 * e], s[2 * e + 1]);
+            drop8(f, rng((uint64_t)g), thr, fac2);
+            for (int e = 0; e < 4; ++e) unpack2f(f[e], s[2 * e], s[2 * e + 1]);
+            for (int e = 0; e < m; ++e) y[g * 8 + e] = __float2bfloat16_rn(s[e]);
         }
     }
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-// Warps a row and vectors a lane for C channels: 4 vectors a lane keep a warp's loads wide and few rows' worth of
-// registers; short rows take fewer.
-struct RowPlan { int vpt, wpr; };
-static RowPlan plan_row(int C) {
+// Warps a row and vectors a lane for C channels.  Forward: 4 vectors a lane keep a warp's loads wide.  Backward: 2, since
+// its three tensors and the column sums of 4 would take 180 registers a thread and leave one block on an SM.
+struct RowPlan { int vpt, wpr, threads, teams; };
+static RowPlan plan_row(int C, bool bwd) {
     const int nv = C / 8;
     RowPlan p;
-    p.vpt = nv <= 32 ? 1 : nv <= 64 ? 2 : 4;
+    p.vpt = nv <= 32 ? 1 : (nv <= 64 || (bwd && nv <= 1024)) ? 2 : 4;
     p.wpr = 1;
     while (p.wpr * 32 * p.vpt < nv) p.wpr *= 2;
+    p.threads = p.wpr * 32 > kBlockThreads ? p.wpr * 32 : kBlockThreads;
+    p.teams = p.threads / (p.wpr * 32);
     return p;
 }
 
-#define MHCL_ROW_DISPATCH(p, ...)                                                        \
-    if ((p).vpt == 1) { constexpr int VPT = 1, WPR = 1; __VA_ARGS__; }                   \
-    else if ((p).vpt == 2) { constexpr int VPT = 2, WPR = 1; __VA_ARGS__; }              \
-    else if ((p).wpr == 1) { constexpr int VPT = 4, WPR = 1; __VA_ARGS__; }              \
-    else if ((p).wpr == 2) { constexpr int VPT = 4, WPR = 2; __VA_ARGS__; }              \
-    else if ((p).wpr == 4) { constexpr int VPT = 4, WPR = 4; __VA_ARGS__; }              \
-    else if ((p).wpr == 8) { constexpr int VPT = 4, WPR = 8; __VA_ARGS__; }              \
-    else { constexpr int VPT = 4, WPR = 16; __VA_ARGS__; }
+#define MHCL_ROW_CASE(V, W, ...) if (p.vpt == V && p.wpr == W) { constexpr int VPT = V, WPR = W; __VA_ARGS__; }
 
 static DropArgs drop_args(float p, const uint64_t* rng) {
     DropArgs d;
@@ -277,51 +301,55 @@ static DropArgs drop_args(float p, const uint64_t* rng) {
 }
 
 int block_parts(int64_t T, int C, int sm_count) {
-    const RowPlan p = plan_row(C);
-    const int threads = p.wpr * 32 > kBlockThreads ? p.wpr * 32 : kBlockThreads, teams = threads / (p.wpr * 32);
-    const int64_t need = (T + teams - 1) / teams, cap = (int64_t)sm_count * (512 / threads);
+    const RowPlan p = plan_row(C, true);
+    const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * (512 / p.threads);
     return (int)(need < cap ? need : cap);
 }
 
 void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C);
-    const int threads = p.wpr * 32 > kBlockThreads ? p.wpr * 32 : kBlockThreads, teams = threads / (p.wpr * 32);
-    const unsigned grid = (unsigned)((T + teams - 1) / teams);
+    const RowPlan p = plan_row(c->C, false);
+    const unsigned grid = (unsigned)((T + p.teams - 1) / p.teams);
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 1;
-    MHCL_ROW_DISPATCH(p, {
-        auto k = gate ? (da.rng ? block_fwd_k<VPT, WPR, true, true> : block_fwd_k<VPT, WPR, true, false>)
-                      : (da.rng ? block_fwd_k<VPT, WPR, false, true> : block_fwd_k<VPT, WPR, false, false>);
-        k<<<grid, threads, 0, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, eps, da, (uint4*)out, rstd);
+#define MHCL_FWD(V, W)                                                                                                  \
+    MHCL_ROW_CASE(V, W, {                                                                                               \
+        auto k = gate ? (da.rng ? block_fwd_k<VPT, WPR, true, true> : block_fwd_k<VPT, WPR, true, false>)               \
+                      : (da.rng ? block_fwd_k<VPT, WPR, false, true> : block_fwd_k<VPT, WPR, false, false>);            \
+        k<<<grid, p.threads, 0, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, eps, da,    \
+                                     (uint4*)out, rstd);                                                                \
     })
+    MHCL_FWD(1, 1) MHCL_FWD(2, 1) MHCL_FWD(4, 1) MHCL_FWD(4, 2) MHCL_FWD(4, 4) MHCL_FWD(4, 8) MHCL_FWD(4, 16)
+#undef MHCL_FWD
 }
 
 void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       const float* rstd, float p_drop, const uint64_t* rng, const void* dy, void* dx, void* dgate, float* dw,
                       float* dscale, int accumulate, float* dw_part, double* ds_part, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C);
-    const int threads = p.wpr * 32 > kBlockThreads ? p.wpr * 32 : kBlockThreads, teams = threads / (p.wpr * 32);
+    const RowPlan p = plan_row(c->C, true);
     const int parts = block_parts(T, c->C, c->sm_count);
-    const size_t smem = (size_t)teams * c->C * sizeof(float);
+    const size_t smem = (size_t)p.teams * c->C * sizeof(float);
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 2;
-    MHCL_ROW_DISPATCH(p, {
-        auto k = gate ? (da.rng ? block_bwd_k<VPT, WPR, true, true> : block_bwd_k<VPT, WPR, true, false>)
-                      : (da.rng ? block_bwd_k<VPT, WPR, false, true> : block_bwd_k<VPT, WPR, false, false>);
-        if (smem > 48 * 1024) cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        k<<<parts, threads, smem, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, rstd, da,
-                                       (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, dscale ? ds_part : nullptr);
+#define MHCL_BWD(V, W)                                                                                                  \
+    MHCL_ROW_CASE(V, W, {                                                                                               \
+        auto k = gate ? (da.rng ? block_bwd_k<VPT, WPR, true, true> : block_bwd_k<VPT, WPR, true, false>)               \
+                      : (da.rng ? block_bwd_k<VPT, WPR, false, true> : block_bwd_k<VPT, WPR, false, false>);            \
+        if (smem > 48 * 1024) cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);          \
+        k<<<parts, p.threads, smem, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, rstd, da, \
+                                         (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, dscale ? ds_part : nullptr); \
     })
+    MHCL_BWD(1, 1) MHCL_BWD(2, 1) MHCL_BWD(2, 2) MHCL_BWD(2, 4) MHCL_BWD(2, 8) MHCL_BWD(2, 16) MHCL_BWD(4, 16)
+#undef MHCL_BWD
     colsum_k<<<(c->C + 31) / 32, 256, 0, s>>>(c->C, parts, dw_part, ds_part, dw, dscale, accumulate);
 }
 
 void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p, const uint64_t* rng, void* y, cudaStream_t s) {
-    const int64_t need = ((count + 7) / 8 + 255) / 256, cap = (int64_t)c->sm_count * 8 * 4;
+    const int64_t groups = (count + 7) / 8, per = 256 * kDropGroups;
     DropArgs da = drop_args(p, rng);
     da.rng = rng;                                          // read for p = 0 too (everything stays)
     c->launches += 1;
-    dropout_k<<<(unsigned)(need < cap ? need : cap), 256, 0, s>>>(count, (const __nv_bfloat16*)x, da, (__nv_bfloat16*)y);
+    dropout_k<<<(unsigned)((groups + per - 1) / per), 256, 0, s>>>(count, (const __nv_bfloat16*)x, da, (__nv_bfloat16*)y);
 }
 
 }  // namespace mhcl

@@ -57,10 +57,14 @@ __global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, 
 }
 
 // ---- stable sort of the tokens by id ---------------------------------------------------------------------------------
-// One cluster sorts (least significant digit first, 8 bits a pass): a warp owns a contiguous range of the list and counts
-// its digits without atomics, the blocks exchange their 256 totals through distributed shared memory, and each warp then
-// walks its range again and places the tokens.  A launch a pass would cost more than the pass.
-constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
+// One cluster of up to 16 blocks sorts, least significant digit first, 9 bits a pass (two passes for tables below
+// 2^18 rows): a warp owns a contiguous range of the list and counts its digits in shared memory, the blocks exchange their
+// totals through distributed shared memory, and each warp then walks its range again and places the tokens.  A range is
+// read eight vectors of 32 entries at a time, so that a pass costs a few memory latencies, which are what bounds it; a
+// launch a pass would cost more than the pass.
+
+constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBits = 9, kSortBins = 1 << kSortBits, kSortAhead = 8, kSortMaxBlocks = 16;
+constexpr int kSortSmem = kSortWarps * kSortBins * 4;
 
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -74,82 +78,115 @@ __device__ __forceinline__ uint32_t ld_peer(const uint32_t* p, uint32_t rank) { 
     return v;
 }
 
-__global__ void __launch_bounds__(kSortThreads) embed_sort_k(int64_t T, int64_t V, int passes, const int64_t* __restrict__ ids,
+// The lanes of `live` whose digit equals this lane's, by one vote a bit: a match instruction visits the distinct values one
+// after the other and took most of the sort's time (65536 tokens of 100000 rows: 59 us, now 27).
+__device__ __forceinline__ uint32_t same_digit(uint32_t live, uint32_t d) {
+    uint32_t m = live;
+#pragma unroll
+    for (int i = 0; i < kSortBits; ++i) {
+        const uint32_t set = (uint32_t)((int32_t)(d << (31 - i)) >> 31);       // all ones where the bit is set
+        m &= ~(__ballot_sync(live, set) ^ set);
+    }
+    return m;
+}
+
+__global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, int passes, const int64_t* __restrict__ ids,
                                                              uint2* buf0, uint2* buf1, uint32_t* mask, int* __restrict__ status) {
-    __shared__ uint32_t cnt[kSortWarps][256];
-    __shared__ uint32_t tot[256], off[256], wsum[8];
+    extern __shared__ uint32_t cnt[];                          // [warp][bin]
+    __shared__ uint32_t tot[kSortBins], off[kSortBins], wsum[kSortBins / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t me = cluster_rank(), nb = cluster_size();
-    const int64_t per = ((T + (int64_t)nb * kSortWarps - 1) / ((int64_t)nb * kSortWarps) + 31) / 32 * 32;
-    const int64_t i0 = ((int64_t)me * kSortWarps + warp) * per, i1 = i0 + per < T ? i0 + per : T;
+    const int me = (int)cluster_rank(), nb = (int)cluster_size();
+    const int warps = nb * kSortWarps, per = ((T - 1) / warps / 32 + 1) * 32;                  // entries a warp, a multiple of 32
+    const int64_t begin = (int64_t)(me * kSortWarps + warp) * per;
+    const int i0 = begin < T ? (int)begin : T, i1 = T - i0 < per ? T : i0 + per;
+    uint32_t* mine = cnt + warp * kSortBins;
     for (int64_t w = (int64_t)me * kSortThreads + tid; w < (V + 31) / 32; w += (int64_t)nb * kSortThreads) mask[w] = 0;
     uint2 *src = buf0, *dst = buf1;
     for (int p = 0; p < passes; ++p) {
-        for (int i = tid; i < kSortWarps * 256; i += kSortThreads) cnt[0][i] = 0;
+        const int shift = p * kSortBits;
+        for (int i = tid; i < kSortWarps * kSortBins / 4; i += kSortThreads) reinterpret_cast<uint4*>(cnt)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-        for (int64_t b = i0; b < i1; b += 32) {
-            const bool in = b + lane < i1;
-            uint32_t key = 0;
-            if (in) {
-                if (p == 0) {
-                    const int64_t id = ids[b + lane];
-                    const bool ok = id >= 0 && id < V;
-                    if (!ok) report_index(status, MHCLITE_OP_EMBED_BWD, b + lane, id);
-                    key = ok ? (uint32_t)id : (uint32_t)V;     // tokens without a row go last
-                    src[b + lane] = make_uint2(key, (uint32_t)(b + lane));
-                } else {
-                    key = __ldcg(src + b + lane).x;
+        for (int b = i0; b < i1; b += 32 * kSortAhead) {
+            uint32_t key[kSortAhead];
+#pragma unroll
+            for (int k = 0; k < kSortAhead; ++k) {
+                const int i = b + k * 32 + lane;
+                if (i < i1) {
+                    if (p == 0) {
+                        const int64_t id = ids[i];
+                        const bool ok = id >= 0 && id < V;
+                        if (!ok) report_index(status, MHCLITE_OP_EMBED_BWD, i, id);
+                        key[k] = ok ? (uint32_t)id : (uint32_t)V;      // tokens without a row go last
+                    } else {
+                        key[k] = __ldcg(src + i).x;
+                    }
                 }
             }
-            const uint32_t live = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const uint32_t d = (key >> (8 * p)) & 255u, peers = __match_any_sync(live, d);
-                if (lane == __ffs(peers) - 1) cnt[warp][d] += __popc(peers);
+#pragma unroll
+            for (int k = 0; k < kSortAhead; ++k) {
+                const int i = b + k * 32 + lane;
+                if (i < i1) {
+                    if (p == 0) src[i] = make_uint2(key[k], (uint32_t)i);
+                    atomicAdd(mine + ((key[k] >> shift) & (kSortBins - 1)), 1u);
+                }
             }
-            __syncwarp();
         }
         __syncthreads();
-        if (tid < 256) {                                       // the warps' counts become offsets within the block
+        if (tid < kSortBins) {                                 // the warps' counts become offsets within the block
             uint32_t run = 0;
-            for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = cnt[w][tid]; cnt[w][tid] = run; run += c; }
+#pragma unroll 16
+            for (int w = 0; w < kSortWarps; ++w) { const uint32_t c = cnt[w * kSortBins + tid]; cnt[w * kSortBins + tid] = run; run += c; }
             tot[tid] = run;
         }
         cluster_sync_all();
-        uint32_t before = 0, all = 0;
-        if (tid < 256) {
-            for (uint32_t r = 0; r < nb; ++r) { const uint32_t c = ld_peer(&tot[tid], r); if (r < me) before += c; all += c; }
-            uint32_t inc = all;                                // inclusive scan over the digits
+        uint32_t before = 0, all = 0, inc = 0;
+        if (tid < kSortBins) {
+            for (int r0 = 0; r0 < nb; r0 += 8) {
+                uint32_t c[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r) c[r] = r0 + r < nb ? ld_peer(&tot[tid], r0 + r) : 0;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) { if (r0 + r < me) before += c[r]; all += c[r]; }
+            }
+            inc = all;                                         // inclusive scan over the digits
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) { const uint32_t u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
             if (lane == 31) wsum[warp] = inc;
-            off[tid] = inc - all + before;
         }
         __syncthreads();
-        if (tid < 256) {
+        if (tid < kSortBins) {
             uint32_t add = 0;
-            for (int w = 0; w < warp; ++w) add += wsum[w];
-            off[tid] += add;
+#pragma unroll
+            for (int w = 0; w < kSortBins / 32; ++w) add += w < warp ? wsum[w] : 0;
+            off[tid] = inc - all + before + add;
         }
         __syncthreads();
-        for (int64_t b = i0; b < i1; b += 32) {
-            const bool in = b + lane < i1;
-            const uint32_t live = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const uint2 kv = __ldcg(src + b + lane);
-                const uint32_t d = (kv.x >> (8 * p)) & 255u, peers = __match_any_sync(live, d);
-                const uint32_t rank = __popc(peers & ((1u << lane) - 1u)), base = off[d] + cnt[warp][d];
-                __syncwarp(live);
-                if (rank == 0) cnt[warp][d] += __popc(peers);
-                if (p == 0) {                                  // one lane an id marks its row
-                    const uint32_t same = __match_any_sync(live, kv.x);
-                    if (kv.x < V && lane == __ffs(same) - 1) atomicOr(mask + (kv.x >> 5), 1u << (kv.x & 31));
+        for (int b = i0; b < i1; b += 32 * kSortAhead) {
+            uint2 kv[kSortAhead];
+#pragma unroll
+            for (int k = 0; k < kSortAhead; ++k)
+                if (b + k * 32 + lane < i1) kv[k] = __ldcg(src + b + k * 32 + lane);
+#pragma unroll
+            for (int k = 0; k < kSortAhead; ++k) {
+                if (b + k * 32 >= i1) break;
+                const bool in = b + k * 32 + lane < i1;
+                const uint32_t live = __ballot_sync(0xffffffffu, in);
+                if (in) {
+                    const uint32_t d = (kv[k].x >> shift) & (kSortBins - 1), peers = same_digit(live, d);
+                    const uint32_t rank = __popc(peers & ((1u << lane) - 1u)), base = mine[d];
+                    __syncwarp(live);
+                    if (rank == 0) mine[d] = base + __popc(peers);
+                    __stcg(dst + off[d] + base + rank, kv[k]);
                 }
-                __stcg(dst + base + rank, kv);
+                __syncwarp();
             }
-            __syncwarp();
         }
         uint2* h = src; src = dst; dst = h;
         cluster_sync_all();
+    }
+    for (int i = i0 + lane; i < i1; i += 32) {                 // the first entry of an id marks its row
+        const uint32_t key = __ldcg(src + i).x, prev = i > 0 ? __ldcg(src + i - 1).x : 0xFFFFFFFFu;
+        if (key != prev && key < V) atomicOr(mask + (key >> 5), 1u << (key & 31));
     }
 }
 
@@ -234,52 +271,83 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int C,
     }
 }
 
-// The ids that span chunks: the block of the chunk in which such an id begins adds its partial rows, eight ranges of
-// them side by side and then in order.
-__global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C, int R, const uint2* __restrict__ list,
-                                                    const float* __restrict__ own, const float* __restrict__ cont, float scale,
-                                                    float* __restrict__ dE, int accumulate) {
-    __shared__ float4 red[8][32][2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
-    const int64_t chunk = blockIdx.x, p0 = chunk * R, p1 = p0 + R;
-    if (p1 >= T) return;
-    const uint32_t key = __ldg(&list[p1 - 1].x);
-    if (key >= V || __ldg(&list[p1].x) != key) return;                              // nothing goes on into the next chunk
-    if (p0 > 0 && __ldg(&list[p0].x) == key && __ldg(&list[p0 - 1].x) == key) return;   // it began in an earlier chunk
-    int64_t lo = p1, hi = T;                                                        // first entry behind the id
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (__ldg(&list[mid].x) <= key) lo = mid + 1; else hi = mid;
-    }
-    const int64_t c1 = (lo - 1) / R, parts = c1 - chunk;                            // chunks chunk + 1 .. c1 hold the rest
-    const int64_t per = (parts + 7) / 8, a0 = chunk + 1 + warp * per, a1 = a0 + per < c1 + 1 ? a0 + per : c1 + 1;
-    const int v = blockIdx.y * 32 + lane;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-    if (v < nv) {
+// The ids that span chunks: the warp of the chunk in which such an id begins adds up its partial rows; ids of more than
+// kJoinAlone parts are shared out among the block's warps, a range of the parts each, joined in order.
+constexpr int kJoinAlone = 16;
+__device__ __forceinline__ void add4(float4& a, const float4& x) { a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w; }
+__device__ __forceinline__ void join_sum(const float* __restrict__ part, int64_t c0, int64_t c1, int C, int v, float4& a, float4& b) {
 #pragma unroll 4
-        for (int64_t c = a0; c < a1; ++c) {
-            const float4* q = (const float4*)(cont + c * C + v * 8);
-            const float4 x = __ldg(q), y = __ldg(q + 1);
-            a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-            b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
-        }
+    for (int64_t c = c0; c < c1; ++c) {
+        const float4* q = (const float4*)(part + c * C + v * 8);
+        add4(a, __ldg(q));
+        add4(b, __ldg(q + 1));
     }
-    red[warp][lane][0] = a;
-    red[warp][lane][1] = b;
-    __syncthreads();
-    if (warp != 0 || v >= nv) return;
-    const float4* q = (const float4*)(own + chunk * C + v * 8);
-    a = __ldg(q); b = __ldg(q + 1);
-    for (int w = 0; w < 8; ++w) {
-        const float4 x = red[w][lane][0], y = red[w][lane][1];
-        a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
-        b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
-    }
+}
+__device__ __forceinline__ void join_store(float* dE, uint32_t key, int C, int v, float scale, int accumulate, const float4& a, const float4& b) {
     float4* o = (float4*)(dE + (int64_t)key * C + v * 8);
     float4 s0 = accumulate ? o[0] : make_float4(0.f, 0.f, 0.f, 0.f), s1 = accumulate ? o[1] : s0;
     s0.x += scale * a.x; s0.y += scale * a.y; s0.z += scale * a.z; s0.w += scale * a.w;
     s1.x += scale * b.x; s1.y += scale * b.y; s1.z += scale * b.z; s1.w += scale * b.w;
     o[0] = s0; o[1] = s1;
+}
+__global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C, int R, const uint2* __restrict__ list,
+                                                    const float* __restrict__ own, const float* __restrict__ cont, float scale,
+                                                    float* __restrict__ dE, int accumulate) {
+    __shared__ float4 red[8][32][2];
+    __shared__ int64_t first_s[8], end_s[8];
+    __shared__ uint32_t key_s[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
+    const int64_t chunk = (int64_t)blockIdx.x * 8 + warp, p0 = chunk * R, p1 = p0 + R;
+    const int v = blockIdx.y * 32 + lane;
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lane == 0) end_s[warp] = 0;
+    if (p1 < T) {
+        const int64_t at[4] = {p1 - 1, p1, p0, p0 > 0 ? p0 - 1 : p0};                // one load for the four
+        const uint32_t mine = __ldg(&list[at[lane & 3]].x);
+        const uint32_t key = __shfl_sync(0xffffffffu, mine, 0), next = __shfl_sync(0xffffffffu, mine, 1);
+        const uint32_t head = __shfl_sync(0xffffffffu, mine, 2), prev = __shfl_sync(0xffffffffu, mine, 3);
+        const bool began_before = p0 > 0 && head == key && prev == key;
+        if (key < V && next == key && !began_before) {
+            int64_t lo = p1, hi = T;                           // the first entry behind the id lies in (lo, hi]
+            while (hi - lo > 1) {
+                const int64_t step = (hi - lo + 31) / 32, probe = lo + lane * step;
+                const uint32_t same = __ballot_sync(0xffffffffu, probe < hi && __ldg(&list[probe < hi ? probe : lo].x) == key);
+                const int n = __popc(same);                    // probes 0 .. n-1 are of the id (probe 0 is)
+                const int64_t l = lo + (int64_t)(n - 1) * step;
+                hi = l + step < hi ? l + step : hi;
+                lo = l;
+            }
+            const int64_t c1 = lo / R + 1;                     // chunks chunk + 1 .. c1 - 1 hold the rest
+            if (c1 - chunk - 1 <= kJoinAlone) {
+                if (v < nv) {
+                    float4 a = zero, b = zero;
+                    join_sum(own, chunk, chunk + 1, C, v, a, b);
+                    join_sum(cont, chunk + 1, c1, C, v, a, b);
+                    join_store(dE, key, C, v, scale, accumulate, a, b);
+                }
+            } else if (lane == 0) {
+                first_s[warp] = chunk; end_s[warp] = c1; key_s[warp] = key;
+            }
+        }
+    }
+    __syncthreads();
+    for (int j = 0; j < 8; ++j) {
+        const int64_t c1 = end_s[j], c0 = first_s[j] + 1;
+        if (c1 == 0) continue;
+        const int64_t per = (c1 - c0 + 7) / 8, a0 = c0 + warp * per, a1 = a0 + per < c1 ? a0 + per : c1;
+        float4 a = zero, b = zero;
+        if (v < nv) join_sum(cont, a0, a1, C, v, a, b);
+        red[warp][lane][0] = a;
+        red[warp][lane][1] = b;
+        __syncthreads();
+        if (warp == 0 && v < nv) {
+            a = b = zero;
+            join_sum(own, c0 - 1, c0, C, v, a, b);
+            for (int w = 0; w < 8; ++w) { add4(a, red[w][lane][0]); add4(b, red[w][lane][1]); }
+            join_store(dE, key_s[j], C, v, scale, accumulate, a, b);
+        }
+        __syncthreads();
+    }
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
@@ -323,28 +391,36 @@ cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const i
     const EmbedScratch p = plan_embed(T, V, c->C, scratch);
     int bits = 1;
     while ((V >> bits) != 0) ++bits;                           // keys run to V
-    const int passes = (bits + 7) / 8;
-    int nb = 1;                                                // blocks of the cluster: about 256 tokens a warp at most
-    while (nb < 8 && T > (int64_t)nb * kSortWarps * 64) nb *= 2;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(nb);
-    cfg.blockDim = dim3(kSortThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = nb; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
+    const int passes = (bits + kSortBits - 1) / kSortBits;
+    int nb = 1;                                                // blocks of the cluster: 64 tokens a warp, then more blocks
+    while (nb < kSortMaxBlocks && T > (int64_t)nb * kSortWarps * 64) nb *= 2;
+    cudaFuncSetAttribute(embed_sort_k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem);
+    cudaFuncSetAttribute(embed_sort_k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     c->launches += 3;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, embed_sort_k, T, V, passes, ids, p.buf0, p.buf1, p.mask, c->op_status);
-    if (e != cudaSuccess) return e;
+    cudaError_t e;
+    for (;; nb /= 2) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(nb);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = kSortSmem;
+        cfg.stream = s;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = nb; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, embed_sort_k, (int)T, V, passes, ids, p.buf0, p.buf1, p.mask, c->op_status);
+        if (e == cudaSuccess) break;
+        if (nb <= 8) return e;                                 // clusters beyond 8 blocks need not exist on every device
+        cudaGetLastError();
+    }
     const uint2* list = (passes & 1) ? p.buf1 : p.buf0;
     const int R = embed_chunk(T, c->C), slices = (c->C / 8 + 31) / 32;
     const int64_t chunks = (T + R - 1) / R, sum_blocks = (chunks * slices + 7) / 8;
     const int64_t zero_blocks = accumulate ? 0 : ((V + 7) / 8 < c->sm_count * 8 ? (V + 7) / 8 : c->sm_count * 8);
     MHCL_DISPATCH_N(c->n, embed_grad_k<N_><<<(unsigned)(sum_blocks + zero_blocks), 256, 0, s>>>(
         T, V, c->C, R, sum_blocks, slices, list, p.mask, (const uint4*)g, scale, dE, p.own, p.cont, accumulate))
-    embed_join_k<<<dim3((unsigned)chunks, (unsigned)slices), 256, 0, s>>>(T, V, c->C, R, list, p.own, p.cont, scale, dE, accumulate);
+    embed_join_k<<<dim3((unsigned)((chunks + 7) / 8), (unsigned)slices), 256, 0, s>>>(T, V, c->C, R, list, p.own, p.cont, scale, dE, accumulate);
     return cudaGetLastError();
 }
 
