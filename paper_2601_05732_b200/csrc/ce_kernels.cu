@@ -38,6 +38,8 @@ struct CeArgs {
     int C;
     int v0, vn;                 // the piece: rows v0 .. v0 + vn of W (vn a multiple of 256 except for the last piece)
     int m_tiles, n_tiles;       // at most; m_tiles of the row-wise modes is cut to `live` on the device
+    int a_box;                  // rows of A that a copy brings in (128; fewer for a handful of tokens)
+    int splits;                 // CE_DH: ranges of the vocabulary that are added up apart
     float scale;
     // CE_STATS
     float2* part;               // [2 n_tiles][Tpad] (maximum, sum) in base 2 of 128 columns each
@@ -51,7 +53,7 @@ struct CeArgs {
     __nv_bfloat16* G;           // [Tpad][pitch]
     int64_t pitch;
     // CE_DH
-    float* dh_acc;              // [Tpad][C] sums over the pieces so far
+    float* dh_acc;              // [splits][Tpad][C] sums over the pieces so far
     __nv_bfloat16* dh;          // [T][C]
     int first, last;
     // CE_DW
@@ -143,7 +145,8 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     volatile int* abort = ctl->abort;
     const int live = *a.live;
-    const int mt = MODE == CE_DW ? a.m_tiles : (live + kCeM - 1) / kCeM, nt = a.n_tiles, tiles = mt * nt;
+    const int mt = MODE == CE_DW ? a.m_tiles : (live + kCeM - 1) / kCeM, nt = a.n_tiles, per = mt * nt;
+    const int splits = MODE == CE_DH ? a.splits : 1, tiles = per * splits;
     const int ksize = MODE == CE_DW ? live : MODE == CE_DH ? a.vn : a.C;
     const int ksteps = (ksize + kCeK - 1) / kCeK;
 
@@ -169,19 +172,24 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
             int it = 0;
             bool ok = true;
             for (int i = pair; i < tiles && ok; i += pairs) {
+                const int split = MODE == CE_DH ? i / per : 0;
                 int m, n;
-                ce_tile(i, mt, nt, m, n);
+                ce_tile(i - split * per, mt, nt, m, n);
                 const int am = m * kCeM + (int)rank * kCeHalf, bn = n * kCeN + (int)rank * kCeHalf;
-                for (int k = 0; k < ksteps; ++k, ++it) {
+                // rows behind the list are not copied: what their half of the accumulator then holds is not read
+                const int a_bytes = A_MN ? kCeABytes : a.a_box * 128;
+                const bool a_second = A_MN || m * kCeM + kCeHalf < live;
+                const int k1 = (int)((int64_t)ksteps * (split + 1) / splits);
+                for (int k = (int)((int64_t)ksteps * split / splits); k < k1; ++k, ++it) {
                     const int s = it % kCeStages;
                     ok = ce_wait(smem_u32(&ctl->empty[s]), ((it / kCeStages) & 1) ^ 1, abort, 1, it);
                     if (!ok) break;
                     const uint32_t own = smem_u32(&ctl->full[s]), full = leader_addr(own);
                     const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
-                    if (rank == 0) mbar_expect_tx(own, 2 * kCeStage);          // the bytes of both CTAs
+                    if (rank == 0) mbar_expect_tx(own, 2 * kCeABytes + (a_second ? 2 : 1) * a_bytes);      // of both CTAs
                     if (A_MN) {
                         for (int b = 0; b < kCeHalf / 64; ++b) tma_load_2d_pair(sa + b * 8192, &tma, full, am + b * 64, k * kCeK);
-                    } else {
+                    } else if (rank == 0 || a_second) {
                         tma_load_2d_pair(sa, &tma, full, k * kCeK, am);
                     }
                     if (B_MN) {
@@ -206,7 +214,9 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 ok = ce_wait(smem_u32(&ctl->acc_empty[buf]), ((j >> 1) & 1) ^ 1, abort, 2, j);
                 if (!ok) break;
                 tc_fence_after();
-                for (int k = 0; k < ksteps; ++k, ++it) {
+                const int split = MODE == CE_DH ? i / per : 0;
+                const int k0 = (int)((int64_t)ksteps * split / splits), k1 = (int)((int64_t)ksteps * (split + 1) / splits);
+                for (int k = k0; k < k1; ++k, ++it) {
                     const int s = it % kCeStages;
                     ok = ce_wait(smem_u32(&ctl->full[s]), (it / kCeStages) & 1, abort, 3, it);
                     if (!ok) break;
@@ -216,7 +226,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                     for (int kk = 0; kk < kCeK / 16; ++kk) {
                         const uint64_t ad = A_MN ? smem_desc(sa + kk * 2048, 8192, 1024, 2) : smem_desc(sa + kk * 32, 16, 1024, 2);
                         const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, 8192, 1024, 2) : smem_desc(sb + kk * 32, 16, 1024, 2);
-                        tc_mma_pair(tmem + buf * kCeN, ad, bd, idesc, (k > 0 || kk > 0) ? 1u : 0u);
+                        tc_mma_pair(tmem + buf * kCeN, ad, bd, idesc, (k > k0 || kk > 0) ? 1u : 0u);
                     }
                     tc_commit_pair(smem_u32(&ctl->empty[s]));
                 }
@@ -233,8 +243,9 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
+            const int split = MODE == CE_DH ? i / per : 0;
             int m, n;
-            ce_tile(i, mt, nt, m, n);
+            ce_tile(i - split * per, mt, nt, m, n);
             const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
             const int n0 = n * kCeN + half * kCeHalf;           // this warp's 128 columns
             const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN + half * kCeHalf;
@@ -290,35 +301,43 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 const bool in = MODE == CE_DH ? r < live : r < a.vn;
                 const int64_t orow = MODE == CE_DH ? (in ? a.rows[r] : 0) : a.v0 + r;
                 const float f = a.scale * ce_ref(a.ref);
+                // no row has a target, or a short last piece has fewer K steps than ranges
+                const bool empty = (int64_t)ksteps * split / splits == (int64_t)ksteps * (split + 1) / splits;
 #pragma unroll 1
                 for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                     float v[32];
                     tc_ld32(acc + c0, v);
                     const int c = n0 + c0;
                     if (!in) continue;
-                    if (MODE == CE_DW && ksteps == 0) {                 // no row has a target: nothing was accumulated
+                    if (empty) {                                        // nothing was accumulated
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
                     }
+                    if (MODE == CE_DH && (splits > 1 || !a.first || !a.last)) {
+                        float* p = a.dh_acc + ((int64_t)split * a.Tpad + r) * a.C + c;
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        if (c + e >= a.C) continue;
-                        if (MODE == CE_DH) {
-                            float4* p = (float4*)(a.dh_acc + (int64_t)r * a.C + c + e);
+                        for (int e = 0; e < 32; e += 8) {
+                            if (c + e >= a.C) continue;
                             if (!a.first) {
-                                const float4 x = p[0], y = p[1];
+                                const float4 x = *(const float4*)(p + e), y = *(const float4*)(p + e + 4);
                                 v[e] += x.x; v[e + 1] += x.y; v[e + 2] += x.z; v[e + 3] += x.w;
                                 v[e + 4] += y.x; v[e + 5] += y.y; v[e + 6] += y.z; v[e + 7] += y.w;
                             }
-                            if (!a.last) {
-                                p[0] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                                p[1] = make_float4(v[e + 4], v[e + 5], v[e + 6], v[e + 7]);
-                                continue;
-                            }
+                            if (splits > 1 || !a.last) st32(p + e, *(const uint4*)(v + e), *(const uint4*)(v + e + 4));
                         }
+                        if (splits > 1 || !a.last) continue;
+                    }
+                    __nv_bfloat16* out = (MODE == CE_DH ? a.dh : a.dW) + orow * a.C + c;
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) v[e + x] *= f;
-                        *reinterpret_cast<uint4*>((MODE == CE_DH ? a.dh : a.dW) + orow * a.C + c + e) = pack8(v + e);
+                    for (int e = 0; e < 32; ++e) v[e] *= f;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 16) {
+                        if (c + e + 16 <= a.C && (a.C & 15) == 0) {     // whole sectors
+                            st32(out + e, pack8(v + e), pack8(v + e + 8));
+                        } else {
+                            if (c + e < a.C) *reinterpret_cast<uint4*>(out + e) = pack8(v + e);
+                            if (c + e + 8 < a.C) *reinterpret_cast<uint4*>(out + e + 8) = pack8(v + e + 8);
+                        }
                     }
                 }
             }
@@ -347,8 +366,8 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 // ---- rows with a target ----------------------------------------------------------------------------------------------
 // Block b handles `per` tokens: counts the targets before them, numbers its own rows, copies their h side by side, and
 // clears the outputs of the rows without a target (loss and lse, or dh).  In the backward it also joins the
-// largest finite |dloss| of its rows (as bits: a maximum does not depend on the order).  The last block pads the list's h
-// with zero rows to the next multiple of 256, which the products read.
+// largest finite |dloss| of its rows (as bits: a maximum does not depend on the order).  The last block pads the
+// list's h with zero rows to the next multiple of 64, the K step of G^T h.
 __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* __restrict__ target,
                                                   const uint4* __restrict__ h, uint4* __restrict__ hl, int* __restrict__ rows,
                                                   int* __restrict__ live, float* __restrict__ loss, float* __restrict__ lse,
@@ -405,22 +424,22 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
     }
     if (t1 == T) {
         if (tid == 0) *live = base;
-        const int pad = min(Tpad, (base + kCeM - 1) / kCeM * kCeM);
+        const int pad = dloss ? min(Tpad, (base + kCeK - 1) / kCeK * kCeK) : base;
         for (int64_t i = tid; i < (int64_t)(pad - base) * nv; i += 1024) hl[(int64_t)base * nv + i] = make_uint4(0, 0, 0, 0);
     }
 }
 
-// Joins the (maximum, sum) pairs of a row: 32 rows a block, eight ranges of tiles side by side.
-__global__ void __launch_bounds__(256) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_parts, int Tpad,
-                                                 const float2* __restrict__ part, const float* __restrict__ tlogit,
-                                                 float* __restrict__ loss, float* __restrict__ lse) {
-    __shared__ float2 red[8][32];
+// Joins the (maximum, sum) pairs of a row: 32 rows a block, 32 ranges of tiles side by side.
+__global__ void __launch_bounds__(1024) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_parts, int Tpad,
+                                                  const float2* __restrict__ part, const float* __restrict__ tlogit,
+                                                  float* __restrict__ loss, float* __restrict__ lse) {
+    __shared__ float2 red[32][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = *live;
+    if (blockIdx.x * 32 >= n) return;
     float m = -INFINITY, s = 0.f;
     if (r < n) {
-        const int per = (n_parts + 7) / 8, n1 = min(n_parts, (warp + 1) * per);
-#pragma unroll 4
-        for (int k = warp * per; k < n1; ++k) {
+#pragma unroll 8
+        for (int k = warp; k < n_parts; k += 32) {
             const float2 p = part[(int64_t)k * Tpad + r];
             const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
             s = s * ex2(m - base) + p.y * ex2(p.x - base);
@@ -432,22 +451,210 @@ __global__ void __launch_bounds__(256) ce_join_k(const int* __restrict__ live, c
     if (warp != 0 || r >= n) return;
     float top = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) top = fmaxf(top, red[w][lane].x);
+    for (int w = 0; w < 32; ++w) top = fmaxf(top, red[w][lane].x);
     const float base = top == -INFINITY ? 0.f : top;
     s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
+    for (int w = 0; w < 32; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
     const float l = (top + lg2(s)) * kLn2;
     const int t = rows[r];
     lse[t] = l;
     loss[t] = l - tlogit[r];
 }
 
+// dh of the rows whose vocabulary was added up in several ranges: the ranges in order, eight channels a thread.
+__global__ void __launch_bounds__(256) ce_dh_join_k(const int* __restrict__ live, const int* __restrict__ rows, int C, int Tpad, int splits,
+                                                    const float* __restrict__ acc, const uint32_t* __restrict__ ref, float scale,
+                                                    __nv_bfloat16* __restrict__ dh) {
+    const int nv = C >> 3, n = *live;
+    const float f = scale * ce_ref(ref);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * nv; i += (int64_t)gridDim.x * 256) {
+        const int r = (int)(i / nv), c = (int)(i - (int64_t)r * nv) * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = (const float4*)(acc + ((int64_t)s * Tpad + r) * C + c);
+            const float4 x = __ldg(p), y = __ldg(p + 1);
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= f;
+        *reinterpret_cast<uint4*>(dh + (int64_t)rows[r] * C + c) = pack8(v);
+    }
+}
+
+// ---- a handful of tokens ---------------------------------------------------------------------------------------------
+// Forward for up to 32 tokens: the weights are read once and everything else is small, so the kernel is a stream over W.
+// The 256-row tiles above leave it waiting: ten microseconds to start and drain, and whole rounds of tiles.  Here a CTA
+// takes 16 (32, 64 for short rows) rows of W at a time (m16n8k16 with the rows of W as M and the tokens as N) and its 16
+// warps share the channels.  A lane takes 16 bytes of a row and uses them as the operands of two products: the sum over k
+// does not mind the order, as long as h is taken in the same one.  So each lane copies (cp.async) just the bytes that it
+// will multiply, STAGES - 1 steps of 32 KB a CTA ahead, and nothing about W is exchanged or waited for between warps.  h
+// stays in shared memory; the warps' partial logits meet there, and a thread keeps the running (maximum, sum) of one (row
+// slot, token) over the CTA's rows.
+// One token, 2048 channels, 50257 words: 45 us, against 62 with the tiles, 51 with one step ahead in registers and 61
+// with bulk copies of a row piece each, of which the copy engine starts too few.
+constexpr int kSmWarps = 16, kSmThreads = kSmWarps * 32, kSmTokens = 32;
+
+// WK (4, 8 or 16) warps share the channels of a row, 64 of them each a step; WR = 16 / WK groups of 16 rows a unit; NB
+// blocks of 8 tokens.
+template <int NB, int STAGES>
+__global__ void __launch_bounds__(kSmThreads, 1)
+ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, const uint4* __restrict__ W,
+           const int64_t* __restrict__ target, float scale, float2* __restrict__ part, float* __restrict__ tlogit) {
+    extern __shared__ __align__(16) unsigned char sm_raw[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+    const int WK = 1 << wk_log, WR = kSmWarps >> wk_log, wk = warp & (WK - 1), wr = warp >> wk_log;
+    const int KB = 64 * WK, blocks = (C + KB - 1) / KB, nv = C >> 3, rows = 16 * WR;
+    const int hpitch = blocks * KB * 2 + 64;                               // 64 more: rows of h meet different banks
+    const uint32_t ring = smem_u32(sm_raw) + tid * 16;                     // [STAGES][4][thread] of 16 bytes
+    unsigned char* hs = sm_raw + STAGES * 4 * kSmThreads * 16;             // [8 NB][hpitch]
+    float* red = reinterpret_cast<float*>(hs + 8 * NB * hpitch);           // [2][16 warps][NB][4][32]
+    const int64_t units = (V + rows - 1) / rows;
+    const int steps = (int)((units - blockIdx.x + gridDim.x - 1) / gridDim.x) * blocks;
+
+    auto fetch = [&](int st) {                                             // 2 chunks of 32 channels of rows g and g + 8
+        if (st < steps) {
+            const int64_t unit = blockIdx.x + (int64_t)(st / blocks) * gridDim.x;
+            int64_t r0 = unit * rows + wr * 16 + g, r1 = r0 + 8;           // rows behind the table are read twice, not joined
+            if (r0 >= V) r0 = V - 1;
+            if (r1 >= V) r1 = V - 1;
+            const int v = ((st % blocks) * KB + wk * 64) / 8 + t4;
+            const uint32_t to = ring + (st % STAGES) * (4 * kSmThreads * 16);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const bool in = v + c * 4 < nv;
+                const int at = in ? v + c * 4 : 0;
+                cp_async16(to + (2 * c) * (kSmThreads * 16), W + r0 * nv + at, in ? 16 : 0);
+                cp_async16(to + (2 * c + 1) * (kSmThreads * 16), W + r1 * nv + at, in ? 16 : 0);
+            }
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int st = 0; st < STAGES - 1; ++st) fetch(st);
+    for (int i = tid; i < 8 * NB * (hpitch / 16); i += kSmThreads) {
+        const int r = i / (hpitch / 16), v = i - r * (hpitch / 16);
+        *reinterpret_cast<uint4*>(hs + r * hpitch + v * 16) = (r < T && v < nv) ? __ldg(h + (int64_t)r * nv + v) : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+    constexpr int kElems = 128 * NB;                                       // logits of a group: 16 rows x 8 NB tokens
+    const int elems = kElems * WR;                                         // at most 512 NB: NB of them a thread
+    float mx[NB], sum[NB], acc[NB][4];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) { mx[i] = -INFINITY; sum[i] = 0.f; }
+    for (int st = 0; st < steps; ++st) {
+        const int b = st % blocks, u = st / blocks;
+        if (b == 0)
+#pragma unroll
+            for (int i = 0; i < NB; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+        cp_async_wait<STAGES - 2>();
+        fetch(st + STAGES - 1);                                            // into the slot of step st - 1
+        const uint32_t wp = ring + (st % STAGES) * (4 * kSmThreads * 16);
+        const uint32_t hp = smem_u32(hs) + g * hpitch + (b * KB + wk * 64) * 2 + t4 * 16;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const uint4 lo = lds128(wp + (2 * c) * (kSmThreads * 16)), hi = lds128(wp + (2 * c + 1) * (kSmThreads * 16));
+#pragma unroll
+            for (int i = 0; i < NB; ++i) {
+                const uint4 x = lds128(hp + i * 8 * hpitch + c * 64);
+                mma_bf16(acc[i], {lo.x, hi.x, lo.y, hi.y}, x.x, x.y);
+                mma_bf16(acc[i], {lo.z, hi.z, lo.w, hi.w}, x.z, x.w);
+            }
+        }
+        if (b + 1 < blocks) continue;
+        float* mine = red + ((u & 1) * kSmWarps + warp) * kElems;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine[(i * 4 + e) * 32 + lane] = acc[i][e];
+        __syncthreads();
+        const int64_t unit = blockIdx.x + (int64_t)u * gridDim.x;
+        const float k2 = scale * kLog2e;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const int x = tid + j * kSmThreads;
+            if (x >= elems) break;
+            const int er = x / kElems, y = x - er * kElems, l = y & 31, e = (y >> 5) & 3, i = y >> 7;
+            const float* p = red + ((u & 1) * kSmWarps + er * WK) * kElems + y;
+            float v = 0.f;
+#pragma unroll 4
+            for (int w = 0; w < WK; ++w) v += p[w * kElems];
+            const int64_t row = unit * rows + er * 16 + (l >> 2) + (e >> 1) * 8;
+            const int tok = i * 8 + (l & 3) * 2 + (e & 1);
+            if (row >= V) continue;
+            if (tok < T && row == target[tok]) tlogit[tok] = v * scale;
+            v *= k2;
+            const float top = fmaxf(mx[j], v), base = top == -INFINITY ? 0.f : top;
+            sum[j] = sum[j] * ex2(mx[j] - base) + ex2(v - base);
+            mx[j] = top;
+        }
+    }
+    __syncthreads();
+    float2* fin = reinterpret_cast<float2*>(red);                      // [elems]
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        if (tid + j * kSmThreads < elems) fin[tid + j * kSmThreads] = make_float2(mx[j], sum[j]);
+    __syncthreads();
+    if (tid < 8 * NB && tid < T) {                                     // a token's 16 WR row slots
+        const int i = tid >> 3, l3 = (tid & 7) >> 1, e0 = tid & 1;
+        float m = -INFINITY, t = 0.f;
+        for (int k = 0; k < rows; ++k) {
+            const int er = k >> 4, l = (k & 7) * 4 + l3, e = e0 + ((k >> 3) & 1) * 2;
+            const float2 p = fin[er * kElems + (i * 4 + e) * 32 + l];
+            const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+            t = t * ex2(m - base) + p.y * ex2(p.x - base);
+            m = top;
+        }
+        part[blockIdx.x * kSmTokens + tid] = make_float2(m, t);
+    }
+}
+// Joins the CTAs' pairs: a lane a token, the warps' shares of the CTAs side by side.
+__global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int parts, const float2* __restrict__ part, const float* __restrict__ tlogit,
+                                                       const int64_t* __restrict__ target, float* __restrict__ loss, float* __restrict__ lse,
+                                                       int* __restrict__ status) {
+    __shared__ float2 red[16][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float m = -INFINITY, s = 0.f;
+    asm volatile("griddepcontrol.wait;" ::: "memory");         // launched beside ce_small_k: its results from here on
+    if (lane < T) {
+#pragma unroll 10
+        for (int k = warp; k < parts; k += 16) {
+            const float2 p = part[k * kSmTokens + lane];
+            const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
+            s = s * ex2(m - base) + p.y * ex2(p.x - base);
+            m = top;
+        }
+    }
+    red[warp][lane] = make_float2(m, s);
+    __syncthreads();
+    if (warp != 0 || lane >= T) return;
+    const int64_t y = target[lane];
+    float l = 0.f, x = 0.f;
+    if (y >= 0 && y < V) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) top = fmaxf(top, red[w][lane].x);
+        const float base = top == -INFINITY ? 0.f : top;
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
+        l = (top + lg2(s)) * kLn2;
+        x = l - tlogit[lane];
+    } else if (y >= V && status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
+        status[1] = MHCLITE_OP_LINEAR_CE; status[2] = (int)y; status[3] = 0; status[4] = lane;
+    }
+    lse[lane] = l;
+    loss[lane] = x;
+}
+
 // ---- host side -------------------------------------------------------------------------------------------------------
-// Pieces of the vocabulary in the backward: G of a piece takes at most about 256 MB.
 struct CePlan {
-    int Tpad, n_tiles;
+    int Tpad, n_tiles, a_box;
     int pieces; int64_t piece;             // vocabulary rows a piece, a multiple of 256
+    int splits;                            // ranges of a piece's vocabulary in the product dh = G W
     int *live, *rows;
     uint32_t* ref;
     __nv_bfloat16* hl;
@@ -455,6 +662,39 @@ struct CePlan {
     __nv_bfloat16* G; float* dh_acc;
     size_t bytes;
 };
+// Rounds that `tiles` tiles take on the pairs of CTAs.
+constexpr int kCePairs = 74;
+static int64_t ce_rounds(int64_t tiles) { return (tiles + kCePairs - 1) / kCePairs; }
+
+// Pieces of the vocabulary in the backward.  G of a piece takes at most about 384 MB; below that, the width whose products
+// leave the fewest pairs of CTAs idle in their last rounds, in steps of K over all pieces (16384 tokens, 2048 channels,
+// 50257 words: 37 tiles a piece fill whole rounds).
+static void ce_pieces(CePlan& p, int64_t V, int C) {
+    const int64_t mt = p.Tpad / kCeM, ct = (C + kCeN - 1) / kCeN, nt = p.n_tiles;
+    int64_t most = ((int64_t)192 << 20) / p.Tpad / kCeN;
+    if (most < 1) most = 1;
+    if (most > nt) most = nt;
+    int64_t best = most, best_cost = INT64_MAX;
+    for (int64_t w = most; w > 0 && w * 2 >= most; --w) {
+        int64_t cost = 0;
+        for (int64_t v = 0; v < nt; v += w) {
+            const int64_t n = nt - v < w ? nt - v : w;
+            cost += ce_rounds(mt * n) * ((C + 63) / 64) + ce_rounds(n * ct) * (p.Tpad / 64) + ce_rounds(mt * ct) * n * 4 + 48;
+        }
+        if (cost < best_cost) { best_cost = cost; best = w; }
+    }
+    p.piece = best * kCeN;
+    p.pieces = (int)((V + p.piece - 1) / p.piece);
+    // dh has few tiles where tokens are few: its K is then split.  A split costs a pass over its partial sums, about a
+    // step of K for every 40 KB an SM pair moves.
+    p.splits = 1;
+    best_cost = INT64_MAX;
+    const int64_t ks = p.piece / kCeK;
+    for (int s = 1; s <= 64 && s * 4 <= ks; ++s) {
+        const int64_t cost = ce_rounds(mt * ct * s) * ((ks + s - 1) / s + 4) + (s > 1 ? 8 + s * (mt * ct * 2 * kCeM * kCeN * 4 / kCePairs / 40000) : 0);
+        if (cost < best_cost) { best_cost = cost; p.splits = s; }
+    }
+}
 static CePlan plan_ce(int64_t T, int64_t V, int C, int grad, void* base) {
     CePlan p;
     char* b = (char*)base;
@@ -462,28 +702,29 @@ static CePlan plan_ce(int64_t T, int64_t V, int C, int grad, void* base) {
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     p.Tpad = (int)round_up64(T > 0 ? T : 1, kCeM);
     p.n_tiles = (int)((V + kCeN - 1) / kCeN);
+    p.a_box = T < kCeHalf ? (int)round_up64(T > 0 ? T : 1, 8) : kCeHalf;
     p.live = (int*)take(256);
     p.ref = (uint32_t*)p.live + 1;
     p.rows = (int*)take((size_t)p.Tpad * 4);
     p.hl = (__nv_bfloat16*)take((size_t)p.Tpad * C * 2);
     p.part = nullptr; p.tlogit = nullptr; p.G = nullptr; p.dh_acc = nullptr;
-    p.pieces = 1; p.piece = 0;
+    p.pieces = 1; p.piece = 0; p.splits = 1;
     if (!grad) {
         p.part = (float2*)take((size_t)p.n_tiles * 2 * p.Tpad * 8);
         p.tlogit = (float*)take((size_t)p.Tpad * 4);
     } else {
-        int64_t most = ((int64_t)128 << 20) / p.Tpad / 256 * 256;
-        if (most < 256) most = 256;
-        p.pieces = (int)((V + most - 1) / most);
-        p.piece = round_up64((V + p.pieces - 1) / p.pieces, 256);
-        p.pieces = (int)((V + p.piece - 1) / p.piece);
+        ce_pieces(p, V, C);
         p.G = (__nv_bfloat16*)take((size_t)p.Tpad * p.piece * 2);
-        p.dh_acc = (float*)take(p.pieces > 1 ? (size_t)p.Tpad * C * 4 : 0);
+        p.dh_acc = (float*)take(p.pieces > 1 || p.splits > 1 ? (size_t)p.splits * p.Tpad * C * 4 : 0);
     }
     p.bytes = off;
     return p;
 }
-size_t ce_scratch_bytes(int64_t T, int64_t V, int C, int grad) { return plan_ce(T, V, C, grad, nullptr).bytes; }
+// (the few-token forward keeps a pair and a logit for each of 32 tokens and up to 256 SMs)
+size_t ce_scratch_bytes(int64_t T, int64_t V, int C, int grad) {
+    const size_t n = plan_ce(T, V, C, grad, nullptr).bytes, few = (256 + 1) * kSmTokens * 8;
+    return n > few ? n : few;
+}
 
 static void launch_ce_rows(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const int64_t* target, const void* h,
                            float* loss, float* lse, void* dh, const float* dloss, cudaStream_t s) {
@@ -498,7 +739,7 @@ static void launch_ce_rows(const mhclite_ctx* c, const CePlan& p, int64_t T, int
 template <int MODE>
 static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const CeArgs& a, cudaStream_t s) {
     constexpr int smem = kCeStages * kCeStage + (int)sizeof(CeCtl) + 1024;
-    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles;
+    const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * (MODE == CE_DH ? a.splits : 1);
     cudaFuncSetAttribute(ce_gemm_k<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     c->launches += 1;
     const int64_t pairs = tiles < c->sm_count / 2 ? tiles : c->sm_count / 2;
@@ -513,19 +754,56 @@ static bool map_mn(CUtensorMap* m, const void* p, int64_t k, int64_t mn, int64_t
     return make_tensor_map_2d(m, p, (uint64_t)mn, (uint64_t)k, (uint64_t)pitch, 64, kCeK, 128);
 }
 
+// Shape of ce_small_k; stages = 0 where it does not apply: more than 32 tokens, or rows of h so long that fewer than three
+// stages of W fit beside them.
+struct SmallPlan { int wk_log, nb, stages, smem; };
+static SmallPlan plan_small(int64_t T, int C) {
+    SmallPlan p = {2, T <= 8 ? 1 : T <= 16 ? 2 : 4, 0, 0};
+    if (T > kSmTokens) return p;
+    while ((64 << p.wk_log) < C && (1 << p.wk_log) < kSmWarps) ++p.wk_log;
+    const int64_t fixed = 8 * p.nb * (round_up64(C, 64 << p.wk_log) * 2 + 64) + 2 * kSmWarps * 128 * p.nb * 4, stage = 4 * kSmThreads * 16;
+    const int64_t fit = (226 * 1024 - fixed) / stage;
+    p.stages = fixed > 226 * 1024 || fit < 3 ? 0 : fit >= 5 ? 5 : 3;
+    p.smem = (int)(fixed + p.stages * stage);
+    return p;
+}
+
 bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
                           float* loss, float* lse, void* scratch, cudaStream_t s) {
+    const SmallPlan q = plan_small(T, c->C);
+    if (q.stages) {
+        float2* part = (float2*)scratch;                       // [CTAs][32], then the targets' logits
+        float* tlogit = (float*)(part + (size_t)c->sm_count * kSmTokens);
+        const int64_t units = (V + (256 >> q.wk_log) - 1) / (256 >> q.wk_log);
+        const int grid = (int)(units < c->sm_count ? units : c->sm_count);
+        auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5> : q.nb == 2 ? ce_small_k<2, 5> : ce_small_k<4, 5>)
+                               : (q.nb == 1 ? ce_small_k<1, 3> : q.nb == 2 ? ce_small_k<2, 3> : ce_small_k<4, 3>);
+        cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, q.smem);
+        c->launches += 2;
+        k<<<grid, kSmThreads, q.smem, s>>>((int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(1);
+        cfg.blockDim = dim3(512);
+        cfg.stream = s;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        cudaLaunchKernelEx(&cfg, ce_small_join_k, (int)T, V, grid, (const float2*)part, (const float*)tlogit, target, loss, lse, c->op_status);
+        return true;
+    }
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);
     CUtensorMap mh, mw;
-    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, kCeHalf) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
+    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, p.a_box) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
     launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, nullptr, s);
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
     a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
-    a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
+    a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
     launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
     c->launches += 1;
-    ce_join_k<<<(unsigned)(p.Tpad / 32), 256, 0, s>>>(p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
+    ce_join_k<<<(unsigned)((T + 31) / 32), 1024, 0, s>>>(p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
     return true;
 }
 
@@ -534,14 +812,14 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     const CePlan p = plan_ce(T, V, c->C, 1, scratch);
     const int C = c->C;
     CUtensorMap mh, mw, mg, mwn, mgt, mhn;
-    if (!map_k(&mh, p.hl, p.Tpad, C, C, kCeHalf) || !map_k(&mw, W, V, C, C, kCeHalf) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, kCeHalf) ||
+    if (!map_k(&mh, p.hl, p.Tpad, C, C, p.a_box) || !map_k(&mw, W, V, C, C, kCeHalf) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, p.a_box) ||
         !map_mn(&mwn, W, V, C, C) || !map_mn(&mgt, p.G, p.Tpad, p.piece, p.piece) || !map_mn(&mhn, p.hl, p.Tpad, C, C))
         return false;
     launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, dloss, s);
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
-    a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.status = c->op_status;
+    a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.a_box = p.a_box; a.splits = p.splits; a.status = c->op_status;
     for (int i = 0; i < p.pieces; ++i) {
         a.v0 = (int)(i * p.piece);
         a.vn = (int)(V - a.v0 < p.piece ? V - a.v0 : p.piece);
@@ -552,6 +830,12 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         launch_ce_gemm<CE_DW>(c, mgt, mhn, a, s);
         a.m_tiles = p.Tpad / kCeM;
         launch_ce_gemm<CE_DH>(c, mg, mwn, a, s);
+    }
+    if (p.splits > 1) {
+        const int64_t blocks = (T * (C / 8) + 255) / 256, most = (int64_t)c->sm_count * 16;
+        c->launches += 1;
+        ce_dh_join_k<<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(p.live, p.rows, C, p.Tpad, p.splits, p.dh_acc, p.ref, scale,
+                                                                               (__nv_bfloat16*)dh);
     }
     return true;
 }

@@ -304,6 +304,8 @@ def test_embed_refusals(ctx_of):
 LOSSES = [  # T, C, V, scale
     (1, 8, 1, 1.0), (1, 64, 50, 1.0), (1, 2048, 5001, 1.0), (3, 72, 257, 0.5), (127, 64, 256, 1.0), (128, 128, 255, 2.0), (129, 200, 1000, 1.0),
     (300, 1024, 2001, 1.0), (700, 520, 3333, 0.7), (257, 1536, 515, 1.0),
+    (8, 64, 33, 1.0), (9, 72, 100, 1.0), (16, 1536, 20001, 1.0), (17, 4096, 777, 1.0), (31, 264, 5000, 0.5), (32, 1000, 4099, 1.0), (32, 4096, 600, 1.0),
+    (33, 128, 3000, 1.0), (2, 8, 70001, 1.0),
 ]
 
 
