@@ -5,32 +5,52 @@
 // with their gradients; and dropout on its own.  drop(z) is z / (1 - p) where the element stays and 0 where not
 // (philox.cuh).  All of them move bf16 rows once and are bound by HBM; everything between load and store is fp32.
 //
-// A row is held by a team of WPR warps in registers (VPT 16-byte vectors a lane, packed), so each tensor is read once:
-// the row's sum comes first, then the outputs from the same registers.  Teams of one warp need no block-wide step.
-// The gradients run persistent teams over the rows, keep the column sums (dw) of their rows in registers and leave one
-// partial row a block; colsum_k adds the blocks up in a fixed order, so results are the same bit for bit from run to run.
+// A row belongs to a team of warps, VPT 16-byte vectors a lane.  Teams are persistent: each lane copies its own vectors of
+// the team's next rows into shared memory (cp.async, STAGES - 1 rows ahead, 50 KB and more in flight on an SM), so a row's
+// latency, its sum over the team and its arithmetic overlap the arrival of the rows behind it, and a tensor is read once.
+// A lane reads back only what it copied itself: the ring needs no barrier.  The gradients keep the column sums (dw) of
+// their rows in registers and leave one partial row a block; colsum_k adds the blocks up in a fixed order, so results are
+// the same bit for bit from run to run.
 #include "common.cuh"
 #include "kernels.h"
+#include "mma.cuh"
 #include "philox.cuh"
+#include "tc.cuh"
 
 namespace mhcl {
 
-constexpr int kBlockThreads = 256;
+constexpr int kMaxTeamWarps = 16;
+constexpr int kFwdBlocks = 3, kBwdBlocks = 2;          // of 256 threads on an SM
+__host__ __device__ constexpr int fwd_stages(int vpt) { return vpt == 4 ? 2 : 4; }
+__host__ __device__ constexpr int bwd_stages(int vpt) { return vpt == 4 ? 2 : 4; }
 
+// The threads' places: `wpr` warps a team, `lt` the thread's index in its team.
+struct Team {
+    int wpr, threads, teams, team, lt;
+    __device__ __forceinline__ explicit Team(int wpr_) : wpr(wpr_), threads(wpr_ * 32) {
+        teams = blockDim.x / threads; team = threadIdx.x / threads; lt = threadIdx.x - team * threads;
+    }
+};
 // Sum over the team's warps; every thread of the team gets it.  `slot` alternates so that one barrier a sum is enough.
-template <int WPR>
-__device__ __forceinline__ float team_sum(float v, float* red, int& slot) {
+__device__ __forceinline__ float team_sum(float v, float* red, int& slot, const Team& tm) {
     v = warp_sum(v);
-    if (WPR == 1) return v;
-    const int warp = threadIdx.x >> 5, team = warp / WPR, w = warp % WPR;
-    float* r = red + (slot * (blockDim.x >> 5)) + team * WPR;
-    if ((threadIdx.x & 31) == 0) r[w] = v;
-    asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(WPR * 32) : "memory");
+    if (tm.wpr == 1) return v;
+    float* r = red + slot * kMaxTeamWarps + tm.team * tm.wpr;
+    if ((threadIdx.x & 31) == 0) r[tm.lt >> 5] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(tm.team + 1), "r"(tm.threads) : "memory");
     float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < WPR; ++i) s += r[i];
+    for (int i = 0; i < tm.wpr; ++i) s += r[i];
     slot ^= 1;
     return s;
+}
+// Copies this lane's vectors of one row into a stage: [vector][thread] of 16 bytes.
+template <int VPT>
+__device__ __forceinline__ void fetch_row(uint32_t to, const uint4* __restrict__ row, const Team& tm, int nv) {
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+        const int v = tm.lt + k * tm.threads;
+        cp_async16(to + k * blockDim.x * 16, row + (v < nv ? v : 0), v < nv ? 16 : 0);
+    }
 }
 
 // sigmoid of a pair: 1 / (1 + 2^(-a log2 e)); 2^x overflows to infinity for a far below 0, whose reciprocal is 0.
@@ -59,111 +79,139 @@ struct DropArgs {
 
 // The arithmetic runs on packed pairs (two fp32 operations an instruction): with gate and dropout a vector of 8 elements
 // takes some 170 instructions forward and 230 backward, and with scalar ones the issue slots, not HBM, bounded the kernels.
-template <int VPT, int WPR, bool GATE, bool DROP>
-__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads, WPR * 32 > kBlockThreads ? 1 : 3)
-block_fwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
+template <int VPT, bool BIG, bool GATE, bool DROP>
+__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : kFwdBlocks)
+block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, float eps, DropArgs da, uint4* __restrict__ out, float* __restrict__ rstd) {
-    __shared__ float red[2 * 16];
-    const int nv = C >> 3, lt = threadIdx.x % (WPR * 32), teams = blockDim.x / (WPR * 32);
-    const int64_t t = (int64_t)blockIdx.x * teams + threadIdx.x / (WPR * 32);
-    if (t >= T) return;                                    // whole teams leave
-    int slot = 0;
-    uint4 xv[VPT], gv[VPT];
-#pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-        const int v = lt + k * WPR * 32;
-        xv[k] = v < nv ? ld_stream(x + t * nv + v) : make_uint4(0, 0, 0, 0);
-        if (GATE) gv[k] = v < nv ? ld_stream(gate + t * nv + v) : make_uint4(0, 0, 0, 0);
-    }
-    uint64_t ss2 = 0;
-#pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-        uint64_t f[4];
-        unpack8x2(xv[k], f);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) ss2 = fma2(f[e], f[e], ss2);
-    }
-    float s0, s1;
-    unpack2f(ss2, s0, s1);
-    const float r = rsqrtf(team_sum<WPR>(s0 + s1, red, slot) / (float)C + eps);
-    if (lt == 0) rstd[t] = r;
-    const float s = scale ? __ldg(scale) : 1.f;
-    const uint64_t r2 = both(r), s2 = both(s), fac2 = both(da.factor);
-    const Philox rng(DROP ? da.rng : nullptr, DROP);
-#pragma unroll
-    for (int k = 0; k < VPT; ++k) {
-        const int v = lt + k * WPR * 32;
-        if (v >= nv) continue;
-        uint64_t f[4], g[4], wf[4];
-        unpack8x2(xv[k], f);
-        load_w(w, v, wf);
-        if (GATE) unpack8x2(gv[k], g);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[e] = mul2(mul2(f[e], r2), wf[e]);
-            if (GATE) f[e] = mul2(f[e], sigmoid2(g[e]));
+    constexpr int STAGES = fwd_stages(VPT), NT = GATE ? 2 : 1;
+    extern __shared__ __align__(16) float sm[];
+    __shared__ float red[2 * kMaxTeamWarps];
+    const Team tm(wpr);
+    const int nv = C >> 3;
+    const uint32_t vec = blockDim.x * 16, ring = smem_u32(sm) + threadIdx.x * 16, stage = NT * VPT * vec;
+    const int64_t t0 = (int64_t)blockIdx.x * tm.teams + tm.team, step = (int64_t)gridDim.x * tm.teams;
+    auto fetch = [&](int64_t t, int s) {
+        if (t < T) {
+            fetch_row<VPT>(ring + s * stage, x + t * nv, tm, nv);
+            if (GATE) fetch_row<VPT>(ring + s * stage + VPT * vec, gate + t * nv, tm, nv);
         }
-        if (DROP) drop8(f, rng((uint64_t)(t * nv + v)), da.threshold << 16, fac2);
+        cp_async_commit();
+    };
 #pragma unroll
-        for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], s2);
-        st_stream(out + t * nv + v, pack8x2(f));
+    for (int i = 0; i < STAGES - 1; ++i) fetch(t0 + i * step, i);
+    int slot = 0, cur = 0;
+    const float s = scale ? __ldg(scale) : 1.f;
+    const float sf = DROP ? s * da.factor : s;
+    const Philox rng(DROP ? da.rng : nullptr, DROP);
+    uint64_t wf[VPT][4];
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+        const int v = tm.lt + k * tm.threads;
+        load_w(w, v < nv ? v : 0, wf[k]);
     }
+    for (int64_t t = t0; t < T; t += step) {
+        cp_async_wait<STAGES - 2>();
+        fetch(t + (STAGES - 1) * step, cur == 0 ? STAGES - 1 : cur - 1);       // into the stage of the row before
+        const uint32_t at = ring + cur * stage;
+        cur = cur == STAGES - 1 ? 0 : cur + 1;
+        uint64_t f[VPT][4], ss2 = 0;
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+            unpack8x2(lds128(at + k * vec), f[k]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ss2 = fma2(f[k][e], f[k][e], ss2);
+        }
+        float a0, a1;
+        unpack2f(ss2, a0, a1);
+        const float r = rsqrtf(team_sum(a0 + a1, red, slot, tm) / (float)C + eps);
+        if (tm.lt == 0) rstd[t] = r;
+        const uint64_t rs2 = both(r * sf);
+#pragma unroll
+        for (int k = 0; k < VPT; ++k) {
+            const int v = tm.lt + k * tm.threads;
+            if (v >= nv) continue;
+            uint64_t g[4];
+            if (GATE) unpack8x2(lds128(at + (VPT + k) * vec), g);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f[k][e] = mul2(mul2(f[k][e], rs2), wf[k][e]);
+                if (GATE) f[k][e] = mul2(f[k][e], sigmoid2(g[e]));
+            }
+            if (DROP) drop8(f[k], rng((uint64_t)(t * nv + v)), da.threshold << 16);
+            st_stream(out + t * nv + v, pack8x2(f[k]));
+        }
+    }
+    cp_async_wait<0>();
 }
 
 // With d = drop'(dy), z = d sig, oh = o r, e = s z w (the gradient with respect to oh):
 //   do = r (e - oh mean(e oh)),  da = e oh (1 - sig),  dw = s sum_t z oh,  ds = sum z w oh.
 // s is applied once to each result.  The scale's sum runs over all T C elements and may cancel: it is added up in 64 bits
 // from the rows on.
-template <int VPT, int WPR, bool GATE, bool DROP>
-__global__ void __launch_bounds__(WPR * 32 > kBlockThreads ? WPR * 32 : kBlockThreads, WPR * 32 > kBlockThreads ? 1 : 2)
-block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
+template <int VPT, bool BIG, bool GATE, bool DROP>
+__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : kBwdBlocks)
+block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, const float* __restrict__ rstd, DropArgs da, const uint4* __restrict__ dy,
-            uint4* __restrict__ dx, uint4* __restrict__ dgate, float* __restrict__ dw_part, double* __restrict__ ds_part) {
-    extern __shared__ float sm[];                          // [teams][C] column sums
-    __shared__ float red[2 * 16];
-    __shared__ double dred[16];
-    const int nv = C >> 3, lt = threadIdx.x % (WPR * 32), teams = blockDim.x / (WPR * 32), team = threadIdx.x / (WPR * 32);
-    int slot = 0;
+            uint4* __restrict__ dx, uint4* __restrict__ dgate, float* __restrict__ dw_part, double* __restrict__ ds_part,
+            float* __restrict__ dw, float* __restrict__ ds, int accumulate) {
+    constexpr int STAGES = bwd_stages(VPT), NT = GATE ? 3 : 2;
+    extern __shared__ __align__(16) float sm[];                    // the ring, then [teams][C] column sums
+    __shared__ float red[2 * kMaxTeamWarps];
+    __shared__ double dred[8];
+    const Team tm(wpr);
+    const int nv = C >> 3;
+    const uint32_t vec = blockDim.x * 16, ring = smem_u32(sm) + threadIdx.x * 16, stage = NT * VPT * vec;
+    const int64_t t0 = (int64_t)blockIdx.x * tm.teams + tm.team, step = (int64_t)gridDim.x * tm.teams;
+    auto fetch = [&](int64_t t, int s) {
+        if (t < T) {
+            fetch_row<VPT>(ring + s * stage, x + t * nv, tm, nv);
+            fetch_row<VPT>(ring + s * stage + VPT * vec, dy + t * nv, tm, nv);
+            if (GATE) fetch_row<VPT>(ring + s * stage + 2 * VPT * vec, gate + t * nv, tm, nv);
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) fetch(t0 + i * step, i);
+    int slot = 0, cur = 0;
     const float s = scale ? __ldg(scale) : 1.f;
+    // dropout's factor rides on the weights, and on s in the column sums
     const uint64_t s2 = both(s), fac2 = both(da.factor), minus1 = both(-1.f);
     const Philox rng(DROP ? da.rng : nullptr, DROP);
-    uint64_t acc[VPT][4];
+    uint64_t acc[VPT][4], wf[VPT][4];
 #pragma unroll
-    for (int k = 0; k < VPT; ++k)
+    for (int k = 0; k < VPT; ++k) {
+        const int v = tm.lt + k * tm.threads;
+        load_w(w, v < nv ? v : 0, wf[k]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[k][e] = 0;
+        for (int e = 0; e < 4; ++e) { acc[k][e] = 0; if (DROP) wf[k][e] = mul2(wf[k][e], fac2); }
+    }
     double dsum = 0.0;
-    for (int64_t t = (int64_t)blockIdx.x * teams + team; t < T; t += (int64_t)gridDim.x * teams) {
-        uint4 xv[VPT], gv[VPT], yv[VPT];
-#pragma unroll
-        for (int k = 0; k < VPT; ++k) {
-            const int v = lt + k * WPR * 32;
-            if (v < nv) {
-                xv[k] = ld_stream(x + t * nv + v);
-                yv[k] = ld_stream(dy + t * nv + v);
-                if (GATE) gv[k] = ld_stream(gate + t * nv + v);
-            }
-        }
-        const float r = __ldg(rstd + t);
+    float r_next = t0 < T ? __ldg(rstd + t0) : 0.f;
+    for (int64_t t = t0; t < T; t += step) {
+        const float r = r_next;
+        if (t + step < T) r_next = __ldg(rstd + t + step);
+        cp_async_wait<STAGES - 2>();
+        fetch(t + (STAGES - 1) * step, cur == 0 ? STAGES - 1 : cur - 1);       // into the stage of the row before
+        const uint32_t at = ring + cur * stage;
+        cur = cur == STAGES - 1 ? 0 : cur + 1;
         const uint64_t r2 = both(r);
         uint64_t ds2 = 0;
-        uint64_t zw[VPT][4];                               // z w
+        uint64_t zw[VPT][4];                                       // z w
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
-            const int v = lt + k * WPR * 32;
+            const int v = tm.lt + k * tm.threads;
             if (v >= nv) continue;
-            uint64_t f[4], g[4], wf[4], dg[4];
-            unpack8x2(xv[k], f);
-            unpack8x2(yv[k], zw[k]);
-            load_w(w, v, wf);
-            if (GATE) unpack8x2(gv[k], g);
-            if (DROP) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16, fac2);
+            uint64_t f[4], g[4], dg[4];
+            unpack8x2(lds128(at + k * vec), f);
+            unpack8x2(lds128(at + (VPT + k) * vec), zw[k]);
+            if (GATE) unpack8x2(lds128(at + (2 * VPT + k) * vec), g);
+            if (DROP) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint64_t oh = mul2(f[e], r2);
                 if (GATE) { g[e] = sigmoid2(g[e]); zw[k][e] = mul2(zw[k][e], g[e]); }
                 acc[k][e] = fma2(zw[k][e], oh, acc[k][e]);
-                zw[k][e] = mul2(zw[k][e], wf[e]);
+                zw[k][e] = mul2(zw[k][e], wf[k][e]);
                 const uint64_t q = mul2(zw[k][e], oh);
                 ds2 = add2(ds2, q);
                 if (GATE) dg[e] = mul2(mul2(q, s2), fma2(g[e], minus1, both(1.f)));
@@ -172,39 +220,45 @@ block_bwd_k(int64_t T, int C, const uint4* __restrict__ x, const uint4* __restri
         }
         float m0, m1;
         unpack2f(ds2, m0, m1);
-        const float m = team_sum<WPR>(m0 + m1, red, slot);         // sum_c of e oh / s: the row's part of ds
-        if (lt == 0) dsum += (double)m;
+        const float m = team_sum(m0 + m1, red, slot, tm);          // sum_c of e oh / s: the row's part of ds
+        if (tm.lt == 0) dsum += (double)m;
         const uint64_t rs2 = both(r * s), c2 = both(-r * (m / (float)C));
 #pragma unroll
         for (int k = 0; k < VPT; ++k) {
-            const int v = lt + k * WPR * 32;
+            const int v = tm.lt + k * tm.threads;
             if (v >= nv) continue;
             uint64_t f[4];
-            unpack8x2(xv[k], f);
+            unpack8x2(lds128(at + k * vec), f);
 #pragma unroll
             for (int e = 0; e < 4; ++e) f[e] = mul2(fma2(f[e], c2, zw[k][e]), rs2);
             st_stream(dx + t * nv + v, pack8x2(f));
         }
     }
+    cp_async_wait<0>();
+    pdl_launch();
+    __syncthreads();
     // column sums of the block: the teams' rows through shared memory, in a fixed order
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
-        const int v = lt + k * WPR * 32;
+        const int v = tm.lt + k * tm.threads;
         if (v < nv)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) *(uint64_t*)(sm + team * C + v * 8 + 2 * e) = acc[k][e];
+            for (int e = 0; e < 4; ++e) *(uint64_t*)(sm + tm.team * C + v * 8 + 2 * e) = acc[k][e];
     }
-    if (lt == 0) dred[team] = dsum;
+    if (tm.lt == 0) dred[tm.team] = dsum;
     __syncthreads();
     for (int c = threadIdx.x; c < C; c += blockDim.x) {
         float a = 0.f;
-        for (int i = 0; i < teams; ++i) a += sm[i * C + c];
-        dw_part[(int64_t)blockIdx.x * C + c] = a * s;
+        for (int i = 0; i < tm.teams; ++i) a += sm[i * C + c];
+        a *= DROP ? s * da.factor : s;
+        if (gridDim.x == 1) dw[c] = accumulate ? dw[c] + a : a;        // few rows: nothing to join
+        else dw_part[(int64_t)blockIdx.x * C + c] = a;
     }
-    if (ds_part && threadIdx.x == 0) {
+    if (ds && threadIdx.x == 0) {
         double a = 0.0;
-        for (int i = 0; i < teams; ++i) a += dred[i];
-        ds_part[blockIdx.x] = a;
+        for (int i = 0; i < tm.teams; ++i) a += dred[i];
+        if (gridDim.x == 1) ds[0] = accumulate ? (float)(ds[0] + a) : (float)a;
+        else ds_part[blockIdx.x] = a;
     }
 }
 
@@ -215,10 +269,12 @@ __global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* _
                                                 float* __restrict__ ds, int accumulate) {
     __shared__ float red[8][33];
     __shared__ double dred[8];
+    pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     const int per = (parts + 7) / 8, p0 = warp * per, p1 = min(parts, p0 + per);
     float a = 0.f;
     if (c < C)
+#pragma unroll 8
         for (int p = p0; p < p1; ++p) a += dw_part[(int64_t)p * C + c];
     red[warp][lane] = a;
     if (ds && blockIdx.x == 0) {
@@ -261,14 +317,16 @@ __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloa
         uint64_t f[4];
         if (g < full) {
             unpack8x2(v[k], f);
-            drop8(f, rng((uint64_t)g), thr, fac2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) f[e] = mul2(f[e], fac2);
+            drop8(f, rng((uint64_t)g), thr);
             st_stream(y + g * 8, pack8x2(f));
         } else if (g * 8 < count) {                        // the last, partial group
             const int m = (int)(count - g * 8);
             float s[8];
             for (int e = 0; e < 8; ++e) s[e] = e < m ? __bfloat162float(x[g * 8 + e]) : 0.f;
-            for (int e = 0; e < 4; ++e) f[e] = pack2f(s[2 * e], s[2 * e + 1]);
-            drop8(f, rng((uint64_t)g), thr, fac2);
+            for (int e = 0; e < 4; ++e) f[e] = mul2(pack2f(s[2 * e], s[2 * e + 1]), fac2);
+            drop8(f, rng((uint64_t)g), thr);
             for (int e = 0; e < 4; ++e) unpack2f(f[e], s[2 * e], s[2 * e + 1]);
             for (int e = 0; e < m; ++e) y[g * 8 + e] = __float2bfloat16_rn(s[e]);
         }
@@ -276,21 +334,23 @@ __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloa
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-// Warps a row and vectors a lane for C channels.  Forward: 4 vectors a lane keep a warp's loads wide.  Backward: 2, since
-// its three tensors and the column sums of 4 would take 180 registers a thread and leave one block on an SM.
+// Vectors a lane and warps a team for C channels: two vectors where that takes at most 16 warps, with as many warps as the
+// row fills (1536 channels: three), and about 256 threads a block, up to 512 for rows beyond 4096 channels.
 struct RowPlan { int vpt, wpr, threads, teams; };
-static RowPlan plan_row(int C, bool bwd) {
+static RowPlan plan_row(int C) {
     const int nv = C / 8;
     RowPlan p;
-    p.vpt = nv <= 32 ? 1 : (nv <= 64 || (bwd && nv <= 1024)) ? 2 : 4;
-    p.wpr = 1;
-    while (p.wpr * 32 * p.vpt < nv) p.wpr *= 2;
-    p.threads = p.wpr * 32 > kBlockThreads ? p.wpr * 32 : kBlockThreads;
-    p.teams = p.threads / (p.wpr * 32);
+    p.vpt = nv <= 32 ? 1 : nv <= 64 * kMaxTeamWarps ? 2 : 4;
+    p.wpr = (nv + 32 * p.vpt - 1) / (32 * p.vpt);
+    p.teams = p.wpr < 8 ? 8 / p.wpr : 1;
+    p.threads = p.teams * p.wpr * 32;
     return p;
 }
-
-#define MHCL_ROW_CASE(V, W, ...) if (p.vpt == V && p.wpr == W) { constexpr int VPT = V, WPR = W; __VA_ARGS__; }
+// Blocks: as many of 256 threads as an SM holds.
+static int row_blocks(const RowPlan& p, int64_t T, int sm_count, int per_sm) {
+    const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * (p.threads > 256 ? 1 : per_sm);
+    return (int)(need < cap ? need : cap);
+}
 
 static DropArgs drop_args(float p, const uint64_t* rng) {
     DropArgs d;
@@ -300,48 +360,52 @@ static DropArgs drop_args(float p, const uint64_t* rng) {
     return d;
 }
 
+// (one block while its teams have at most two rows each: its column sums are then the result, without a second launch)
 int block_parts(int64_t T, int C, int sm_count) {
-    const RowPlan p = plan_row(C, true);
-    const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * (512 / p.threads);
-    return (int)(need < cap ? need : cap);
+    const RowPlan p = plan_row(C);
+    return T <= 2 * p.teams ? 1 : row_blocks(p, T, sm_count, kBwdBlocks);
 }
 
 void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C, false);
-    const unsigned grid = (unsigned)((T + p.teams - 1) / p.teams);
+    const RowPlan p = plan_row(c->C);
+    const int grid = row_blocks(p, T, c->sm_count, kFwdBlocks), smem = p.threads * 16 * p.vpt * (gate ? 2 : 1) * fwd_stages(p.vpt);
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 1;
-#define MHCL_FWD(V, W)                                                                                                  \
-    MHCL_ROW_CASE(V, W, {                                                                                               \
-        auto k = gate ? (da.rng ? block_fwd_k<VPT, WPR, true, true> : block_fwd_k<VPT, WPR, true, false>)               \
-                      : (da.rng ? block_fwd_k<VPT, WPR, false, true> : block_fwd_k<VPT, WPR, false, false>);            \
-        k<<<grid, p.threads, 0, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, eps, da,    \
-                                     (uint4*)out, rstd);                                                                \
-    })
-    MHCL_FWD(1, 1) MHCL_FWD(2, 1) MHCL_FWD(4, 1) MHCL_FWD(4, 2) MHCL_FWD(4, 4) MHCL_FWD(4, 8) MHCL_FWD(4, 16)
+#define MHCL_FWD(V, B)                                                                                                  \
+    if (p.vpt == V && (p.threads > 256) == B) {                                                                                                \
+        auto k = gate ? (da.rng ? block_fwd_k<V, B, true, true> : block_fwd_k<V, B, true, false>)                             \
+                      : (da.rng ? block_fwd_k<V, B, false, true> : block_fwd_k<V, B, false, false>);                          \
+        if (smem > 40 * 1024) { static SmemOnce once[2][2]; smem_limit(once[gate != nullptr][da.rng != nullptr], k, c->device, 226 * 1024); }               \
+        k<<<grid, p.threads, smem, s>>>(T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, eps, da, \
+                                        (uint4*)out, rstd);                                                             \
+    }
+    MHCL_FWD(1, false) MHCL_FWD(2, false) MHCL_FWD(2, true) MHCL_FWD(4, true)
 #undef MHCL_FWD
 }
 
 void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       const float* rstd, float p_drop, const uint64_t* rng, const void* dy, void* dx, void* dgate, float* dw,
                       float* dscale, int accumulate, float* dw_part, double* ds_part, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C, true);
+    const RowPlan p = plan_row(c->C);
     const int parts = block_parts(T, c->C, c->sm_count);
-    const size_t smem = (size_t)p.teams * c->C * sizeof(float);
+    int smem = p.threads * 16 * p.vpt * (gate ? 3 : 2) * bwd_stages(p.vpt);
+    if (smem < p.teams * c->C * 4) smem = p.teams * c->C * 4;
     const DropArgs da = drop_args(p_drop, rng);
-    c->launches += 2;
-#define MHCL_BWD(V, W)                                                                                                  \
-    MHCL_ROW_CASE(V, W, {                                                                                               \
-        auto k = gate ? (da.rng ? block_bwd_k<VPT, WPR, true, true> : block_bwd_k<VPT, WPR, true, false>)               \
-                      : (da.rng ? block_bwd_k<VPT, WPR, false, true> : block_bwd_k<VPT, WPR, false, false>);            \
-        if (smem > 48 * 1024) cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);          \
-        k<<<parts, p.threads, smem, s>>>(T, c->C, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, rstd, da, \
-                                         (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, dscale ? ds_part : nullptr); \
-    })
-    MHCL_BWD(1, 1) MHCL_BWD(2, 1) MHCL_BWD(2, 2) MHCL_BWD(2, 4) MHCL_BWD(2, 8) MHCL_BWD(2, 16) MHCL_BWD(4, 16)
+    c->launches += 1;
+#define MHCL_BWD(V, B)                                                                                                  \
+    if (p.vpt == V && (p.threads > 256) == B) {                                                                                                \
+        auto k = gate ? (da.rng ? block_bwd_k<V, B, true, true> : block_bwd_k<V, B, true, false>)                             \
+                      : (da.rng ? block_bwd_k<V, B, false, true> : block_bwd_k<V, B, false, false>);                          \
+        if (smem > 40 * 1024) { static SmemOnce once[2][2]; smem_limit(once[gate != nullptr][da.rng != nullptr], k, c->device, 226 * 1024); }               \
+        k<<<parts, p.threads, smem, s>>>(T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, rstd, da, \
+                                         (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
+    }
+    MHCL_BWD(1, false) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, true)
 #undef MHCL_BWD
-    colsum_k<<<(c->C + 31) / 32, 256, 0, s>>>(c->C, parts, dw_part, ds_part, dw, dscale, accumulate);
+    if (parts == 1) return;
+    c->launches += 1;
+    launch_after(colsum_k, dim3((c->C + 31) / 32), dim3(256), 0, s, c->C, parts, dw_part, ds_part, dw, dscale, accumulate);
 }
 
 void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p, const uint64_t* rng, void* y, cudaStream_t s) {

@@ -504,7 +504,7 @@ __global__ void __launch_bounds__(kSmThreads, 1)
 ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, const uint4* __restrict__ W,
            const int64_t* __restrict__ target, float scale, float2* __restrict__ part, float* __restrict__ tlogit) {
     extern __shared__ __align__(16) unsigned char sm_raw[];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    pdl_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const int WK = 1 << wk_log, WR = kSmWarps >> wk_log, wk = warp & (WK - 1), wr = warp >> wk_log;
     const int KB = 64 * WK, blocks = (C + KB - 1) / KB, nv = C >> 3, rows = 16 * WR;
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int par
     __shared__ float2 red[16][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float m = -INFINITY, s = 0.f;
-    asm volatile("griddepcontrol.wait;" ::: "memory");         // launched beside ce_small_k: its results from here on
+    pdl_wait();                                                // launched beside ce_small_k: its results from here on
     if (lane < T) {
 #pragma unroll 10
         for (int k = warp; k < parts; k += 16) {
@@ -740,7 +740,8 @@ template <int MODE>
 static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, const CeArgs& a, cudaStream_t s) {
     constexpr int smem = kCeStages * kCeStage + (int)sizeof(CeCtl) + 1024;
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * (MODE == CE_DH ? a.splits : 1);
-    cudaFuncSetAttribute(ce_gemm_k<MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    static SmemOnce once;
+    smem_limit(once, ce_gemm_k<MODE>, c->device, smem);
     c->launches += 1;
     const int64_t pairs = tiles < c->sm_count / 2 ? tiles : c->sm_count / 2;
     ce_gemm_k<MODE><<<(unsigned)(2 * pairs), kCeThreads, smem, s>>>(ma, mb, a);
@@ -778,19 +779,11 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         const int grid = (int)(units < c->sm_count ? units : c->sm_count);
         auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5> : q.nb == 2 ? ce_small_k<2, 5> : ce_small_k<4, 5>)
                                : (q.nb == 1 ? ce_small_k<1, 3> : q.nb == 2 ? ce_small_k<2, 3> : ce_small_k<4, 3>);
-        cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, q.smem);
+        static SmemOnce once[3][2];
+        smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
         c->launches += 2;
         k<<<grid, kSmThreads, q.smem, s>>>((int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(1);
-        cfg.blockDim = dim3(512);
-        cfg.stream = s;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[0].val.programmaticStreamSerializationAllowed = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        cudaLaunchKernelEx(&cfg, ce_small_join_k, (int)T, V, grid, (const float2*)part, (const float*)tlogit, target, loss, lse, c->op_status);
+        launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, loss, lse, c->op_status);
         return true;
     }
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);

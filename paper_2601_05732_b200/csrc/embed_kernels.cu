@@ -3,12 +3,12 @@
 //   dE[v,:] (+)= scale sum_{t: id_t = v} sum_j g[t,j,:].
 //
 // The forward is bound by the n rows it writes a token.  The gradient is bound by the n rows it reads a token and the
-// table it writes; its sums must not depend on the order in which blocks run, so the tokens are sorted first
-// (embed_sort_k, stable: tokens of one id stay in ascending order), then embed_grad_k walks the sorted list in chunks,
-// one warp a chunk and 256 channels, and keeps the running sum of the current id in fp32 registers.  An id whose tokens
-// span several chunks leaves one partial row a chunk, which embed_join_k adds up in order: a token as frequent as the
-// commonest word does not serialise.  Rows that no token meets are zeroed by further blocks of embed_grad_k, from a bit
-// mask that the sort leaves, so each row of dE is written once.
+// table it writes; its sums must not depend on the order in which blocks run, so the tokens are sorted first (stable:
+// tokens of one id stay in ascending order; embed_rank_k for up to 6144 tokens, embed_sort_k beyond), then embed_grad_k
+// walks the sorted list in chunks, one warp a chunk and 256 channels, and keeps the running sum of the current id in fp32
+// registers.  An id whose tokens span several chunks leaves one partial row a chunk, which embed_join_k adds up in order: a
+// token as frequent as the commonest word does not serialise.  Rows that no token meets are zeroed by further blocks of
+// embed_grad_k, so each row of dE is written once.  The three launches overlap their starts (programmatic launch).
 #include "common.cuh"
 #include "kernels.h"
 
@@ -57,12 +57,72 @@ __global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, 
 }
 
 // ---- stable sort of the tokens by id ---------------------------------------------------------------------------------
-// One cluster of up to 16 blocks sorts, least significant digit first, 9 bits a pass (two passes for tables below
-// 2^18 rows): a warp owns a contiguous range of the list and counts its digits in shared memory, the blocks exchange their
-// totals through distributed shared memory, and each warp then walks its range again and places the tokens.  A range is
-// read eight vectors of 32 entries at a time, so that a pass costs a few memory latencies, which are what bounds it; a
-// launch a pass would cost more than the pass.
+// Few tokens: every block holds all keys in shared memory and ranks 32 tokens at a time by counting the keys below theirs
+// (T^2 comparisons, spread over all SMs), which needs no exchange between blocks.  The whole gradient, 3 streams of 1536
+// channels and 1000 rows: 2048 tokens 21 us (29 with the cluster's sort), 4096 27.5 (34), 8192 39 (38).
+constexpr int kRankMax = 6144;
+__device__ __forceinline__ uint32_t embed_key(int64_t id, int64_t i, int64_t V, bool say, int* status) {
+    const bool ok = id >= 0 && id < V;
+    if (!ok && say) report_index(status, MHCLITE_OP_EMBED_BWD, i, id);
+    return ok ? (uint32_t)id : (uint32_t)V;                    // tokens without a row go last
+}
+__global__ void __launch_bounds__(256) embed_rank_k(int T, int64_t V, const int64_t* __restrict__ ids, uint2* __restrict__ list,
+                                                    int* __restrict__ status) {
+    __shared__ __align__(16) uint32_t key[kRankMax];
+    __shared__ int below[8][32];
+    pdl_wait();
+    pdl_launch();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quads = (T + 3) / 4;
+    for (int i0 = tid; i0 < quads * 4; i0 += 256 * 8) {        // eight loads in flight
+        int64_t id[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) id[k] = i0 + k * 256 < T ? __ldg(ids + i0 + k * 256) : 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = i0 + k * 256;
+            if (i >= quads * 4) break;
+            key[i] = i < T ? embed_key(id[k], i, V, blockIdx.x == 0, status) : 0xFFFFFFFFu;
+        }
+    }
+    __syncthreads();
+    for (int b = blockIdx.x * 32; b < T; b += gridDim.x * 32) {
+        // a lane takes one token, a warp an eighth of the keys
+        const int i = b + lane;
+        const uint32_t mine = i < T ? key[i] : 0;
+        const int per = (quads + 7) / 8, q0 = warp * per, q1 = q0 + per < quads ? q0 + per : quads;
+        int n = 0;
+        // keys of earlier tokens count when equal too: below mine + 1 before this block of 32 tokens, below mine behind it
+        auto count = [&](int qa, int qb, uint32_t limit) {
+#pragma unroll 8
+            for (int q = qa; q < qb; ++q) {
+                const uint4 k = *reinterpret_cast<const uint4*>(key + 4 * q);
+                if (k.x < limit) ++n;
+                if (k.y < limit) ++n;
+                if (k.z < limit) ++n;
+                if (k.w < limit) ++n;
+            }
+        };
+        const int qb = b / 4, qe = qb + 8;
+        count(q0, min(q1, qb), mine + 1);
+        for (int j = max(4 * q0, 4 * qb); j < min(4 * q1, 4 * qe); ++j) n += key[j] < mine + (j < i ? 1 : 0) ? 1 : 0;
+        count(max(q0, qe), q1, mine);
+        below[warp][lane] = n;
+        __syncthreads();
+        if (warp == 0 && i < T) {
+            int rank = 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) rank += below[w][lane];
+            list[rank] = make_uint2(mine, (uint32_t)i);
+        }
+        __syncthreads();
+    }
+}
 
+// More tokens: one cluster of up to 16 blocks sorts, least significant digit first, 9 bits a pass (two passes for tables
+// below 2^18 rows): a warp owns a contiguous range of the list and counts its digits in shared memory, the blocks exchange
+// their totals through distributed shared memory, and each warp then walks its range again and places the tokens.  A range
+// is read eight vectors of 32 entries at a time, so that a pass costs a few memory latencies, which are what bounds it; a
+// launch a pass would cost more than the pass.
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32, kSortBits = 9, kSortBins = 1 << kSortBits, kSortAhead = 8, kSortMaxBlocks = 16;
 constexpr int kSortSmem = kSortWarps * kSortBins * 4;
 
@@ -91,7 +151,7 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t live, uint32_t d) {
 }
 
 __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, int passes, const int64_t* __restrict__ ids,
-                                                             uint2* buf0, uint2* buf1, uint32_t* mask, int* __restrict__ status) {
+                                                             uint2* buf0, uint2* buf1, int* __restrict__ status) {
     extern __shared__ uint32_t cnt[];                          // [warp][bin]
     __shared__ uint32_t tot[kSortBins], off[kSortBins], wsum[kSortBins / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -100,7 +160,8 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
     const int64_t begin = (int64_t)(me * kSortWarps + warp) * per;
     const int i0 = begin < T ? (int)begin : T, i1 = T - i0 < per ? T : i0 + per;
     uint32_t* mine = cnt + warp * kSortBins;
-    for (int64_t w = (int64_t)me * kSortThreads + tid; w < (V + 31) / 32; w += (int64_t)nb * kSortThreads) mask[w] = 0;
+    pdl_wait();
+    pdl_launch();
     uint2 *src = buf0, *dst = buf1;
     for (int p = 0; p < passes; ++p) {
         const int shift = p * kSortBits;
@@ -111,16 +172,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k) {
                 const int i = b + k * 32 + lane;
-                if (i < i1) {
-                    if (p == 0) {
-                        const int64_t id = ids[i];
-                        const bool ok = id >= 0 && id < V;
-                        if (!ok) report_index(status, MHCLITE_OP_EMBED_BWD, i, id);
-                        key[k] = ok ? (uint32_t)id : (uint32_t)V;      // tokens without a row go last
-                    } else {
-                        key[k] = __ldcg(src + i).x;
-                    }
-                }
+                if (i < i1) key[k] = p == 0 ? embed_key(__ldg(ids + i), i, V, true, status) : __ldcg(src + i).x;
             }
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k) {
@@ -184,25 +236,52 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
         uint2* h = src; src = dst; dst = h;
         cluster_sync_all();
     }
-    for (int i = i0 + lane; i < i1; i += 32) {                 // the first entry of an id marks its row
-        const uint32_t key = __ldcg(src + i).x, prev = i > 0 ? __ldcg(src + i - 1).x : 0xFFFFFFFFu;
-        if (key != prev && key < V) atomicOr(mask + (key >> 5), 1u << (key & 31));
-    }
 }
 
 // ---- sums over the sorted list ---------------------------------------------------------------------------------------
+constexpr int kZeroRows = 64;          // rows a block looks over for those that no token meets
+
 // Warp (chunk, slice) adds up `R` list entries for channels [256 slice, 256 slice + 256), 8 a lane.
 template <int N_>
 __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int C, int R, int64_t sum_blocks, int slices,
-                                                    const uint2* __restrict__ list, const uint32_t* __restrict__ mask,
+                                                    const uint2* __restrict__ list,
                                                     const uint4* __restrict__ g, float scale, float* __restrict__ dE,
                                                     float* __restrict__ own, float* __restrict__ cont, int accumulate) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
+    pdl_wait();
+    pdl_launch();
     if (blockIdx.x >= sum_blocks) {                            // rows that no token meets
-        const int64_t zb = blockIdx.x - sum_blocks, nzb = gridDim.x - sum_blocks;
+        __shared__ uint32_t met[kZeroRows / 32];
+        __shared__ int64_t range[2];
+        const int64_t v0 = (int64_t)(blockIdx.x - sum_blocks) * kZeroRows, v1 = v0 + kZeroRows < V ? v0 + kZeroRows : V;
+        if (threadIdx.x < kZeroRows / 32) met[threadIdx.x] = 0;
+        if (warp < 2) {                                        // the entries of these rows: a warp finds each end
+            const int64_t bound = warp == 0 ? v0 : v1;
+            int64_t lo = -1, hi = T;                           // the first entry not below `bound` lies in (lo, hi]
+            while (hi - lo > 1) {
+                const int64_t step = (hi - lo + 31) / 32, probe = lo + 1 + lane * step;
+                const int n = __popc(__ballot_sync(0xffffffffu, probe < hi && __ldg(&list[probe < hi ? probe : 0].x) < bound));
+                const int64_t end = lo + 1 + n * step;
+                if (n > 0) lo += 1 + (n - 1) * step;
+                hi = end < hi ? end : hi;
+                if (n == 0) break;
+            }
+            if (lane == 0) range[warp] = hi;
+        }
+        __syncthreads();
+        if (threadIdx.x < kZeroRows) {                         // a thread a row: is it among them?
+            const int64_t v = v0 + threadIdx.x, end = range[1];
+            int64_t lo = range[0], hi = end;
+            while (lo < hi) {
+                const int64_t mid = (lo + hi) >> 1;
+                if (__ldg(&list[mid].x) < v) lo = mid + 1; else hi = mid;
+            }
+            if (lo < end && __ldg(&list[lo].x) == v) atomicOr(&met[threadIdx.x >> 5], 1u << lane);
+        }
+        __syncthreads();
         const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int64_t v = zb * 8 + warp; v < V; v += nzb * 8) {
-            if (__ldg(mask + (v >> 5)) >> (v & 31) & 1u) continue;
+        for (int64_t v = v0 + warp; v < v1; v += 8) {
+            if (met[(v - v0) >> 5] >> ((v - v0) & 31) & 1u) continue;
             float4* row = (float4*)(dE + v * C);
             for (int c = lane; c < C / 4; c += 32) __stcs(row + c, zero);
         }
@@ -300,6 +379,7 @@ __global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C,
     const int64_t chunk = (int64_t)blockIdx.x * 8 + warp, p0 = chunk * R, p1 = p0 + R;
     const int v = blockIdx.y * 32 + lane;
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    pdl_wait();
     if (lane == 0) end_s[warp] = 0;
     if (p1 < T) {
         const int64_t at[4] = {p1 - 1, p1, p0, p0 > 0 ? p0 - 1 : p0};                // one load for the four
@@ -308,7 +388,11 @@ __global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C,
         const uint32_t head = __shfl_sync(0xffffffffu, mine, 2), prev = __shfl_sync(0xffffffffu, mine, 3);
         const bool began_before = p0 > 0 && head == key && prev == key;
         if (key < V && next == key && !began_before) {
-            int64_t lo = p1, hi = T;                           // the first entry behind the id lies in (lo, hi]
+            // chunks of this id in a row, mostly few: one look at the next 32, and a search only where all are
+            const int64_t head_at = p1 + (int64_t)lane * R;
+            const uint32_t same = __ballot_sync(0xffffffffu, head_at < T && __ldg(&list[head_at < T ? head_at : p1].x) == key);
+            const int run = same == 0xffffffffu ? 32 : __ffs(~same) - 1;
+            int64_t lo = p1 + (int64_t)(run - 1) * R, hi = run < 32 ? lo + 1 : T;     // the last entry known to be of the id
             while (hi - lo > 1) {
                 const int64_t step = (hi - lo + 31) / 32, probe = lo + lane * step;
                 const uint32_t same = __ballot_sync(0xffffffffu, probe < hi && __ldg(&list[probe < hi ? probe : lo].x) == key);
@@ -369,8 +453,8 @@ static int embed_chunk(int64_t T, int C) {
     return R;
 }
 
-struct EmbedScratch { uint2 *buf0, *buf1; uint32_t* mask; float *own, *cont; size_t bytes; };
-static EmbedScratch plan_embed(int64_t T, int64_t V, int C, void* base) {
+struct EmbedScratch { uint2 *buf0, *buf1; float *own, *cont; size_t bytes; };
+static EmbedScratch plan_embed(int64_t T, int C, void* base) {
     EmbedScratch p;
     char* b = (char*)base;
     size_t off = 0;
@@ -378,50 +462,63 @@ static EmbedScratch plan_embed(int64_t T, int64_t V, int C, void* base) {
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     p.buf0 = (uint2*)take((size_t)T * 8);
     p.buf1 = (uint2*)take((size_t)T * 8);
-    p.mask = (uint32_t*)take((size_t)((V + 31) / 32) * 4);
     p.own = (float*)take((size_t)chunks * C * 4);
     p.cont = (float*)take((size_t)chunks * C * 4);
     p.bytes = off;
     return p;
 }
-size_t embed_scratch_bytes(int64_t T, int64_t V, int C) { return plan_embed(T, V, C, nullptr).bytes; }
+size_t embed_scratch_bytes(int64_t T, int C) { return plan_embed(T, C, nullptr).bytes; }
 
 cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* g, float scale, float* dE,
                              int accumulate, void* scratch, cudaStream_t s) {
-    const EmbedScratch p = plan_embed(T, V, c->C, scratch);
-    int bits = 1;
-    while ((V >> bits) != 0) ++bits;                           // keys run to V
-    const int passes = (bits + kSortBits - 1) / kSortBits;
-    int nb = 1;                                                // blocks of the cluster: 64 tokens a warp, then more blocks
-    while (nb < kSortMaxBlocks && T > (int64_t)nb * kSortWarps * 64) nb *= 2;
-    cudaFuncSetAttribute(embed_sort_k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortSmem);
-    cudaFuncSetAttribute(embed_sort_k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    c->launches += 3;
-    cudaError_t e;
-    for (;; nb /= 2) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(nb);
-        cfg.blockDim = dim3(kSortThreads);
-        cfg.dynamicSmemBytes = kSortSmem;
-        cfg.stream = s;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeClusterDimension;
-        at[0].val.clusterDim.x = nb; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        e = cudaLaunchKernelEx(&cfg, embed_sort_k, (int)T, V, passes, ids, p.buf0, p.buf1, p.mask, c->op_status);
-        if (e == cudaSuccess) break;
-        if (nb <= 8) return e;                                 // clusters beyond 8 blocks need not exist on every device
-        cudaGetLastError();
+    const EmbedScratch p = plan_embed(T, c->C, scratch);
+    c->launches += 2;
+    const uint2* list = p.buf0;
+    cudaError_t e = cudaSuccess;
+    if (T <= kRankMax) {
+        const int blocks = (int)((T + 31) / 32);
+        e = launch_after(embed_rank_k, dim3(blocks < c->sm_count * 2 ? blocks : c->sm_count * 2), dim3(256), 0, s, (int)T, V, ids, p.buf0,
+                         c->op_status);
+        if (e != cudaSuccess) return e;
+    } else {
+        int bits = 1;
+        while ((V >> bits) != 0) ++bits;                       // keys run to V
+        const int passes = (bits + kSortBits - 1) / kSortBits;
+        int nb = kSortMaxBlocks;                               // blocks of the cluster, with at least 64 tokens a warp
+        while (nb > 1 && T <= (int64_t)(nb / 2) * kSortWarps * 64) nb /= 2;
+        static SmemOnce once;
+        smem_limit(once, embed_sort_k, c->device, kSortSmem);
+        cudaFuncSetAttribute(embed_sort_k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        for (;; nb /= 2) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3(nb);
+            cfg.blockDim = dim3(kSortThreads);
+            cfg.dynamicSmemBytes = kSortSmem;
+            cfg.stream = s;
+            cudaLaunchAttribute at[2];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = nb; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+            at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            at[1].val.programmaticStreamSerializationAllowed = 1;
+            cfg.attrs = at;
+            cfg.numAttrs = 2;
+            e = cudaLaunchKernelEx(&cfg, embed_sort_k, (int)T, V, passes, ids, p.buf0, p.buf1, c->op_status);
+            if (e == cudaSuccess) break;
+            if (nb <= 8) return e;                             // clusters beyond 8 blocks need not exist on every device
+            cudaGetLastError();
+        }
+        if (passes & 1) list = p.buf1;
     }
-    const uint2* list = (passes & 1) ? p.buf1 : p.buf0;
     const int R = embed_chunk(T, c->C), slices = (c->C / 8 + 31) / 32;
     const int64_t chunks = (T + R - 1) / R, sum_blocks = (chunks * slices + 7) / 8;
-    const int64_t zero_blocks = accumulate ? 0 : ((V + 7) / 8 < c->sm_count * 8 ? (V + 7) / 8 : c->sm_count * 8);
-    MHCL_DISPATCH_N(c->n, embed_grad_k<N_><<<(unsigned)(sum_blocks + zero_blocks), 256, 0, s>>>(
-        T, V, c->C, R, sum_blocks, slices, list, p.mask, (const uint4*)g, scale, dE, p.own, p.cont, accumulate))
-    embed_join_k<<<dim3((unsigned)((chunks + 7) / 8), (unsigned)slices), 256, 0, s>>>(T, V, c->C, R, list, p.own, p.cont, scale, dE, accumulate);
-    return cudaGetLastError();
+    const int64_t zero_blocks = accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
+    MHCL_DISPATCH_N(c->n, e = launch_after(embed_grad_k<N_>, dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, T, V, c->C, R,
+                                           sum_blocks, slices, list, (const uint4*)g, scale, dE, p.own, p.cont, accumulate))
+    if (e != cudaSuccess) return e;
+    if (chunks < 2) return cudaSuccess;                        // no id can span chunks
+    c->launches += 1;
+    return launch_after(embed_join_k, dim3((unsigned)((chunks + 7) / 8), (unsigned)slices), dim3(256), 0, s, T, V, c->C, R, list, p.own,
+                        p.cont, scale, dE, accumulate);
 }
 
 }  // namespace mhcl

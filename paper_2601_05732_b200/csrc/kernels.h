@@ -115,6 +115,37 @@ void launch_tail_mma(const mhclite_ctx* c, int64_t T, int N, const TailPlan& p, 
                      const float* H_pre, const float* W, const float* gain, void* dx, int acc_dx, float* Gpart,
                      float* dW, float* dgain, int acc_params, cudaStream_t s);
 
+// Launches a kernel that may begin while the one before it on the stream still runs (programmatic dependent launch): it
+// waits for that kernel's results itself (pdl_wait), before its first access to global memory.
+template <typename... P, typename... A>
+inline cudaError_t launch_after(void (*k)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k, static_cast<P>(args)...);
+}
+#ifdef __CUDACC__
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
+
+// Raises a kernel's limit of dynamic shared memory once a device (the call costs more than the launch's other set-up).
+struct SmemOnce { unsigned long long done = 0; };
+template <typename K>
+inline void smem_limit(SmemOnce& once, K k, int device, int bytes) {
+    const unsigned long long bit = 1ull << (device & 63);
+    if (__atomic_load_n(&once.done, __ATOMIC_RELAXED) & bit) return;
+    cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    __atomic_fetch_or(&once.done, bit, __ATOMIC_RELAXED);
+}
+
 // block_kernels.cu : the norms around a sublayer, with gate, scale and dropout, and dropout alone
 constexpr int kMaxRowC = 16384;               // channels of a row that a team of warps holds in registers
 int block_parts(int64_t T, int C, int sm_count);
@@ -129,7 +160,7 @@ void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p,
 // embed_kernels.cu : token rows into the residual streams, and the table's gradient
 void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* E, int table_f32, float scale,
                       void* x0, cudaStream_t s);
-size_t embed_scratch_bytes(int64_t T, int64_t V, int C);
+size_t embed_scratch_bytes(int64_t T, int C);
 cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* g, float scale, float* dE,
                              int accumulate, void* scratch, cudaStream_t s);
 

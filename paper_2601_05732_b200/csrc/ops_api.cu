@@ -63,7 +63,7 @@ int mhclite_embed_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, const int64_t* ids
 
 size_t mhclite_embed_scratch_bytes(int C, int64_t T, int64_t V) {
     if (C <= 0 || C % 8 || T < 0 || V < 1 || T >= kMaxTokens || V >= kMaxTokens) return 0;
-    return embed_scratch_bytes(T, V, C);
+    return embed_scratch_bytes(T, C);
 }
 
 int mhclite_embed_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const int64_t* ids, const mhclite_bf16* g, float scale, float* dE,
@@ -79,7 +79,7 @@ int mhclite_embed_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const int64_t* ids
     }
     MHCL_PTR8(ctx, ids); MHCL_PTR(ctx, g);
     MHCL_NO_ALIAS(ctx, dE, g); MHCL_NO_ALIAS(ctx, dE, ids);
-    if ((rc = check_scratch(ctx, scratch, scratch_bytes, embed_scratch_bytes(T, V, ctx->C)))) return rc;
+    if ((rc = check_scratch(ctx, scratch, scratch_bytes, embed_scratch_bytes(T, ctx->C)))) return rc;
     MHCL_DEVICE(ctx);
     return check_cuda(ctx, launch_embed_bwd(ctx, T, V, ids, g, scale, dE, accumulate, scratch, (cudaStream_t)stream), "embed_bwd");
 }

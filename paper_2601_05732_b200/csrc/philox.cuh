@@ -42,14 +42,15 @@ struct Philox {
         return make_uint4(c0, c1, c2, c3);
     }
 };
-// f[e] (packed pairs) <- f * factor where the element stays, 0 (whatever f is) where it is dropped.  `thr_hi` is the
-// threshold in the upper half-word: the upper 16 bits of a word are compared as they lie, the lower ones shifted up.
-__device__ __forceinline__ void drop8(uint64_t* f, const uint4& w, uint32_t thr_hi, uint64_t factor2) {
+// f[e] (packed pairs) <- f where the element stays, 0 (whatever f is) where it is dropped; the caller multiplies by the
+// factor together with what else it has.  `thr_hi` is the threshold in the upper half-word: the upper 16 bits of a word are
+// compared as they lie, the lower ones shifted up.
+__device__ __forceinline__ void drop8(uint64_t* f, const uint4& w, uint32_t thr_hi) {
     const uint32_t r[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float lo, hi;
-        unpack2f(mul2(f[e], factor2), lo, hi);
+        unpack2f(f[e], lo, hi);
         f[e] = pack2f((r[e] << 16) >= thr_hi ? lo : 0.f, r[e] >= thr_hi ? hi : 0.f);
     }
 }

@@ -227,6 +227,7 @@ def test_embed_fwd(ctx_of, T, n, C, V, f32):
 EMBEDS = [  # T, n, C, V, ids
     (1, 4, 64, 9, "even"), (5, 2, 8, 1, "even"), (31, 3, 72, 300, "even"), (1000, 4, 256, 70, "even"), (5003, 3, 264, 5000, "text"),
     (4096, 4, 64, 100, "one"), (2500, 5, 1536, 70000, "text"), (70000, 2, 16, 1000, "text"), (33, 4, 520, 255, "one"), (256, 4, 64, 256, "even"),
+    (6144, 2, 64, 300, "text"), (6145, 2, 64, 300000, "text"), (20000, 2, 8, 64, "even"),
 ]
 
 
