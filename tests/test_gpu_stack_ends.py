@@ -461,6 +461,63 @@ def test_linear_ce_refusals(ctx_of):
     assert (dW == 0).all()
 
 
+# ---- offsets beyond 32 bits --------------------------------------------------------------------------------------------
+def test_offsets_beyond_32_bits_rows(ctx_of):
+    """1.1 M rows of 2048 channels: more than 2^31 elements, 4.5 GB of bf16.  The last rows give what they give alone."""
+    c, C, T, m = ctx_of(2, 2048), 2048, 1_100_000, 7
+    x = torch.empty(T, C, dtype=BF, device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    w, y, r = randn(2, C, std=0.2, mean=1.0, dtype=F32), torch.empty(T, C, dtype=BF, device=DEV), torch.empty(T, device=DEV)
+    c.block_in_fwd(x, w, 1e-6, y, r)
+    y2, r2 = empty(m, C), empty(m, dtype=F32)
+    c.block_in_fwd(x[-m:].clone(), w, 1e-6, y2, r2)
+    assert torch.equal(y[-m:], y2) and torch.equal(r[-m:], r2)
+    rng = rng_of(4, 2)
+    c.dropout(x, 0.5, rng, y)
+    g0 = (T - m) * C // 8                                       # the mask of the last rows, from the oracle's counter
+    keep = np.array([[((S.philox4x32((g & 0xFFFFFFFF, g >> 32, 2, 0), (4, 0))[e // 2] >> (16 * (e % 2))) & 0xFFFF) >= 32768
+                      for e in range(8)] for g in range(g0, g0 + m * C // 8)]).reshape(m, C)
+    ref = np.where(keep, f64(x[-m:]) * 2.0, 0.0)
+    close("dropout", y[-m:], ref, HALF * np.abs(ref))
+    du, dw = y, empty(C, dtype=F32)
+    c.block_in_bwd(x, w, r, x, du, dw)
+    du2, dw2 = empty(m, C), empty(C, dtype=F32)
+    c.block_in_bwd(x[-m:].clone(), w, r[-m:].clone(), x[-m:].clone(), du2, dw2)
+    assert torch.equal(du[-m:], du2)
+
+
+def test_offsets_beyond_32_bits_tables(ctx_of):
+    """A table and a head of 1.1 M rows x 2048: the last rows lie beyond 2^31 elements."""
+    c, C, V, n = ctx_of(2, 2048), 2048, 1_100_000, 2
+    W = torch.empty(V, C, dtype=BF, device=DEV).normal_(std=0.02, generator=torch.Generator(device=DEV).manual_seed(1))
+    ids = torch.tensor([V - 1, 5, V - 2, V - 1], device=DEV)
+    x0 = empty(4, n, C)
+    c.embed_fwd(ids, W, 2.0, x0)
+    assert torch.equal(x0, (W[ids].float() * 2.0).to(BF)[:, None, :].expand(4, n, C))
+    dE = torch.full((V, C), 3.0, device=DEV)
+    c.embed_bwd(ids, torch.ones(4, n, C, dtype=BF, device=DEV), 0.5, dE)
+    assert (dE[V - 1] == 2.0).all() and (dE[V - 2] == 1.0).all() and (dE[5] == 1.0).all()
+    dE[[5, V - 1, V - 2]] = 0
+    assert not dE.any()
+    del dE
+    for T in (3, 40):                                           # the streaming kernel and the tiles
+        h, target = randn(7, T, C), torch.full((T,), V - 1, device=DEV)
+        target[1] = 12
+        loss, lse, dl = empty(T, dtype=F32), empty(T, dtype=F32), torch.ones(T, device=DEV)
+        c.linear_ce_fwd(h, W, target, 1.0, loss, lse)
+        parts = [h.double() @ W[v:v + 100_000].double().T for v in range(0, V, 100_000)]
+        ref = torch.logsumexp(torch.cat([torch.logsumexp(p, 1)[:, None] for p in parts], 1), 1)
+        tl = (h.double() * W[target].double()).sum(1)
+        # logits of about 1: 128 steps of 16 products, V / 256 sums; as in check_loss
+        assert (lse - ref).abs().max() < 1e-4 and (loss - (ref - tl)).abs().max() < 1e-4
+        dh, dW = empty(T, C), torch.empty(V, C, dtype=BF, device=DEV)
+        c.linear_ce_bwd(h, W, target, 1.0, lse, dl, dh, dW)
+        p = torch.exp(parts[-1] - ref[:, None])                 # the last piece of 100 000 rows
+        p[:, -1] -= (target == V - 1).double()
+        want = p.T @ h.double()
+        assert (dW[-100_000:].double() - want).norm() <= 2 * HALF * want.norm()
+        del dW, parts
+
+
 # ---- streams, graphs, repeated runs ------------------------------------------------------------------------------------
 def test_two_streams_at_once_and_bitwise_repeats(ctx_of):
     c = ctx_of(4, 256)
