@@ -148,6 +148,7 @@ class MhcLite:
         self._scratch_need = {}
         # status words of the calls around the stack (lookup, loss): part of device_status()
         self._status = torch.empty(8, dtype=torch.int32, device=f"cuda:{device}")
+        self._bytes = self._status.view(torch.uint8)        # the type and device of scratch
         self._check(self.lib.mhclite_set_status_words(h, self._status.data_ptr()), "mhclite_set_status_words")
 
     def close(self):
@@ -430,7 +431,7 @@ class MhcLite:
             if len(self._scratch_need) > 256:
                 self._scratch_need.clear()
             self._scratch_need[kind, sizes] = need
-        return self._torch.empty(need, dtype=self._torch.uint8, device=self._status.device)
+        return self._bytes.new_empty(need)
 
     def embed_fwd(self, ids, E, scale, x0):
         """x0[t,j,:] = bf16(scale * E[ids[t],:]) for the n streams j; E fp32 or bf16 [V,C], x0 [T,n,C] bf16."""

@@ -86,6 +86,8 @@ block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
     constexpr int STAGES = fwd_stages(VPT), NT = GATE ? 2 : 1;
     extern __shared__ __align__(16) float sm[];
     __shared__ float red[2 * kMaxTeamWarps];
+    pdl_wait();
+    pdl_launch();
     const Team tm(wpr);
     const int nv = C >> 3;
     const uint32_t vec = blockDim.x * 16, ring = smem_u32(sm) + threadIdx.x * 16, stage = NT * VPT * vec;
@@ -158,6 +160,8 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
     extern __shared__ __align__(16) float sm[];                    // the ring, then [teams][C] column sums
     __shared__ float red[2 * kMaxTeamWarps];
     __shared__ double dred[8];
+    pdl_wait();
+    pdl_launch();
     const Team tm(wpr);
     const int nv = C >> 3;
     const uint32_t vec = blockDim.x * 16, ring = smem_u32(sm) + threadIdx.x * 16, stage = NT * VPT * vec;
@@ -235,7 +239,6 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
         }
     }
     cp_async_wait<0>();
-    pdl_launch();
     __syncthreads();
     // column sums of the block: the teams' rows through shared memory, in a fixed order
 #pragma unroll
@@ -270,6 +273,7 @@ __global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* _
     __shared__ float red[8][33];
     __shared__ double dred[8];
     pdl_wait();
+    pdl_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     const int per = (parts + 7) / 8, p0 = warp * per, p1 = min(parts, p0 + per);
     float a = 0.f;
@@ -303,6 +307,8 @@ __global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* _
 constexpr int kDropGroups = 4;
 __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloat16* __restrict__ x, DropArgs da,
                                                  __nv_bfloat16* __restrict__ y) {
+    pdl_wait();
+    pdl_launch();
     const Philox rng(da.rng, true);
     const uint32_t thr = da.threshold << 16;
     const uint64_t fac2 = both(da.factor);
@@ -377,8 +383,8 @@ void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void
         auto k = gate ? (da.rng ? block_fwd_k<V, B, true, true> : block_fwd_k<V, B, true, false>)                             \
                       : (da.rng ? block_fwd_k<V, B, false, true> : block_fwd_k<V, B, false, false>);                          \
         if (smem > 40 * 1024) { static SmemOnce once[2][2]; smem_limit(once[gate != nullptr][da.rng != nullptr], k, c->device, 226 * 1024); }               \
-        k<<<grid, p.threads, smem, s>>>(T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, eps, da, \
-                                        (uint4*)out, rstd);                                                             \
+        launch_after(k, dim3(grid), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, \
+                     eps, da, (uint4*)out, rstd);                                                                       \
     }
     MHCL_FWD(1, false) MHCL_FWD(2, false) MHCL_FWD(2, true) MHCL_FWD(4, true)
 #undef MHCL_FWD
@@ -398,8 +404,8 @@ void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void
         auto k = gate ? (da.rng ? block_bwd_k<V, B, true, true> : block_bwd_k<V, B, true, false>)                             \
                       : (da.rng ? block_bwd_k<V, B, false, true> : block_bwd_k<V, B, false, false>);                          \
         if (smem > 40 * 1024) { static SmemOnce once[2][2]; smem_limit(once[gate != nullptr][da.rng != nullptr], k, c->device, 226 * 1024); }               \
-        k<<<parts, p.threads, smem, s>>>(T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, rstd, da, \
-                                         (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
+        launch_after(k, dim3(parts), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, \
+                     scale, rstd, da, (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
     }
     MHCL_BWD(1, false) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, true)
 #undef MHCL_BWD
@@ -413,7 +419,7 @@ void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p,
     DropArgs da = drop_args(p, rng);
     da.rng = rng;                                          // read for p = 0 too (everything stays)
     c->launches += 1;
-    dropout_k<<<(unsigned)((groups + per - 1) / per), 256, 0, s>>>(count, (const __nv_bfloat16*)x, da, (__nv_bfloat16*)y);
+    launch_after(dropout_k, dim3((unsigned)((groups + per - 1) / per)), dim3(256), 0, s, count, (const __nv_bfloat16*)x, da, (__nv_bfloat16*)y);
 }
 
 }  // namespace mhcl

@@ -517,6 +517,7 @@ __global__ void __launch_bounds__(kSmThreads, 1)
 ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, const uint4* __restrict__ W,
            const int64_t* __restrict__ target, float scale, float2* __restrict__ part, float* __restrict__ tlogit) {
     extern __shared__ __align__(16) unsigned char sm_raw[];
+    pdl_wait();
     pdl_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
     const int WK = 1 << wk_log, WR = kSmWarps >> wk_log, wk = warp & (WK - 1), wr = warp >> wk_log;
@@ -801,7 +802,7 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         static SmemOnce once[3][2];
         smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
         c->launches += 2;
-        k<<<grid, kSmThreads, q.smem, s>>>((int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
+        launch_after(k, dim3(grid), dim3(kSmThreads), q.smem, s, (int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
         launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, loss, lse, c->op_status);
         return true;
     }

@@ -27,6 +27,8 @@ template <bool F32>
 __global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, int n, int tpt, const int64_t* __restrict__ ids,
                                                    const void* __restrict__ E, float scale, uint4* __restrict__ x0,
                                                    int* __restrict__ status) {
+    pdl_wait();
+    pdl_launch();
     const int nv = C >> 3, per = 256 / tpt, lt = threadIdx.x % tpt;
     const int64_t t = (int64_t)blockIdx.x * per + threadIdx.x / tpt;
     if (t >= T) return;
@@ -442,7 +444,7 @@ void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t*
     const unsigned grid = (unsigned)((T + 256 / tpt - 1) / (256 / tpt));
     c->launches += 1;
     auto k = table_f32 ? embed_fwd_k<true> : embed_fwd_k<false>;
-    k<<<grid, 256, 0, s>>>(T, V, c->C, c->n, tpt, ids, E, scale, (uint4*)x0, c->op_status);
+    launch_after(k, dim3(grid), dim3(256), 0, s, T, V, c->C, c->n, tpt, ids, E, scale, (uint4*)x0, c->op_status);
 }
 
 // List entries a warp adds up: 32 where that leaves enough warps to fill the GPU, fewer for short lists.
