@@ -20,7 +20,6 @@
 namespace mhcl {
 
 constexpr int kMaxTeamWarps = 16;
-constexpr int kFwdBlocks = 3, kBwdBlocks = 2;          // of 256 threads on an SM
 __host__ __device__ constexpr int fwd_stages(int vpt) { return vpt == 4 ? 2 : 4; }
 __host__ __device__ constexpr int bwd_stages(int vpt) { return vpt == 4 ? 2 : 4; }
 
@@ -80,7 +79,7 @@ struct DropArgs {
 // The arithmetic runs on packed pairs (two fp32 operations an instruction): with gate and dropout a vector of 8 elements
 // takes some 170 instructions forward and 230 backward, and with scalar ones the issue slots, not HBM, bounded the kernels.
 template <int VPT, bool BIG, bool GATE, bool DROP>
-__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : kFwdBlocks)
+__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : VPT == 4 ? 2 : 3)
 block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, float eps, DropArgs da, uint4* __restrict__ out, float* __restrict__ rstd) {
     constexpr int STAGES = fwd_stages(VPT), NT = GATE ? 2 : 1;
@@ -151,7 +150,7 @@ block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
 // s is applied once to each result.  The scale's sum runs over all T C elements and may cancel: it is added up in 64 bits
 // from the rows on.
 template <int VPT, bool BIG, bool GATE, bool DROP>
-__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : kBwdBlocks)
+__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : 2)
 block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
             const float* __restrict__ scale, const float* __restrict__ rstd, DropArgs da, const uint4* __restrict__ dy,
             uint4* __restrict__ dx, uint4* __restrict__ dgate, float* __restrict__ dw_part, double* __restrict__ ds_part,
@@ -340,13 +339,19 @@ __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloa
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-// Vectors a lane and warps a team for C channels: two vectors where that takes at most 16 warps, with as many warps as the
-// row fills (1536 channels: three), and about 256 threads a block, up to 512 for rows beyond 4096 channels.
+// Vectors a lane and warps a team for C channels, with as many warps as the row fills, and about 256 threads a block (up to
+// 512 for long rows).  Four vectors a lane forward: less of a row's fixed work a vector (16384 x 2048 with gate and dropout:
+// the two norms 67 -> 61 us), and backward without a gate where a row fills its warps (each 42 -> 40 us; 1536 channels would
+// leave a quarter of the lanes idle: 36 -> 39 us for 4099 rows).  With a gate, two backward while a team has at most 16
+// warps, since its third tensor takes the registers (four: 72 -> 76 us).
 struct RowPlan { int vpt, wpr, threads, teams; };
-static RowPlan plan_row(int C) {
+enum RowUse { ROW_FWD, ROW_BWD, ROW_BWD_GATED };
+static RowPlan plan_row(int C, RowUse use) {
     const int nv = C / 8;
+    const bool full = nv * 10 >= (nv + 127) / 128 * 128 * 9;
+    const bool two = use != ROW_FWD && (use == ROW_BWD_GATED || !full) && nv <= 64 * kMaxTeamWarps;
     RowPlan p;
-    p.vpt = nv <= 32 ? 1 : nv <= 64 * kMaxTeamWarps ? 2 : 4;
+    p.vpt = nv <= 32 ? 1 : nv <= 64 || two ? 2 : 4;
     p.wpr = (nv + 32 * p.vpt - 1) / (32 * p.vpt);
     p.teams = p.wpr < 8 ? 8 / p.wpr : 1;
     p.threads = p.teams * p.wpr * 32;
@@ -367,15 +372,15 @@ static DropArgs drop_args(float p, const uint64_t* rng) {
 }
 
 // (one block while its teams have at most two rows each: its column sums are then the result, without a second launch)
-int block_parts(int64_t T, int C, int sm_count) {
-    const RowPlan p = plan_row(C);
-    return T <= 2 * p.teams ? 1 : row_blocks(p, T, sm_count, kBwdBlocks);
+int block_parts(int64_t T, int C, int sm_count, bool gate) {
+    const RowPlan p = plan_row(C, gate ? ROW_BWD_GATED : ROW_BWD);
+    return T <= 2 * p.teams ? 1 : row_blocks(p, T, sm_count, 2);
 }
 
 void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C);
-    const int grid = row_blocks(p, T, c->sm_count, kFwdBlocks), smem = p.threads * 16 * p.vpt * (gate ? 2 : 1) * fwd_stages(p.vpt);
+    const RowPlan p = plan_row(c->C, ROW_FWD);
+    const int grid = row_blocks(p, T, c->sm_count, p.vpt == 4 ? 2 : 3), smem = p.threads * 16 * p.vpt * (gate ? 2 : 1) * fwd_stages(p.vpt);
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 1;
 #define MHCL_FWD(V, B)                                                                                                  \
@@ -386,15 +391,15 @@ void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void
         launch_after(k, dim3(grid), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, scale, \
                      eps, da, (uint4*)out, rstd);                                                                       \
     }
-    MHCL_FWD(1, false) MHCL_FWD(2, false) MHCL_FWD(2, true) MHCL_FWD(4, true)
+    MHCL_FWD(1, false) MHCL_FWD(2, false) MHCL_FWD(4, false) MHCL_FWD(4, true)
 #undef MHCL_FWD
 }
 
 void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       const float* rstd, float p_drop, const uint64_t* rng, const void* dy, void* dx, void* dgate, float* dw,
                       float* dscale, int accumulate, float* dw_part, double* ds_part, cudaStream_t s) {
-    const RowPlan p = plan_row(c->C);
-    const int parts = block_parts(T, c->C, c->sm_count);
+    const RowPlan p = plan_row(c->C, gate ? ROW_BWD_GATED : ROW_BWD);
+    const int parts = block_parts(T, c->C, c->sm_count, gate != nullptr);
     int smem = p.threads * 16 * p.vpt * (gate ? 3 : 2) * bwd_stages(p.vpt);
     if (smem < p.teams * c->C * 4) smem = p.teams * c->C * 4;
     const DropArgs da = drop_args(p_drop, rng);
@@ -407,7 +412,7 @@ void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void
         launch_after(k, dim3(parts), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, \
                      scale, rstd, da, (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
     }
-    MHCL_BWD(1, false) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, true)
+    MHCL_BWD(1, false) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, false) MHCL_BWD(4, true)
 #undef MHCL_BWD
     if (parts == 1) return;
     c->launches += 1;

@@ -148,7 +148,7 @@ inline void smem_limit(SmemOnce& once, K k, int device, int bytes) {
 
 // block_kernels.cu : the norms around a sublayer, with gate, scale and dropout, and dropout alone
 constexpr int kMaxRowC = 16384;               // channels of a row that a team of warps holds in registers
-int block_parts(int64_t T, int C, int sm_count);
+int block_parts(int64_t T, int C, int sm_count, bool gate);
 void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s);
 // dw_part [block_parts][C], ds_part [block_parts] (used when dscale is given)

@@ -38,7 +38,8 @@ static int check_row(mhclite_ctx* ctx) {
 struct BlockScratch { float* dw; double* ds; size_t bytes; };
 static BlockScratch plan_block(int C, int64_t T, int sm_count, void* base) {
     BlockScratch b;
-    const size_t parts = (size_t)block_parts(T, C, sm_count), dw = (parts * C * 4 + 255) & ~(size_t)255;
+    const int gated = block_parts(T, C, sm_count, true), plain = block_parts(T, C, sm_count, false);
+    const size_t parts = (size_t)(gated > plain ? gated : plain), dw = (parts * C * 4 + 255) & ~(size_t)255;
     b.dw = (float*)base;
     b.ds = (double*)((char*)base + dw);
     b.bytes = dw + ((parts * 8 + 255) & ~(size_t)255);
