@@ -264,25 +264,24 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
     }
 }
 
-// dw[c] (+)= sum over the blocks' partial rows, ds (+)= sum of their scalars; a block takes 32 columns, its 8 warps a
-// range of the partial rows each.
-__global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* __restrict__ dw_part,
-                                                const double* __restrict__ ds_part, float* __restrict__ dw,
-                                                float* __restrict__ ds, int accumulate) {
-    __shared__ float red[8][33];
-    __shared__ double dred[8];
+// dw[c] (+)= sum over the blocks' partial rows, ds (+)= sum of their scalars; a block takes 32 columns, its 32 warps a
+// range of the partial rows each (latency is all it costs: few rows a warp, loaded together).
+__global__ void __launch_bounds__(1024) colsum_k(int C, int parts, const float* __restrict__ dw_part,
+                                                 const double* __restrict__ ds_part, float* __restrict__ dw,
+                                                 float* __restrict__ ds, int accumulate) {
+    __shared__ float red[32][33];
+    __shared__ double dred[32];
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
-    const int per = (parts + 7) / 8, p0 = warp * per, p1 = min(parts, p0 + per);
+    const int per = (parts + 31) / 32, p0 = warp * per, p1 = min(parts, p0 + per);
     float a = 0.f;
     if (c < C)
-#pragma unroll 8
+#pragma unroll 10
         for (int p = p0; p < p1; ++p) a += dw_part[(int64_t)p * C + c];
     red[warp][lane] = a;
     if (ds && blockIdx.x == 0) {
-        double d = 0.0;
-        for (int p = p0 + lane; p < p1; p += 32) d += ds_part[p];
+        double d = p0 + lane < p1 ? ds_part[p0 + lane] : 0.0;  // per <= 32: at most 1024 parts
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
         if (lane == 0) dred[warp] = d;
@@ -291,12 +290,12 @@ __global__ void __launch_bounds__(256) colsum_k(int C, int parts, const float* _
     if (warp == 0 && c < C) {
         a = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a += red[i][lane];
+        for (int i = 0; i < 32; ++i) a += red[i][lane];
         dw[c] = accumulate ? dw[c] + a : a;
     }
-    if (ds && blockIdx.x == 0 && threadIdx.x == 0) {
+    if (ds && blockIdx.x == 0 && threadIdx.x == 32) {
         double d = 0.0;
-        for (int i = 0; i < 8; ++i) d += dred[i];
+        for (int i = 0; i < 32; ++i) d += dred[i];
         ds[0] = accumulate ? (float)(ds[0] + d) : (float)d;
     }
 }
@@ -416,7 +415,7 @@ void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void
 #undef MHCL_BWD
     if (parts == 1) return;
     c->launches += 1;
-    launch_after(colsum_k, dim3((c->C + 31) / 32), dim3(256), 0, s, c->C, parts, dw_part, ds_part, dw, dscale, accumulate);
+    launch_after(colsum_k, dim3((c->C + 31) / 32), dim3(1024), 0, s, c->C, parts, dw_part, ds_part, dw, dscale, accumulate);
 }
 
 void launch_dropout(const mhclite_ctx* c, int64_t count, const void* x, float p, const uint64_t* rng, void* y, cudaStream_t s) {
