@@ -311,8 +311,8 @@ MHCLITE_API int mhclite_relative_range(mhclite_ctx* ctx, int64_t T, const float*
  * the loss of the last hidden rows.  (Paper Section 4 trains such models; it takes these parts as given.)
  *   - C and n are the context's, C at most 16384 for the block calls.
  *   - Calls that need scratch take it as an argument (device, 256-byte aligned, at least the stated bytes, no contents
- *     to keep between calls), not from the attached workspace: calls with scratch of their own may overlap on the GPU, and
- *     each captured graph keeps its own.
+ *     to keep between calls; NULL where 0 bytes are stated), not from the attached workspace: calls with scratch of their
+ *     own may overlap on the GPU, and each captured graph keeps its own.
  *   - Token ids and targets are int64 (8-byte aligned); other pointers 16-byte aligned.
  *   - T == 0 launches no kernel, but parameter gradients that are not accumulated are then set to zero.
  *   - Results are the same bit for bit from run to run. */

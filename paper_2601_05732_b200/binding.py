@@ -423,7 +423,7 @@ class MhcLite:
         raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device}")
 
     def _scratch(self, kind, *sizes):
-        """Scratch of one call: allocated with torch on the current stream, which returns it in stream order (and keeps
+        """(pointer, bytes, owner) of one call's scratch: allocated with torch on the current stream, which returns it in stream order (and keeps
         it to a captured graph), so that calls on several streams and several graphs do not share any."""
         need = self._scratch_need.get((kind, sizes))
         if need is None:
@@ -431,7 +431,10 @@ class MhcLite:
             if len(self._scratch_need) > 256:
                 self._scratch_need.clear()
             self._scratch_need[kind, sizes] = need
-        return self._bytes.new_empty(need)
+        if need == 0:
+            return None, 0, None
+        t = self._bytes.new_empty(need)
+        return t.data_ptr(), need, t
 
     def embed_fwd(self, ids, E, scale, x0):
         """x0[t,j,:] = bf16(scale * E[ids[t],:]) for the n streams j; E fp32 or bf16 [V,C], x0 [T,n,C] bf16."""
@@ -447,8 +450,8 @@ class MhcLite:
         torch, T, V = self._torch, ids.shape[0], dE.shape[0]
         a = (self._arg("ids", ids, torch.int64, T), self._arg("g", g, torch.bfloat16, T, self.n, self.C), float(scale),
              self._arg("dE", dE, torch.float32, V, self.C), int(accumulate))
-        ws = self._scratch("embed", T, V)
-        self._check(self.lib.mhclite_embed_bwd(self._h, T, V, *a, ws.data_ptr(), ws.numel(), self._stream()),
+        ws, ws_bytes, _owner = self._scratch("embed", T, V)
+        self._check(self.lib.mhclite_embed_bwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
                     "mhclite_embed_bwd")
 
     def block_in_fwd(self, u, w, eps, v, rstd):
@@ -465,8 +468,8 @@ class MhcLite:
         a = (self._arg("u", u, b, T, self.C), self._arg("w", w, f, self.C), self._arg("rstd", rstd, f, T),
              self._arg("dv", dv, b, T, self.C), self._arg("du", du, b, T, self.C), self._arg("dw", dw, f, self.C),
              int(accumulate_params))
-        ws = self._scratch("block", T)
-        self._check(self.lib.mhclite_block_in_bwd(self._h, T, *a, ws.data_ptr(), ws.numel(), self._stream()),
+        ws, ws_bytes, _owner = self._scratch("block", T)
+        self._check(self.lib.mhclite_block_in_bwd(self._h, T, *a, ws, ws_bytes, self._stream()),
                     "mhclite_block_in_bwd")
 
     def _gate_args(self, T, gate, scale, p_drop, rng):
@@ -494,8 +497,8 @@ class MhcLite:
              rng_p, self._arg("dy", dy, b, T, self.C), self._arg("d_o", d_o, b, T, self.C),
              None if dgate is None else self._arg("dgate", dgate, b, T, self.C), self._arg("dw", dw, f, self.C),
              None if dscale is None else self._arg("dscale", dscale, f, 1), int(accumulate_params))
-        ws = self._scratch("block", T)
-        self._check(self.lib.mhclite_block_out_bwd(self._h, T, *a, ws.data_ptr(), ws.numel(), self._stream()),
+        ws, ws_bytes, _owner = self._scratch("block", T)
+        self._check(self.lib.mhclite_block_out_bwd(self._h, T, *a, ws, ws_bytes, self._stream()),
                     "mhclite_block_out_bwd")
 
     def dropout(self, x, p, rng, y):
@@ -514,8 +517,8 @@ class MhcLite:
         b, f = torch.bfloat16, torch.float32
         a = (self._arg("h", h, b, T, self.C), self._arg("W", W, b, V, self.C), self._arg("target", target, torch.int64, T),
              float(logit_scale), self._arg("loss", loss, f, T), self._arg("lse", lse, f, T))
-        ws = self._scratch("linear_ce", T, V, 0)
-        self._check(self.lib.mhclite_linear_ce_fwd(self._h, T, V, *a, ws.data_ptr(), ws.numel(), self._stream()),
+        ws, ws_bytes, _owner = self._scratch("linear_ce", T, V, 0)
+        self._check(self.lib.mhclite_linear_ce_fwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
                     "mhclite_linear_ce_fwd")
 
     def linear_ce_bwd(self, h, W, target, logit_scale, lse, dloss, dh, dW):
@@ -525,6 +528,6 @@ class MhcLite:
         a = (self._arg("h", h, b, T, self.C), self._arg("W", W, b, V, self.C), self._arg("target", target, torch.int64, T),
              float(logit_scale), self._arg("lse", lse, f, T), self._arg("dloss", dloss, f, T),
              self._arg("dh", dh, b, T, self.C), self._arg("dW", dW, b, V, self.C))
-        ws = self._scratch("linear_ce", T, V, 1)
-        self._check(self.lib.mhclite_linear_ce_bwd(self._h, T, V, *a, ws.data_ptr(), ws.numel(), self._stream()),
+        ws, ws_bytes, _owner = self._scratch("linear_ce", T, V, 1)
+        self._check(self.lib.mhclite_linear_ce_bwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
                     "mhclite_linear_ce_bwd")

@@ -23,7 +23,7 @@ namespace mhcl {
 
 constexpr int kCeM = 256, kCeN = 256, kCeK = 64;       // tile of a pair
 constexpr int kCeHalf = 128;                           // rows of A, columns of B and accumulator rows of one CTA
-constexpr int kCeStages = 6;
+constexpr int kCeStages = 6;                           // at most: the modes that write bf16 tiles give one up for staging
 constexpr int kCeABytes = kCeHalf * kCeK * 2, kCeStage = 2 * kCeABytes;
 constexpr int kCeEpiWarps = 8;                         // two per tensor-memory quadrant: columns 0..127 and 128..255
 constexpr int kCeThreads = 64 + 32 * kCeEpiWarps;      // warp 0: TMA, warp 1: MMA, the others: epilogue
@@ -62,6 +62,16 @@ struct CeArgs {
     __nv_bfloat16* dW;          // [V][C]
     int* status;
 };
+
+// The modes whose epilogue writes bf16 tiles send them through shared memory, 64 columns of a warp's 32 rows at a time, so
+// that a store covers whole 128-byte lines: a thread a row writes 32 bytes here and there, which held dW of few tokens (all
+// epilogue) at 2.7 TB/s.
+constexpr int kCeStagePitch = 144;                     // bytes a row: 128 and 16, so that neither side meets a bank twice
+__host__ __device__ constexpr bool ce_staged(int mode) { return mode == CE_GRAD || mode == CE_DW; }
+__host__ __device__ constexpr int ce_stages(int mode) { return ce_staged(mode) ? kCeStages - 1 : kCeStages; }
+__host__ __device__ constexpr int ce_smem(int mode) {
+    return ce_stages(mode) * kCeStage + (ce_staged(mode) ? kCeEpiWarps * 32 * kCeStagePitch : 0) + 256 + 1024;
+}
 
 struct CeCtl {
     uint64_t full[kCeStages], empty[kCeStages], acc_full[2], acc_empty[2];
@@ -128,8 +138,10 @@ __device__ __forceinline__ bool ce_wait(uint32_t bar, uint32_t parity, volatile 
     abort[0] = 1;
     return false;
 }
+// Arrives on a barrier of the pair's leader.  It orders tensor-memory reads alone (after tcgen05.fence), so it asks for no
+// release at cluster scope: that would wait for the warp's stores to global memory.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // Tile order: groups of row tiles, column tiles inside a group, so that the CTAs of a wave share operands in L2.
@@ -143,9 +155,11 @@ template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCeThreads, 1)
 ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb, const CeArgs a) {
     constexpr bool A_MN = MODE == CE_DW, B_MN = MODE == CE_DH || MODE == CE_DW;
+    constexpr int STAGES = ce_stages(MODE);
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    CeCtl* ctl = reinterpret_cast<CeCtl*>(smem + kCeStages * kCeStage);
+    CeCtl* ctl = reinterpret_cast<CeCtl*>(smem + STAGES * kCeStage);
+    static_assert(sizeof(CeCtl) <= 256, "control block");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = cta_rank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
@@ -159,7 +173,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
     const int ksteps = (ksize + kCeK - 1) / kCeK;
 
     if (tid == 0) {
-        for (int s = 0; s < kCeStages; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
+        for (int s = 0; s < STAGES; ++s) { mbar_init(smem_u32(&ctl->full[s]), 1); mbar_init(smem_u32(&ctl->empty[s]), 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(smem_u32(&ctl->acc_full[s]), 1); mbar_init(smem_u32(&ctl->acc_empty[s]), 2 * kCeEpiWarps); }
         abort[0] = abort[1] = abort[2] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -189,8 +203,8 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 const bool a_second = A_MN || m * kCeM + kCeHalf < live;
                 const int k1 = (int)((int64_t)ksteps * (split + 1) / splits);
                 for (int k = (int)((int64_t)ksteps * split / splits); k < k1; ++k, ++it) {
-                    const int s = it % kCeStages;
-                    ok = ce_wait(smem_u32(&ctl->empty[s]), ((it / kCeStages) & 1) ^ 1, abort, 1, it);
+                    const int s = it % STAGES;
+                    ok = ce_wait(smem_u32(&ctl->empty[s]), ((it / STAGES) & 1) ^ 1, abort, 1, it);
                     if (!ok) break;
                     const uint32_t own = smem_u32(&ctl->full[s]), full = leader_addr(own);
                     const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
@@ -209,8 +223,8 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 }
             }
             // the last products release their stages on both CTAs' barriers: neither CTA leaves before they have
-            for (int d = 0; d < kCeStages && ok; ++d, ++it)
-                if (it >= kCeStages) ok = ce_wait(smem_u32(&ctl->empty[it % kCeStages]), ((it / kCeStages) & 1) ^ 1, abort, 5, it);
+            for (int d = 0; d < STAGES && ok; ++d, ++it)
+                if (it >= STAGES) ok = ce_wait(smem_u32(&ctl->empty[it % STAGES]), ((it / STAGES) & 1) ^ 1, abort, 5, it);
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
@@ -225,8 +239,8 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 const int split = MODE == CE_DH ? i / per : 0;
                 const int k0 = (int)((int64_t)ksteps * split / splits), k1 = (int)((int64_t)ksteps * (split + 1) / splits);
                 for (int k = k0; k < k1; ++k, ++it) {
-                    const int s = it % kCeStages;
-                    ok = ce_wait(smem_u32(&ctl->full[s]), (it / kCeStages) & 1, abort, 3, it);
+                    const int s = it % STAGES;
+                    ok = ce_wait(smem_u32(&ctl->full[s]), (it / STAGES) & 1, abort, 3, it);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t sa = smem_u32(smem + s * kCeStage), sb = sa + kCeABytes;
@@ -244,6 +258,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
     } else {
         const int quad = warp & 3, half = (warp - 2) >> 2, row = (int)rank * kCeHalf + quad * 32 + lane;
         const float ref = MODE == CE_STATS ? 1.f : ce_ref(a.ref, a.refs);
+        const uint32_t staging = smem_u32(smem + STAGES * kCeStage + 256) + (warp - 2) * (32 * kCeStagePitch);
         bool ok = true;
         int j = 0;
         for (int i = pair; i < tiles && ok; i += pairs, ++j) {
@@ -258,6 +273,12 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
             const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
             const int n0 = n * kCeN + half * kCeHalf;           // this warp's 128 columns
             const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN + half * kCeHalf;
+            // once the tile has been read from tensor memory, before what was read is written out
+            auto hand_back = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&ctl->acc_empty[buf])));
+            };
             if (MODE == CE_STATS || MODE == CE_GRAD) {
                 const bool in = r < live;
                 const int t = in ? a.rows[r] : 0;
@@ -288,41 +309,79 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         for (int e = 0; e < 32; ++e) sum += ex2(v[e] - base);
                         mx = top;
                     }
+                    hand_back();
                     if (in) a.part[(int64_t)(2 * n + half) * a.Tpad + r] = make_float2(mx, sum);
                 } else {
                     const float lse2 = in ? a.lse[t] * kLog2e : 0.f, f = in ? a.dloss[t] / ref : 0.f;
-                    __nv_bfloat16* out = a.G + (int64_t)r * a.pitch + n0;
+                    __nv_bfloat16* out = a.G + (int64_t)(r - lane) * a.pitch + n0;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
-                        float v[32];
-                        tc_ld32(acc + c0, v);
+                    for (int c0 = 0; c0 < kCeHalf; c0 += 64) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            v[e] = ex2(fmaf(v[e], k2, -lse2));
-                            if (tgt == c0 + e) v[e] -= 1.f;
-                            v[e] = (in && c0 + e < cols) ? v[e] * f : 0.f;
+                        for (int h = 0; h < 64; h += 32) {
+                            float v[32];
+                            tc_ld32(acc + c0 + h, v);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                v[e] = ex2(fmaf(v[e], k2, -lse2));
+                                if (tgt == c0 + h + e) v[e] -= 1.f;
+                                v[e] = (in && c0 + h + e < cols) ? v[e] * f : 0.f;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 32; e += 8) sts128(staging + lane * kCeStagePitch + (h + e) * 2, pack8(v + e));
                         }
+                        if (c0 + 64 == kCeHalf) hand_back();
+                        __syncwarp();
 #pragma unroll
-                        for (int e = 0; e < 32; e += 16) st32(out + c0 + e, pack8(v + e), pack8(v + e + 8));
+                        for (int i8 = 0; i8 < 8; ++i8) {
+                            const int rr = i8 * 4 + (lane >> 3), cc = (lane & 7) * 8;
+                            *reinterpret_cast<uint4*>(out + (int64_t)rr * a.pitch + c0 + cc) = lds128(staging + rr * kCeStagePitch + cc * 2);
+                        }
+                        __syncwarp();
                     }
                 }
+            } else if (MODE == CE_DW) {
+                const float f = ksteps == 0 ? 0.f : a.scale * ref;          // no row has a target: nothing was accumulated
+                __nv_bfloat16* out = a.dW + (int64_t)(a.v0 + r - lane) * a.C + n0;
+                const int rows_in = a.vn - (r - lane);                      // of this warp's 32
+#pragma unroll 1
+                for (int c0 = 0; c0 < kCeHalf; c0 += 64) {
+#pragma unroll
+                    for (int h = 0; h < 64; h += 32) {
+                        float v[32];
+                        tc_ld32(acc + c0 + h, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = ksteps == 0 ? 0.f : v[e] * f;
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) sts128(staging + lane * kCeStagePitch + (h + e) * 2, pack8(v + e));
+                    }
+                    if (c0 + 64 == kCeHalf) hand_back();
+                    __syncwarp();
+#pragma unroll
+                    for (int i8 = 0; i8 < 8; ++i8) {
+                        const int rr = i8 * 4 + (lane >> 3), cc = (lane & 7) * 8;
+                        if (rr < rows_in && n0 + c0 + cc < a.C)
+                            *reinterpret_cast<uint4*>(out + (int64_t)rr * a.C + c0 + cc) = lds128(staging + rr * kCeStagePitch + cc * 2);
+                    }
+                    __syncwarp();
+                }
             } else {
-                const bool in = MODE == CE_DH ? r < live : r < a.vn;
-                const int64_t orow = MODE == CE_DH ? (in ? a.rows[r] : 0) : a.v0 + r;
+                const bool in = r < live;
+                const int64_t orow = in ? a.rows[r] : 0;
                 const float f = a.scale * ref;
-                // no row has a target, or a short last piece has fewer K steps than ranges
+                // a short last piece may have fewer K steps than ranges
                 const bool empty = (int64_t)ksteps * split / splits == (int64_t)ksteps * (split + 1) / splits;
 #pragma unroll 1
                 for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                     float v[32];
                     tc_ld32(acc + c0, v);
+                    if (c0 + 32 == kCeHalf) hand_back();
                     const int c = n0 + c0;
                     if (!in) continue;
                     if (empty) {                                        // nothing was accumulated
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = 0.f;
                     }
-                    if (MODE == CE_DH && (splits > 1 || !a.first || !a.last)) {
+                    if (splits > 1 || !a.first || !a.last) {
                         float* p = a.dh_acc + ((int64_t)split * a.Tpad + r) * a.C + c;
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
@@ -336,7 +395,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         }
                         if (splits > 1 || !a.last) continue;
                     }
-                    __nv_bfloat16* out = (MODE == CE_DH ? a.dh : a.dW) + orow * a.C + c;
+                    __nv_bfloat16* out = a.dh + orow * a.C + c;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[e] *= f;
 #pragma unroll
@@ -350,9 +409,6 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                     }
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&ctl->acc_empty[buf])));
         }
     }
     tc_fence_before();
@@ -754,7 +810,7 @@ static void launch_ce_rows(const mhclite_ctx* c, const CePlan& p, int64_t T, int
 
 template <int MODE>
 static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CUtensorMap& mb, CeArgs a, cudaStream_t s) {
-    constexpr int smem = kCeStages * kCeStage + (int)sizeof(CeCtl) + 1024;
+    constexpr int smem = ce_smem(MODE);
     const int64_t tiles = (int64_t)a.m_tiles * a.n_tiles * (MODE == CE_DH ? a.splits : 1);
     static SmemOnce once;
     smem_limit(once, ce_gemm_k<MODE>, c->device, smem);

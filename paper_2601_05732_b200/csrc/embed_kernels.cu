@@ -4,7 +4,7 @@
 //
 // The forward is bound by the n rows it writes a token.  The gradient is bound by the n rows it reads a token and the
 // table it writes; its sums must not depend on the order in which blocks run, so the tokens are sorted first (stable:
-// tokens of one id stay in ascending order; embed_rank_k for up to 6144 tokens, embed_sort_k beyond), then embed_grad_k
+// tokens of one id stay in ascending order; embed_rank_k for up to 6144 tokens, embed_sort_k beyond, embed_few_k without a sort for up to 192), then embed_grad_k
 // walks the sorted list in chunks, one warp a chunk and 256 channels, and keeps the running sum of the current id in fp32
 // registers.  An id whose tokens span several chunks leaves one partial row a chunk, which embed_join_k adds up in order: a
 // token as frequent as the commonest word does not serialise.  Rows that no token meets are zeroed by further blocks of
@@ -447,6 +447,86 @@ __global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C,
     }
 }
 
+// ---- a handful of tokens ---------------------------------------------------------------------------------------------
+// Up to 192 tokens: every block sees all keys at once, so nothing is sorted and one launch does it all.  The block of an
+// id's first token and of 256 channels adds up the id's tokens, an eighth of the list a warp in ascending order, then the
+// warps in order; further blocks clear the rows that no token meets.  3 streams of 1536 channels, 1000 rows: 64
+// tokens 11 us, with the sort and its two further launches 14; 200 tokens 13.0 and 14.2, 512 tokens 16.5 and 15.6.
+constexpr int kFewTokens = 192;
+template <int N_>
+__global__ void __launch_bounds__(256) embed_few_k(int T, int64_t V, int C, int64_t sum_blocks, int slices, const int64_t* __restrict__ ids,
+                                                   const uint4* __restrict__ g, float scale, float* __restrict__ dE, int accumulate,
+                                                   int* __restrict__ status) {
+    __shared__ uint32_t key[kFewTokens];
+    __shared__ uint32_t met[kZeroRows / 32];
+    __shared__ float4 red[8][32][2];
+    pdl_wait();
+    pdl_launch();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = C >> 3;
+    for (int i = tid; i < T; i += 256) key[i] = embed_key(__ldg(ids + i), i, V, blockIdx.x == 0, status);
+    if (tid < kZeroRows / 32) met[tid] = 0;
+    __syncthreads();
+    if (blockIdx.x >= sum_blocks) {
+        const int64_t v0 = (int64_t)(blockIdx.x - sum_blocks) * kZeroRows, v1 = v0 + kZeroRows < V ? v0 + kZeroRows : V;
+        for (int i = tid; i < T; i += 256)
+            if (key[i] >= v0 && key[i] < v1) atomicOr(&met[(key[i] - v0) >> 5], 1u << ((key[i] - v0) & 31));
+        __syncthreads();
+        const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int64_t v = v0 + warp; v < v1; v += 8) {
+            if (met[(v - v0) >> 5] >> ((v - v0) & 31) & 1u) continue;
+            float4* row = (float4*)(dE + v * C);
+            for (int c = lane; c < C / 4; c += 32) __stcs(row + c, zero);
+        }
+        return;
+    }
+    const int i = (int)(blockIdx.x / slices), v = (int)(blockIdx.x - (int64_t)i * slices) * 32 + lane;
+    const uint32_t k = key[i];
+    bool earlier = false;
+    for (int j = tid; j < i; j += 256) earlier |= key[j] == k;
+    if (__syncthreads_or(earlier || k >= V)) return;           // another block has the id's first token, or it has no row
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int per = ((T + 7) / 8 + 31) / 32 * 32;              // tokens a warp
+    constexpr int U = 16 / N_ > 4 ? 4 : 16 / N_;
+    for (int b = warp * per; b < T && b < (warp + 1) * per; b += 32) {
+        uint32_t same = __ballot_sync(0xffffffffu, b + lane < T && key[min(b + lane, T - 1)] == k);
+        while (same) {
+            uint4 d[U][N_];
+            int n = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (same) {
+                    const int t = b + __ffs(same) - 1;
+                    same &= same - 1;
+                    ++n;
+                    if (v < nv) {
+#pragma unroll
+                        for (int j = 0; j < N_; ++j) d[u][j] = ld_stream(g + ((int64_t)t * N_ + j) * nv + v);
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u >= n || v >= nv) break;
+#pragma unroll
+                for (int j = 0; j < N_; ++j) {
+                    float f[8];
+                    unpack8(d[u][j], f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) acc[e] += f[e];
+                }
+            }
+        }
+    }
+    red[warp][lane][0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    red[warp][lane][1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    __syncthreads();
+    if (warp != 0 || v >= nv) return;
+    float4 a = red[0][lane][0], c = red[0][lane][1];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) { add4(a, red[w][lane][0]); add4(c, red[w][lane][1]); }
+    join_store(dE, k, C, v, scale, accumulate, a, c);
+}
+
 // ---- host side -------------------------------------------------------------------------------------------------------
 void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* E, int table_f32, float scale,
                       void* x0, cudaStream_t s) {
@@ -480,15 +560,24 @@ static EmbedScratch plan_embed(int64_t T, int C, void* base) {
     p.bytes = off;
     return p;
 }
-size_t embed_scratch_bytes(int64_t T, int C) { return plan_embed(T, C, nullptr).bytes; }
+size_t embed_scratch_bytes(int64_t T, int C) { return T <= kFewTokens ? 0 : plan_embed(T, C, nullptr).bytes; }
 
 cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t* ids, const void* g, float scale, float* dE,
                              int accumulate, void* scratch, cudaStream_t s) {
+    const int slices = (c->C / 8 + 31) / 32;
+    cudaError_t e = cudaSuccess;
+    if (T <= kFewTokens) {
+        const int64_t sum_blocks = T * slices;
+        const int64_t zero_blocks = accumulate ? 0 : (V + kZeroRows - 1) / kZeroRows;
+        c->launches += 1;
+        MHCL_DISPATCH_N(c->n, e = launch_after(embed_few_k<N_>, dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, (int)T, V, c->C,
+                                               sum_blocks, slices, ids, (const uint4*)g, scale, dE, accumulate, c->op_status))
+        return e;
+    }
     const EmbedScratch p = plan_embed(T, c->C, scratch);
     c->launches += 2;
     int64_t to_zero = accumulate ? 0 : V;                      // the table's first rows, left to embed_grad_k
     const uint2* list = p.buf0;
-    cudaError_t e = cudaSuccess;
     if (T <= kRankMax) {
         const int blocks = (int)((T + 31) / 32);
         e = launch_after(embed_rank_k, dim3(blocks < c->sm_count * 2 ? blocks : c->sm_count * 2), dim3(256), 0, s, (int)T, V, ids, p.buf0,
@@ -530,7 +619,7 @@ cudaError_t launch_embed_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const i
             if (e != cudaSuccess) return e;
         }
     }
-    const int R = embed_chunk(T, c->C), slices = (c->C / 8 + 31) / 32;
+    const int R = embed_chunk(T, c->C);
     const int64_t chunks = (T + R - 1) / R, sum_blocks = (chunks * slices + 7) / 8;
     const int64_t zero_blocks = (to_zero + kZeroRows - 1) / kZeroRows;
     MHCL_DISPATCH_N(c->n, e = launch_after(embed_grad_k<N_>, dim3((unsigned)(sum_blocks + zero_blocks)), dim3(256), 0, s, T, V, to_zero, c->C, R,

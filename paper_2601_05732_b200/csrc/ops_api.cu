@@ -13,6 +13,7 @@ using namespace mhcl;
     } while (0)
 
 static int check_scratch(mhclite_ctx* ctx, const void* scratch, size_t given, size_t need) {
+    if (need == 0) return MHCLITE_OK;
     if (!scratch || given < need)
         return fail(ctx, MHCLITE_ERR_WORKSPACE, "scratch of %zu bytes needed, %zu given", need, scratch ? given : (size_t)0);
     if ((uintptr_t)scratch & 255) return fail(ctx, MHCLITE_ERR_BAD_ARG, "scratch not 256-byte aligned");
@@ -42,7 +43,7 @@ static BlockScratch plan_block(int C, int64_t T, int sm_count, void* base) {
     const size_t parts = (size_t)(gated > plain ? gated : plain), dw = (parts * C * 4 + 255) & ~(size_t)255;
     b.dw = (float*)base;
     b.ds = (double*)((char*)base + dw);
-    b.bytes = dw + ((parts * 8 + 255) & ~(size_t)255);
+    b.bytes = parts <= 1 ? 0 : dw + ((parts * 8 + 255) & ~(size_t)255);      // one block writes the sums itself
     return b;
 }
 

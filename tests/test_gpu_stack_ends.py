@@ -227,7 +227,7 @@ def test_embed_fwd(ctx_of, T, n, C, V, f32):
 EMBEDS = [  # T, n, C, V, ids
     (1, 4, 64, 9, "even"), (5, 2, 8, 1, "even"), (31, 3, 72, 300, "even"), (1000, 4, 256, 70, "even"), (5003, 3, 264, 5000, "text"),
     (4096, 4, 64, 100, "one"), (2500, 5, 1536, 70000, "text"), (70000, 2, 16, 1000, "text"), (33, 4, 520, 255, "one"), (256, 4, 64, 256, "even"),
-    (6144, 2, 64, 300, "text"), (6145, 2, 64, 300000, "text"), (20000, 2, 8, 64, "even"),
+    (64, 4, 2048, 500, "text"), (64, 2, 24, 3, "one"), (65, 2, 24, 3, "even"), (192, 3, 520, 2000, "text"), (192, 2, 24, 3, "one"), (193, 2, 24, 3, "even"), (6144, 2, 64, 300, "text"), (6145, 2, 64, 300000, "text"), (20000, 2, 8, 64, "even"),
 ]
 
 
@@ -290,10 +290,11 @@ def test_embed_refusals(ctx_of):
         c.embed_fwd(ids, E, 1.0, empty(2, 3, 16))
     with pytest.raises(ValueError):
         c.embed_fwd(ids.cpu(), E, 1.0, x0)
-    lib, g, dE = c.lib, randn(2, 2, 2, 16), empty(10, 16, dtype=F32)
-    need = lib.mhclite_embed_scratch_bytes(16, 2, 10)
+    ids = torch.zeros(1000, dtype=torch.int64, device=DEV)
+    lib, g, dE = c.lib, randn(2, 1000, 2, 16), empty(10, 16, dtype=F32)
+    need = lib.mhclite_embed_scratch_bytes(16, 1000, 10)
     ws = torch.empty(need, dtype=torch.uint8, device=DEV)
-    args = (c._h, 2, 10, ids.data_ptr(), g.data_ptr(), 1.0, dE.data_ptr(), 0)
+    args = (c._h, 1000, 10, ids.data_ptr(), g.data_ptr(), 1.0, dE.data_ptr(), 0)
     assert lib.mhclite_embed_bwd(*args, ws.data_ptr(), need - 1, None) == binding.ERR_WORKSPACE
     assert lib.mhclite_embed_bwd(*args, None, need, None) == binding.ERR_WORKSPACE
     assert lib.mhclite_embed_bwd(*args, ws.data_ptr() + 8, need, None) == binding.ERR_BAD_ARG
