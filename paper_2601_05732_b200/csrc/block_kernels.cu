@@ -208,11 +208,15 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
             unpack8x2(lds128(at + k * vec), f);
             unpack8x2(lds128(at + (VPT + k) * vec), zw[k]);
             if (GATE) unpack8x2(lds128(at + (2 * VPT + k) * vec), g);
-            if (DROP) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16);
+            if (GATE)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) g[e] = sigmoid2(g[e]);
+            if (DROP && GATE) drop8(zw[k], g, rng((uint64_t)(t * nv + v)), da.threshold << 16);
+            if (DROP && !GATE) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint64_t oh = mul2(f[e], r2);
-                if (GATE) { g[e] = sigmoid2(g[e]); zw[k][e] = mul2(zw[k][e], g[e]); }
+                if (GATE) zw[k][e] = mul2(zw[k][e], g[e]);
                 acc[k][e] = fma2(zw[k][e], oh, acc[k][e]);
                 zw[k][e] = mul2(zw[k][e], wf[k][e]);
                 const uint64_t q = mul2(zw[k][e], oh);

@@ -2,8 +2,8 @@
 //   l[t,v] = scale <h_t, W_v>,  lse_t = log sum_v exp l[t,v],  loss_t = lse_t - l[t,target_t],
 //   G[t,v] = scale dloss_t (exp(l[t,v] - lse_t) - [v = target_t]),  dh = G W,  dW = G^T h.
 //
-// Forward: one tcgen05 matrix product whose epilogue reduces each 128 x 256 tile of logits, still in tensor memory, to a
-// (maximum, sum) pair a row; ce_join_k joins a row's pairs.  Backward: the vocabulary in pieces.  A piece's logits are
+// Forward: one tcgen05 matrix product whose epilogue reduces each tile of logits, still in tensor memory, to (maximum, sum)
+// pairs of 128 columns of a row; ce_join_k joins a row's pairs.  Backward: the vocabulary in pieces.  A piece's logits are
 // computed again (2 T V C operations more, against T V values written and read back, and in fp32, where logits stored in
 // 16 bits would move exp(l - lse) by percents), turned into G in bf16, and G enters the two products.  A piece holds all
 // tokens, so its rows of dW are complete at once; dh adds up over the pieces in fp32.
@@ -34,7 +34,7 @@ enum CeMode { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
 struct CeArgs {
     const int* live;            // number of rows with a target
     const int* rows;            // [live] their token indices
-    int64_t T, V;
+    int64_t V;
     int C;
     int v0, vn;                 // the piece: rows v0 .. v0 + vn of W (vn a multiple of 256 except for the last piece)
     int m_tiles, n_tiles;       // at most; m_tiles of the row-wise modes is cut to `live` on the device
@@ -430,9 +430,9 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 
 // ---- rows with a target ----------------------------------------------------------------------------------------------
 // Block b handles `per` tokens: counts the targets before them, numbers its own rows, copies their h side by side, and
-// clears the outputs of the rows without a target (loss and lse, or dh).  In the backward it also leaves
-// the largest finite |dloss| of its rows (as bits).  The last block pads the
-// list's h with zero rows to the next multiple of 64, the K step of G^T h.
+// clears the outputs of the rows without a target (loss and lse, or dh).  In the backward it also leaves the largest finite
+// |dloss| of its rows (as bits), and the last block pads the list's h with zero rows to the next multiple of 64, the K step
+// of G^T h.
 __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* __restrict__ target,
                                                   const uint4* __restrict__ h, uint4* __restrict__ hl, int* __restrict__ rows,
                                                   int* __restrict__ live, float* __restrict__ loss, float* __restrict__ lse,
@@ -562,7 +562,7 @@ __global__ void __launch_bounds__(256) ce_dh_join_k(const int* __restrict__ live
 // will multiply, STAGES - 1 steps of 32 KB a CTA ahead, and nothing about W is exchanged or waited for between warps.  h
 // stays in shared memory; the warps' partial logits meet there, and a thread keeps the running (maximum, sum) of one (row
 // slot, token) over the CTA's rows.
-// One token, 2048 channels, 50257 words: 45 us, against 62 with the tiles, 51 with one step ahead in registers and 61
+// One token, 2048 channels, 50257 words: 43 us, against 62 with the tiles, 51 with one step ahead in registers and 61
 // with bulk copies of a row piece each, of which the copy engine starts too few.
 constexpr int kSmWarps = 16, kSmThreads = kSmWarps * 32, kSmTokens = 32;
 
@@ -747,7 +747,7 @@ static void ce_pieces(CePlan& p, int64_t V, int C) {
     if (most < 1) most = 1;
     if (most > nt) most = nt;
     int64_t best = most, best_cost = INT64_MAX;
-    for (int64_t w = most; w > 0 && w * 2 >= most; --w) {
+    for (int64_t w = most; w > 0 && w * 2 >= most; w -= 1 + most / 128) {
         int64_t cost = 0;
         for (int64_t v = 0; v < nt; v += w) {
             const int64_t n = nt - v < w ? nt - v : w;
@@ -867,7 +867,7 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, p.a_box) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
     launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, nullptr, s);
     CeArgs a = {};
-    a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
+    a.live = p.live; a.rows = p.rows; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
     a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
     a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
     launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
@@ -886,7 +886,7 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         return false;
     launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, dloss, s);
     CeArgs a = {};
-    a.live = p.live; a.rows = p.rows; a.T = T; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
+    a.live = p.live; a.rows = p.rows; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
     a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.refs = p.row_blocks; a.a_box = p.a_box; a.splits = p.splits; a.status = c->op_status;
     for (int i = 0; i < p.pieces; ++i) {

@@ -54,6 +54,11 @@ __device__ __forceinline__ void drop8(uint64_t* f, const uint4& w, uint32_t thr_
         f[e] = pack2f((r[e] << 16) >= thr_hi ? lo : 0.f, r[e] >= thr_hi ? hi : 0.f);
     }
 }
+// The same for two factors of a gradient, neither of which may leave anything of a dropped element (0 times NaN).
+__device__ __forceinline__ void drop8(uint64_t* f, uint64_t* g, const uint4& w, uint32_t thr_hi) {
+    drop8(f, w, thr_hi);
+    drop8(g, w, thr_hi);
+}
 #endif
 
 }  // namespace mhcl

@@ -154,9 +154,13 @@ def test_block_mask_is_the_dropout_mask(ctx_of):
     c.dropout(torch.ones(T, C, dtype=BF, device=DEV), 0.3, rng, m)
     assert torch.equal(m == 0, y == 0)
     gate[m == 0] = float("nan")                                   # what a dropped element holds does not matter
-    o2 = o.clone()
-    c.block_out_fwd(o2, gate, w, None, 1e-6, 0.3, rng, y, r)
+    c.block_out_fwd(o, gate, w, None, 1e-6, 0.3, rng, y, r)
     assert torch.isfinite(y).all()
+    dy = randn(4, T, C)
+    dy[m == 0] = float("inf")                                     # nor what its gradient holds
+    d_o, dg, dw = empty(T, C), empty(T, C), empty(C, dtype=F32)
+    c.block_out_bwd(o, gate, w, None, r, 0.3, rng, dy, d_o, dg, dw, None)
+    assert torch.isfinite(d_o).all() and torch.isfinite(dw).all() and (dg[m == 0] == 0).all() and torch.isfinite(dg).all()
 
 
 def test_block_large_and_zero_rows(ctx_of):
