@@ -82,6 +82,17 @@ struct CeCtl {
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 __device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t ex2_pair(uint64_t x) {
+    float a, b;
+    unpack2f(x, a, b);
+    return pack2f(ex2(a), ex2(b));
+}
+
 // The bracket of a row is kept as (p - [v = target]) dloss / ref in bf16, with ref the largest |dloss|; the products'
 // epilogues multiply by scale ref in fp32.  Equal dloss (a mean over the tokens) then cost no rounding, where 1 / T rounded
 // to bf16 would put one common error of up to 2^-9 on every gradient.
@@ -123,16 +134,21 @@ __device__ __forceinline__ void tc_commit_pair(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// A wait on a barrier that gives up after four seconds, or when another role of the CTA has.
+// A wait on a barrier that gives up after some four seconds, or when another role of the CTA has.  The hint lets the
+// hardware keep the warp asleep meanwhile.
 __device__ __forceinline__ bool ce_wait(uint32_t bar, uint32_t parity, volatile int* abort, int where, int index) {
-    if (mbar_try_wait(bar, parity)) return true;
     uint64_t t0 = 0, t;
     for (uint32_t i = 0;; ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
+        if (ok) return true;
         if (abort[0]) return false;
-        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-        if (i == 0) t0 = t;
-        if (t - t0 > 4000000000ull) break;
+        if ((i & 63) == 63) {
+            asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+            if (t0 == 0) t0 = t;
+            if (t - t0 > 4000000000ull) break;
+        }
     }
     if (abort[0] == 0) { abort[1] = where; abort[2] = index; }
     abort[0] = 1;
@@ -297,6 +313,24 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                             for (int e = 0; e < 32; ++e)
                                 if (tgt == c0 + e) a.tlogit[r] = v[e] * a.scale;
                         }
+                        if (k2 > 0.f && c0 + 32 <= cols) {             // the usual case, in as few instructions as it takes
+                            float t0 = v[0], t1 = v[1];
+#pragma unroll
+                            for (int e = 2; e < 30; e += 4) { t0 = max3(t0, v[e], v[e + 1]); t1 = max3(t1, v[e + 2], v[e + 3]); }
+                            const float top = fmaxf(mx, max3(fmaxf(t0, t1), v[30], v[31]) * k2), base = top == -INFINITY ? 0.f : top;
+                            const uint64_t kk = pack2f(k2, k2), bb = pack2f(-base, -base);
+                            uint64_t s0 = 0, s1 = 0;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4) {
+                                s0 = add2(s0, ex2_pair(fma2(pack2f(v[e], v[e + 1]), kk, bb)));
+                                s1 = add2(s1, ex2_pair(fma2(pack2f(v[e + 2], v[e + 3]), kk, bb)));
+                            }
+                            float x, y;
+                            unpack2f(add2(s0, s1), x, y);
+                            sum = sum * ex2(mx - base) + (x + y);
+                            mx = top;
+                            continue;
+                        }
                         float top = mx;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) {
@@ -320,6 +354,19 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         for (int h = 0; h < 64; h += 32) {
                             float v[32];
                             tc_ld32(acc + c0 + h, v);
+                            // the usual case: every row and column counts, and no row's target is among the columns
+                            if (__all_sync(0xffffffffu, in && c0 + h + 32 <= cols && (tgt < c0 + h || tgt >= c0 + h + 32))) {
+                                const uint64_t kk = pack2f(k2, k2), ll = pack2f(-lse2, -lse2), ff = pack2f(f, f);
+#pragma unroll
+                                for (int e = 0; e < 32; e += 8) {
+                                    uint64_t p[4];
+#pragma unroll
+                                    for (int i2 = 0; i2 < 4; ++i2)
+                                        p[i2] = mul2(ex2_pair(fma2(pack2f(v[e + 2 * i2], v[e + 2 * i2 + 1]), kk, ll)), ff);
+                                    sts128(staging + lane * kCeStagePitch + (h + e) * 2, pack8x2(p));
+                                }
+                                continue;
+                            }
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
                                 v[e] = ex2(fmaf(v[e], k2, -lse2));
