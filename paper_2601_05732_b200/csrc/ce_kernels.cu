@@ -11,6 +11,10 @@
 // Rows without a target (padding, prompts) are left out before the products: ce_rows_k lists the others and copies their
 // h side by side, so such rows cost nothing, and what they hold (NaN included) reaches neither loss nor gradients.
 //
+// What bounds it: the tensor cores, and behind them the power cap.  16384 x 2048 x 50257 on one B200: the forward's product
+// takes 1.97 ms alone (1.71 PFLOP/s, 94 % of the tensor cycles) and 2.34 ms in a long run at 985 W (1.44 PFLOP/s), where
+// each instruction of the other warps counts: the waits sleep in hardware and the usual-case epilogues run on packed pairs.
+//
 // Tiles: 256 x 256 a pair of CTAs (tcgen05 cta_group::2: each CTA stages 128 rows of A and 128 columns of B, and holds 128
 // rows of the accumulator), K in steps of 64 (one 128-byte swizzle row of bf16) through a ring of TMA stages, accumulators
 // double buffered in tensor memory so that the epilogue of one tile overlaps the products of the next.
@@ -787,7 +791,7 @@ static int64_t ce_rounds(int64_t tiles) { return (tiles + kCePairs - 1) / kCePai
 
 // Pieces of the vocabulary in the backward.  G of a piece takes at most about 384 MB; below that, the width whose products
 // leave the fewest pairs of CTAs idle in their last rounds, in steps of K over all pieces (16384 tokens, 2048 channels,
-// 50257 words: 37 tiles a piece fill whole rounds).
+// 50257 words: five pieces of 45 tiles, 3 % more rounds than tiles would fill).
 static void ce_pieces(CePlan& p, int64_t V, int C) {
     const int64_t mt = p.Tpad / kCeM, ct = (C + kCeN - 1) / kCeN, nt = p.n_tiles;
     int64_t most = ((int64_t)192 << 20) / p.Tpad / kCeN;
