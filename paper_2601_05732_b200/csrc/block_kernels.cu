@@ -178,7 +178,7 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
     int slot = 0, cur = 0;
     const float s = scale ? __ldg(scale) : 1.f;
     // dropout's factor rides on the weights, and on s in the column sums
-    const uint64_t s2 = both(s), fac2 = both(da.factor), minus1 = both(-1.f);
+    const uint64_t s2 = both(s), fac2 = both(da.factor), minus_s2 = both(-s);
     const Philox rng(DROP ? da.rng : nullptr, DROP);
     uint64_t acc[VPT][4], wf[VPT][4];
 #pragma unroll
@@ -219,9 +219,13 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
                 if (GATE) zw[k][e] = mul2(zw[k][e], g[e]);
                 acc[k][e] = fma2(zw[k][e], oh, acc[k][e]);
                 zw[k][e] = mul2(zw[k][e], wf[k][e]);
-                const uint64_t q = mul2(zw[k][e], oh);
-                ds2 = add2(ds2, q);
-                if (GATE) dg[e] = mul2(mul2(q, s2), fma2(g[e], minus1, both(1.f)));
+                if (GATE) {
+                    const uint64_t q = mul2(zw[k][e], oh);
+                    ds2 = add2(ds2, q);
+                    dg[e] = mul2(q, fma2(g[e], minus_s2, s2));             // s (1 - sig)
+                } else {
+                    ds2 = fma2(zw[k][e], oh, ds2);
+                }
             }
             if (GATE) st_stream(dgate + t * nv + v, pack8x2(dg));
         }

@@ -208,6 +208,18 @@ def test_block_refusals(ctx_of):
     assert (z == 1).all()
 
 
+def test_no_tokens_at_all(ctx_of):
+    """T = 0 launches nothing and leaves the outputs alone, forward; the backward's zero sums are tested with the refusals."""
+    c, C = ctx_of(4, 64), 64
+    none, nof, noi = empty(0, C), empty(0, dtype=F32), torch.empty(0, dtype=torch.int64, device=DEV)
+    w, W, before = torch.ones(C, device=DEV), randn(1, 10, C), c.kernel_launches()
+    c.block_in_fwd(none, w, 1e-6, none, nof)
+    c.block_out_fwd(none, none, w, None, 1e-6, 0.5, rng_of(1, 2), none, nof)
+    c.embed_fwd(noi, W, 1.0, empty(0, 4, C))
+    c.linear_ce_fwd(none, W, noi, 1.0, nof, nof)
+    assert c.kernel_launches() == before
+
+
 # ---- lookup ------------------------------------------------------------------------------------------------------------
 def some_ids(seed, T, V, kind):
     r = np.random.default_rng(seed)
