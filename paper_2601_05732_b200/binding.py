@@ -4,15 +4,18 @@ Every method of :class:`MhcLite` has the name of the C entry point it calls
 (``include/mhclite.h``) and passes the tensors' device pointers straight through;
 no step of the path runs in Python or on the CPU.  PyTorch supplies device memory
 and the CUDA stream.  Without the compiled library or without a CUDA device the
-calls raise.
+calls raise.  The calls around the stack, made once a token when a model decodes, are
+marshalled by a small extension module (``csrc/marshal.cpp``), the others by ctypes.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib
 import math
 import os
 
 _LIB = None
+_MARSHAL = None
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libmhclite.so")
 
@@ -106,6 +109,24 @@ def load(path: str | None = None):
     return lib
 
 
+def load_marshal():
+    """The extension module that marshals the calls around the stack, bound to the loaded library's entry points."""
+    global _MARSHAL
+    if _MARSHAL is None:
+        import torch  # noqa: F401  (its libraries have to be loaded before the extension's)
+        lib = load()
+        try:
+            from . import _marshal
+        except ImportError:
+            from . import build as _build
+            _build.build_marshal()
+            importlib.invalidate_caches()
+            from . import _marshal
+        _marshal.bind({name: C.cast(getattr(lib, name), _p).value for name in SIGNATURES})
+        _MARSHAL = _marshal
+    return _MARSHAL
+
+
 def status_string(status: int) -> str:
     return load().mhclite_status_string(int(status)).decode()
 
@@ -145,16 +166,16 @@ class MhcLite:
             raise MhcLiteError(rc, "mhclite_create")
         self._h = h
         self._ws = None
-        self._scratch_need = {}
         # status words of the calls around the stack (lookup, loss): part of device_status()
         self._status = torch.empty(8, dtype=torch.int32, device=f"cuda:{device}")
-        self._bytes = self._status.view(torch.uint8)        # the type and device of scratch
         self._check(self.lib.mhclite_set_status_words(h, self._status.data_ptr()), "mhclite_set_status_words")
+        self._m = load_marshal()
+        self._c = self._m.make(h.value, device, n, C_)
 
     def close(self):
         if getattr(self, "_h", None):
             self.lib.mhclite_destroy(self._h)
-            self._h = None
+            self._h = self._c = None
 
     __del__ = close
 
@@ -414,120 +435,64 @@ class MhcLite:
                                             self._ptr(colsum_dev, f), self._stream()), "mhclite_ds_gap")
 
     # -- around the stack: lookup, block norms, dropout, loss ------------------------------------------
-    def _arg(self, name, t, dtype, *shape):
-        """Device pointer of a contiguous tensor of exactly this type and shape on the context's device."""
-        if t.dtype is dtype and t.shape == shape and t.get_device() == self.device and t.is_contiguous():
-            return t.data_ptr()
-        if t.dtype != dtype or tuple(t.shape) != shape:
-            raise ValueError(f"{name}: expected {dtype} of shape {shape}, got {t.dtype} of shape {tuple(t.shape)}")
-        raise ValueError(f"{name}: expected a contiguous tensor on cuda:{self.device}")
-
-    def _scratch(self, kind, *sizes):
-        """(pointer, bytes, owner) of one call's scratch: allocated with torch on the current stream, which returns it in stream order (and keeps
-        it to a captured graph), so that calls on several streams and several graphs do not share any."""
-        need = self._scratch_need.get((kind, sizes))
-        if need is None:
-            need = int(getattr(self.lib, f"mhclite_{kind}_scratch_bytes")(self.C, *sizes))
-            if len(self._scratch_need) > 256:
-                self._scratch_need.clear()
-            self._scratch_need[kind, sizes] = need
-        if need == 0:
-            return None, 0, None
-        t = self._bytes.new_empty(need)
-        return t.data_ptr(), need, t
-
+    # Every tensor is contiguous, on the context's device, and of exactly the stated type and shape (ValueError otherwise).
+    # Scratch is allocated a call with torch on the current stream, which takes it back in stream order (and keeps it to a
+    # captured graph): calls on several streams and several graphs do not share any.
     def embed_fwd(self, ids, E, scale, x0):
-        """x0[t,j,:] = bf16(scale * E[ids[t],:]) for the n streams j; E fp32 or bf16 [V,C], x0 [T,n,C] bf16."""
-        torch, T, V = self._torch, ids.shape[0], E.shape[0]
-        f32 = E.dtype == torch.float32
-        self._check(self.lib.mhclite_embed_fwd(
-            self._h, T, V, self._arg("ids", ids, torch.int64, T),
-            self._arg("E", E, torch.float32 if f32 else torch.bfloat16, V, self.C), int(f32), float(scale),
-            self._arg("x0", x0, torch.bfloat16, T, self.n, self.C), self._stream()), "mhclite_embed_fwd")
+        """x0[t,j,:] = bf16(scale * E[ids[t],:]) for the n streams j; ids [T] int64, E fp32 or bf16 [V,C], x0 [T,n,C] bf16."""
+        rc = self._m.embed_fwd(self._c, ids, E, scale, x0)
+        if rc:
+            self._check(rc, "mhclite_embed_fwd")
 
     def embed_bwd(self, ids, g, scale, dE, accumulate=False):
-        """dE[v,:] (+)= scale * sum of g[t,j,:] over the streams j and the tokens t with ids[t] = v; dE [V,C] fp32."""
-        torch, T, V = self._torch, ids.shape[0], dE.shape[0]
-        a = (self._arg("ids", ids, torch.int64, T), self._arg("g", g, torch.bfloat16, T, self.n, self.C), float(scale),
-             self._arg("dE", dE, torch.float32, V, self.C), int(accumulate))
-        ws, ws_bytes, _owner = self._scratch("embed", T, V)
-        self._check(self.lib.mhclite_embed_bwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
-                    "mhclite_embed_bwd")
+        """dE[v,:] (+)= scale * sum of g[t,j,:] over the streams j and the tokens t with ids[t] = v; g [T,n,C] bf16,
+        dE [V,C] fp32."""
+        rc = self._m.embed_bwd(self._c, ids, g, scale, dE, accumulate)
+        if rc:
+            self._check(rc, "mhclite_embed_bwd")
 
     def block_in_fwd(self, u, w, eps, v, rstd):
-        """v = u rstd w with rstd = (mean u^2 + eps)^-1/2: the norm that opens a sublayer."""
-        torch, T = self._torch, u.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        self._check(self.lib.mhclite_block_in_fwd(
-            self._h, T, self._arg("u", u, b, T, self.C), self._arg("w", w, f, self.C), float(eps),
-            self._arg("v", v, b, T, self.C), self._arg("rstd", rstd, f, T), self._stream()), "mhclite_block_in_fwd")
+        """v = u rstd w with rstd = (mean u^2 + eps)^-1/2: the norm that opens a sublayer.  u, v [T,C] bf16; w [C], rstd [T]
+        fp32."""
+        rc = self._m.block_in_fwd(self._c, u, w, eps, v, rstd)
+        if rc:
+            self._check(rc, "mhclite_block_in_fwd")
 
     def block_in_bwd(self, u, w, rstd, dv, du, dw, accumulate_params=False):
-        torch, T = self._torch, u.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        a = (self._arg("u", u, b, T, self.C), self._arg("w", w, f, self.C), self._arg("rstd", rstd, f, T),
-             self._arg("dv", dv, b, T, self.C), self._arg("du", du, b, T, self.C), self._arg("dw", dw, f, self.C),
-             int(accumulate_params))
-        ws, ws_bytes, _owner = self._scratch("block", T)
-        self._check(self.lib.mhclite_block_in_bwd(self._h, T, *a, ws, ws_bytes, self._stream()),
-                    "mhclite_block_in_bwd")
-
-    def _gate_args(self, T, gate, scale, p_drop, rng):
-        torch = self._torch
-        return (None if gate is None else self._arg("gate", gate, torch.bfloat16, T, self.C),
-                None if scale is None else self._arg("scale", scale, torch.float32, 1),
-                float(p_drop), None if rng is None else self._arg("rng", rng, torch.int64, 2))
+        """Gradient of block_in_fwd: du [T,C] bf16, dw [C] fp32 from dv [T,C] bf16."""
+        rc = self._m.block_in_bwd(self._c, u, w, rstd, dv, du, dw, accumulate_params)
+        if rc:
+            self._check(rc, "mhclite_block_in_bwd")
 
     def block_out_fwd(self, o, gate, w, scale, eps, p_drop, rng, y, rstd):
         """y = scale * dropout(sigmoid(gate) o rstd w): what closes a sublayer before the merge.  gate (bf16 [T,C]) and
         scale (fp32 [1]) may be None; rng is an int64 tensor (seed, offset) on the device, None where p_drop is 0."""
-        torch, T = self._torch, o.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        gate_p, scale_p, p, rng_p = self._gate_args(T, gate, scale, p_drop, rng)
-        self._check(self.lib.mhclite_block_out_fwd(
-            self._h, T, self._arg("o", o, b, T, self.C), gate_p, self._arg("w", w, f, self.C), scale_p, float(eps), p, rng_p,
-            self._arg("y", y, b, T, self.C), self._arg("rstd", rstd, f, T), self._stream()), "mhclite_block_out_fwd")
+        rc = self._m.block_out_fwd(self._c, o, gate, w, scale, eps, p_drop, rng, y, rstd)
+        if rc:
+            self._check(rc, "mhclite_block_out_fwd")
 
     def block_out_bwd(self, o, gate, w, scale, rstd, p_drop, rng, dy, d_o, dgate, dw, dscale, accumulate_params=False):
         """Gradient of block_out_fwd with the same rng values; dgate is given exactly where gate is, dscale may be None."""
-        torch, T = self._torch, o.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        gate_p, scale_p, p, rng_p = self._gate_args(T, gate, scale, p_drop, rng)
-        a = (self._arg("o", o, b, T, self.C), gate_p, self._arg("w", w, f, self.C), scale_p, self._arg("rstd", rstd, f, T), p,
-             rng_p, self._arg("dy", dy, b, T, self.C), self._arg("d_o", d_o, b, T, self.C),
-             None if dgate is None else self._arg("dgate", dgate, b, T, self.C), self._arg("dw", dw, f, self.C),
-             None if dscale is None else self._arg("dscale", dscale, f, 1), int(accumulate_params))
-        ws, ws_bytes, _owner = self._scratch("block", T)
-        self._check(self.lib.mhclite_block_out_bwd(self._h, T, *a, ws, ws_bytes, self._stream()),
-                    "mhclite_block_out_bwd")
+        rc = self._m.block_out_bwd(self._c, o, gate, w, scale, rstd, p_drop, rng, dy, d_o, dgate, dw, dscale, accumulate_params)
+        if rc:
+            self._check(rc, "mhclite_block_out_bwd")
 
     def dropout(self, x, p, rng, y):
         """y = x / (1 - p) where an element stays, 0 where not; the same call on a gradient is the backward.  x, y: bf16
         of one shape; the mask is a function of rng = (seed, offset), int64 on the device, and is not stored."""
-        torch = self._torch
-        b, shape = torch.bfloat16, tuple(x.shape)
-        self._check(self.lib.mhclite_dropout(
-            self._h, x.numel(), self._arg("x", x, b, *shape), float(p), self._arg("rng", rng, torch.int64, 2),
-            self._arg("y", y, b, *shape), self._stream()), "mhclite_dropout")
+        rc = self._m.dropout(self._c, x, p, rng, y)
+        if rc:
+            self._check(rc, "mhclite_dropout")
 
     def linear_ce_fwd(self, h, W, target, logit_scale, loss, lse):
         """loss[t] = lse[t] - l[t, target[t]] and lse[t] = log sum exp l[t,:] of l = logit_scale h W^T, which is not stored;
         h [T,C], W [V,C] bf16, target [T] int64 (negative: no target, loss and lse 0), loss and lse [T] fp32."""
-        torch, T, V = self._torch, h.shape[0], W.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        a = (self._arg("h", h, b, T, self.C), self._arg("W", W, b, V, self.C), self._arg("target", target, torch.int64, T),
-             float(logit_scale), self._arg("loss", loss, f, T), self._arg("lse", lse, f, T))
-        ws, ws_bytes, _owner = self._scratch("linear_ce", T, V, 0)
-        self._check(self.lib.mhclite_linear_ce_fwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
-                    "mhclite_linear_ce_fwd")
+        rc = self._m.linear_ce_fwd(self._c, h, W, target, logit_scale, loss, lse)
+        if rc:
+            self._check(rc, "mhclite_linear_ce_fwd")
 
     def linear_ce_bwd(self, h, W, target, logit_scale, lse, dloss, dh, dW):
         """dh [T,C], dW [V,C] bf16 from dloss [T] fp32 and the forward's lse."""
-        torch, T, V = self._torch, h.shape[0], W.shape[0]
-        b, f = torch.bfloat16, torch.float32
-        a = (self._arg("h", h, b, T, self.C), self._arg("W", W, b, V, self.C), self._arg("target", target, torch.int64, T),
-             float(logit_scale), self._arg("lse", lse, f, T), self._arg("dloss", dloss, f, T),
-             self._arg("dh", dh, b, T, self.C), self._arg("dW", dW, b, V, self.C))
-        ws, ws_bytes, _owner = self._scratch("linear_ce", T, V, 1)
-        self._check(self.lib.mhclite_linear_ce_bwd(self._h, T, V, *a, ws, ws_bytes, self._stream()),
-                    "mhclite_linear_ce_bwd")
+        rc = self._m.linear_ce_bwd(self._c, h, W, target, logit_scale, lse, dloss, dh, dW)
+        if rc:
+            self._check(rc, "mhclite_linear_ce_bwd")

@@ -1,4 +1,5 @@
-"""Builds libmhclite.so in-tree with nvcc for sm_100a (cross-compiles without a GPU).
+"""Builds libmhclite.so (nvcc for sm_100a, cross-compiles without a GPU) and the Python extension _marshal.so (the host
+compiler against the installed torch) in-tree.
 
     python -m paper_2601_05732_b200.build [--force] [--verbose]
 """
@@ -15,6 +16,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libmhclite.so")
+MARSHAL_PATH = os.path.join(PKG_DIR, "_marshal.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -49,8 +51,38 @@ def _all_inputs():
     return files
 
 
+def build_marshal(force: bool = False) -> str:
+    """Compiles csrc/marshal.cpp, the argument marshalling of the calls around the stack; returns the module's path."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    root = os.path.dirname(torch.__file__)
+    src, header = os.path.join(CSRC, "marshal.cpp"), os.path.join(os.path.dirname(PKG_DIR), "include", "mhclite.h")
+    libs = os.path.join(root, "lib")
+    cuda = os.environ.get("CUDA_HOME") or os.path.dirname(os.path.dirname(_nvcc()))
+    fresh = os.path.join(OBJ_DIR, f"marshal.{os.getpid()}")           # moved into place whole: several processes may build
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{sysconfig.get_paths()['include']}",
+           *[f"-I{p}" for p in cpp_extension.include_paths()], f"-I{os.path.join(cuda, 'include')}", src, "-o", fresh,
+           f"-L{libs}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{libs}"]
+    digest = hashlib.sha256("\0".join([*(a for a in cmd if a != fresh), torch.__version__, sys.version, open(src).read(), open(header).read()]).encode()).hexdigest()
+    stamp = os.path.join(OBJ_DIR, "marshal.stamp")
+    if not force and os.path.exists(MARSHAL_PATH) and os.path.exists(stamp) and open(stamp).read() == digest:
+        return MARSHAL_PATH
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed on marshal.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(fresh, MARSHAL_PATH)
+    with open(stamp, "w") as f:
+        f.write(digest)
+    return MARSHAL_PATH
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compiles every .cu under csrc/ and links libmhclite.so; returns its path."""
+    """Compiles every .cu under csrc/ and links libmhclite.so, after _marshal.so; returns the library's path."""
+    build_marshal(force)
     stamp = os.path.join(OBJ_DIR, "stamp")
     digest = _digest(_all_inputs())
     if not force and os.path.exists(LIB_PATH) and os.path.exists(stamp) and open(stamp).read() == digest:

@@ -535,6 +535,36 @@ def test_offsets_beyond_32_bits_tables(ctx_of):
         del dW, parts
 
 
+# ---- marshalling -------------------------------------------------------------------------------------------------------
+def test_scratch_that_cannot_be_had_is_an_error_not_an_abort(ctx_of):
+    c, T, V = ctx_of(4, 64), 4096, 60000
+    h, W, target, dloss = loss_case(T, 64, V, 0.0)
+    lse, dh, dW = torch.zeros(T, device=DEV), empty(T, 64), empty(V, 64)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    total = torch.cuda.get_device_properties(0).total_memory
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (8 << 20)) / total)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            c.linear_ce_bwd(h, W, target, 1.0, lse, dloss, dh, dW)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    check_loss(c, h[:40], W[:300].contiguous(), target[:40] % 300, 1.0, dloss[:40].contiguous())
+
+
+def test_arguments_of_other_kinds_are_refused(ctx_of):
+    c, x, r = ctx_of(4, 64), randn(1, 4, 64), rng_of(1, 2)
+    for bad in (None, 3, "x", [1.0]):
+        with pytest.raises(TypeError):
+            c.dropout(bad, 0.1, r, x)
+    with pytest.raises(TypeError):
+        c.dropout(x, "much", r, empty(4, 64))
+    with pytest.raises(ValueError):
+        c.dropout(x.cpu(), 0.1, r, empty(4, 64))
+    with pytest.raises(ValueError):
+        c.block_in_fwd(torch.zeros((), dtype=BF, device=DEV), r, 1e-6, x, x)
+
+
 # ---- streams, graphs, repeated runs ------------------------------------------------------------------------------------
 def test_two_streams_at_once_and_bitwise_repeats(ctx_of):
     c = ctx_of(4, 256)

@@ -1,6 +1,9 @@
 """Host logic of the operators around the stack without a GPU: scratch planning and refusals that need no context."""
 import ctypes
 
+import pytest
+import torch
+
 from paper_2601_05732_b200 import binding
 
 
@@ -29,3 +32,24 @@ def test_null_context_is_refused():
             zero = [0.0 if a is ctypes.c_float else None if a is ctypes.c_void_p else 0 for a in args]
             assert getattr(lib, name)(*zero) == binding.ERR_BAD_ARG, name
     assert binding.status_string(binding.ERR_INDEX) not in ("ok", "unknown status")
+
+
+def test_arguments_are_refused_before_the_library_sees_them():
+    m = binding.load_marshal()
+    c = m.make(1234, 0, 4, 64)                            # a handle that no call gets as far as using
+    bf, f32, i64 = (lambda *s, t=t: torch.zeros(*s, dtype=t) for t in (torch.bfloat16, torch.float32, torch.int64))
+    value = [(m.dropout, f32(3), 0.1, None, None), (m.dropout, bf(3), 0.1, None, None),            # type, then device
+             (m.block_in_fwd, bf(3, 65), f32(64), 1e-6, bf(3, 64), f32(3)), (m.block_in_fwd, bf(()), f32(64), 1e-6, bf(64), f32(1)),
+             (m.embed_fwd, i64(3, 1), bf(9, 64), 1.0, bf(3, 4, 64)), (m.embed_bwd, i64(3), bf(3, 4, 64), 1.0, f32(()), False),
+             (m.linear_ce_fwd, bf(3, 64), bf(9, 63), i64(3), 1.0, f32(3), f32(3))]
+    kind = [(m.dropout, 3, 0.1, None, None), (m.dropout, bf(3)), (m.linear_ce_bwd, bf(3, 64), None, None, 1.0, None, None, None, None)]
+    for error, calls in ((ValueError, value), (TypeError, kind)):
+        for f, *args in calls:
+            with pytest.raises(error):
+                f(c, *args)
+    with pytest.raises(ValueError, match="closed"):
+        m.dropout(None, bf(3), 0.1, None, None)
+    with pytest.raises(ValueError):
+        m.dropout(object(), bf(3), 0.1, None, None)
+    with pytest.raises(KeyError):
+        m.bind({})
