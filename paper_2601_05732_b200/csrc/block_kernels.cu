@@ -158,7 +158,7 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
     constexpr int STAGES = bwd_stages(VPT), NT = GATE ? 3 : 2;
     extern __shared__ __align__(16) float sm[];                    // the ring, then [teams][C] column sums
     __shared__ float red[2 * kMaxTeamWarps];
-    __shared__ double dred[8];
+    __shared__ double dred[kMaxTeamWarps];
     pdl_wait();
     pdl_launch();
     const Team tm(wpr);
@@ -346,8 +346,9 @@ __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloa
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
-// Vectors a lane and warps a team for C channels, with as many warps as the row fills, and about 256 threads a block (up to
-// 512 for long rows).  Four vectors a lane forward: less of a row's fixed work a vector (16384 x 2048 with gate and dropout:
+// Vectors a lane and warps a team for C channels, with as many warps as the row fills, and about 256 threads a block forward
+// (up to 512 for long rows), about 512 backward, which leaves half as many partial rows to join (1536 channels, without a
+// gate: 512 rows 8.1 -> 6.6 us, 8192 rows 19.6 -> 18.0).  Four vectors a lane forward: less of a row's fixed work a vector (16384 x 2048 with gate and dropout:
 // the two norms 67 -> 61 us), and backward without a gate where a row fills its warps (each 42 -> 40 us; 1536 channels would
 // leave a quarter of the lanes idle: 36 -> 39 us for 4099 rows).  With a gate, two backward while a team has at most 16
 // warps, since its third tensor takes the registers (four: 72 -> 76 us).
@@ -360,11 +361,12 @@ static RowPlan plan_row(int C, RowUse use) {
     RowPlan p;
     p.vpt = nv <= 32 ? 1 : nv <= 64 || two ? 2 : 4;
     p.wpr = (nv + 32 * p.vpt - 1) / (32 * p.vpt);
-    p.teams = p.wpr < 8 ? 8 / p.wpr : 1;
+    const int most = use == ROW_FWD ? 8 : kMaxTeamWarps;
+    p.teams = p.wpr < most ? most / p.wpr : 1;
     p.threads = p.teams * p.wpr * 32;
     return p;
 }
-// Blocks: as many of 256 threads as an SM holds.
+// Blocks: as many of up to 256 threads as an SM holds, or one of more.
 static int row_blocks(const RowPlan& p, int64_t T, int sm_count, int per_sm) {
     const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * (p.threads > 256 ? 1 : per_sm);
     return (int)(need < cap ? need : cap);
@@ -419,7 +421,7 @@ void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void
         launch_after(k, dim3(parts), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, \
                      scale, rstd, da, (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
     }
-    MHCL_BWD(1, false) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, false) MHCL_BWD(4, true)
+    MHCL_BWD(1, false) MHCL_BWD(1, true) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, false) MHCL_BWD(4, true)
 #undef MHCL_BWD
     if (parts == 1) return;
     c->launches += 1;
