@@ -61,6 +61,7 @@ struct CeArgs {
     // CE_DH
     float* dh_acc;              // [splits][Tpad][C] sums over the pieces so far
     __nv_bfloat16* dh;          // [T][C]
+    int wide;                   // every run of 16 channels of dh begins on a 32-byte boundary
     int first, last;
     // CE_DW
     __nv_bfloat16* dW;          // [V][C]
@@ -107,7 +108,8 @@ __device__ __forceinline__ float ce_ref(const uint32_t* ref, int refs) {        
     return top > 0 ? __uint_as_float(top) : 1.f;
 }
 
-// 32 bytes to global memory in one instruction (a full sector a thread).
+// 32 bytes to global memory in one instruction (a full sector a thread); p has to be 32-byte aligned, which callers' tensors
+// need not be.
 __device__ __forceinline__ void st32(void* p, const uint4& a, const uint4& b) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x),
                  "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
@@ -451,7 +453,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                     for (int e = 0; e < 32; ++e) v[e] *= f;
 #pragma unroll
                     for (int e = 0; e < 32; e += 16) {
-                        if (c + e + 16 <= a.C && (a.C & 15) == 0) {     // whole sectors
+                        if (a.wide && c + e + 16 <= a.C) {              // whole sectors
                             st32(out + e, pack8(v + e), pack8(v + e + 8));
                         } else {
                             if (c + e < a.C) *reinterpret_cast<uint4*>(out + e) = pack8(v + e);
@@ -939,6 +941,7 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
+    a.wide = C % 16 == 0 && ((uintptr_t)dh & 31) == 0;
     a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.refs = p.row_blocks; a.a_box = p.a_box; a.splits = p.splits; a.status = c->op_status;
     for (int i = 0; i < p.pieces; ++i) {
         a.v0 = (int)(i * p.piece);

@@ -478,6 +478,65 @@ def test_linear_ce_refusals(ctx_of):
     assert (dW == 0).all()
 
 
+# ---- tensors that begin 16 bytes into their buffers ---------------------------------------------------------------------
+def inside(t):
+    """The same values in a view 16 bytes (one element, for int64: 8) into a buffer: the least alignment the calls allow."""
+    k = max(1, 16 // t.element_size()) if t.dtype != torch.int64 else 1
+    v = torch.empty(t.numel() + 2 * k, dtype=t.dtype, device=DEV)[k:k + t.numel()].view(t.shape)
+    assert v.data_ptr() % 32 in (8, 16)
+    return v.copy_(t)
+
+
+class InnerViews:
+    """A context whose calls get every tensor as such a view; what they wrote is copied back to the caller's tensors."""
+
+    def __init__(self, c):
+        self.c, self.n, self.C = c, c.n, c.C
+
+    def __getattr__(self, name):
+        def call(*args, **kw):
+            views = [inside(a) if torch.is_tensor(a) else a for a in args]
+            getattr(self.c, name)(*views, **kw)
+            for a, v in zip(args, views):
+                if torch.is_tensor(a) and a.dtype != torch.int64:
+                    a.copy_(v)
+        return call
+
+
+# (up to 256 columns the product dh = G W is not split, and its tiles go straight to dh)
+@pytest.mark.parametrize("T,C,V", [(40, 64, 200), (300, 72, 256), (300, 128, 2001), (3, 64, 500), (1, 1024, 300)])
+def test_linear_ce_on_inner_views(ctx_of, T, C, V):
+    h, W, target, dloss = loss_case(T, C, V, 0.0 if T == 1 else 0.2)
+    check_loss(InnerViews(ctx_of(4, C)), h, W, target, 1.0, dloss)
+
+
+@pytest.mark.parametrize("T,C,V,f32", [(5, 64, 40, True), (300, 72, 300, False), (7000, 16, 50, True)])
+def test_embed_on_inner_views(ctx_of, T, C, V, f32):
+    c = ctx_of(3, C)
+    E, ids = randn(1, V, C, dtype=F32 if f32 else BF), torch.from_numpy(some_ids(2, T, V, "text")).to(DEV)
+    x0, x1, dE, dE1, g = empty(T, 3, C), empty(T, 3, C), empty(V, C, dtype=F32), empty(V, C, dtype=F32), randn(3, T, 3, C)
+    for k, x, d in ((c, x0, dE), (InnerViews(c), x1, dE1)):
+        k.embed_fwd(ids, E, 1.5, x)
+        k.embed_bwd(ids, g, 1.5, d)
+    assert torch.isfinite(x0).all() and torch.equal(x0, x1) and torch.isfinite(dE).all() and torch.equal(dE, dE1)
+
+
+@pytest.mark.parametrize("T,C,gated,p", [(2, 64, True, 0.2), (700, 1536, False, 0.1), (300, 1040, True, 0.0)])
+def test_block_and_dropout_on_inner_views(ctx_of, T, C, gated, p):
+    c, rng = ctx_of(4, C), rng_of(8, 9)
+    o, gate, dy = randn(1, T, C), randn(2, T, C) if gated else None, randn(3, T, C)
+    w, s, outs = randn(4, C, mean=1.0, dtype=F32), torch.full((1,), 0.3, device=DEV), []
+    for k in (c, InnerViews(c)):
+        y, r, d_o, dg = empty(T, C), empty(T, dtype=F32), empty(T, C), empty(T, C) if gated else None
+        dw, ds, z = empty(C, dtype=F32), empty(1, dtype=F32), empty(T, C)
+        k.block_out_fwd(o, gate, w, s, 1e-6, p, rng, y, r)
+        k.block_out_bwd(o, gate, w, s, r, p, rng, dy, d_o, dg, dw, ds)
+        k.dropout(o, 0.4, rng, z)
+        outs.append([t for t in (y, r, d_o, dg, dw, ds, z) if t is not None])
+    for a, b in zip(*outs):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
 # ---- offsets beyond 32 bits --------------------------------------------------------------------------------------------
 def test_offsets_beyond_32_bits_rows(ctx_of):
     """1.1 M rows of 2048 channels: more than 2^31 elements, 4.5 GB of bf16.  The last rows give what they give alone."""
