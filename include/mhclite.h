@@ -317,8 +317,9 @@ MHCLITE_API int mhclite_relative_range(mhclite_ctx* ctx, int64_t T, const float*
  *   - T == 0 launches no kernel, but parameter gradients that are not accumulated are then set to zero.
  *   - Results are the same bit for bit from run to run. */
 
-/* Attaches 8 device ints (caller-owned, cleared by this call, synchronous; NULL detaches) in which the calls below record
- * the first token index outside its table, or a wait that gave up; mhclite_device_status reports it.  They must stay valid
+/* Attaches 8 device ints (caller-owned; NULL detaches) in which the calls below record the first token index outside its
+ * table, or a wait that gave up; mhclite_device_status reports it.  The words are cleared by this call, which waits for all
+ * work queued on the device before and for the clearing (not while a stream is being captured).  They must stay valid
  * as long as calls made, or captured into a graph, while they were attached can run. */
 MHCLITE_API int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words);
 typedef enum mhclite_op {          /* the operator named in such a report */
@@ -431,8 +432,8 @@ MHCLITE_API int mhclite_set_kernel_timing(mhclite_ctx* ctx, int on);
 MHCLITE_API int mhclite_kernel_time_ms(mhclite_ctx* ctx, int kernel, float* ms);
 
 /* Synchronous check of the device status word: kernels that wait on hardware barriers do so with a bound
- * and, instead of hanging, record MHCLITE_ERR_TIMEOUT there and return.  Copies one int device->host
- * (synchronises the device); returns MHCLITE_OK or the recorded status. */
+ * and, instead of hanging, record MHCLITE_ERR_TIMEOUT there and return.  Waits for all work queued on the
+ * device, whatever its stream, then copies the words to the host; returns MHCLITE_OK or the recorded status. */
 MHCLITE_API int mhclite_device_status(mhclite_ctx* ctx);
 
 /* Number of kernels this context has launched since it was created (for accounting; host counter). */

@@ -837,8 +837,13 @@ int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words) {
     MHCL_REQUIRE_CTX(ctx);
     MHCL_OPT_PTR(ctx, words);
     if (words) {
+        // Kernels that still report into the words, or write whatever held their memory before, may run on streams that
+        // do not wait for the one that clears; and a call that follows must not overtake the clearing.
         MHCL_DEVICE(ctx);
-        int rc = check_cuda(ctx, cudaMemset(words, 0, 32), "clearing the status words");
+        cudaError_t e = cudaDeviceSynchronize();
+        if (e == cudaSuccess) e = cudaMemset(words, 0, 32);
+        if (e == cudaSuccess) e = cudaDeviceSynchronize();
+        int rc = check_cuda(ctx, e, "clearing the status words");
         if (rc) return rc;
     }
     ctx->op_status = words;
@@ -849,10 +854,12 @@ int mhclite_device_status(mhclite_ctx* ctx) {
     MHCL_REQUIRE_CTX(ctx);
     if (!ctx->status_word && !ctx->op_status) return MHCLITE_OK;
     MHCL_DEVICE(ctx);
+    int rc = check_cuda(ctx, cudaDeviceSynchronize(), "waiting for the device");      // a copy alone waits for some streams only
+    if (rc) return rc;
     for (const int* words : {ctx->status_word, ctx->op_status}) {
         if (!words) continue;
         int v[5] = {0, 0, 0, 0, 0};
-        int rc = check_cuda(ctx, cudaMemcpy(v, words, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
+        rc = check_cuda(ctx, cudaMemcpy(v, words, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
         if (rc) return rc;
         if (v[0] == MHCLITE_ERR_INDEX)
             return fail(ctx, v[0], "operator %d met token index %d (low 32 bits) outside the table, at token %lld", v[1], v[2],

@@ -686,6 +686,54 @@ def test_captured_and_replayed_with_new_inputs(ctx_of):
                 assert torch.equal(b[name], ref[name]), (k, name)
 
 
+# ---- status words ------------------------------------------------------------------------------------------------------
+BUSY = 100_000_000                  # cycles a stream is kept busy: some 50 ms
+
+
+def test_status_words_are_cleared_behind_work_on_other_streams():
+    """What is queued on any stream when the words are attached has no part in what they say afterwards."""
+    c, side = binding.MhcLite(2, 16, 0), torch.cuda.Stream()
+    words = torch.zeros(8, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+        words.fill_(binding.ERR_INDEX)
+    assert c.lib.mhclite_set_status_words(c._h, words.data_ptr()) == binding.OK
+    assert (words == 0).all()
+    c.device_status()
+    # cleared once the call is back: a report that follows at once, on another stream, stays
+    torch.cuda._sleep(BUSY)
+    assert c.lib.mhclite_set_status_words(c._h, words.data_ptr()) == binding.OK
+    with torch.cuda.stream(side):
+        c.embed_fwd(torch.tensor([99], device=DEV), randn(1, 10, 16), 1.0, empty(1, 2, 16))
+    torch.cuda.synchronize()
+    assert words[0] == binding.ERR_INDEX
+
+
+def test_context_made_on_a_side_stream_starts_clean():
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        last = torch.empty(8, dtype=torch.int32, device=DEV)
+        torch.cuda._sleep(BUSY)
+        last.fill_(binding.ERR_INDEX)
+        del last                                                         # the next allocation of this size gets its memory
+        c = binding.MhcLite(2, 16, 0)
+    torch.cuda.synchronize()
+    c.device_status()
+
+
+def test_status_waits_for_work_on_other_streams():
+    c, side, E, x0 = binding.MhcLite(2, 16, 0), torch.cuda.Stream(), randn(1, 10, 16), empty(1, 2, 16)
+    ids = torch.tensor([99], device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+        c.embed_fwd(ids, E, 1.0, x0)
+    with pytest.raises(binding.MhcLiteError) as e:
+        c.device_status()
+    assert e.value.status == binding.ERR_INDEX
+
+
 # ---- a whole model step ------------------------------------------------------------------------------------------------
 def test_model_step_runs_and_its_gradients_match_differences():
     """ids -> loss through two mixing layers with a gated sublayer, dropout on, and back.  The activations between the
