@@ -13,6 +13,7 @@ import ctypes as C
 import importlib
 import math
 import os
+import threading
 
 _LIB = None
 _MARSHAL = None
@@ -145,6 +146,22 @@ def workspace_bytes(n: int, Cc: int, T: int, kind: int = 0) -> int:
     return int(load().mhclite_workspace_bytes(n, Cc, T, kind))
 
 
+# Status words (8 int32 a context) that kernels report into when a token index or a wait goes wrong.  A captured graph, or work
+# queued on any stream, can still report after its context is gone, so the memory is never given back: 32 bytes a context.
+_status_slabs: dict = {}                # device -> (tensors [_STATUS_SLAB, 8], rows of the last one in use)
+_status_lock = threading.Lock()
+_STATUS_SLAB = 128
+
+
+def _status_words(torch, device: int):
+    with _status_lock:
+        slabs, used = _status_slabs.get(device, ([], _STATUS_SLAB))
+        if used == _STATUS_SLAB:
+            slabs, used = slabs + [torch.empty(_STATUS_SLAB, 8, dtype=torch.int32, device=f"cuda:{device}")], 0
+        _status_slabs[device] = (slabs, used + 1)
+        return slabs[-1][used]
+
+
 class MhcLite:
     """One library context: n residual streams of C channels on one CUDA device."""
 
@@ -167,7 +184,7 @@ class MhcLite:
         self._h = h
         self._ws = None
         # status words of the calls around the stack (lookup, loss): part of device_status()
-        self._status = torch.empty(8, dtype=torch.int32, device=f"cuda:{device}")
+        self._status = _status_words(torch, device)
         self._check(self.lib.mhclite_set_status_words(h, self._status.data_ptr()), "mhclite_set_status_words")
         self._m = load_marshal()
         self._c = self._m.make(h.value, device, n, C_)

@@ -734,6 +734,22 @@ def test_status_waits_for_work_on_other_streams():
     assert e.value.status == binding.ERR_INDEX
 
 
+def test_graph_that_outlives_its_context_writes_to_no_other_tensor():
+    E, x0, ids = randn(1, 10, 16), empty(2, 2, 16), torch.tensor([1, 2], device=DEV)
+    c = binding.MhcLite(2, 16, 0)
+    c.embed_fwd(ids, E, 1.0, x0)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.embed_fwd(ids, E, 1.0, x0)
+    del c
+    others = [torch.zeros(8, dtype=torch.int32, device=DEV) for _ in range(4000)]
+    ids.fill_(99)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert (x0 == 0).all() and not any(t.any().item() for t in others)
+
+
 # ---- a whole model step ------------------------------------------------------------------------------------------------
 def test_model_step_runs_and_its_gradients_match_differences():
     """ids -> loss through two mixing layers with a gated sublayer, dropout on, and back.  The activations between the

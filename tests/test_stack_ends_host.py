@@ -53,3 +53,14 @@ def test_arguments_are_refused_before_the_library_sees_them():
         m.dropout(object(), bf(3), 0.1, None, None)
     with pytest.raises(KeyError):
         m.bind({})
+
+
+def test_status_words_are_never_shared_or_given_back(monkeypatch):
+    class Torch:                                          # device memory of the host
+        int32 = torch.int32
+        empty = staticmethod(lambda *s, dtype, device: torch.empty(*s, dtype=dtype))
+    monkeypatch.setattr(binding, "_status_slabs", {})
+    rows = [binding._status_words(Torch, d).data_ptr() for _ in range(300) for d in (0, 1)]      # the tensors are dropped
+    assert len(set(rows)) == 600 and all(r % 16 == 0 for r in rows)
+    held = {s.data_ptr() + 32 * i for slabs, _ in binding._status_slabs.values() for s in slabs for i in range(len(s))}
+    assert set(rows) <= held
