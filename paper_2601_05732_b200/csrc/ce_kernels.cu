@@ -468,10 +468,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
     __syncthreads();
     if (ctl->abort[0]) {
         for (int i = 0; i < 64; ++i) __nanosleep(2000);        // copies in flight land before the memory is given up
-        if (tid == 0 && a.status && atomicCAS(a.status, 0, MHCLITE_ERR_TIMEOUT) == 0) {
-            a.status[1] = MHCLITE_OP_LINEAR_CE + 100 * MODE; a.status[2] = ctl->abort[1]; a.status[3] = blockIdx.x;
-            a.status[4] = ctl->abort[2];
-        }
+        if (tid == 0) report_wait(a.status, MHCLITE_OP_LINEAR_CE + 100 * MODE, ctl->abort[1], (int)blockIdx.x, ctl->abort[2]);
     }
     __syncthreads();
     pair_sync();                                               // the other CTA's products may read this one's memory until here
@@ -522,9 +519,7 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
                 }
             } else {
                 if (loss) { loss[t] = 0.f; lse[t] = 0.f; }
-                if (y >= V && status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
-                    status[1] = MHCLITE_OP_LINEAR_CE; status[2] = (int)y; status[3] = (int)(t >> 31); status[4] = (int)(t & 0x7FFFFFFF);
-                }
+                if (y >= V) report_index(status, MHCLITE_OP_LINEAR_CE, t, y);
             }
         }
         for (int i = warp; i < 32 && b + i < t1; i += 32) {     // a warp a row
@@ -766,8 +761,8 @@ __global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int par
         for (int w = 0; w < 16; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
         l = (top + lg2(s)) * kLn2;
         x = l - tlogit[lane];
-    } else if (y >= V && status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
-        status[1] = MHCLITE_OP_LINEAR_CE; status[2] = (int)y; status[3] = 0; status[4] = lane;
+    } else if (y >= V) {
+        report_index(status, MHCLITE_OP_LINEAR_CE, lane, y);
     }
     lse[lane] = l;
     loss[lane] = x;

@@ -44,6 +44,28 @@ struct mhclite_ctx {
 
 namespace mhcl {
 
+// The eight status words (mhclite_set_status_words): 0 to 4 the first token index outside its table, 5 to 7 the first wait that
+// gave up, so that neither report hides the other.
+constexpr int kStatusWait = 5;
+struct WaitReport { int kernel, wait, block; };
+inline WaitReport unpack_wait(int w) { return {w & 0xFFF, w >> 12 & 0xF, w >> 16 & 0x7FFF}; }
+#ifdef __CUDACC__
+__device__ __forceinline__ void report_wait(int* status, int kernel, int wait, int block, int index) {
+    if (status && atomicCAS(status + kStatusWait, 0, MHCLITE_ERR_TIMEOUT) == 0) {
+        status[kStatusWait + 1] = kernel | wait << 12 | block << 16;
+        status[kStatusWait + 2] = index;
+    }
+}
+__device__ __forceinline__ void report_index(int* status, int kernel, int64_t where, int64_t value) {
+    if (status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
+        status[1] = kernel;
+        status[2] = (int)value;
+        status[3] = (int)(where >> 31);
+        status[4] = (int)(where & 0x7FFFFFFF);
+    }
+}
+#endif
+
 inline int ipow_fact(int n) { int f = 1; for (int i = 2; i <= n; ++i) f *= i; return f; }
 inline int round_up(int v, int m) { return (v + m - 1) / m * m; }
 inline int64_t round_up64(int64_t v, int64_t m) { return (v + m - 1) / m * m; }

@@ -14,15 +14,6 @@
 
 namespace mhcl {
 
-__device__ __forceinline__ void report_index(int* status, int kernel, int64_t where, int64_t value) {
-    if (status && atomicCAS(status, 0, MHCLITE_ERR_INDEX) == 0) {
-        status[1] = kernel;
-        status[2] = (int)value;
-        status[3] = (int)(where >> 31);
-        status[4] = (int)(where & 0x7FFFFFFF);
-    }
-}
-
 template <bool F32>
 __global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, int n, int tpt, const int64_t* __restrict__ ids,
                                                    const void* __restrict__ E, float scale, uint4* __restrict__ x0,

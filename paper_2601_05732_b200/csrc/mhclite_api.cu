@@ -856,18 +856,20 @@ int mhclite_device_status(mhclite_ctx* ctx) {
     MHCL_DEVICE(ctx);
     int rc = check_cuda(ctx, cudaDeviceSynchronize(), "waiting for the device");      // a copy alone waits for some streams only
     if (rc) return rc;
-    for (const int* words : {ctx->status_word, ctx->op_status}) {
-        if (!words) continue;
-        int v[5] = {0, 0, 0, 0, 0};
-        rc = check_cuda(ctx, cudaMemcpy(v, words, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
-        if (rc) return rc;
-        if (v[0] == MHCLITE_ERR_INDEX)
-            return fail(ctx, v[0], "operator %d met token index %d (low 32 bits) outside the table, at token %lld", v[1], v[2],
-                        (long long)(((int64_t)v[3] << 31) | v[4]));
-        if (v[0] != 0)
-            return fail(ctx, v[0], "a kernel gave up on a bounded wait (kernel %d, wait %d, block %d, index %d)", v[1], v[2],
-                        v[3], v[4]);
+    int v[5] = {0, 0, 0, 0, 0}, o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (ctx->status_word) rc = check_cuda(ctx, cudaMemcpy(v, ctx->status_word, sizeof(v), cudaMemcpyDeviceToHost), "read status word");
+    if (!rc && ctx->op_status) rc = check_cuda(ctx, cudaMemcpy(o, ctx->op_status, sizeof(o), cudaMemcpyDeviceToHost), "read status words");
+    if (rc) return rc;
+    if (v[0] != 0)
+        return fail(ctx, v[0], "a kernel gave up on a bounded wait (kernel %d, wait %d, block %d, index %d)", v[1], v[2], v[3], v[4]);
+    if (o[kStatusWait] != 0) {
+        const WaitReport w = unpack_wait(o[kStatusWait + 1]);
+        return fail(ctx, o[kStatusWait], "a kernel gave up on a bounded wait (kernel %d, wait %d, block %d, index %d)", w.kernel, w.wait, w.block,
+                    o[kStatusWait + 2]);
     }
+    if (o[0] != 0)
+        return fail(ctx, o[0], "operator %d met token index %d (low 32 bits) outside the table, at token %lld", o[1], o[2],
+                    (long long)(((int64_t)o[3] << 31) | o[4]));
     return MHCLITE_OK;
 }
 

@@ -734,6 +734,23 @@ def test_status_waits_for_work_on_other_streams():
     assert e.value.status == binding.ERR_INDEX
 
 
+def test_a_report_hides_no_other():
+    """The words, as kernels leave them: an index in 0 to 4, a wait that gave up in 5 to 7 (kernel, wait and block in one)."""
+    c, words = binding.MhcLite(2, 16, 0), torch.zeros(8, dtype=torch.int32, device=DEV)
+    assert c.lib.mhclite_set_status_words(c._h, words.data_ptr()) == binding.OK
+    c.embed_fwd(torch.tensor([1, 99], device=DEV), randn(1, 10, 16), 1.0, empty(2, 2, 16))
+    torch.cuda.synchronize()
+    assert words.tolist() == [binding.ERR_INDEX, 20, 99, 0, 1, 0, 0, 0]
+    words[5], words[6], words[7] = binding.ERR_TIMEOUT, 122 | 4 << 12 | 147 << 16, 77
+    with pytest.raises(binding.MhcLiteError, match="kernel 122, wait 4, block 147, index 77") as e:
+        c.device_status()
+    assert e.value.status == binding.ERR_TIMEOUT
+    words[5] = 0
+    with pytest.raises(binding.MhcLiteError, match="index 99 .* at token 1$") as e:
+        c.device_status()
+    assert e.value.status == binding.ERR_INDEX
+
+
 def test_graph_that_outlives_its_context_writes_to_no_other_tensor():
     E, x0, ids = randn(1, 10, 16), empty(2, 2, 16), torch.tensor([1, 2], device=DEV)
     c = binding.MhcLite(2, 16, 0)
