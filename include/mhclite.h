@@ -319,9 +319,9 @@ MHCLITE_API int mhclite_relative_range(mhclite_ctx* ctx, int64_t T, const float*
 
 /* Attaches 8 device ints (caller-owned; NULL detaches) in which the calls below record the first token index outside its
  * table and the first wait that gave up; mhclite_device_status reports them, the wait before the index, until the words are
- * attached again.  The words are cleared by this call, which waits for all work queued on the device before and for the
- * clearing (not while a stream is being captured).  They must stay valid as long as calls made, or captured into a graph,
- * while they were attached can run. */
+ * attached again.  The words, and the attached workspace's, are cleared by this call, which waits for all work queued on the
+ * device before and for the clearing (not while a stream is being captured).  They must stay valid as long as calls made,
+ * or captured into a graph, while they were attached can run. */
 MHCLITE_API int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words);
 typedef enum mhclite_op {          /* the operator named in such a report */
     MHCLITE_OP_EMBED = 20,

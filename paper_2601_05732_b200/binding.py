@@ -185,7 +185,7 @@ class MhcLite:
         self._ws = None
         # status words of the calls around the stack (lookup, loss): part of device_status()
         self._status = _status_words(torch, device)
-        self._check(self.lib.mhclite_set_status_words(h, self._status.data_ptr()), "mhclite_set_status_words")
+        self.clear_device_status()
         self._m = load_marshal()
         self._c = self._m.make(h.value, device, n, C_)
 
@@ -396,8 +396,13 @@ class MhcLite:
         return float(ms.value)
 
     def device_status(self):
-        """Raises if a kernel recorded a timed-out wait (synchronises the device)."""
+        """Raises if a kernel recorded a timed-out wait or a token index outside its table (synchronises the device)."""
         self._check(self.lib.mhclite_device_status(self._h), "mhclite_device_status")
+
+    def clear_device_status(self):
+        """Forgets what device_status reports, so that later reports are seen: waits for all work queued on the device, then
+        attaches the status words anew."""
+        self._check(self.lib.mhclite_set_status_words(self._h, self._status.data_ptr()), "mhclite_set_status_words")
 
     def kernel_launches(self) -> int:
         return int(self.lib.mhclite_kernel_launches(self._h))

@@ -842,6 +842,7 @@ int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words) {
         MHCL_DEVICE(ctx);
         cudaError_t e = cudaDeviceSynchronize();
         if (e == cudaSuccess) e = cudaMemset(words, 0, 32);
+        if (e == cudaSuccess && ctx->status_word) e = cudaMemset(ctx->status_word, 0, 32);
         if (e == cudaSuccess) e = cudaDeviceSynchronize();
         int rc = check_cuda(ctx, e, "clearing the status words");
         if (rc) return rc;

@@ -751,6 +751,20 @@ def test_a_report_hides_no_other():
     assert e.value.status == binding.ERR_INDEX
 
 
+def test_reports_can_be_cleared():
+    c, E, x0 = binding.MhcLite(2, 16, 0), randn(1, 10, 16), empty(3, 2, 16)
+    c.premix_fwd(randn(2, 3, 2, 16), torch.full((3, 2), 0.5, device=DEV), empty(3, 16))
+    c.ensure_workspace(64)
+    for ids, at in (([1, 99, 2], 1), ([1, 2, -4], 2)):
+        c.embed_fwd(torch.tensor(ids, device=DEV), E, 1.0, x0)
+        with pytest.raises(binding.MhcLiteError, match="at token %d$" % at):
+            c.device_status()
+        with pytest.raises(binding.MhcLiteError):
+            c.device_status()                                            # it stays until it is cleared
+        c.clear_device_status()
+        c.device_status()
+
+
 def test_graph_that_outlives_its_context_writes_to_no_other_tensor():
     E, x0, ids = randn(1, 10, 16), empty(2, 2, 16), torch.tensor([1, 2], device=DEV)
     c = binding.MhcLite(2, 16, 0)
