@@ -44,7 +44,7 @@ __device__ __forceinline__ float team_sum(float v, float* red, int& slot, const 
 }
 // Copies this lane's vectors of one row into a stage: [vector][thread] of 16 bytes.
 template <int VPT>
-__device__ __forceinline__ void fetch_row(uint32_t to, const uint4* __restrict__ row, const Team& tm, int nv) {
+__device__ __forceinline__ void fetch_row(uint32_t to, const uint4* row, const Team& tm, int nv) {
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
         const int v = tm.lt + k * tm.threads;
@@ -65,8 +65,8 @@ __device__ __forceinline__ uint64_t sigmoid2(uint64_t a) {
 }
 __device__ __forceinline__ uint64_t both(float x) { return pack2f(x, x); }
 // the 8 weights of a vector, as packed pairs
-__device__ __forceinline__ void load_w(const float4* __restrict__ w, int v, uint64_t* o) {
-    const ulonglong2 a = __ldg((const ulonglong2*)w + 2 * v), b = __ldg((const ulonglong2*)w + 2 * v + 1);
+__device__ __forceinline__ void load_w(const float4* w, int v, uint64_t* o) {
+    const ulonglong2 a = ld_dep((const ulonglong2*)w + 2 * v), b = ld_dep((const ulonglong2*)w + 2 * v + 1);
     o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
 }
 
@@ -80,8 +80,8 @@ struct DropArgs {
 // takes some 170 instructions forward and 230 backward, and with scalar ones the issue slots, not HBM, bounded the kernels.
 template <int VPT, bool BIG, bool GATE, bool DROP>
 __global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : VPT == 4 ? 2 : 3)
-block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
-            const float* __restrict__ scale, float eps, DropArgs da, uint4* __restrict__ out, float* __restrict__ rstd) {
+block_fwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const float4* w,
+            const float* scale, float eps, DropArgs da, uint4* out, float* rstd) {
     constexpr int STAGES = fwd_stages(VPT), NT = GATE ? 2 : 1;
     extern __shared__ __align__(16) float sm[];
     __shared__ float red[2 * kMaxTeamWarps];
@@ -101,7 +101,7 @@ block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) fetch(t0 + i * step, i);
     int slot = 0, cur = 0;
-    const float s = scale ? __ldg(scale) : 1.f;
+    const float s = scale ? ld_dep(scale) : 1.f;
     const float sf = DROP ? s * da.factor : s;
     const Philox rng(DROP ? da.rng : nullptr, DROP);
     uint64_t wf[VPT][4];
@@ -151,10 +151,10 @@ block_fwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
 // from the rows on.
 template <int VPT, bool BIG, bool GATE, bool DROP>
 __global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : 2)
-block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4* __restrict__ gate, const float4* __restrict__ w,
-            const float* __restrict__ scale, const float* __restrict__ rstd, DropArgs da, const uint4* __restrict__ dy,
-            uint4* __restrict__ dx, uint4* __restrict__ dgate, float* __restrict__ dw_part, double* __restrict__ ds_part,
-            float* __restrict__ dw, float* __restrict__ ds, int accumulate) {
+block_bwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const float4* w,
+            const float* scale, const float* rstd, DropArgs da, const uint4* dy,
+            uint4* dx, uint4* dgate, float* dw_part, double* ds_part,
+            float* dw, float* ds, int accumulate) {
     constexpr int STAGES = bwd_stages(VPT), NT = GATE ? 3 : 2;
     extern __shared__ __align__(16) float sm[];                    // the ring, then [teams][C] column sums
     __shared__ float red[2 * kMaxTeamWarps];
@@ -176,7 +176,7 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) fetch(t0 + i * step, i);
     int slot = 0, cur = 0;
-    const float s = scale ? __ldg(scale) : 1.f;
+    const float s = scale ? ld_dep(scale) : 1.f;
     // dropout's factor rides on the weights, and on s in the column sums
     const uint64_t s2 = both(s), fac2 = both(da.factor), minus_s2 = both(-s);
     const Philox rng(DROP ? da.rng : nullptr, DROP);
@@ -189,10 +189,10 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
         for (int e = 0; e < 4; ++e) { acc[k][e] = 0; if (DROP) wf[k][e] = mul2(wf[k][e], fac2); }
     }
     double dsum = 0.0;
-    float r_next = t0 < T ? __ldg(rstd + t0) : 0.f;
+    float r_next = t0 < T ? ld_dep(rstd + t0) : 0.f;
     for (int64_t t = t0; t < T; t += step) {
         const float r = r_next;
-        if (t + step < T) r_next = __ldg(rstd + t + step);
+        if (t + step < T) r_next = ld_dep(rstd + t + step);
         cp_async_wait<STAGES - 2>();
         fetch(t + (STAGES - 1) * step, cur == 0 ? STAGES - 1 : cur - 1);       // into the stage of the row before
         const uint32_t at = ring + cur * stage;
@@ -274,9 +274,9 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* __restrict__ x, const uint4*
 
 // dw[c] (+)= sum over the blocks' partial rows, ds (+)= sum of their scalars; a block takes 32 columns, its 32 warps a
 // range of the partial rows each (latency is all it costs: few rows a warp, loaded together).
-__global__ void __launch_bounds__(1024) colsum_k(int C, int parts, const float* __restrict__ dw_part,
-                                                 const double* __restrict__ ds_part, float* __restrict__ dw,
-                                                 float* __restrict__ ds, int accumulate) {
+__global__ void __launch_bounds__(1024) colsum_k(int C, int parts, const float* dw_part,
+                                                 const double* ds_part, float* dw,
+                                                 float* ds, int accumulate) {
     __shared__ float red[32][33];
     __shared__ double dred[32];
     pdl_wait();
@@ -311,8 +311,8 @@ __global__ void __launch_bounds__(1024) colsum_k(int C, int parts, const float* 
 // A thread takes four groups of 8 elements 256 apart: their loads are in flight together, and the round keys are made
 // once for the four.
 constexpr int kDropGroups = 4;
-__global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloat16* __restrict__ x, DropArgs da,
-                                                 __nv_bfloat16* __restrict__ y) {
+__global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloat16* x, DropArgs da,
+                                                 __nv_bfloat16* y) {
     pdl_wait();
     pdl_launch();
     const Philox rng(da.rng, true);
@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(256) dropout_k(int64_t count, const __nv_bfloa
     uint4 v[kDropGroups];
 #pragma unroll
     for (int k = 0; k < kDropGroups; ++k)
-        if (g0 + k * 256 < full) v[k] = ld_stream(x + (g0 + k * 256) * 8);
+        if (g0 + k * 256 < full) v[k] = ld_dep_stream(x + (g0 + k * 256) * 8);
 #pragma unroll
     for (int k = 0; k < kDropGroups; ++k) {
         const int64_t g = g0 + k * 256;

@@ -483,11 +483,11 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 // clears the outputs of the rows without a target (loss and lse, or dh).  In the backward it also leaves the largest finite
 // |dloss| of its rows (as bits), and the last block pads the list's h with zero rows to the next multiple of 64, the K step
 // of G^T h.
-__global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* __restrict__ target,
-                                                  const uint4* __restrict__ h, uint4* __restrict__ hl, int* __restrict__ rows,
-                                                  int* __restrict__ live, float* __restrict__ loss, float* __restrict__ lse,
-                                                  uint4* __restrict__ dh, const float* __restrict__ dloss, uint32_t* ref,
-                                                  int* __restrict__ status) {
+__global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, int64_t per, int Tpad, const int64_t* target,
+                                                  const uint4* h, uint4* hl, int* rows,
+                                                  int* live, float* loss, float* lse,
+                                                  uint4* dh, const float* dloss, uint32_t* ref,
+                                                  int* status) {
     __shared__ int wcnt[32], base_s;
     pdl_wait();
     pdl_launch();
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
             if (m >> i & 1u) {
                 uint4* to = hl + (int64_t)(base + __popc(m & ((1u << i) - 1u))) * nv;
                 const uint4* from = h + (b + i) * nv;
-                for (int v = lane; v < nv; v += 32) to[v] = ld_stream(from + v);
+                for (int v = lane; v < nv; v += 32) to[v] = ld_dep_stream(from + v);
             } else if (dh) {
                 for (int v = lane; v < nv; v += 32) dh[(b + i) * nv + v] = make_uint4(0, 0, 0, 0);
             }
@@ -545,9 +545,9 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
 }
 
 // Joins the (maximum, sum) pairs of a row: 32 rows a block, 32 ranges of tiles side by side.
-__global__ void __launch_bounds__(1024) ce_join_k(const int* __restrict__ live, const int* __restrict__ rows, int n_parts, int Tpad,
-                                                  const float2* __restrict__ part, const float* __restrict__ tlogit,
-                                                  float* __restrict__ loss, float* __restrict__ lse) {
+__global__ void __launch_bounds__(1024) ce_join_k(const int* live, const int* rows, int n_parts, int Tpad,
+                                                  const float2* part, const float* tlogit,
+                                                  float* loss, float* lse) {
     __shared__ float2 red[32][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = *live;
@@ -579,9 +579,9 @@ __global__ void __launch_bounds__(1024) ce_join_k(const int* __restrict__ live, 
 }
 
 // dh of the rows whose vocabulary was added up in several ranges: the ranges in order, eight channels a thread.
-__global__ void __launch_bounds__(256) ce_dh_join_k(const int* __restrict__ live, const int* __restrict__ rows, int C, int Tpad, int splits,
-                                                    const float* __restrict__ acc, const uint32_t* __restrict__ ref, int refs, float scale,
-                                                    __nv_bfloat16* __restrict__ dh) {
+__global__ void __launch_bounds__(256) ce_dh_join_k(const int* live, const int* rows, int C, int Tpad, int splits,
+                                                    const float* acc, const uint32_t* ref, int refs, float scale,
+                                                    __nv_bfloat16* dh) {
     pdl_wait();
     const int nv = C >> 3, n = *live;
     const float f = scale * ce_ref(ref, refs);
@@ -591,7 +591,7 @@ __global__ void __launch_bounds__(256) ce_dh_join_k(const int* __restrict__ live
 #pragma unroll 4
         for (int s = 0; s < splits; ++s) {
             const float4* p = (const float4*)(acc + ((int64_t)s * Tpad + r) * C + c);
-            const float4 x = __ldg(p), y = __ldg(p + 1);
+            const float4 x = ld_dep(p), y = ld_dep(p + 1);
             v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
             v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
         }
@@ -618,8 +618,8 @@ constexpr int kSmWarps = 16, kSmThreads = kSmWarps * 32, kSmTokens = 32;
 // blocks of 8 tokens.
 template <int NB, int STAGES>
 __global__ void __launch_bounds__(kSmThreads, 1)
-ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, const uint4* __restrict__ W,
-           const int64_t* __restrict__ target, float scale, float2* __restrict__ part, float* __restrict__ tlogit) {
+ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
+           const int64_t* target, float scale, float2* part, float* tlogit) {
     extern __shared__ __align__(16) unsigned char sm_raw[];
     pdl_wait();
     pdl_launch();
@@ -655,7 +655,7 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, con
     for (int st = 0; st < STAGES - 1; ++st) fetch(st);
     for (int i = tid; i < 8 * NB * (hpitch / 16); i += kSmThreads) {
         const int r = i / (hpitch / 16), v = i - r * (hpitch / 16);
-        *reinterpret_cast<uint4*>(hs + r * hpitch + v * 16) = (r < T && v < nv) ? __ldg(h + (int64_t)r * nv + v) : make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(hs + r * hpitch + v * 16) = (r < T && v < nv) ? ld_dep(h + (int64_t)r * nv + v) : make_uint4(0, 0, 0, 0);
     }
     __syncthreads();
     constexpr int kElems = 128 * NB;                                       // logits of a group: 16 rows x 8 NB tokens
@@ -730,9 +730,9 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* __restrict__ h, con
     }
 }
 // Joins the CTAs' pairs: a lane a token, the warps' shares of the CTAs side by side.
-__global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int parts, const float2* __restrict__ part, const float* __restrict__ tlogit,
-                                                       const int64_t* __restrict__ target, float* __restrict__ loss, float* __restrict__ lse,
-                                                       int* __restrict__ status) {
+__global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int parts, const float2* part, const float* tlogit,
+                                                       const int64_t* target, float* loss, float* lse,
+                                                       int* status) {
     __shared__ float2 red[16][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     float m = -INFINITY, s = 0.f;

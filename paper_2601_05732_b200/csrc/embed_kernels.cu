@@ -15,9 +15,9 @@
 namespace mhcl {
 
 template <bool F32>
-__global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, int n, int tpt, const int64_t* __restrict__ ids,
-                                                   const void* __restrict__ E, float scale, uint4* __restrict__ x0,
-                                                   int* __restrict__ status) {
+__global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, int n, int tpt, const int64_t* ids,
+                                                   const void* E, float scale, uint4* x0,
+                                                   int* status) {
     pdl_wait();
     pdl_launch();
     const int nv = C >> 3, per = 256 / tpt, lt = threadIdx.x % tpt;
@@ -34,10 +34,10 @@ __global__ void __launch_bounds__(256) embed_fwd_k(int64_t T, int64_t V, int C, 
             for (int e = 0; e < 8; ++e) f[e] = 0.f;
         } else if (F32) {
             const float4* p = (const float4*)E + (id * nv + v) * 2;
-            const float4 a = __ldg(p), b = __ldg(p + 1);
+            const float4 a = ld_dep(p), b = ld_dep(p + 1);
             f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
         } else {
-            unpack8(__ldg((const uint4*)E + id * nv + v), f);
+            unpack8(ld_dep((const uint4*)E + id * nv + v), f);
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] *= scale;
@@ -59,8 +59,8 @@ __device__ __forceinline__ uint32_t embed_key(int64_t id, int64_t i, int64_t V, 
     if (!ok && say) report_index(status, MHCLITE_OP_EMBED_BWD, i, id);
     return ok ? (uint32_t)id : (uint32_t)V;                    // tokens without a row go last
 }
-__global__ void __launch_bounds__(256) embed_rank_k(int T, int64_t V, const int64_t* __restrict__ ids, uint2* __restrict__ list,
-                                                    int* __restrict__ status) {
+__global__ void __launch_bounds__(256) embed_rank_k(int T, int64_t V, const int64_t* ids, uint2* list,
+                                                    int* status) {
     __shared__ __align__(16) uint32_t key[kRankMax];
     __shared__ int below[8][32];
     pdl_wait();
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256) embed_rank_k(int T, int64_t V, const int6
     for (int i0 = tid; i0 < quads * 4; i0 += 256 * 8) {        // eight loads in flight
         int64_t id[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) id[k] = i0 + k * 256 < T ? __ldg(ids + i0 + k * 256) : 0;
+        for (int k = 0; k < 8; ++k) id[k] = i0 + k * 256 < T ? ld_dep(ids + i0 + k * 256) : 0;
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int i = i0 + k * 256;
@@ -143,8 +143,8 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t live, uint32_t d) {
     return m;
 }
 
-__global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, int passes, const int64_t* __restrict__ ids,
-                                                             uint2* buf0, uint2* buf1, int* __restrict__ status) {
+__global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, int passes, const int64_t* ids,
+                                                             uint2* buf0, uint2* buf1, int* status) {
     extern __shared__ uint32_t cnt[];                          // [warp][bin]
     __shared__ uint32_t tot[kSortBins], off[kSortBins], wsum[kSortBins / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k) {
                 const int i = b + k * 32 + lane;
-                if (i < i1) key[k] = p == 0 ? embed_key(__ldg(ids + i), i, V, true, status) : __ldcg(src + i).x;
+                if (i < i1) key[k] = p == 0 ? embed_key(ld_dep(ids + i), i, V, true, status) : ld_dep_l2(src + i).x;
             }
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k) {
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
             uint2 kv[kSortAhead];
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k)
-                if (b + k * 32 + lane < i1) kv[k] = __ldcg(src + b + k * 32 + lane);
+                if (b + k * 32 + lane < i1) kv[k] = ld_dep_l2(src + b + k * 32 + lane);
 #pragma unroll
             for (int k = 0; k < kSortAhead; ++k) {
                 if (b + k * 32 >= i1) break;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kSortThreads) embed_sort_k(int T, int64_t V, i
 // cleared meanwhile, met or not (rare words stand there in the tables of text).  This launch starts once the sort has begun
 // and by then has seen the stream's earlier work done; it ends after the sort, so that what follows may wait for it alone.
 constexpr int64_t kEarlyZero = (int64_t)96 << 20;         // 65536 x 1024, 100000 rows: 176 us without, 172 with 64 MB, 170
-__global__ void __launch_bounds__(256) embed_zero_k(float4* __restrict__ to, int64_t n) {
+__global__ void __launch_bounds__(256) embed_zero_k(float4* to, int64_t n) {
     pdl_launch();
     const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) __stcs(to + i, zero);
@@ -248,9 +248,9 @@ constexpr int kZeroRows = 64;          // rows a block looks over for those that
 // Warp (chunk, slice) adds up `R` list entries for channels [256 slice, 256 slice + 256), 8 a lane.
 template <int N_>
 __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_t to_zero, int C, int R, int64_t sum_blocks, int slices,
-                                                    const uint2* __restrict__ list,
-                                                    const uint4* __restrict__ g, float scale, float* __restrict__ dE,
-                                                    float* __restrict__ own, float* __restrict__ cont, int accumulate) {
+                                                    const uint2* list,
+                                                    const uint4* g, float scale, float* dE,
+                                                    float* own, float* cont, int accumulate) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nv = C >> 3;
     pdl_wait();
     pdl_launch();
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_
             int64_t lo = -1, hi = T;                           // the first entry not below `bound` lies in (lo, hi]
             while (hi - lo > 1) {
                 const int64_t step = (hi - lo + 31) / 32, probe = lo + 1 + lane * step;
-                const int n = __popc(__ballot_sync(0xffffffffu, probe < hi && __ldg(&list[probe < hi ? probe : 0].x) < bound));
+                const int n = __popc(__ballot_sync(0xffffffffu, (probe < hi) & (ld_dep(&list[probe < hi ? probe : 0].x) < bound)));
                 const int64_t end = lo + 1 + n * step;
                 if (n > 0) lo += 1 + (n - 1) * step;
                 hi = end < hi ? end : hi;
@@ -278,9 +278,9 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_
             int64_t lo = range[0], hi = end;
             while (lo < hi) {
                 const int64_t mid = (lo + hi) >> 1;
-                if (__ldg(&list[mid].x) < v) lo = mid + 1; else hi = mid;
+                if (ld_dep(&list[mid].x) < v) lo = mid + 1; else hi = mid;
             }
-            if (lo < end && __ldg(&list[lo].x) == v) atomicOr(&met[threadIdx.x >> 5], 1u << lane);
+            if (lo < end && ld_dep(&list[lo].x) == v) atomicOr(&met[threadIdx.x >> 5], 1u << lane);
         }
         __syncthreads();
         const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -297,9 +297,9 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_
     const int64_t p0 = chunk * R;
     if (p0 >= T) return;
     const int cnt = (int)(T - p0 < R ? T - p0 : R);
-    const uint2 mine = lane < cnt ? __ldg(list + p0 + lane) : make_uint2(0xFFFFFFFFu, 0);
-    const uint32_t prev = p0 > 0 ? __ldg(&list[p0 - 1].x) : 0xFFFFFFFFu;
-    const uint32_t next = p0 + cnt < T ? __ldg(&list[p0 + cnt].x) : 0xFFFFFFFFu;
+    const uint2 mine = lane < cnt ? ld_dep(list + p0 + lane) : make_uint2(0xFFFFFFFFu, 0);
+    const uint32_t prev = p0 > 0 ? ld_dep(&list[p0 - 1].x) : 0xFFFFFFFFu;
+    const uint32_t next = p0 + cnt < T ? ld_dep(&list[p0 + cnt].x) : 0xFFFFFFFFu;
     const bool act = v < nv;
     float acc[8];
 #pragma unroll
@@ -312,7 +312,7 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_
             const uint32_t t = __shfl_sync(0xffffffffu, mine.y, (i + k) & 31);
             if (act && i + k < cnt) {
 #pragma unroll
-                for (int j = 0; j < N_; ++j) d[k][j] = ld_stream(g + ((int64_t)t * N_ + j) * nv + v);
+                for (int j = 0; j < N_; ++j) d[k][j] = ld_dep_stream(g + ((int64_t)t * N_ + j) * nv + v);
             }
         }
 #pragma unroll
@@ -358,12 +358,12 @@ __global__ void __launch_bounds__(256) embed_grad_k(int64_t T, int64_t V, int64_
 // kJoinAlone parts are shared out among the block's warps, a range of the parts each, joined in order.
 constexpr int kJoinAlone = 16;
 __device__ __forceinline__ void add4(float4& a, const float4& x) { a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w; }
-__device__ __forceinline__ void join_sum(const float* __restrict__ part, int64_t c0, int64_t c1, int C, int v, float4& a, float4& b) {
+__device__ __forceinline__ void join_sum(const float* part, int64_t c0, int64_t c1, int C, int v, float4& a, float4& b) {
 #pragma unroll 4
     for (int64_t c = c0; c < c1; ++c) {
         const float4* q = (const float4*)(part + c * C + v * 8);
-        add4(a, __ldg(q));
-        add4(b, __ldg(q + 1));
+        add4(a, ld_dep(q));
+        add4(b, ld_dep(q + 1));
     }
 }
 __device__ __forceinline__ void join_store(float* dE, uint32_t key, int C, int v, float scale, int accumulate, const float4& a, const float4& b) {
@@ -373,9 +373,9 @@ __device__ __forceinline__ void join_store(float* dE, uint32_t key, int C, int v
     s1.x += scale * b.x; s1.y += scale * b.y; s1.z += scale * b.z; s1.w += scale * b.w;
     o[0] = s0; o[1] = s1;
 }
-__global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C, int R, const uint2* __restrict__ list,
-                                                    const float* __restrict__ own, const float* __restrict__ cont, float scale,
-                                                    float* __restrict__ dE, int accumulate) {
+__global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C, int R, const uint2* list,
+                                                    const float* own, const float* cont, float scale,
+                                                    float* dE, int accumulate) {
     __shared__ float4 red[8][32][2];
     __shared__ int64_t first_s[8], end_s[8];
     __shared__ uint32_t key_s[8];
@@ -387,19 +387,19 @@ __global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C,
     if (lane == 0) end_s[warp] = 0;
     if (p1 < T) {
         const int64_t at[4] = {p1 - 1, p1, p0, p0 > 0 ? p0 - 1 : p0};                // one load for the four
-        const uint32_t mine = __ldg(&list[at[lane & 3]].x);
+        const uint32_t mine = ld_dep(&list[at[lane & 3]].x);
         const uint32_t key = __shfl_sync(0xffffffffu, mine, 0), next = __shfl_sync(0xffffffffu, mine, 1);
         const uint32_t head = __shfl_sync(0xffffffffu, mine, 2), prev = __shfl_sync(0xffffffffu, mine, 3);
         const bool began_before = p0 > 0 && head == key && prev == key;
         if (key < V && next == key && !began_before) {
             // chunks of this id in a row, mostly few: one look at the next 32, and a search only where all are
             const int64_t head_at = p1 + (int64_t)lane * R;
-            const uint32_t same = __ballot_sync(0xffffffffu, head_at < T && __ldg(&list[head_at < T ? head_at : p1].x) == key);
+            const uint32_t same = __ballot_sync(0xffffffffu, (head_at < T) & (ld_dep(&list[head_at < T ? head_at : p1].x) == key));
             const int run = same == 0xffffffffu ? 32 : __ffs(~same) - 1;
             int64_t lo = p1 + (int64_t)(run - 1) * R, hi = run < 32 ? lo + 1 : T;     // the last entry known to be of the id
             while (hi - lo > 1) {
                 const int64_t step = (hi - lo + 31) / 32, probe = lo + lane * step;
-                const uint32_t same = __ballot_sync(0xffffffffu, probe < hi && __ldg(&list[probe < hi ? probe : lo].x) == key);
+                const uint32_t same = __ballot_sync(0xffffffffu, (probe < hi) & (ld_dep(&list[probe < hi ? probe : lo].x) == key));
                 const int n = __popc(same);                    // probes 0 .. n-1 are of the id (probe 0 is)
                 const int64_t l = lo + (int64_t)(n - 1) * step;
                 hi = l + step < hi ? l + step : hi;
@@ -445,16 +445,16 @@ __global__ void __launch_bounds__(256) embed_join_k(int64_t T, int64_t V, int C,
 // tokens 11 us, with the sort and its two further launches 14; 200 tokens 13.0 and 14.2, 512 tokens 16.5 and 15.6.
 constexpr int kFewTokens = 192;
 template <int N_>
-__global__ void __launch_bounds__(256) embed_few_k(int T, int64_t V, int C, int64_t sum_blocks, int slices, const int64_t* __restrict__ ids,
-                                                   const uint4* __restrict__ g, float scale, float* __restrict__ dE, int accumulate,
-                                                   int* __restrict__ status) {
+__global__ void __launch_bounds__(256) embed_few_k(int T, int64_t V, int C, int64_t sum_blocks, int slices, const int64_t* ids,
+                                                   const uint4* g, float scale, float* dE, int accumulate,
+                                                   int* status) {
     __shared__ uint32_t key[kFewTokens];
     __shared__ uint32_t met[kZeroRows / 32];
     __shared__ float4 red[8][32][2];
     pdl_wait();
     pdl_launch();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nv = C >> 3;
-    for (int i = tid; i < T; i += 256) key[i] = embed_key(__ldg(ids + i), i, V, blockIdx.x == 0, status);
+    for (int i = tid; i < T; i += 256) key[i] = embed_key(ld_dep(ids + i), i, V, blockIdx.x == 0, status);
     if (tid < kZeroRows / 32) met[tid] = 0;
     __syncthreads();
     if (blockIdx.x >= sum_blocks) {
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(256) embed_few_k(int T, int64_t V, int C, int6
                     ++n;
                     if (v < nv) {
 #pragma unroll
-                        for (int j = 0; j < N_; ++j) d[u][j] = ld_stream(g + ((int64_t)t * N_ + j) * nv + v);
+                        for (int j = 0; j < N_; ++j) d[u][j] = ld_dep_stream(g + ((int64_t)t * N_ + j) * nv + v);
                     }
                 }
             }

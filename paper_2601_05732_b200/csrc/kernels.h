@@ -134,6 +134,25 @@ inline cudaError_t launch_after(void (*k)(P...), dim3 grid, dim3 block, size_t s
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// Loads of such a kernel.  Its life begins while its predecessor may still write what it is going to read, so the read-only
+// path, whose promise is that nobody writes the data while the kernel lives, is not open to it: neither __ldg, nor ld.global.nc,
+// nor a const __restrict__ pointer, behind which the compiler may choose either and lift it over pdl_wait.  Its pointers are
+// plain ones and its loads ordinary ones, which pdl_wait holds back.
+template <typename T>
+__device__ __forceinline__ T ld_dep(const T* p) { return *p; }
+// what other blocks of the same kernel wrote: from L2
+__device__ __forceinline__ uint2 ld_dep_l2(const uint2* p) {
+    uint2 r;
+    asm volatile("ld.global.cg.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p) : "memory");
+    return r;
+}
+// activations, touched once
+__device__ __forceinline__ uint4 ld_dep_stream(const void* p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
 #endif
 
 // Raises a kernel's limit of dynamic shared memory once a device (the call costs more than the launch's other set-up).

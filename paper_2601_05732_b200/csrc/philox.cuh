@@ -8,6 +8,7 @@
 // factor 1 / (1 - p) uses the rounded p, so the expectation is exact.
 #pragma once
 #include "common.cuh"
+#include "kernels.h"
 
 namespace mhcl {
 
@@ -21,7 +22,7 @@ inline float drop_factor(int threshold) { return (float)(65536.0 / (65536 - thre
 struct Philox {
     uint32_t s0, s1, o0, o1;
     __device__ __forceinline__ Philox(const uint64_t* rng, bool use) {     // rng is read only if it is to be used
-        const uint64_t seed = use ? __ldg((const unsigned long long*)rng) : 0, offset = use ? __ldg((const unsigned long long*)rng + 1) : 0;
+        const uint64_t seed = use ? ld_dep(rng) : 0, offset = use ? ld_dep(rng + 1) : 0;
         s0 = (uint32_t)seed; s1 = (uint32_t)(seed >> 32);
         o0 = (uint32_t)offset; o1 = (uint32_t)(offset >> 32);
     }

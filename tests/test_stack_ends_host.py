@@ -1,5 +1,7 @@
 """Host logic of the operators around the stack without a GPU: scratch planning and refusals that need no context."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -64,3 +66,16 @@ def test_status_words_are_never_shared_or_given_back(monkeypatch):
     assert len(set(rows)) == 600 and all(r % 16 == 0 for r in rows)
     held = {s.data_ptr() + 32 * i for slabs, _ in binding._status_slabs.values() for s in slabs for i in range(len(s))}
     assert set(rows) <= held
+
+
+def test_overlapped_kernels_do_not_read_by_the_read_only_path():
+    """A kernel launched while its predecessor runs must not promise that nobody writes what it reads (csrc/kernels.h)."""
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    launched = 0
+    for name in sorted(os.listdir(csrc)):
+        src = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, name)).read())
+        if name == "philox.cuh" or "launch_after(" in src and name.endswith(".cu"):
+            launched += 1
+            for word in ("__ldg", "__ldcg", ".nc.", "ld_stream(", "__restrict__"):
+                assert word not in src.replace("ld_dep_stream(", ""), (name, word)
+    assert launched == 4
