@@ -318,6 +318,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (tgt == c0 + e) a.tlogit[r] = v[e] * a.scale;
+                            __syncwarp();
                         }
                         if (k2 > 0.f && c0 + 32 <= cols) {             // the usual case, in as few instructions as it takes
                             float t0 = v[0], t1 = v[1];
@@ -426,6 +427,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
 #pragma unroll 1
                 for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                     float v[32];
+                    __syncwarp();                                       // rows behind the list skip the stores below
                     tc_ld32(acc + c0, v);
                     if (c0 + 32 == kCeHalf) hand_back();
                     const int c = n0 + c0;
