@@ -84,7 +84,7 @@ def block_out_bwd(o, gate, w, s, eps, dy, keep=None, factor=1.0):
         "mag_dscale": np.abs(d * sg * oh * w).sum(),
     }
     if gate is not None:
-        res["dgate"] = z * oh * w * sg * (1.0 - sg)
+        res["dgate"] = z * oh * w * sg * sigmoid(-gate)
     return res
 
 

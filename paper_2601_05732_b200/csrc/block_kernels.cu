@@ -17,6 +17,8 @@
 #include "philox.cuh"
 #include "tc.cuh"
 
+#include <float.h>
+
 namespace mhcl {
 
 constexpr int kMaxTeamWarps = 16;
@@ -52,16 +54,28 @@ __device__ __forceinline__ void fetch_row(uint32_t to, const uint4* row, const T
     }
 }
 
-// sigmoid of a pair: 1 / (1 + 2^(-a log2 e)); 2^x overflows to infinity for a far below 0, whose reciprocal is 0.
-__device__ __forceinline__ uint64_t sigmoid2(uint64_t a) {
+// A gate's pair a as x = e^-a = 2^(-a log2 e), from which sigma(a) = 1 / (1 + x) and 1 - sigma(a) = x sigma(a), both without
+// cancellation (1 - sigma formed by subtraction has no digit left from a = 17 on).  x overflows to infinity for a far below 0;
+// its reciprocal is 0, and so is the product, formed with the largest finite number in its place.
+__device__ __forceinline__ uint64_t exp_minus2(uint64_t a) {
     float x, y;
     unpack2f(mul2(a, pack2f(-1.4426950408889634f, -1.4426950408889634f)), x, y);
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(x));
     asm("ex2.approx.ftz.f32 %0, %0;" : "+f"(y));
-    unpack2f(add2(pack2f(x, y), pack2f(1.f, 1.f)), x, y);
+    return pack2f(x, y);
+}
+__device__ __forceinline__ uint64_t sigmoid_of_exp2(uint64_t xy) {
+    float x, y;
+    unpack2f(add2(xy, pack2f(1.f, 1.f)), x, y);
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(x));
     asm("rcp.approx.ftz.f32 %0, %0;" : "+f"(y));
     return pack2f(x, y);
+}
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t a) { return sigmoid_of_exp2(exp_minus2(a)); }
+__device__ __forceinline__ uint64_t finite2(uint64_t xy) {
+    float x, y;
+    unpack2f(xy, x, y);
+    return pack2f(fminf(x, FLT_MAX), fminf(y, FLT_MAX));
 }
 __device__ __forceinline__ uint64_t both(float x) { return pack2f(x, x); }
 // the 8 weights of a vector, as packed pairs
@@ -178,7 +192,7 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const 
     int slot = 0, cur = 0;
     const float s = scale ? ld_dep(scale) : 1.f;
     // dropout's factor rides on the weights, and on s in the column sums
-    const uint64_t s2 = both(s), fac2 = both(da.factor), minus_s2 = both(-s);
+    const uint64_t s2 = both(s), fac2 = both(da.factor);
     const Philox rng(DROP ? da.rng : nullptr, DROP);
     uint64_t acc[VPT][4], wf[VPT][4];
 #pragma unroll
@@ -210,19 +224,20 @@ block_bwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const 
             if (GATE) unpack8x2(lds128(at + (2 * VPT + k) * vec), g);
             if (GATE)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) g[e] = sigmoid2(g[e]);
+                for (int e = 0; e < 4; ++e) g[e] = exp_minus2(g[e]);
             if (DROP && GATE) drop8(zw[k], g, rng((uint64_t)(t * nv + v)), da.threshold << 16);
             if (DROP && !GATE) drop8(zw[k], rng((uint64_t)(t * nv + v)), da.threshold << 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint64_t oh = mul2(f[e], r2);
-                if (GATE) zw[k][e] = mul2(zw[k][e], g[e]);
+                const uint64_t sg = GATE ? sigmoid_of_exp2(g[e]) : 0;
+                if (GATE) zw[k][e] = mul2(zw[k][e], sg);
                 acc[k][e] = fma2(zw[k][e], oh, acc[k][e]);
                 zw[k][e] = mul2(zw[k][e], wf[k][e]);
                 if (GATE) {
                     const uint64_t q = mul2(zw[k][e], oh);
                     ds2 = add2(ds2, q);
-                    dg[e] = mul2(q, fma2(g[e], minus_s2, s2));             // s (1 - sig)
+                    dg[e] = mul2(mul2(q, s2), mul2(finite2(g[e]), sg));    // 1 - sig
                 } else {
                     ds2 = fma2(zw[k][e], oh, ds2);
                 }

@@ -46,19 +46,20 @@ struct Philox {
 // f[e] (packed pairs) <- f where the element stays, 0 (whatever f is) where it is dropped; the caller multiplies by the
 // factor together with what else it has.  `thr_hi` is the threshold in the upper half-word: the upper 16 bits of a word are
 // compared as they lie, the lower ones shifted up.
-__device__ __forceinline__ void drop8(uint64_t* f, const uint4& w, uint32_t thr_hi) {
+__device__ __forceinline__ void drop8(uint64_t* f, const uint4& w, uint32_t thr_hi, float dropped = 0.f) {
     const uint32_t r[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         float lo, hi;
         unpack2f(f[e], lo, hi);
-        f[e] = pack2f((r[e] << 16) >= thr_hi ? lo : 0.f, r[e] >= thr_hi ? hi : 0.f);
+        f[e] = pack2f((r[e] << 16) >= thr_hi ? lo : dropped, r[e] >= thr_hi ? hi : dropped);
     }
 }
-// The same for two factors of a gradient, neither of which may leave anything of a dropped element (0 times NaN).
-__device__ __forceinline__ void drop8(uint64_t* f, uint64_t* g, const uint4& w, uint32_t thr_hi) {
+// The same for a gradient and its gate, of which nothing may be left where the element is dropped (0 times NaN): x = e^-a
+// becomes infinite there, which closes the gate.
+__device__ __forceinline__ void drop8(uint64_t* f, uint64_t* x, const uint4& w, uint32_t thr_hi) {
     drop8(f, w, thr_hi);
-    drop8(g, w, thr_hi);
+    drop8(x, w, thr_hi, INFINITY);
 }
 #endif
 

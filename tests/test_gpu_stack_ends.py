@@ -129,6 +129,31 @@ def test_block_out(ctx_of, T, C, gated, p):
     assert torch.equal(dw2, dw + dw) and torch.equal(ds2, ds + ds)          # doubling is exact
 
 
+@pytest.mark.parametrize("C,p", [(64, 0.0), (520, 0.25), (9000, 0.0)])
+def test_block_gates_far_open_and_shut(ctx_of, C, p):
+    """1 - sigmoid(a) keeps its digits however far the gate is open; infinite gates give zeros, not NaN."""
+    T, inf = 24, float("inf")
+    c, rng = ctx_of(4, C), rng_of(5, 6) if p else None
+    o, dy, w = randn(1, T, C), randn(2, T, C), randn(3, C, std=0.2, mean=1.0, dtype=F32)
+    gate = torch.linspace(-30, 30, T * C).reshape(T, C)
+    gate.view(-1)[:16] = torch.tensor([inf, -inf, 100, -100, 88.5, -88.5, 87, -87, 60, -60, 45, -45, 3e38, -3e38, 0, -0.0])
+    gate = gate.view(-1)[torch.randperm(T * C, generator=torch.Generator().manual_seed(4))].reshape(T, C).to(BF).to(DEV)
+    y, r, d_o, dg, dw = empty(T, C), empty(T, dtype=F32), empty(T, C), empty(T, C), empty(C, dtype=F32)
+    c.block_out_fwd(o, gate, w, None, 1e-6, p, rng, y, r)
+    c.block_out_bwd(o, gate, w, None, r, p, rng, dy, d_o, dg, dw, None)
+    keep, fac = (S.keep_mask(T * C, p, 5, 6).reshape(T, C), S.drop_factor(p)) if p else (None, 1.0)
+    ref, _ = S.block_out_fwd(f64(o), f64(gate), f64(w), 1.0, 1e-6, keep, fac)
+    b = S.block_out_bwd(f64(o), f64(gate), f64(w), 1.0, 1e-6, f64(dy), keep, fac)
+    # the row's sum as in test_block_out; e^-a for |a| <= 100: its argument in base 2 is rounded once, 145 x 2^-24 x ln 2 < 2^-17
+    fine = (C / 32 + 32) * 2.0 ** -24 + 2.0 ** -16
+    # below 2^-126 e^-a, the sigmoid and the products after them may each become 0: 2^-126 at most, times the factors that follow
+    oh = np.abs(f64(o)) / np.sqrt((f64(o) ** 2).mean(1, keepdims=True))
+    tiny = 4 * 2.0 ** -126 * (1 + fac * np.abs(f64(dy))) * (1 + np.abs(f64(w))) * (1 + oh)
+    close("y", y, ref, (HALF + fine) * np.abs(ref) + tiny)
+    close("dgate", dg, b["dgate"], (HALF + 4 * fine) * np.abs(b["dgate"]) + tiny)
+    close("d_o", d_o, b["d_o"], HALF * np.abs(b["d_o"]) + 4 * fine * b["mag_d_o"] + tiny)
+
+
 @pytest.mark.parametrize("T,C", [(1, 8), (1, 2048), (300, 1536), (33, 4096), (4100, 256)])
 def test_block_in(ctx_of, T, C):
     c = ctx_of(2, C)
