@@ -129,6 +129,11 @@ def test_block_out(ctx_of, T, C, gated, p):
     assert torch.equal(dw2, dw + dw) and torch.equal(ds2, ds + ds)          # doubling is exact
 
 
+@pytest.mark.parametrize("T,C,gated,p", [(300, 10000, True, 0.0), (19, 16384, True, 0.2), (150, 8200, False, 0.0)])
+def test_block_out_long_rows_over_several_blocks(ctx_of, T, C, gated, p):
+    test_block_out(ctx_of, T, C, gated, p)
+
+
 @pytest.mark.parametrize("C,p", [(64, 0.0), (520, 0.25), (9000, 0.0)])
 def test_block_gates_far_open_and_shut(ctx_of, C, p):
     """1 - sigmoid(a) keeps its digits however far the gate is open; infinite gates give zeros, not NaN."""
