@@ -48,7 +48,7 @@ struct CeArgs {
     float scale;
     // CE_STATS
     float2* part;               // [2 n_tiles][Tpad] (maximum, sum) in base 2 of 128 columns each
-    float* tlogit;              // [Tpad] the target's logit
+    float* tlogit;              // [Tpad] <h_t, W_target>, before the scale
     const int64_t* target;
     int Tpad;
     // CE_GRAD
@@ -85,7 +85,15 @@ struct CeCtl {
 };
 
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
-__device__ __forceinline__ float lg2(float x) { float y; asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+
+// lse and loss of a row from the largest logit `top` in base 2, the sum s of 2^(l - top) and the target's product x: the loss
+// is the difference log s - (l - top), formed before either is added to a logit in size, so that a target as likely as 1 does
+// not lose its digits.  l - top comes unrounded (fused) as it does in s; at one common rounding error the two cancel.
+__device__ __forceinline__ void lse_and_loss(float top, float s, float x, float k2, float& lse, float& loss) {
+    const float b = log2f(s), d = (b - fmaf(x, k2, top == -INFINITY ? 0.f : -top)) * kLn2;
+    lse = (top + b) * kLn2;
+    loss = d < 0.f ? 0.f : d;                  // by the last bits of s
+}
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -317,7 +325,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         if (__any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                if (tgt == c0 + e) a.tlogit[r] = v[e] * a.scale;
+                                if (tgt == c0 + e) a.tlogit[r] = v[e];
                             __syncwarp();
                         }
                         if (k2 > 0.f && c0 + 32 <= cols) {             // the usual case, in as few instructions as it takes
@@ -340,14 +348,11 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         }
                         float top = mx;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) {
-                            v[e] = c0 + e < cols ? v[e] * k2 : -INFINITY;
-                            top = fmaxf(top, v[e]);
-                        }
+                        for (int e = 0; e < 32; ++e) top = fmaxf(top, c0 + e < cols ? v[e] * k2 : -INFINITY);
                         const float base = top == -INFINITY ? 0.f : top;
                         sum *= ex2(mx - base);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) sum += ex2(v[e] - base);
+                        for (int e = 0; e < 32; ++e) sum += c0 + e < cols ? ex2(fmaf(v[e], k2, -base)) : 0.f;
                         mx = top;
                     }
                     hand_back();
@@ -549,7 +554,7 @@ __global__ void __launch_bounds__(1024) ce_rows_k(int64_t T, int64_t V, int C, i
 // Joins the (maximum, sum) pairs of a row: 32 rows a block, 32 ranges of tiles side by side.
 __global__ void __launch_bounds__(1024) ce_join_k(const int* live, const int* rows, int n_parts, int Tpad,
                                                   const float2* part, const float* tlogit,
-                                                  float* loss, float* lse) {
+                                                  float k2, float* loss, float* lse) {
     __shared__ float2 red[32][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = *live;
@@ -574,10 +579,11 @@ __global__ void __launch_bounds__(1024) ce_join_k(const int* live, const int* ro
     s = 0.f;
 #pragma unroll
     for (int w = 0; w < 32; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
-    const float l = (top + lg2(s)) * kLn2;
     const int t = rows[r];
+    float l, x;
+    lse_and_loss(top, s, tlogit[r], k2, l, x);
     lse[t] = l;
-    loss[t] = l - tlogit[r];
+    loss[t] = x;
 }
 
 // dh of the rows whose vocabulary was added up in several ranges: the ranges in order, eight channels a thread.
@@ -705,10 +711,9 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
             const int64_t row = unit * rows + er * 16 + (l >> 2) + (e >> 1) * 8;
             const int tok = i * 8 + (l & 3) * 2 + (e & 1);
             if (row >= V) continue;
-            if (tok < T && row == target[tok]) tlogit[tok] = v * scale;
-            v *= k2;
-            const float top = fmaxf(mx[j], v), base = top == -INFINITY ? 0.f : top;
-            sum[j] = sum[j] * ex2(mx[j] - base) + ex2(v - base);
+            if (tok < T && row == target[tok]) tlogit[tok] = v;
+            const float top = fmaxf(mx[j], v * k2), base = top == -INFINITY ? 0.f : top;
+            sum[j] = sum[j] * ex2(mx[j] - base) + ex2(fmaf(v, k2, -base));
             mx[j] = top;
         }
     }
@@ -733,7 +738,7 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
 }
 // Joins the CTAs' pairs: a lane a token, the warps' shares of the CTAs side by side.
 __global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int parts, const float2* part, const float* tlogit,
-                                                       const int64_t* target, float* loss, float* lse,
+                                                       const int64_t* target, float k2, float* loss, float* lse,
                                                        int* status) {
     __shared__ float2 red[16][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -761,8 +766,7 @@ __global__ void __launch_bounds__(512) ce_small_join_k(int T, int64_t V, int par
         s = 0.f;
 #pragma unroll
         for (int w = 0; w < 16; ++w) s += red[w][lane].y * ex2(red[w][lane].x - base);
-        l = (top + lg2(s)) * kLn2;
-        x = l - tlogit[lane];
+        lse_and_loss(top, s, tlogit[lane], k2, l, x);
     } else if (y >= V) {
         report_index(status, MHCLITE_OP_LINEAR_CE, lane, y);
     }
@@ -909,7 +913,7 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
         c->launches += 2;
         launch_after(k, dim3(grid), dim3(kSmThreads), q.smem, s, (int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
-        launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, loss, lse, c->op_status);
+        launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, scale * kLog2e, loss, lse, c->op_status);
         return true;
     }
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);
@@ -922,7 +926,7 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
     launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
     c->launches += 1;
-    launch_after(ce_join_k, dim3((unsigned)((T + 31) / 32)), dim3(1024), 0, s, p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, loss, lse);
+    launch_after(ce_join_k, dim3((unsigned)((T + 31) / 32)), dim3(1024), 0, s, p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, scale * kLog2e, loss, lse);
     return true;
 }
 

@@ -469,6 +469,29 @@ def test_linear_ce_sharp_logits_and_ties(ctx_of):
     assert torch.allclose(loss, torch.full_like(loss, float(np.log(V))), rtol=0, atol=2e-5)
 
 
+@pytest.mark.parametrize("T,V,scale", [(1, 1, 1.0), (7, 1, 1.0), (20, 301, 1.0), (60, 1, 1.0), (60, 700, 1.0), (60, 300, -0.7), (20, 300, -0.7)])
+def test_linear_ce_of_likely_targets_keeps_its_digits(ctx_of, T, V, scale):
+    """Logits around 60 whose largest is the target's: the loss is a small difference of large numbers.  A logit is one
+    product of two bf16 numbers here, exact in fp32 before the scale."""
+    c, C = ctx_of(4, 64), 64
+    h, W = torch.zeros(T, C, dtype=BF, device=DEV), torch.zeros(V, C, dtype=BF, device=DEV)
+    r = np.random.default_rng(T + V)
+    h[:, 3] = torch.from_numpy(r.uniform(50, 70, T)).to(BF).to(DEV)
+    target = torch.from_numpy(r.integers(0, V, T)).to(DEV)
+    W[:, 3] = torch.from_numpy(r.uniform(0.5, 0.8, V)).to(BF).to(DEV)
+    likely = int(target[0])
+    W[likely, 3] = 1.0625
+    W[:, 3] *= -1 if scale < 0 else 1
+    target[: T // 2 + 1] = likely
+    loss, lse = empty(T, dtype=F32), empty(T, dtype=F32)
+    c.linear_ce_fwd(h, W, target, scale, loss, lse)
+    rl, _ = S.linear_ce_fwd(f64(h), f64(W), target.cpu().numpy(), float(np.float32(scale)))
+    # exp2 and log2 to 2^-22 each, up to V terms of one sign; the exponents, up to 150, are rounded once to fp32 and the base's
+    # constant once: 2^-23 of them, which moves a term by 150 x 2^-23 x ln 2 < 2^-16 of itself
+    close("loss", loss, rl, 2.0 ** -20 + 2.0 ** -16 * rl)
+    assert (loss >= 0).all() and rl.min() < 1e-3
+
+
 def test_linear_ce_targets_beyond_the_table_are_reported():
     c = binding.MhcLite(2, 64, 0)
     h, W, target, dloss = loss_case(50, 64, 100, 0.0)
