@@ -163,8 +163,8 @@ block_fwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const 
 //   do = r (e - oh mean(e oh)),  da = e oh (1 - sig),  dw = s sum_t z oh,  ds = sum z w oh.
 // s is applied once to each result.  The scale's sum runs over all T C elements and may cancel: it is added up in 64 bits
 // from the rows on.
-template <int VPT, bool BIG, bool GATE, bool DROP>
-__global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : 2)
+template <int VPT, bool GATE, bool DROP>
+__global__ void __launch_bounds__(512, 1)
 block_bwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const float4* w,
             const float* scale, const float* rstd, DropArgs da, const uint4* dy,
             uint4* dx, uint4* dgate, float* dw_part, double* ds_part,
@@ -381,9 +381,9 @@ static RowPlan plan_row(int C, RowUse use) {
     p.threads = p.teams * p.wpr * 32;
     return p;
 }
-// Blocks: as many of up to 256 threads as an SM holds, or one of more.
+// Blocks: as many as are resident, or as there are rows for.
 static int row_blocks(const RowPlan& p, int64_t T, int sm_count, int per_sm) {
-    const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * (p.threads > 256 ? 1 : per_sm);
+    const int64_t need = (T + p.teams - 1) / p.teams, cap = (int64_t)sm_count * per_sm;
     return (int)(need < cap ? need : cap);
 }
 
@@ -398,13 +398,13 @@ static DropArgs drop_args(float p, const uint64_t* rng) {
 // (one block while its teams have at most two rows each: its column sums are then the result, without a second launch)
 int block_parts(int64_t T, int C, int sm_count, bool gate) {
     const RowPlan p = plan_row(C, gate ? ROW_BWD_GATED : ROW_BWD);
-    return T <= 2 * p.teams ? 1 : row_blocks(p, T, sm_count, 2);
+    return T <= 2 * p.teams ? 1 : row_blocks(p, T, sm_count, 1);
 }
 
 void launch_block_fwd(const mhclite_ctx* c, int64_t T, const void* x, const void* gate, const float* w, const float* scale,
                       float eps, float p_drop, const uint64_t* rng, void* out, float* rstd, cudaStream_t s) {
     const RowPlan p = plan_row(c->C, ROW_FWD);
-    const int grid = row_blocks(p, T, c->sm_count, p.vpt == 4 ? 2 : 3), smem = p.threads * 16 * p.vpt * (gate ? 2 : 1) * fwd_stages(p.vpt);
+    const int grid = row_blocks(p, T, c->sm_count, p.threads > 256 ? 1 : p.vpt == 4 ? 2 : 3), smem = p.threads * 16 * p.vpt * (gate ? 2 : 1) * fwd_stages(p.vpt);
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 1;
 #define MHCL_FWD(V, B)                                                                                                  \
@@ -428,15 +428,15 @@ void launch_block_bwd(const mhclite_ctx* c, int64_t T, const void* x, const void
     if (smem < p.teams * c->C * 4) smem = p.teams * c->C * 4;
     const DropArgs da = drop_args(p_drop, rng);
     c->launches += 1;
-#define MHCL_BWD(V, B)                                                                                                  \
-    if (p.vpt == V && (p.threads > 256) == B) {                                                                                                \
-        auto k = gate ? (da.rng ? block_bwd_k<V, B, true, true> : block_bwd_k<V, B, true, false>)                             \
-                      : (da.rng ? block_bwd_k<V, B, false, true> : block_bwd_k<V, B, false, false>);                          \
+#define MHCL_BWD(V)                                                                                                     \
+    if (p.vpt == V) {                                                                                                                          \
+        auto k = gate ? (da.rng ? block_bwd_k<V, true, true> : block_bwd_k<V, true, false>)                             \
+                      : (da.rng ? block_bwd_k<V, false, true> : block_bwd_k<V, false, false>);                          \
         if (smem > 40 * 1024) { static SmemOnce once[2][2]; smem_limit(once[gate != nullptr][da.rng != nullptr], k, c->device, 226 * 1024); }               \
         launch_after(k, dim3(parts), dim3(p.threads), smem, s, T, c->C, p.wpr, (const uint4*)x, (const uint4*)gate, (const float4*)w, \
                      scale, rstd, da, (const uint4*)dy, (uint4*)dx, (uint4*)dgate, dw_part, ds_part, dw, dscale, accumulate); \
     }
-    MHCL_BWD(1, false) MHCL_BWD(1, true) MHCL_BWD(2, false) MHCL_BWD(2, true) MHCL_BWD(4, false) MHCL_BWD(4, true)
+    MHCL_BWD(1) MHCL_BWD(2) MHCL_BWD(4)
 #undef MHCL_BWD
     if (parts == 1) return;
     c->launches += 1;
