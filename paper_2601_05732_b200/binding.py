@@ -186,8 +186,16 @@ class MhcLite:
         # status words of the calls around the stack (lookup, loss): part of device_status()
         self._status = _status_words(torch, device)
         self.clear_device_status()
+
+    def __getattr__(self, name):
+        # the extension module and its view of the context, with the first call around the stack: the mixing step does
+        # without them, and they cost an attribute of the object from then on
+        if name not in ("_m", "_c"):
+            raise AttributeError(f"{type(self).__name__!r} object has no attribute {name!r}")
         self._m = load_marshal()
-        self._c = self._m.make(h.value, device, n, C_)
+        if "_c" not in self.__dict__:
+            self._c = self._m.make(self._h.value, self.device, self.n, self.C)
+        return self.__dict__[name]
 
     def close(self):
         if getattr(self, "_h", None):

@@ -63,7 +63,7 @@ def build_marshal(force: bool = False) -> str:
     cuda = os.environ.get("CUDA_HOME") or os.path.dirname(os.path.dirname(_nvcc()))
     fresh = os.path.join(OBJ_DIR, f"marshal.{os.getpid()}")           # moved into place whole: several processes may build
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-w",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{sysconfig.get_paths()['include']}",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DMHCL_TORCH_VERSION="{torch.__version__}"', f"-I{sysconfig.get_paths()['include']}",
            *[f"-I{p}" for p in cpp_extension.include_paths()], f"-I{os.path.join(cuda, 'include')}", src, "-o", fresh,
            f"-L{libs}", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda", f"-Wl,-rpath,{libs}"]
     digest = hashlib.sha256("\0".join([*(a for a in cmd if a != fresh), torch.__version__, sys.version, open(src).read(), open(header).read()]).encode()).hexdigest()

@@ -294,6 +294,13 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__marshal(void) {
     PyObject* torch = PyImport_ImportModule("torch");                   // the tensor class has to be there
     if (!torch) return nullptr;
+    PyObject* version = PyObject_GetAttrString(torch, "__version__");
     Py_DECREF(torch);
+    const bool same = version && PyUnicode_Check(version) && PyUnicode_CompareWithASCIIString(version, MHCL_TORCH_VERSION) == 0;
+    Py_XDECREF(version);
+    if (!same) {                                                        // its tensors may be laid out differently
+        PyErr_SetString(PyExc_ImportError, "_marshal was built against torch " MHCL_TORCH_VERSION);
+        return nullptr;
+    }
     return PyModule_Create(&module);
 }

@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -79,3 +81,56 @@ def test_overlapped_kernels_do_not_read_by_the_read_only_path():
             for word in ("__ldg", "__ldcg", ".nc.", "ld_stream(", "__restrict__"):
                 assert word not in src.replace("ld_dep_stream(", ""), (name, word)
     assert launched == 4
+
+
+def test_contexts_do_without_the_extension_until_a_call_needs_it(monkeypatch):
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: 0
+
+    def missing():
+        raise ImportError("no extension here")
+    monkeypatch.setattr(torch.cuda, "is_available", lambda: True)
+    monkeypatch.setattr(binding, "load", Lib)
+    monkeypatch.setattr(binding, "_status_words", lambda t, d: torch.zeros(8, dtype=torch.int32))
+    monkeypatch.setattr(binding, "load_marshal", missing)
+    c = binding.MhcLite(4, 64)
+    c.set_kernel_timing(True)
+    with pytest.raises(ImportError, match="no extension here"):
+        c.dropout(torch.zeros(3), 0.1, None, None)
+    with pytest.raises(AttributeError):
+        c.no_such_call
+
+    class Module:
+        make = staticmethod(lambda *a: a)
+        dropout = staticmethod(lambda c, *a: seen.append(c) or 0)
+    seen = []
+    monkeypatch.setattr(binding, "load_marshal", lambda: Module)
+    c._h.value = 77
+    c.dropout(None, 0.1, None, None)
+    c.close()
+    c.dropout(None, 0.1, None, None)
+    assert seen == [(77, 0, 4, 64), None]                 # a closed context is passed as such
+    d = binding.MhcLite(4, 64)
+    d._h.value = 78
+    d.close()                                             # closed before its first call
+    d.dropout(None, 0.1, None, None)
+    assert seen[2] is None
+
+
+def test_extension_built_against_another_torch_is_built_anew():
+    code = """
+import torch
+torch.__version__ = "0.0"
+from paper_2601_05732_b200 import binding, build
+calls = []
+build.build_marshal = lambda force=False: calls.append(force)
+try:
+    binding.load_marshal()
+except ImportError as e:
+    assert "built against torch" in str(e) and len(calls) == 1
+else:
+    raise SystemExit("an extension of another torch was loaded")
+"""
+    root = os.path.dirname(os.path.dirname(binding.__file__))
+    subprocess.run([sys.executable, "-c", code], cwd=root, check=True, timeout=300)
