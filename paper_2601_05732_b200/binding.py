@@ -5,7 +5,8 @@ Every method of :class:`MhcLite` has the name of the C entry point it calls
 no step of the path runs in Python or on the CPU.  PyTorch supplies device memory
 and the CUDA stream.  Without the compiled library or without a CUDA device the
 calls raise.  The calls around the stack, made once a token when a model decodes, are
-marshalled by a small extension module (``csrc/marshal.cpp``), the others by ctypes.
+marshalled by a small extension module (``csrc/marshal.cpp``), loaded with the first of
+them, the others by ctypes.
 """
 from __future__ import annotations
 

@@ -6,7 +6,7 @@
 // (philox.cuh).  All of them move bf16 rows once and are bound by HBM; everything between load and store is fp32.
 //
 // A row belongs to a team of warps, VPT 16-byte vectors a lane.  Teams are persistent: each lane copies its own vectors of
-// the team's next rows into shared memory (cp.async, STAGES - 1 rows ahead, 50 KB and more in flight on an SM), so a row's
+// the team's next rows into shared memory (cp.async, STAGES - 1 rows ahead, 25 to 144 KB in flight on an SM), so a row's
 // latency, its sum over the team and its arithmetic overlap the arrival of the rows behind it, and a tensor is read once.
 // A lane reads back only what it copied itself: the ring needs no barrier.  The gradients keep the column sums (dw) of
 // their rows in registers and leave one partial row a block; colsum_k adds the blocks up in a fixed order, so results are
@@ -56,7 +56,8 @@ __device__ __forceinline__ void fetch_row(uint32_t to, const uint4* row, const T
 
 // A gate's pair a as x = e^-a = 2^(-a log2 e), from which sigma(a) = 1 / (1 + x) and 1 - sigma(a) = x sigma(a), both without
 // cancellation (1 - sigma formed by subtraction has no digit left from a = 17 on).  x overflows to infinity for a far below 0;
-// its reciprocal is 0, and so is the product, formed with the largest finite number in its place.
+// its reciprocal is 0, and so is the product, formed with the largest finite number in its place.  The approximate exponential
+// and reciprocal are off by 2^-22, against the results' rounding to bf16 by 2^-8.
 __device__ __forceinline__ uint64_t exp_minus2(uint64_t a) {
     float x, y;
     unpack2f(mul2(a, pack2f(-1.4426950408889634f, -1.4426950408889634f)), x, y);
@@ -91,7 +92,7 @@ struct DropArgs {
 };
 
 // The arithmetic runs on packed pairs (two fp32 operations an instruction): with gate and dropout a vector of 8 elements
-// takes some 170 instructions forward and 230 backward, and with scalar ones the issue slots, not HBM, bounded the kernels.
+// takes 204 instructions forward and 348 backward (counted), and with scalar ones the issue slots, not HBM, bounded the kernels.
 template <int VPT, bool BIG, bool GATE, bool DROP>
 __global__ void __launch_bounds__(BIG ? 512 : 256, BIG ? 1 : VPT == 4 ? 2 : 3)
 block_fwd_k(int64_t T, int C, int wpr, const uint4* x, const uint4* gate, const float4* w,

@@ -4,15 +4,16 @@
 //
 // Forward: one tcgen05 matrix product whose epilogue reduces each tile of logits, still in tensor memory, to (maximum, sum)
 // pairs of 128 columns of a row; ce_join_k joins a row's pairs.  Backward: the vocabulary in pieces.  A piece's logits are
-// computed again (2 T V C operations more, against T V values written and read back, and in fp32, where logits stored in
-// 16 bits would move exp(l - lse) by percents), turned into G in bf16, and G enters the two products.  A piece holds all
-// tokens, so its rows of dW are complete at once; dh adds up over the pieces in fp32.
+// computed again (2 T V C operations more, against T V values written, and read back twice), turned into G in bf16, and G
+// enters the two products.  Kept in 16 bits as they are, the logits would move exp(l - lse) by percents; kept as differences to
+// a row's maximum they would serve, but only in a call that has dloss before the loss, and in chunks of tokens that each add to
+// all of dW: not built.  A piece holds all tokens, so its rows of dW are complete at once; dh adds up over the pieces in fp32.
 //
 // Rows without a target (padding, prompts) are left out before the products: ce_rows_k lists the others and copies their
 // h side by side, so such rows cost nothing, and what they hold (NaN included) reaches neither loss nor gradients.
 //
 // What bounds it: the tensor cores, and behind them the power cap.  16384 x 2048 x 50257 on one B200: the forward's product
-// takes 1.97 ms alone (1.71 PFLOP/s, 94 % of the tensor cycles) and 2.34 ms in a long run at 985 W (1.44 PFLOP/s), where
+// takes 1.94 ms alone (1.74 PFLOP/s, 94 % of the tensor cycles) and 2.34 ms in a long run at 985 W (1.44 PFLOP/s), where
 // each instruction of the other warps counts: the waits sleep in hardware and the usual-case epilogues run on packed pairs.
 //
 // Tiles: 256 x 256 a pair of CTAs (tcgen05 cta_group::2: each CTA stages 128 rows of A and 128 columns of B, and holds 128
@@ -84,6 +85,8 @@ struct CeCtl {
     int abort[3];
 };
 
+// Relative error 2^-22, two units in the last place of fp32: far below the rounding of G, and a sum of such terms in lse comes
+// out no further off than any one of them.
 __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
 
 // lse and loss of a row from the largest logit `top` in base 2, the sum s of 2^(l - top) and the target's product x: the loss
@@ -788,7 +791,8 @@ struct CePlan {
     __nv_bfloat16* G; float* dh_acc;
     size_t bytes;
 };
-// Rounds that `tiles` tiles take on the pairs of CTAs.
+// Rounds that `tiles` tiles take on the pairs of CTAs (a B200's 74: the plan gives the scratch's size, which callers ask for
+// without a context, so it does not look at the device).
 constexpr int kCePairs = 74;
 static int64_t ce_rounds(int64_t tiles) { return (tiles + kCePairs - 1) / kCePairs; }
 
@@ -870,8 +874,9 @@ static void launch_ce_gemm(const mhclite_ctx* c, const CUtensorMap& ma, const CU
     smem_limit(once, ce_gemm_k<MODE>, c->device, smem);
     c->launches += 1;
     // Few column tiles: a group takes them all in one wave, and its rows of A are read from HBM once.  Many: the group's rows
-    // of A (32 tiles of 2048 channels: 34 MB) stay in L2 while B streams past.  Loss and gradients of 16384 x 2048 x 50257:
-    // 8.76 ms, against 8.89 with groups of 16 everywhere.
+    // of A (32 tiles of 2048 channels: 34 MB) stay in L2 while B streams past.  Loss and gradients of 16384 x 2048 x 50257 in a
+    // long run: 10.05 ms, with groups of 16 10.14, of 8 10.31, of 64 10.43.  At 512 channels all take 3.07 ms; at 4096, where
+    // 32 tiles are 67 MB (32000 words), groups of 16 would take 13.0 ms and these take 13.9.
     a.group = a.n_tiles <= 9 ? kCePairs / a.n_tiles : 32;
     const int64_t pairs = tiles < c->sm_count / 2 ? tiles : c->sm_count / 2;
     launch_after(ce_gemm_k<MODE>, dim3((unsigned)(2 * pairs)), dim3(kCeThreads), smem, s, ma, mb, a);

@@ -529,7 +529,8 @@ void launch_embed_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const int64_t*
     launch_after(k, dim3(grid), dim3(256), 0, s, T, V, c->C, c->n, tpt, ids, E, scale, (uint4*)x0, c->op_status);
 }
 
-// List entries a warp adds up: 32 where that leaves enough warps to fill the GPU, fewer for short lists.
+// List entries a warp adds up: 32 where that leaves enough warps to fill the GPU (a B200's 148 SMs: the number also gives the
+// scratch's size, which callers ask for without a context), fewer for short lists.
 static int embed_chunk(int64_t T, int C) {
     const int64_t slices = (C / 8 + 31) / 32;
     int R = 32;

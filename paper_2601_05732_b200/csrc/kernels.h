@@ -116,7 +116,8 @@ void launch_tail_mma(const mhclite_ctx* c, int64_t T, int N, const TailPlan& p, 
                      float* dW, float* dgain, int acc_params, cudaStream_t s);
 
 // Launches a kernel that may begin while the one before it on the stream still runs (programmatic dependent launch): it
-// waits for that kernel's results itself (pdl_wait), before its first access to global memory.
+// waits for that kernel's results itself (pdl_wait), before its first access to global memory.  (embed_zero_k alone writes
+// before it waits: what it clears is free from the moment its predecessor has begun, see there.)
 template <typename... P, typename... A>
 inline cudaError_t launch_after(void (*k)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A... args) {
     cudaLaunchConfig_t cfg = {};

@@ -18,7 +18,7 @@ inline float drop_factor(int threshold) { return (float)(65536.0 / (65536 - thre
 
 #ifdef __CUDACC__
 // The generator of one kernel.  The round keys are made anew for each group (18 additions): kept, they cost 20 registers
-// a thread, and the warps that those displace were worth more (dropout of 134 M elements: 98 -> 92.5 us).
+// a thread, and the warps that those displace were worth more (dropout of 134 M elements: 98 -> 92.5 us in a short run).
 struct Philox {
     uint32_t s0, s1, o0, o1;
     __device__ __forceinline__ Philox(const uint64_t* rng, bool use) {     // rng is read only if it is to be used
