@@ -739,6 +739,80 @@ def test_captured_and_replayed_with_new_inputs(ctx_of):
                 assert torch.equal(b[name], ref[name]), (k, name)
 
 
+def test_inputs_that_another_stream_writes(ctx_of):
+    """A kernel that may start beside the one before it still waits for what its stream waits for."""
+    c, T, C, side = ctx_of(4, 256), 300, 256, torch.cuda.Stream()
+    x, w = torch.zeros(T, C, dtype=BF, device=DEV), torch.ones(C, device=DEV)
+    new, rng = randn(1, T, C), rng_of(1, 2)
+    y, v, r, z = empty(T, C), empty(T, C), empty(T, dtype=F32), empty(T, C)
+    c.dropout(new, 0.5, rng, z)
+    c.block_in_fwd(new, w, 1e-6, v, r)
+    want, torch_done = (v.clone(), z.clone()), torch.cuda.Event()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        x.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(5_000_000)
+            x.copy_(new)
+            torch_done.record()
+        c.dropout(new, 0.5, rng, y)                                      # the kernel before, which lets the next one begin
+        torch.cuda.current_stream().wait_event(torch_done)
+        c.block_in_fwd(x, w, 1e-6, v, r)
+        c.dropout(x, 0.5, rng, z)
+        torch.cuda.synchronize()
+        assert torch.equal(v, want[0]) and torch.equal(z, want[1])
+
+
+def test_captured_behind_copies_and_joined_streams(ctx_of):
+    """In a graph a call may follow a copy, a clearing, or several nodes of joined streams, not only a kernel."""
+    c, T, C, V, rows, n = ctx_of(4, 256), 7000, 256, 3000, 40000, 4      # a table of which part is cleared beside the sort
+    src, g, ids = randn(1, T, n, C), torch.zeros(T, n, C, dtype=BF, device=DEV), torch.from_numpy(some_ids(2, T, rows, "text")).to(DEV)
+    none, w, side = ids[:0], torch.ones(C, device=DEV), torch.cuda.Stream()
+    h, W, target, dloss = loss_case(T, C, V)
+    b = {"dE": empty(rows, C, dtype=F32), "dE2": empty(rows, C, dtype=F32), "v": empty(T, C), "r": empty(T, dtype=F32), "z": empty(T, C), "loss": empty(T, dtype=F32),
+         "lse": empty(T, dtype=F32), "dh": empty(T, C), "dW": empty(V, C)}
+    x, rng = torch.zeros(T, C, dtype=BF, device=DEV), rng_of(3, 4)
+
+    def step():
+        g.copy_(src)                                                     # a copy
+        c.embed_bwd(ids, g, 0.5, b["dE"])
+        c.embed_bwd(none, g[:0], 0.5, b["dE"])                           # no tokens: a clearing
+        c.embed_bwd(ids, g, 0.5, b["dE"], accumulate=True)
+        b["dE2"].copy_(b["dE"])                                          # read before the next call clears it
+        c.embed_bwd(ids, g, 2.0, b["dE"])
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            x.copy_(h)
+            c.block_in_fwd(x, w, 1e-6, b["v"], b["r"])
+        c.linear_ce_fwd(h, W, target, 1.0, b["loss"], b["lse"])
+        main.wait_stream(side)
+        c.dropout(b["v"], 0.25, rng, b["z"])                             # two nodes before it
+        c.linear_ce_bwd(b["z"], W, target, 1.0, b["lse"], dloss, b["dh"], b["dW"])
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for k in range(3):
+        src.copy_(randn(10 + k, T, n, C))
+        h.copy_(randn(20 + k, T, C))
+        torch.cuda.synchronize()
+        step()
+        torch.cuda.synchronize()
+        want = {name: t.clone() for name, t in b.items()}
+        assert torch.equal(want["dE"], 4 * want["dE2"])                  # powers of two: exact
+        for t in (*b.values(), x):
+            t.fill_(float("nan"))
+        g.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in b:
+            assert torch.isfinite(want[name]).all() and torch.equal(b[name], want[name]), name
+
+
 # ---- status words ------------------------------------------------------------------------------------------------------
 BUSY = 100_000_000                  # cycles a stream is kept busy: some 50 ms
 
