@@ -326,7 +326,8 @@ MHCLITE_API int mhclite_set_status_words(mhclite_ctx* ctx, int32_t* words);
 typedef enum mhclite_op {          /* the operator named in such a report */
     MHCLITE_OP_EMBED = 20,
     MHCLITE_OP_EMBED_BWD = 21,
-    MHCLITE_OP_LINEAR_CE = 22
+    MHCLITE_OP_LINEAR_CE = 22,
+    MHCLITE_OP_LINEAR_DISTILL = 23
 } mhclite_op;
 
 /* x0[t,j,:] = bf16(scale * E[ids[t],:]) for each of the n streams j.  E [V,C], fp32 when table_f32 != 0, else bf16;
@@ -389,6 +390,32 @@ MHCLITE_API int mhclite_linear_ce_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, co
 MHCLITE_API int mhclite_linear_ce_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const mhclite_bf16* h, const mhclite_bf16* W,
                         const int64_t* target, float logit_scale, const float* lse, const float* dloss,
                         mhclite_bf16* dh, mhclite_bf16* dW, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Distillation from a teacher's top logits.  The student's distribution q = softmax(l / temperature) over the vocabulary, of
+ * the logits l[t,v] = logit_scale <h[t,:], W[v,:]>, which are never stored, against the teacher's over its K entries of a row:
+ *   lse[t] = log sum_v exp(l[t,v] / temperature)                                          [T] f32
+ *   logp[t,k] = l[t,ids[t,k]] / temperature - lse[t]                                      [T,K] f32
+ *   p[t,k] = exp(teacher[t,k] / temperature) / sum over the row's present entries
+ *   loss[t] = sum_k p[t,k] (log p[t,k] - logp[t,k])                                       [T] f32
+ * h [T,C], W [V,C] bf16; ids [T,K] int64; teacher [T,K] f32 when teacher_f32 != 0, else bf16 (logits, or log probabilities up
+ * to a constant a row).  1 <= K <= 256.  An entry whose id is negative is absent: its teacher logit is not used (NaN included)
+ * and its logp is 0; an id of V or more counts as absent and is reported.  A teacher logit of -inf gives the entry weight 0;
+ * its logp is formed all the same.  An id that occurs several times in a row has the sum of its
+ * weights in the gradients; in the loss its entries count one by one, as the formula says (which may then be negative).  Rows
+ * without an entry of weight have no teacher: loss, lse and logp are 0, h is not used.  (The factor temperature^2 that is
+ * often put before the loss is the caller's, in dloss.)  T V < 2^46. */
+MHCLITE_API size_t mhclite_linear_distill_scratch_bytes(int C, int64_t T, int64_t V, int K, int backward);
+MHCLITE_API int mhclite_linear_distill_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, int K, const mhclite_bf16* h, const mhclite_bf16* W,
+                        const int64_t* ids, const void* teacher, int teacher_f32, float logit_scale, float temperature,
+                        float* loss, float* lse, float* logp, void* scratch, size_t scratch_bytes, void* stream);
+/* Gradient from dloss [T] f32 and the forward's lse and logp, with a = dloss[t] logit_scale / temperature:
+ *   dh[t,:] = a (sum_v q[t,v] W[v,:] - sum_k p[t,k] W[ids[t,k],:])                        [T,C] bf16, 0 without a teacher
+ *   dW[v,:] = sum_t a (q[t,v] - sum_{k: ids[t,k] = v} p[t,k]) h[t,:]                      [V,C] bf16 (overwritten)
+ * The bracket of dW enters both products rounded to bf16; sums are fp32. */
+MHCLITE_API int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, int K, const mhclite_bf16* h, const mhclite_bf16* W,
+                        const int64_t* ids, const void* teacher, int teacher_f32, float logit_scale, float temperature,
+                        const float* lse, const float* logp, const float* dloss, mhclite_bf16* dh, mhclite_bf16* dW,
+                        void* scratch, size_t scratch_bytes, void* stream);
 
 /* ---- whole step from host buffers -------------------------------------------------------------- */
 

@@ -91,6 +91,9 @@ SIGNATURES = {
     "mhclite_linear_ce_scratch_bytes": (_sz, [_i, _i64, _i64, _i]),
     "mhclite_linear_ce_fwd": (_i, [_p, _i64, _i64, _p, _p, _p, _f, _p, _p, _p, _sz, _p]),
     "mhclite_linear_ce_bwd": (_i, [_p, _i64, _i64, _p, _p, _p, _f, _p, _p, _p, _p, _p, _sz, _p]),
+    "mhclite_linear_distill_scratch_bytes": (_sz, [_i, _i64, _i64, _i, _i]),
+    "mhclite_linear_distill_fwd": (_i, [_p, _i64, _i64, _i, _p, _p, _p, _p, _i, _f, _f, _p, _p, _p, _p, _sz, _p]),
+    "mhclite_linear_distill_bwd": (_i, [_p, _i64, _i64, _i, _p, _p, _p, _p, _i, _f, _f, _p, _p, _p, _p, _p, _p, _sz, _p]),
 }
 
 
@@ -527,3 +530,18 @@ class MhcLite:
         rc = self._m.linear_ce_bwd(self._c, h, W, target, logit_scale, lse, dloss, dh, dW)
         if rc:
             self._check(rc, "mhclite_linear_ce_bwd")
+
+    def linear_distill_fwd(self, h, W, ids, teacher, logit_scale, temperature, loss, lse, logp):
+        """Divergence of a teacher's top entries from the student: with x = logit_scale / temperature h W^T, which is not
+        stored, lse[t] = log sum exp x[t,:], logp[t,k] = x[t, ids[t,k]] - lse[t] and p = softmax(teacher / temperature) over a
+        row's present entries, loss[t] = sum_k p (log p - logp).  h [T,C], W [V,C] bf16; ids [T,K] int64 (negative: absent,
+        logp 0), teacher [T,K] fp32 or bf16; loss, lse [T], logp [T,K] fp32 (0 in rows without a teacher)."""
+        rc = self._m.linear_distill_fwd(self._c, h, W, ids, teacher, logit_scale, temperature, loss, lse, logp)
+        if rc:
+            self._check(rc, "mhclite_linear_distill_fwd")
+
+    def linear_distill_bwd(self, h, W, ids, teacher, logit_scale, temperature, lse, logp, dloss, dh, dW):
+        """dh [T,C], dW [V,C] bf16 from dloss [T] fp32 and the forward's lse and logp."""
+        rc = self._m.linear_distill_bwd(self._c, h, W, ids, teacher, logit_scale, temperature, lse, logp, dloss, dh, dW)
+        if rc:
+            self._check(rc, "mhclite_linear_distill_bwd")

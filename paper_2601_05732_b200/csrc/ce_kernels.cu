@@ -50,7 +50,7 @@ struct CeArgs {
     // CE_STATS
     float2* part;               // [2 n_tiles][Tpad] (maximum, sum) in base 2 of 128 columns each
     float* tlogit;              // [Tpad] <h_t, W_target>, before the scale
-    const int64_t* target;
+    const int64_t* target;      // null: the rows have none (distillation)
     int Tpad;
     // CE_GRAD
     const float* lse;
@@ -315,7 +315,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
             if (MODE == CE_STATS || MODE == CE_GRAD) {
                 const bool in = r < live;
                 const int t = in ? a.rows[r] : 0;
-                const int tgt = in ? (int)(a.target[t] - a.v0) - n0 : -1;            // the target's column among them
+                const int tgt = in && a.target ? (int)(a.target[t] - a.v0) - n0 : -1;        // the target's column among them
                 const int cols = (int)(a.V - a.v0) - n0;                             // of the vocabulary (the rest is padding)
                 const float k2 = a.scale * kLog2e;
                 if (MODE == CE_STATS) {
@@ -714,7 +714,7 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
             const int64_t row = unit * rows + er * 16 + (l >> 2) + (e >> 1) * 8;
             const int tok = i * 8 + (l & 3) * 2 + (e & 1);
             if (row >= V) continue;
-            if (tok < T && row == target[tok]) tlogit[tok] = v;
+            if (target && tok < T && row == target[tok]) tlogit[tok] = v;
             const float top = fmaxf(mx[j], v * k2), base = top == -INFINITY ? 0.f : top;
             sum[j] = sum[j] * ex2(mx[j] - base) + ex2(fmaf(v, k2, -base));
             mx[j] = top;
@@ -904,46 +904,60 @@ static SmallPlan plan_small(int64_t T, int C) {
     return p;
 }
 
+// The few-token forward's pairs; returns the CTAs that leave one each.
+static int launch_ce_small(const mhclite_ctx* c, const SmallPlan& q, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target,
+                           float scale, float2* part, float* tlogit, cudaStream_t s) {
+    const int64_t units = (V + (256 >> q.wk_log) - 1) / (256 >> q.wk_log);
+    const int grid = (int)(units < c->sm_count ? units : c->sm_count);
+    auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5> : q.nb == 2 ? ce_small_k<2, 5> : ce_small_k<4, 5>)
+                           : (q.nb == 1 ? ce_small_k<1, 3> : q.nb == 2 ? ce_small_k<2, 3> : ce_small_k<4, 3>);
+    static SmemOnce once[3][2];
+    smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
+    c->launches += 2;                                          // with the join that follows
+    launch_after(k, dim3(grid), dim3(kSmThreads), q.smem, s, (int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
+    return grid;
+}
+// The pairs of the rows that `listed` (the targets, or the like) has 0 to V - 1 for; what is picked on the way is the epilogue's.
+static bool launch_ce_stats(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const void* h, const void* W, const int64_t* listed,
+                            const int64_t* target, float scale, float* loss, float* lse, cudaStream_t s) {
+    CUtensorMap mh, mw;
+    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, p.a_box) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
+    launch_ce_rows(c, p, T, V, listed, h, loss, lse, nullptr, nullptr, s);
+    CeArgs a = {};
+    a.live = p.live; a.rows = p.rows; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
+    a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
+    a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
+    launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
+    c->launches += 1;                                          // the join that follows
+    return true;
+}
+
 bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
                           float* loss, float* lse, void* scratch, cudaStream_t s) {
     const SmallPlan q = plan_small(T, c->C);
     if (q.stages) {
         float2* part = (float2*)scratch;                       // [CTAs][32], then the targets' logits
         float* tlogit = (float*)(part + (size_t)c->sm_count * kSmTokens);
-        const int64_t units = (V + (256 >> q.wk_log) - 1) / (256 >> q.wk_log);
-        const int grid = (int)(units < c->sm_count ? units : c->sm_count);
-        auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5> : q.nb == 2 ? ce_small_k<2, 5> : ce_small_k<4, 5>)
-                               : (q.nb == 1 ? ce_small_k<1, 3> : q.nb == 2 ? ce_small_k<2, 3> : ce_small_k<4, 3>);
-        static SmemOnce once[3][2];
-        smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
-        c->launches += 2;
-        launch_after(k, dim3(grid), dim3(kSmThreads), q.smem, s, (int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
+        const int grid = launch_ce_small(c, q, T, V, h, W, target, scale, part, tlogit, s);
         launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, scale * kLog2e, loss, lse, c->op_status);
         return true;
     }
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);
-    CUtensorMap mh, mw;
-    if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, p.a_box) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
-    launch_ce_rows(c, p, T, V, target, h, loss, lse, nullptr, nullptr, s);
-    CeArgs a = {};
-    a.live = p.live; a.rows = p.rows; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
-    a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
-    a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
-    launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
-    c->launches += 1;
+    if (!launch_ce_stats(c, p, T, V, h, W, target, target, scale, loss, lse, s)) return false;
     launch_after(ce_join_k, dim3((unsigned)((T + 31) / 32)), dim3(1024), 0, s, p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, scale * kLog2e, loss, lse);
     return true;
 }
 
-bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
-                          const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s) {
-    const CePlan p = plan_ce(T, V, c->C, 1, scratch);
+// dh and dW of the rows that `listed` has 0 to V - 1 for; `fix(v0, vn)` is called between a piece's G and its products.
+template <typename F>
+static bool launch_ce_grads(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const void* h, const void* W, const int64_t* listed,
+                            const int64_t* target, float scale, const float* lse, const float* dloss, void* dh, void* dW, cudaStream_t s, F fix) {
     const int C = c->C;
     CUtensorMap mh, mw, mg, mwn, mgt, mhn;
     if (!map_k(&mh, p.hl, p.Tpad, C, C, p.a_box) || !map_k(&mw, W, V, C, C, kCeHalf) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, p.a_box) ||
         !map_mn(&mwn, W, V, C, C) || !map_mn(&mgt, p.G, p.Tpad, p.piece, p.piece) || !map_mn(&mhn, p.hl, p.Tpad, C, C))
         return false;
-    launch_ce_rows(c, p, T, V, target, h, nullptr, nullptr, dh, dloss, s);
+    launch_ce_rows(c, p, T, V, listed, h, nullptr, nullptr, dh, dloss, s);
     CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
@@ -955,6 +969,7 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         a.first = i == 0; a.last = i + 1 == p.pieces;
         a.m_tiles = p.Tpad / kCeM; a.n_tiles = (a.vn + kCeN - 1) / kCeN;
         launch_ce_gemm<CE_GRAD>(c, mh, mw, a, s);
+        fix(a.v0, a.vn);
         a.m_tiles = (a.vn + kCeM - 1) / kCeM; a.n_tiles = (C + kCeN - 1) / kCeN;
         launch_ce_gemm<CE_DW>(c, mgt, mhn, a, s);
         a.m_tiles = p.Tpad / kCeM;
@@ -969,4 +984,12 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     return true;
 }
 
+bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
+                          const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s) {
+    return launch_ce_grads(c, plan_ce(T, V, c->C, 1, scratch), T, V, h, W, target, target, scale, lse, dloss, dh, dW, s, [](int, int) {});
+}
+
 }  // namespace mhcl
+
+#include "distill.cuh"
+

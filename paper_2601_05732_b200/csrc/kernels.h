@@ -190,5 +190,14 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
                           float* loss, float* lse, void* scratch, cudaStream_t s);
 bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
                           const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s);
+// distill.cuh : distillation from a teacher's top logits on the same tiles; scale includes 1 / temperature
+constexpr int kDistillMaxK = 256;             // a teacher's entries a row
+size_t distill_scratch_bytes(int64_t T, int64_t V, int K, int C, int grad);
+bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids,
+                               const void* z, int z_f32, float scale, float inv_tau, float* loss, float* lse, float* logp, void* scratch,
+                               cudaStream_t s);
+bool launch_linear_distill_bwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids,
+                               const void* z, int z_f32, float scale, float inv_tau, const float* lse, const float* logp, const float* dloss,
+                               void* dh, void* dW, void* scratch, cudaStream_t s);
 
 }  // namespace mhcl

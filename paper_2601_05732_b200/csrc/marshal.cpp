@@ -18,20 +18,23 @@ namespace {
 
 // The C entry points, taken from the loaded library by name (bind).
 struct Entry { const char* name; void* fn; };
-enum Id { EMBED_FWD, EMBED_BWD, BLOCK_IN_FWD, BLOCK_IN_BWD, BLOCK_OUT_FWD, BLOCK_OUT_BWD, DROPOUT, CE_FWD, CE_BWD, EMBED_BYTES, BLOCK_BYTES, CE_BYTES, COUNT };
+enum Id { EMBED_FWD, EMBED_BWD, BLOCK_IN_FWD, BLOCK_IN_BWD, BLOCK_OUT_FWD, BLOCK_OUT_BWD, DROPOUT, CE_FWD, CE_BWD, EMBED_BYTES, BLOCK_BYTES, CE_BYTES,
+          DISTILL_FWD, DISTILL_BWD, DISTILL_BYTES, COUNT };
 Entry entries[COUNT] = {{"mhclite_embed_fwd", nullptr}, {"mhclite_embed_bwd", nullptr}, {"mhclite_block_in_fwd", nullptr},
                         {"mhclite_block_in_bwd", nullptr}, {"mhclite_block_out_fwd", nullptr}, {"mhclite_block_out_bwd", nullptr},
                         {"mhclite_dropout", nullptr}, {"mhclite_linear_ce_fwd", nullptr}, {"mhclite_linear_ce_bwd", nullptr},
                         {"mhclite_embed_scratch_bytes", nullptr}, {"mhclite_block_scratch_bytes", nullptr},
-                        {"mhclite_linear_ce_scratch_bytes", nullptr}};
+                        {"mhclite_linear_ce_scratch_bytes", nullptr},
+                        {"mhclite_linear_distill_fwd", nullptr}, {"mhclite_linear_distill_bwd", nullptr},
+                        {"mhclite_linear_distill_scratch_bytes", nullptr}};
 template <typename F> F* entry(Id id, F*) { return reinterpret_cast<F*>(entries[id].fn); }
 #define CALL(id, fn, ...) entry(id, &fn)(__VA_ARGS__)
 
-struct Memo { int64_t T = -1, V = -1; size_t bytes = 0; };           // the last sizes whose scratch was asked for
+struct Memo { int64_t T = -1, V = -1; size_t bytes = 0; int K = 0; };    // the last sizes whose scratch was asked for
 struct Context {
     mhclite_ctx* h;
     int device, n, C;
-    Memo embed, block, ce[2];
+    Memo embed, block, ce[2], distill[2];
 };
 const char* kCapsule = "mhclite.context";
 Context* context(PyObject* o) { return static_cast<Context*>(PyCapsule_GetPointer(o, kCapsule)); }
@@ -262,6 +265,57 @@ PyObject* linear_ce_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {   
     RUN(CALL(CE_BWD, mhclite_linear_ce_bwd, x.c->h, T, V, h, W, target, scale, lse, dloss, dh, dW, address(ws), bytes, st))
 }
 
+// A teacher's entries: ids [T, K] and its logits, fp32 or bf16.
+struct Teacher { const int64_t* ids; const void* z; bool f32; int K; };
+Teacher teacher(Args& x, int ids, int z, int64_t T) {
+    Teacher e = {};
+    const at::Tensor *t = x.tensor(ids, "ids"), *v = x.tensor(z, "teacher");
+    if (x.bad) return e;
+    if (t->dim() != 2 || t->size(1) > 0x7FFFFFFF) {
+        PyErr_SetString(PyExc_ValueError, "ids: expected two axes");
+        x.bad = true;
+        return e;
+    }
+    e.K = (int)t->size(1);
+    e.f32 = v->scalar_type() == at::kFloat;
+    e.ids = x.i64(ids, "ids", {T, e.K});
+    e.z = x.ptr(z, "teacher", e.f32 ? at::kFloat : at::kBFloat16, {T, e.K});
+    return e;
+}
+size_t distill_bytes(Context* c, int64_t T, int64_t V, int K, int backward) {
+    Memo& m = c->distill[backward];
+    if (m.T != T || m.V != V || m.K != K) m = {T, V, CALL(DISTILL_BYTES, mhclite_linear_distill_scratch_bytes, c->C, T, V, K, backward), K};
+    return m.bytes;
+}
+
+// h, W, ids, teacher, logit_scale, temperature, loss, lse, logp
+PyObject* linear_distill_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    TAKE(10)
+    const int64_t T = x.rows(0, "h"), V = x.rows(1, "W");
+    const mhclite_bf16 *h = x.bf16(0, "h", {T, C}), *W = x.bf16(1, "W", {V, C});
+    const Teacher e = teacher(x, 2, 3, T);
+    const float scale = x.number(4), tau = x.number(5);
+    float *loss = x.f32(6, "loss", {T}), *lse = x.f32(7, "lse", {T}), *logp = x.f32(8, "logp", {T, e.K});
+    if (x.bad) return nullptr;
+    const size_t bytes = distill_bytes(x.c, T, V, e.K, 0);
+    const at::Tensor ws = x.scratch(bytes);
+    RUN(CALL(DISTILL_FWD, mhclite_linear_distill_fwd, x.c->h, T, V, e.K, h, W, e.ids, e.z, e.f32, scale, tau, loss, lse, logp, address(ws), bytes, st))
+}
+
+// h, W, ids, teacher, logit_scale, temperature, lse, logp, dloss, dh, dW
+PyObject* linear_distill_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    TAKE(12)
+    const int64_t T = x.rows(0, "h"), V = x.rows(1, "W");
+    const mhclite_bf16 *h = x.bf16(0, "h", {T, C}), *W = x.bf16(1, "W", {V, C});
+    const Teacher e = teacher(x, 2, 3, T);
+    const float scale = x.number(4), tau = x.number(5), *lse = x.f32(6, "lse", {T}), *logp = x.f32(7, "logp", {T, e.K}), *dloss = x.f32(8, "dloss", {T});
+    mhclite_bf16 *dh = x.bf16(9, "dh", {T, C}), *dW = x.bf16(10, "dW", {V, C});
+    if (x.bad) return nullptr;
+    const size_t bytes = distill_bytes(x.c, T, V, e.K, 1);
+    const at::Tensor ws = x.scratch(bytes);
+    RUN(CALL(DISTILL_BWD, mhclite_linear_distill_bwd, x.c->h, T, V, e.K, h, W, e.ids, e.z, e.f32, scale, tau, lse, logp, dloss, dh, dW, address(ws), bytes, st))
+}
+
 // bind({name: address}): where the loaded library has the entry points.
 PyObject* bind(PyObject*, PyObject* table) {
     for (Entry& e : entries) {
@@ -278,14 +332,14 @@ PyObject* make(PyObject*, PyObject* args) {
     unsigned long long h;
     int device, n, C;
     if (!PyArg_ParseTuple(args, "Kiii", &h, &device, &n, &C)) return nullptr;
-    Context* c = new (std::nothrow) Context{reinterpret_cast<mhclite_ctx*>(h), device, n, C, {}, {}, {}};
+    Context* c = new (std::nothrow) Context{reinterpret_cast<mhclite_ctx*>(h), device, n, C, {}, {}, {}, {}};
     if (!c) return PyErr_NoMemory();
     return PyCapsule_New(c, kCapsule, [](PyObject* o) { delete static_cast<Context*>(PyCapsule_GetPointer(o, kCapsule)); });
 }
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(embed_fwd), METHOD(embed_bwd), METHOD(block_in_fwd), METHOD(block_in_bwd), METHOD(block_out_fwd),
-                         METHOD(block_out_bwd), METHOD(dropout), METHOD(linear_ce_fwd), METHOD(linear_ce_bwd),
+                         METHOD(block_out_bwd), METHOD(dropout), METHOD(linear_ce_fwd), METHOD(linear_ce_bwd), METHOD(linear_distill_fwd), METHOD(linear_distill_bwd),
                          {"bind", bind, METH_O, nullptr}, {"make", make, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -217,4 +217,64 @@ int mhclite_linear_ce_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, const mhclite_
     return MHCLITE_OK;
 }
 
+size_t mhclite_linear_distill_scratch_bytes(int C, int64_t T, int64_t V, int K, int backward) {
+    if (mhclite_linear_ce_scratch_bytes(C, T, V, backward) == 0 || K < 1 || K > kDistillMaxK) return 0;
+    return distill_scratch_bytes(T, V, K, C, backward);
+}
+
+// The student's scale with the temperature in it, in `scale`.
+static int check_distill(mhclite_ctx* ctx, int64_t T, int64_t V, int K, float logit_scale, float temperature, float* scale) {
+    if (K < 1 || K > kDistillMaxK) return fail(ctx, MHCLITE_ERR_BAD_ARG, "K must be in [1, %d]", kDistillMaxK);
+    const float inv = 1.f / temperature;
+    if (!(temperature > 0.f && inv > 0.f && inv - inv == 0.f)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "temperature must be positive, it and its reciprocal finite");
+    *scale = (float)((double)logit_scale / temperature);
+    return check_ce(ctx, T, V, *scale);
+}
+
+int mhclite_linear_distill_fwd(mhclite_ctx* ctx, int64_t T, int64_t V, int K, const mhclite_bf16* h, const mhclite_bf16* W, const int64_t* ids,
+                               const void* teacher, int teacher_f32, float logit_scale, float temperature, float* loss, float* lse,
+                               float* logp, void* scratch, size_t scratch_bytes, void* stream) {
+    MHCL_REQUIRE_CTX(ctx); MHCL_REQUIRE_T(ctx, T);
+    float scale;
+    int rc = check_distill(ctx, T, V, K, logit_scale, temperature, &scale);
+    if (rc) return rc;
+    if (T == 0) return MHCLITE_OK;
+    MHCL_PTR(ctx, h); MHCL_PTR(ctx, W); MHCL_PTR8(ctx, ids); MHCL_PTR(ctx, teacher); MHCL_PTR(ctx, loss); MHCL_PTR(ctx, lse);
+    MHCL_PTR(ctx, logp);
+    MHCL_NO_ALIAS(ctx, loss, lse); MHCL_NO_ALIAS(ctx, loss, logp); MHCL_NO_ALIAS(ctx, lse, logp); MHCL_NO_ALIAS(ctx, logp, teacher);
+    MHCL_NO_ALIAS(ctx, loss, teacher); MHCL_NO_ALIAS(ctx, lse, teacher);
+    if ((rc = check_scratch(ctx, scratch, scratch_bytes, distill_scratch_bytes(T, V, K, ctx->C, 0)))) return rc;
+    MHCL_DEVICE(ctx);
+    if (!launch_linear_distill_fwd(ctx, T, V, K, h, W, ids, teacher, teacher_f32, scale, 1.f / temperature, loss, lse, logp, scratch,
+                                   (cudaStream_t)stream))
+        return fail(ctx, MHCLITE_ERR_CUDA, "linear_distill_fwd: building a tensor map failed");
+    MHCL_LAUNCH_CHECK(ctx, "linear_distill_fwd");
+    return MHCLITE_OK;
+}
+
+int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, int K, const mhclite_bf16* h, const mhclite_bf16* W, const int64_t* ids,
+                               const void* teacher, int teacher_f32, float logit_scale, float temperature, const float* lse,
+                               const float* logp, const float* dloss, mhclite_bf16* dh, mhclite_bf16* dW, void* scratch,
+                               size_t scratch_bytes, void* stream) {
+    MHCL_REQUIRE_CTX(ctx); MHCL_REQUIRE_T(ctx, T);
+    float scale;
+    int rc = check_distill(ctx, T, V, K, logit_scale, temperature, &scale);
+    if (rc) return rc;
+    MHCL_PTR(ctx, dW);
+    if (T == 0) {
+        MHCL_DEVICE(ctx);
+        return check_cuda(ctx, cudaMemsetAsync(dW, 0, (size_t)V * ctx->C * 2, (cudaStream_t)stream), "zero dW");
+    }
+    MHCL_PTR(ctx, h); MHCL_PTR(ctx, W); MHCL_PTR8(ctx, ids); MHCL_PTR(ctx, teacher); MHCL_PTR(ctx, lse); MHCL_PTR(ctx, logp);
+    MHCL_PTR(ctx, dloss); MHCL_PTR(ctx, dh);
+    MHCL_NO_ALIAS(ctx, dh, h); MHCL_NO_ALIAS(ctx, dh, W); MHCL_NO_ALIAS(ctx, dW, h); MHCL_NO_ALIAS(ctx, dW, W); MHCL_NO_ALIAS(ctx, dh, dW);
+    if ((rc = check_scratch(ctx, scratch, scratch_bytes, distill_scratch_bytes(T, V, K, ctx->C, 1)))) return rc;
+    MHCL_DEVICE(ctx);
+    if (!launch_linear_distill_bwd(ctx, T, V, K, h, W, ids, teacher, teacher_f32, scale, 1.f / temperature, lse, logp, dloss, dh, dW, scratch,
+                                   (cudaStream_t)stream))
+        return fail(ctx, MHCLITE_ERR_CUDA, "linear_distill_bwd: building a tensor map failed");
+    MHCL_LAUNCH_CHECK(ctx, "linear_distill_bwd");
+    return MHCLITE_OK;
+}
+
 }  // extern "C"

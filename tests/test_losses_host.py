@@ -1,0 +1,65 @@
+"""Host logic of the losses behind a first training without a GPU: scratch planning, and refusals that need no context."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2601_05732_b200 import binding
+
+
+def test_scratch_bytes_of_distillation():
+    lib = binding.load()
+    d, c = lib.mhclite_linear_distill_scratch_bytes, lib.mhclite_linear_ce_scratch_bytes
+    for back in (0, 1):
+        assert d(64, 100, 1000, 8, back) > c(64, 100, 1000, back) > 0
+        assert d(64, 0, 100, 8, back) > 0 and d(64, 100, 1000, 256, back) > 0
+        for bad in ((63, 10, 100, 8), (64, -1, 100, 8), (64, 10, 0, 8), (64, 10, 100, 0), (64, 10, 100, 257), (64, 10, 100, -1), (64, 2**30, 2**20, 8)):
+            assert d(*bad, back) == 0, bad
+    for T in (0, 1, 2**31, 2**62):                        # no size ends the process
+        for V in (1, 2**31, 2**62):
+            d(64, T, V, 4, 0), d(64, T, V, 4, 1)
+    # entries of 16384 x 64: some megabytes on top of the tiles' scratch, whatever the vocabulary
+    assert d(2048, 16384, 100000, 64, 1) - c(2048, 16384, 100000, 1) < 32 << 20
+
+
+def test_null_context_is_refused():
+    lib = binding.load()
+    names = [n for n in binding.SIGNATURES if n.startswith("mhclite_linear_distill") and not n.endswith("_bytes")]
+    assert len(names) == 2
+    for name in names:
+        zero = [0.0 if a is ctypes.c_float else None if a is ctypes.c_void_p else 0 for a in binding.SIGNATURES[name][1]]
+        assert getattr(lib, name)(*zero) == binding.ERR_BAD_ARG, name
+
+
+def test_arguments_are_refused_before_the_library_sees_them():
+    m = binding.load_marshal()
+    c = m.make(1234, 0, 4, 64)                            # a handle that no call gets as far as using
+    bf, f32, i64 = (lambda *s, t=t: torch.zeros(*s, dtype=t) for t in (torch.bfloat16, torch.float32, torch.int64))
+    out = (f32(3), f32(3), f32(3, 5))
+    value = [(m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3), f32(3, 5), 1.0, 1.0, *out),             # one axis
+             (m.linear_distill_fwd, bf(3, 64), bf(9, 63), i64(3, 5), f32(3, 5), 1.0, 1.0, *out),
+             (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out)]           # not on the device
+    kind = [(m.linear_distill_fwd, bf(3, 64), bf(9, 64), None, f32(3, 5), 1.0, 1.0, *out), (m.linear_distill_bwd, bf(3, 64)),
+            (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), 7, 1.0, 1.0, *out)]
+    for error, calls in ((ValueError, value), (TypeError, kind)):
+        for f, *args in calls:
+            with pytest.raises(error):
+                f(c, *args)
+    with pytest.raises(ValueError, match="closed"):
+        m.linear_distill_fwd(None, bf(3, 64), bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out)
+
+
+def test_included_kernels_do_not_read_by_the_read_only_path():
+    """Kernels that begin while their predecessor runs, kept in files that others include (csrc/kernels.h tells why)."""
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    seen = 0
+    for name in sorted(os.listdir(csrc)):
+        src = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, name)).read())
+        if "launch_after(" in src and name.endswith(".cuh"):
+            seen += 1
+            assert src.count("pdl_wait();") == src.count("__global__"), name
+            for word in ("__ldg", "__ldcg", ".nc.", "ld_stream(", "__restrict__"):
+                assert word not in src.replace("ld_dep_stream(", ""), (name, word)
+    assert seen >= 1
