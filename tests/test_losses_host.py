@@ -41,8 +41,8 @@ def test_arguments_are_refused_before_the_library_sees_them():
     value = [(m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3), f32(3, 5), 1.0, 1.0, *out),             # one axis
              (m.linear_distill_fwd, bf(3, 64), bf(9, 63), i64(3, 5), f32(3, 5), 1.0, 1.0, *out),
              (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out)]           # not on the device
-    kind = [(m.linear_distill_fwd, bf(3, 64), bf(9, 64), None, f32(3, 5), 1.0, 1.0, *out), (m.linear_distill_bwd, bf(3, 64)),
-            (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), 7, 1.0, 1.0, *out)]
+    kind = [(m.linear_distill_fwd, None, bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out), (m.linear_distill_bwd, bf(3, 64)),
+            (m.linear_distill_fwd, bf(3, 64), 7, i64(3, 5), f32(3, 5), 1.0, 1.0, *out)]
     for error, calls in ((ValueError, value), (TypeError, kind)):
         for f, *args in calls:
             with pytest.raises(error):
