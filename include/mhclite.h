@@ -327,7 +327,8 @@ typedef enum mhclite_op {          /* the operator named in such a report */
     MHCLITE_OP_EMBED = 20,
     MHCLITE_OP_EMBED_BWD = 21,
     MHCLITE_OP_LINEAR_CE = 22,
-    MHCLITE_OP_LINEAR_DISTILL = 23
+    MHCLITE_OP_LINEAR_DISTILL = 23,
+    MHCLITE_OP_SEQUENCES = 24
 } mhclite_op;
 
 /* x0[t,j,:] = bf16(scale * E[ids[t],:]) for each of the n streams j.  E [V,C], fp32 when table_f32 != 0, else bf16;
@@ -416,6 +417,40 @@ MHCLITE_API int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t 
                         const int64_t* ids, const void* teacher, int teacher_f32, float logit_scale, float temperature,
                         const float* lse, const float* logp, const float* dloss, mhclite_bf16* dh, mhclite_bf16* dW,
                         void* scratch, size_t scratch_bytes, void* stream);
+
+/* Losses of whole sequences, from the losses of their tokens as mhclite_linear_ce_fwd leaves them (nll[t] = -log probability of
+ * token t), and their gradient with respect to these, which mhclite_linear_ce_bwd takes as dloss.
+ *   - T tokens; starts [S+1] int64, not falling, within 0 .. T: sequence s holds the tokens starts[s] .. starts[s+1] - 1 and may
+ *     be empty.  Other starts are reported (MHCLITE_ERR_INDEX); the results of such sequences are then unspecified.
+ *   - A token counts where target[t] >= 0 and it lies in a sequence.  Others have no part in the losses, whatever is stored for
+ *     them (NaN included), and their dnll is 0.
+ *   - mean != 0: the sum over a sequence's tokens that count is divided by their number (0 where there are none).
+ *   - dloss (dL/dloss) and dnll [T] are given both or neither; one call gives losses and gradient.
+ *   - T == 0: the losses are those of empty sequences.  S < 2^30.  All but target and starts are f32.
+ *
+ * Clipped policy loss with a KL term.  x = nll_old - nll, r = exp(x), A = adv[s] (or adv[t] when token_adv != 0):
+ *   pg[t] = max(-A r, -A min(max(r, 1 - clip_low), 1 + clip_high)),   d = nll - nll_ref,   kl[t] = exp(d) - d - 1
+ *   loss[s] = sum (or mean) of pg + kl_weight kl                                          [S]
+ *   stats[s] = (tokens that count, those where the clipped term is the larger, sum (or mean) of kl)      [S,3]
+ *   dnll[t] = dloss[s] (/ tokens) ((0 where the clipped term is the larger, else A r) + kl_weight (exp(d) - 1))
+ * nll_ref may be NULL: no KL term.  0 <= clip_low <= 1, clip_high >= 0 (infinity: no upper border).  Which side of a border a
+ * ratio is on is decided in 64 bits. */
+MHCLITE_API size_t mhclite_policy_scratch_bytes(int64_t T, int64_t S);
+MHCLITE_API int mhclite_policy_loss(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll, const float* nll_old, const float* nll_ref,
+                        const int64_t* target, const int64_t* starts, const float* adv, int token_adv, double clip_low, double clip_high,
+                        double kl_weight, int mean, const float* dloss, float* loss, float* stats, float* dnll,
+                        void* scratch, size_t scratch_bytes, void* stream);
+/* Preference loss of P pairs: sequence 2 p is the chosen one, 2 p + 1 the rejected (starts [2P+1]).
+ *   R[s] = sum (or mean) of nll_ref - nll (of -nll when nll_ref is NULL)
+ *   x = beta (R[2p] - R[2p+1]) - margin
+ *   loss[p] = -(1 - smoothing) log sigmoid(x) - smoothing log sigmoid(-x)                 [P]
+ *   reward[p] = (beta R[2p], beta R[2p+1])                                                [P,2]
+ *   dnll[t] = -+ beta dloss[p] (/ tokens) (smoothing - sigmoid(-x)), - in the chosen sequence, + in the rejected
+ * 0 <= smoothing <= 1. */
+MHCLITE_API size_t mhclite_preference_scratch_bytes(int64_t T, int64_t P);
+MHCLITE_API int mhclite_preference_loss(mhclite_ctx* ctx, int64_t T, int64_t P, const float* nll, const float* nll_ref, const int64_t* target,
+                        const int64_t* starts, double beta, double margin, double smoothing, int mean, const float* dloss,
+                        float* loss, float* reward, float* dnll, void* scratch, size_t scratch_bytes, void* stream);
 
 /* ---- whole step from host buffers -------------------------------------------------------------- */
 

@@ -68,9 +68,12 @@ def policy_loss(nll, nll_old, nll_ref, target, starts, adv, token_adv, clip_low,
         if n == 0:
             continue
         A = adv[at] if token_adv else np.full(n, adv[s])
-        r = np.exp(nll_old[at] - nll[at])
+        x = nll_old[at] - nll[at]
+        r = np.exp(x)
         free, held = -A * r, -A * np.clip(r, 1 - clip_low, 1 + clip_high)
-        cut = held > free
+        # e^x is above 1 + c where x is above log(1 + c): the exponential of an x below 2^-53 would be rounded to 1
+        with np.errstate(divide="ignore"):
+            cut = ((x > np.log1p(clip_high)) & (A > 0)) | ((x < np.log1p(-clip_low)) & (A < 0))
         l, g = np.where(cut, held, free), np.where(cut, 0.0, A * r)
         kl = np.zeros(n)
         if nll_ref is not None:

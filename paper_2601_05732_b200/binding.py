@@ -30,7 +30,7 @@ class MhcLiteError(RuntimeError):
         super().__init__(f"{where}: status {status} ({status_string(status)}) {detail}".rstrip())
 
 
-_p, _i, _i64, _f, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
+_p, _i, _i64, _f, _d, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_double, C.c_size_t
 
 # name -> (restype, argtypes); mirrors include/mhclite.h
 SIGNATURES = {
@@ -94,6 +94,10 @@ SIGNATURES = {
     "mhclite_linear_distill_scratch_bytes": (_sz, [_i, _i64, _i64, _i, _i]),
     "mhclite_linear_distill_fwd": (_i, [_p, _i64, _i64, _i, _p, _p, _p, _p, _i, _f, _f, _p, _p, _p, _p, _sz, _p]),
     "mhclite_linear_distill_bwd": (_i, [_p, _i64, _i64, _i, _p, _p, _p, _p, _i, _f, _f, _p, _p, _p, _p, _p, _p, _sz, _p]),
+    "mhclite_policy_scratch_bytes": (_sz, [_i64, _i64]),
+    "mhclite_policy_loss": (_i, [_p, _i64, _i64, _p, _p, _p, _p, _p, _p, _i, _d, _d, _d, _i, _p, _p, _p, _p, _p, _sz, _p]),
+    "mhclite_preference_scratch_bytes": (_sz, [_i64, _i64]),
+    "mhclite_preference_loss": (_i, [_p, _i64, _i64, _p, _p, _p, _p, _d, _d, _d, _i, _p, _p, _p, _p, _p, _sz, _p]),
 }
 
 
@@ -545,3 +549,25 @@ class MhcLite:
         rc = self._m.linear_distill_bwd(self._c, h, W, ids, teacher, logit_scale, temperature, lse, logp, dloss, dh, dW)
         if rc:
             self._check(rc, "mhclite_linear_distill_bwd")
+
+    def policy_loss(self, nll, nll_old, nll_ref, target, starts, adv, token_adv, clip_low, clip_high, kl_weight, mean, loss, stats,
+                    dloss=None, dnll=None):
+        """Clipped policy loss of S sequences with a KL term, and with dloss its gradient: r = exp(nll_old - nll),
+        d = nll - nll_ref, loss[s] = sum (mean: mean) over a sequence's tokens with target >= 0 of
+        max(-A r, -A clip(r, 1 - clip_low, 1 + clip_high)) + kl_weight (exp(d) - d - 1).  nll, nll_old, nll_ref (or None),
+        dnll [T] fp32, target [T] int64, all as linear_ce_fwd takes and leaves them; starts [S+1] int64: sequence s holds the
+        tokens starts[s] .. starts[s+1] - 1; adv [S] fp32, or [T] with token_adv; loss, dloss [S], stats [S,3] fp32 (tokens
+        that count, clipped ones, sum or mean of the divergence).  dnll is what linear_ce_bwd takes as dloss."""
+        rc = self._m.policy_loss(self._c, nll, nll_old, nll_ref, target, starts, adv, token_adv, clip_low, clip_high, kl_weight, mean,
+                                 loss, stats, dloss, dnll)
+        if rc:
+            self._check(rc, "mhclite_policy_loss")
+
+    def preference_loss(self, nll, nll_ref, target, starts, beta, margin, smoothing, mean, loss, reward, dloss=None, dnll=None):
+        """Preference loss of P pairs of sequences (2 p chosen, 2 p + 1 rejected; starts [2P+1]), and with dloss its gradient:
+        R = sum (mean: mean) of nll_ref - nll over a sequence's tokens with target >= 0, x = beta (R_chosen - R_rejected) -
+        margin, loss[p] = -(1 - smoothing) log sigmoid(x) - smoothing log sigmoid(-x), reward[p] = beta R of both.  Without
+        nll_ref (None) R is of -nll.  loss, dloss [P], reward [P,2]; the others as in policy_loss."""
+        rc = self._m.preference_loss(self._c, nll, nll_ref, target, starts, beta, margin, smoothing, mean, loss, reward, dloss, dnll)
+        if rc:
+            self._check(rc, "mhclite_preference_loss")

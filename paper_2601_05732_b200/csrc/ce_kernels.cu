@@ -992,4 +992,5 @@ bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
 }  // namespace mhcl
 
 #include "distill.cuh"
+#include "seq_losses.cuh"
 

@@ -199,5 +199,13 @@ bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
 bool launch_linear_distill_bwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids,
                                const void* z, int z_f32, float scale, float inv_tau, const float* lse, const float* logp, const float* dloss,
                                void* dh, void* dW, void* scratch, cudaStream_t s);
+// seq_losses.cuh : losses of whole sequences from the losses of their tokens, with their gradients (dnll null: without)
+size_t seq_scratch_bytes(int64_t T, int64_t S);
+void launch_policy_loss(const mhclite_ctx* c, int64_t T, int64_t S, const float* nll, const float* nll_old, const float* nll_ref,
+                        const int64_t* target, const int64_t* starts, const float* adv, int token_adv, double clip_low, double clip_high,
+                        double kl_weight, int mean, const float* dloss, float* loss, float* stats, float* dnll, void* scratch, cudaStream_t s);
+void launch_preference_loss(const mhclite_ctx* c, int64_t T, int64_t P, const float* nll, const float* nll_ref, const int64_t* target,
+                            const int64_t* starts, double beta, double margin, double smoothing, int mean, const float* dloss, float* loss,
+                            float* reward, float* dnll, void* scratch, cudaStream_t s);
 
 }  // namespace mhcl

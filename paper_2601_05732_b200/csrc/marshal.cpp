@@ -19,14 +19,16 @@ namespace {
 // The C entry points, taken from the loaded library by name (bind).
 struct Entry { const char* name; void* fn; };
 enum Id { EMBED_FWD, EMBED_BWD, BLOCK_IN_FWD, BLOCK_IN_BWD, BLOCK_OUT_FWD, BLOCK_OUT_BWD, DROPOUT, CE_FWD, CE_BWD, EMBED_BYTES, BLOCK_BYTES, CE_BYTES,
-          DISTILL_FWD, DISTILL_BWD, DISTILL_BYTES, COUNT };
+          DISTILL_FWD, DISTILL_BWD, DISTILL_BYTES, POLICY, PREFERENCE, POLICY_BYTES, PREFERENCE_BYTES, COUNT };
 Entry entries[COUNT] = {{"mhclite_embed_fwd", nullptr}, {"mhclite_embed_bwd", nullptr}, {"mhclite_block_in_fwd", nullptr},
                         {"mhclite_block_in_bwd", nullptr}, {"mhclite_block_out_fwd", nullptr}, {"mhclite_block_out_bwd", nullptr},
                         {"mhclite_dropout", nullptr}, {"mhclite_linear_ce_fwd", nullptr}, {"mhclite_linear_ce_bwd", nullptr},
                         {"mhclite_embed_scratch_bytes", nullptr}, {"mhclite_block_scratch_bytes", nullptr},
                         {"mhclite_linear_ce_scratch_bytes", nullptr},
                         {"mhclite_linear_distill_fwd", nullptr}, {"mhclite_linear_distill_bwd", nullptr},
-                        {"mhclite_linear_distill_scratch_bytes", nullptr}};
+                        {"mhclite_linear_distill_scratch_bytes", nullptr}, {"mhclite_policy_loss", nullptr},
+                        {"mhclite_preference_loss", nullptr}, {"mhclite_policy_scratch_bytes", nullptr},
+                        {"mhclite_preference_scratch_bytes", nullptr}};
 template <typename F> F* entry(Id id, F*) { return reinterpret_cast<F*>(entries[id].fn); }
 #define CALL(id, fn, ...) entry(id, &fn)(__VA_ARGS__)
 
@@ -34,7 +36,7 @@ struct Memo { int64_t T = -1, V = -1; size_t bytes = 0; int K = 0; };    // the 
 struct Context {
     mhclite_ctx* h;
     int device, n, C;
-    Memo embed, block, ce[2], distill[2];
+    Memo embed, block, ce[2], distill[2], policy, preference;
 };
 const char* kCapsule = "mhclite.context";
 Context* context(PyObject* o) { return static_cast<Context*>(PyCapsule_GetPointer(o, kCapsule)); }
@@ -92,12 +94,13 @@ struct Args {
     float* f32(int i, const char* name, at::IntArrayRef shape) { return (float*)ptr(i, name, at::kFloat, shape); }
     int64_t* i64(int i, const char* name, at::IntArrayRef shape) { return (int64_t*)ptr(i, name, at::kLong, shape); }
     bool none(int i) const { return a[i] == Py_None; }
-    float number(int i) {
-        if (bad) return 0.f;
+    double real(int i) {
+        if (bad) return 0.0;
         const double v = PyFloat_AsDouble(a[i]);
         if (v == -1.0 && PyErr_Occurred()) bad = true;
-        return (float)v;
+        return v;
     }
+    float number(int i) { return (float)real(i); }
     int truth(int i) {
         if (bad) return 0;
         const int v = PyObject_IsTrue(a[i]);
@@ -316,6 +319,52 @@ PyObject* linear_distill_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs)
     RUN(CALL(DISTILL_BWD, mhclite_linear_distill_bwd, x.c->h, T, V, e.K, h, W, e.ids, e.z, e.f32, scale, tau, lse, logp, dloss, dh, dW, address(ws), bytes, st))
 }
 
+// nll, nll_old, nll_ref, target, starts, adv, token_adv, clip_low, clip_high, kl_weight, mean, loss, stats, dloss, dnll
+PyObject* policy_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    TAKE(16)
+    (void)C;
+    const int64_t T = x.rows(0, "nll"), S = x.rows(11, "loss");
+    const float *nll = x.f32(0, "nll", {T}), *old = x.f32(1, "nll_old", {T}), *ref = x.none(2) ? nullptr : x.f32(2, "nll_ref", {T});
+    const int64_t *target = x.i64(3, "target", {T}), *starts = x.i64(4, "starts", {S + 1});
+    const int each = x.truth(6);
+    const float* adv = x.f32(5, "adv", {each ? T : S});
+    const double low = x.real(7), high = x.real(8), weight = x.real(9);
+    const int mean = x.truth(10);
+    float *loss = x.f32(11, "loss", {S}), *stats = x.f32(12, "stats", {S, 3});
+    const float* dloss = x.none(13) ? nullptr : x.f32(13, "dloss", {S});
+    float* dnll = x.none(14) ? nullptr : x.f32(14, "dnll", {T});
+    if (x.bad) return nullptr;
+    if (x.none(13) != x.none(14)) { PyErr_SetString(PyExc_ValueError, "dloss and dnll are given both or neither"); return nullptr; }
+    Memo& m = x.c->policy;
+    if (m.T != T || m.V != S) m = {T, S, CALL(POLICY_BYTES, mhclite_policy_scratch_bytes, T, S)};
+    const size_t bytes = m.bytes;
+    const at::Tensor ws = x.scratch(bytes);
+    RUN(CALL(POLICY, mhclite_policy_loss, x.c->h, T, S, nll, old, ref, target, starts, adv, each, low, high, weight, mean, dloss, loss, stats, dnll,
+             address(ws), bytes, st))
+}
+
+// nll, nll_ref, target, starts, beta, margin, smoothing, mean, loss, reward, dloss, dnll
+PyObject* preference_loss(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+    TAKE(13)
+    (void)C;
+    const int64_t T = x.rows(0, "nll"), P = x.rows(8, "loss");
+    const float *nll = x.f32(0, "nll", {T}), *ref = x.none(1) ? nullptr : x.f32(1, "nll_ref", {T});
+    const int64_t *target = x.i64(2, "target", {T}), *starts = x.i64(3, "starts", {2 * P + 1});
+    const double beta = x.real(4), margin = x.real(5), smoothing = x.real(6);
+    const int mean = x.truth(7);
+    float *loss = x.f32(8, "loss", {P}), *reward = x.f32(9, "reward", {P, 2});
+    const float* dloss = x.none(10) ? nullptr : x.f32(10, "dloss", {P});
+    float* dnll = x.none(11) ? nullptr : x.f32(11, "dnll", {T});
+    if (x.bad) return nullptr;
+    if (x.none(10) != x.none(11)) { PyErr_SetString(PyExc_ValueError, "dloss and dnll are given both or neither"); return nullptr; }
+    Memo& m = x.c->preference;
+    if (m.T != T || m.V != P) m = {T, P, CALL(PREFERENCE_BYTES, mhclite_preference_scratch_bytes, T, P)};
+    const size_t bytes = m.bytes;
+    const at::Tensor ws = x.scratch(bytes);
+    RUN(CALL(PREFERENCE, mhclite_preference_loss, x.c->h, T, P, nll, ref, target, starts, beta, margin, smoothing, mean, dloss, loss, reward, dnll,
+             address(ws), bytes, st))
+}
+
 // bind({name: address}): where the loaded library has the entry points.
 PyObject* bind(PyObject*, PyObject* table) {
     for (Entry& e : entries) {
@@ -332,7 +381,7 @@ PyObject* make(PyObject*, PyObject* args) {
     unsigned long long h;
     int device, n, C;
     if (!PyArg_ParseTuple(args, "Kiii", &h, &device, &n, &C)) return nullptr;
-    Context* c = new (std::nothrow) Context{reinterpret_cast<mhclite_ctx*>(h), device, n, C, {}, {}, {}, {}};
+    Context* c = new (std::nothrow) Context{reinterpret_cast<mhclite_ctx*>(h), device, n, C, {}, {}, {}, {}, {}, {}};
     if (!c) return PyErr_NoMemory();
     return PyCapsule_New(c, kCapsule, [](PyObject* o) { delete static_cast<Context*>(PyCapsule_GetPointer(o, kCapsule)); });
 }
@@ -340,6 +389,7 @@ PyObject* make(PyObject*, PyObject* args) {
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(embed_fwd), METHOD(embed_bwd), METHOD(block_in_fwd), METHOD(block_in_bwd), METHOD(block_out_fwd),
                          METHOD(block_out_bwd), METHOD(dropout), METHOD(linear_ce_fwd), METHOD(linear_ce_bwd), METHOD(linear_distill_fwd), METHOD(linear_distill_bwd),
+                         METHOD(policy_loss), METHOD(preference_loss),
                          {"bind", bind, METH_O, nullptr}, {"make", make, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,4 +1,6 @@
 // C ABI of the operators around the stack: argument checks, scratch planning and kernel sequencing.
+#include <math.h>
+
 #include "api_checks.cuh"
 #include "common.cuh"
 #include "kernels.h"
@@ -274,6 +276,83 @@ int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, int K, co
                                    (cudaStream_t)stream))
         return fail(ctx, MHCLITE_ERR_CUDA, "linear_distill_bwd: building a tensor map failed");
     MHCL_LAUNCH_CHECK(ctx, "linear_distill_bwd");
+    return MHCLITE_OK;
+}
+
+constexpr int64_t kMaxSequences = (int64_t)1 << 30;            // their number stays below it
+
+size_t mhclite_policy_scratch_bytes(int64_t T, int64_t S) {
+    if (T < 0 || T >= kMaxTokens || S < 0 || S >= kMaxSequences) return 0;
+    return seq_scratch_bytes(T, S);
+}
+size_t mhclite_preference_scratch_bytes(int64_t T, int64_t P) { return P < 0 || P >= kMaxSequences / 2 ? 0 : mhclite_policy_scratch_bytes(T, 2 * P); }
+
+// What both losses check beside their own arguments.
+static int check_sequences(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll, const int64_t* target, const int64_t* starts,
+                           const float* dloss, const float* loss, const float* table, const float* dnll) {
+    if (T >= kMaxTokens) return fail(ctx, MHCLITE_ERR_BAD_ARG, "T must be below 2^31 - 256");
+    if (S < 0 || S >= kMaxSequences) return fail(ctx, MHCLITE_ERR_BAD_ARG, "the number of sequences must be in [0, 2^30)");
+    if (S > 0) {
+        MHCL_PTR8(ctx, starts); MHCL_PTR(ctx, loss); MHCL_PTR(ctx, table);
+        MHCL_NO_ALIAS(ctx, loss, table);
+        if (T > 0) { MHCL_PTR(ctx, nll); MHCL_PTR8(ctx, target); }
+    }
+    if (T > 0 && S > 0 && !dloss != !dnll) return fail(ctx, MHCLITE_ERR_BAD_ARG, "dloss and dnll are given both or neither");
+    MHCL_OPT_PTR(ctx, dloss); MHCL_OPT_PTR(ctx, dnll);
+    if (dnll) {
+        MHCL_NO_ALIAS(ctx, dnll, nll); MHCL_NO_ALIAS(ctx, dnll, dloss); MHCL_NO_ALIAS(ctx, dnll, loss); MHCL_NO_ALIAS(ctx, dnll, table);
+    }
+    return MHCLITE_OK;
+}
+// Without a sequence the gradient is 0.
+static int no_sequences(mhclite_ctx* ctx, int64_t T, float* dnll, void* stream) {
+    if (T == 0 || !dnll) return MHCLITE_OK;
+    MHCL_DEVICE(ctx);
+    return check_cuda(ctx, cudaMemsetAsync(dnll, 0, (size_t)T * 4, (cudaStream_t)stream), "zero dnll");
+}
+
+int mhclite_policy_loss(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll, const float* nll_old, const float* nll_ref,
+                        const int64_t* target, const int64_t* starts, const float* adv, int token_adv, double clip_low, double clip_high,
+                        double kl_weight, int mean, const float* dloss, float* loss, float* stats, float* dnll, void* scratch,
+                        size_t scratch_bytes, void* stream) {
+    MHCL_REQUIRE_CTX(ctx); MHCL_REQUIRE_T(ctx, T);
+    if (!(clip_low >= 0 && clip_low <= 1)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "clip_low must be in [0, 1]");
+    if (!(clip_high >= 0)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "clip_high must be >= 0");
+    if (!(fabs(kl_weight) <= 3e38)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "kl_weight must be finite");
+    int rc = check_sequences(ctx, T, S, nll, target, starts, dloss, loss, stats, dnll);
+    if (rc) return rc;
+    if (S == 0) return no_sequences(ctx, T, dnll, stream);
+    if (T > 0) {
+        MHCL_PTR(ctx, nll_old); MHCL_OPT_PTR(ctx, nll_ref); MHCL_PTR(ctx, adv);
+        if (dnll) { MHCL_NO_ALIAS(ctx, dnll, nll_old); MHCL_NO_ALIAS(ctx, dnll, nll_ref); MHCL_NO_ALIAS(ctx, dnll, adv); }
+    }
+    if ((rc = check_scratch(ctx, scratch, scratch_bytes, seq_scratch_bytes(T, S)))) return rc;
+    MHCL_DEVICE(ctx);
+    launch_policy_loss(ctx, T, S, nll, nll_old, nll_ref, target, starts, adv, token_adv, clip_low, clip_high, kl_weight, mean, dloss, loss, stats,
+                       T > 0 ? dnll : nullptr, scratch, (cudaStream_t)stream);
+    MHCL_LAUNCH_CHECK(ctx, "policy_loss");
+    return MHCLITE_OK;
+}
+
+int mhclite_preference_loss(mhclite_ctx* ctx, int64_t T, int64_t P, const float* nll, const float* nll_ref, const int64_t* target,
+                            const int64_t* starts, double beta, double margin, double smoothing, int mean, const float* dloss, float* loss,
+                            float* reward, float* dnll, void* scratch, size_t scratch_bytes, void* stream) {
+    MHCL_REQUIRE_CTX(ctx); MHCL_REQUIRE_T(ctx, T);
+    if (!(fabs(beta) <= 3e38) || !(fabs(margin) <= 3e38)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "beta and margin must be finite");
+    if (!(smoothing >= 0 && smoothing <= 1)) return fail(ctx, MHCLITE_ERR_BAD_ARG, "smoothing must be in [0, 1]");
+    if (P < 0 || P >= kMaxSequences / 2) return fail(ctx, MHCLITE_ERR_BAD_ARG, "the number of pairs must be in [0, 2^29)");
+    int rc = check_sequences(ctx, T, 2 * P, nll, target, starts, dloss, loss, reward, dnll);
+    if (rc) return rc;
+    if (P == 0) return no_sequences(ctx, T, dnll, stream);
+    if (T > 0) {
+        MHCL_OPT_PTR(ctx, nll_ref);
+        if (dnll) MHCL_NO_ALIAS(ctx, dnll, nll_ref);
+    }
+    if ((rc = check_scratch(ctx, scratch, scratch_bytes, seq_scratch_bytes(T, 2 * P)))) return rc;
+    MHCL_DEVICE(ctx);
+    launch_preference_loss(ctx, T, P, nll, nll_ref, target, starts, beta, margin, smoothing, mean, dloss, loss, reward, T > 0 ? dnll : nullptr,
+                           scratch, (cudaStream_t)stream);
+    MHCL_LAUNCH_CHECK(ctx, "preference_loss");
     return MHCLITE_OK;
 }
 

@@ -208,22 +208,69 @@ class ModelEnds:
         self.dE, self.dw, self.dW = f32(*E.shape), f32(C), bf(*W.shape)
 
 
-def model_fwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, sublayer, eps=1e-6, fuse_layers=True):
+class Teacher:
+    """A teacher's top entries of each token: ids [T,K] int64 (negative: absent), logits [T,K] fp32 or bf16, the temperature
+    of both distributions, and the student's log probabilities at the entries, which the forward leaves."""
+
+    def __init__(self, ids: torch.Tensor, logits: torch.Tensor, temperature: float = 1.0):
+        self.ids, self.logits, self.temperature = ids, logits, float(temperature)
+        self.logp = torch.empty(ids.shape, dtype=torch.float32, device=ids.device)
+
+
+class Answers:
+    """S sequences (with `pairs`: S / 2 pairs of a chosen and a rejected one) over the T tokens of a step: where they begin
+    (starts [S+1] int64), their losses and what goes with them, and the gradient that model_bwd takes as dloss."""
+
+    def __init__(self, starts: torch.Tensor, T: int, pairs: bool = False):
+        f32 = lambda *s: torch.empty(*s, dtype=torch.float32, device=starts.device)
+        S = starts.numel() - 1
+        self.starts, self.pairs, self.dnll = starts, pairs, f32(T)
+        self.loss = f32(S // 2 if pairs else S)
+        self.reward, self.stats = (f32(S // 2, 2), None) if pairs else (None, f32(S, 3))
+
+
+def policy_loss(ctx: MhcLite, A: Answers, nll, nll_old, nll_ref, target, adv, dloss, token_adv=False, clip_low=0.2, clip_high=0.2,
+                kl_weight=0.0, mean=True):
+    """Clipped policy loss of each sequence from the token losses of model_fwd (nll), of the policy that sampled them
+    (nll_old) and of the reference (nll_ref, None: no KL term).  Leaves A.loss, A.stats and, with dloss [S], A.dnll."""
+    ctx.policy_loss(nll, nll_old, nll_ref, target, A.starts, adv, token_adv, clip_low, clip_high, kl_weight, mean, A.loss, A.stats,
+                    dloss, None if dloss is None else A.dnll)
+    return A.loss
+
+
+def preference_loss(ctx: MhcLite, A: Answers, nll, nll_ref, target, dloss, beta=0.1, margin=0.0, smoothing=0.0, mean=False):
+    """Preference loss of each pair from the token losses of model_fwd (nll) and of the reference (nll_ref, or None).  Leaves
+    A.loss, A.reward and, with dloss [S / 2], A.dnll."""
+    ctx.preference_loss(nll, nll_ref, target, A.starts, beta, margin, smoothing, mean, A.loss, A.reward, dloss,
+                        None if dloss is None else A.dnll)
+    return A.loss
+
+
+def model_fwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, sublayer, eps=1e-6, fuse_layers=True, teacher: Teacher | None = None):
     """Token ids [T] to the loss of each token [T] (0 where target is negative): lookup into the streams, the stack, the
-    mean of the streams, the last norm, cross entropy.  Everything the backward needs stays in M, Bs and the sublayer's
-    buffers."""
+    mean of the streams, the last norm, cross entropy; with a teacher the divergence from its entries instead (target is not
+    used).  Everything the backward needs stays in M, Bs, the teacher and the sublayer's buffers."""
     ctx.embed_fwd(ids, M.E, M.embed_scale, M.x0)
     M.x_top = stack_fwd(ctx, Ps, Bs, M.x0, sublayer, eps, fuse_layers)
     ctx.premix_fwd(M.x_top, M.mix, M.top)
     ctx.block_in_fwd(M.top, M.w, eps, M.h, M.r)
-    ctx.linear_ce_fwd(M.h, M.W, target, M.logit_scale, M.loss, M.lse)
+    if teacher is None:
+        ctx.linear_ce_fwd(M.h, M.W, target, M.logit_scale, M.loss, M.lse)
+    else:
+        ctx.linear_distill_fwd(M.h, M.W, teacher.ids, teacher.logits, M.logit_scale, teacher.temperature, M.loss, M.lse, teacher.logp)
     return M.loss
 
 
-def model_bwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, dloss, sublayer_bwd, eps=1e-6, accumulate_params=False):
-    """Backward of model_fwd from dloss [T] fp32: M.dW, M.dw, M.dE, and the layers' gradients in Bs.  accumulate_params
-    concerns the fp32 gradients M.dw and M.dE; M.dW is overwritten, and the layers' gradients are as stack_bwd leaves them."""
-    ctx.linear_ce_bwd(M.h, M.W, target, M.logit_scale, M.lse, dloss, M.dh, M.dW)
+def model_bwd(ctx: MhcLite, M: ModelEnds, Ps, Bs, ids, target, dloss, sublayer_bwd, eps=1e-6, accumulate_params=False,
+              teacher: Teacher | None = None):
+    """Backward of model_fwd from dloss [T] fp32 (of a loss of sequences: Answers.dnll): M.dW, M.dw, M.dE, and the layers'
+    gradients in Bs.  accumulate_params concerns the fp32 gradients M.dw and M.dE; M.dW is overwritten, and the layers'
+    gradients are as stack_bwd leaves them."""
+    if teacher is None:
+        ctx.linear_ce_bwd(M.h, M.W, target, M.logit_scale, M.lse, dloss, M.dh, M.dW)
+    else:
+        ctx.linear_distill_bwd(M.h, M.W, teacher.ids, teacher.logits, M.logit_scale, teacher.temperature, M.lse, teacher.logp, dloss,
+                               M.dh, M.dW)
     ctx.block_in_bwd(M.top, M.w, M.r, M.dh, M.dtop, M.dw, accumulate_params)
     ctx.premix_bwd(M.x_top, M.mix, M.dtop, M.dmix, M.dx, False)
     g0 = stack_bwd(ctx, Ps, Bs, M.dx, sublayer_bwd, eps)

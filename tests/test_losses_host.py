@@ -24,12 +24,23 @@ def test_scratch_bytes_of_distillation():
     assert d(2048, 16384, 100000, 64, 1) - c(2048, 16384, 100000, 1) < 32 << 20
 
 
+def test_scratch_bytes_of_sequences():
+    lib = binding.load()
+    p, q = lib.mhclite_policy_scratch_bytes, lib.mhclite_preference_scratch_bytes
+    assert p(1, 1) > 0 and p(0, 3) > 0 and q(1000, 4) == p(1000, 8) > 0
+    for bad in ((-1, 3), (10, -1), (2**31, 3), (2**62, 3), (10, 2**30), (10, 2**62)):
+        assert p(*bad) == 0 and q(*bad) == 0, bad
+    assert q(10, 2**29) == 0 and p(2**31 - 257, 2**30 - 1) > 0
+    # a bit a token and 28 bytes a sequence; the pieces' number has a bound
+    assert p(2**24, 1000) < (2**24 // 8) + 64 * 1000 + (1 << 20)
+
+
 def test_null_context_is_refused():
     lib = binding.load()
-    names = [n for n in binding.SIGNATURES if n.startswith("mhclite_linear_distill") and not n.endswith("_bytes")]
-    assert len(names) == 2
+    names = [n for n in binding.SIGNATURES if n.startswith(("mhclite_linear_distill", "mhclite_policy", "mhclite_preference")) and not n.endswith("_bytes")]
+    assert len(names) == 4
     for name in names:
-        zero = [0.0 if a is ctypes.c_float else None if a is ctypes.c_void_p else 0 for a in binding.SIGNATURES[name][1]]
+        zero = [0.0 if a in (ctypes.c_float, ctypes.c_double) else None if a is ctypes.c_void_p else 0 for a in binding.SIGNATURES[name][1]]
         assert getattr(lib, name)(*zero) == binding.ERR_BAD_ARG, name
 
 
@@ -40,8 +51,11 @@ def test_arguments_are_refused_before_the_library_sees_them():
     out = (f32(3), f32(3), f32(3, 5))
     value = [(m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3), f32(3, 5), 1.0, 1.0, *out),             # one axis
              (m.linear_distill_fwd, bf(3, 64), bf(9, 63), i64(3, 5), f32(3, 5), 1.0, 1.0, *out),
-             (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out)]           # not on the device
+             (m.linear_distill_fwd, bf(3, 64), bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out),           # not on the device
+             (m.policy_loss, f32(9), f32(9), None, i64(9), i64(3), f32(2), False, 0.2, 0.2, 0.0, True, f32(2), f32(2, 3), None, None),
+             (m.preference_loss, f32(9), None, i64(9), i64(3), 0.1, 0.0, 0.0, True, f32(1), f32(1, 2), None, None)]
     kind = [(m.linear_distill_fwd, None, bf(9, 64), i64(3, 5), f32(3, 5), 1.0, 1.0, *out), (m.linear_distill_bwd, bf(3, 64)),
+            (m.policy_loss, f32(9)), (m.preference_loss, 3, None, i64(9), i64(3), 0.1, 0.0, 0.0, True, f32(1), f32(1, 2), None, None),
             (m.linear_distill_fwd, bf(3, 64), 7, i64(3, 5), f32(3, 5), 1.0, 1.0, *out)]
     for error, calls in ((ValueError, value), (TypeError, kind)):
         for f, *args in calls:
