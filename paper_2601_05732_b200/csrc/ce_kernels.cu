@@ -34,7 +34,8 @@ constexpr int kCeEpiWarps = 8;                         // two per tensor-memory 
 constexpr int kCeThreads = 64 + 32 * kCeEpiWarps;      // warp 0: TMA, warp 1: MMA, the others: epilogue
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-enum CeMode { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3 };
+// CE_PICK and CE_PATCH: CE_STATS and CE_GRAD of rows that have a teacher's entries (distill.cuh) instead of a target
+enum CeMode { CE_STATS = 0, CE_GRAD = 1, CE_DH = 2, CE_DW = 3, CE_PICK = 4, CE_PATCH = 5 };
 
 struct CeArgs {
     const int* live;            // number of rows with a target
@@ -50,8 +51,13 @@ struct CeArgs {
     // CE_STATS
     float2* part;               // [2 n_tiles][Tpad] (maximum, sum) in base 2 of 128 columns each
     float* tlogit;              // [Tpad] <h_t, W_target>, before the scale
-    const int64_t* target;      // null: the rows have none (distillation)
+    const int64_t* target;
     int Tpad;
+    // CE_PICK, CE_PATCH
+    const uint2* entries;       // [T][K + 1] by rising id (ds_sort_k), the last of each row behind all ids
+    const uint16_t* first_entry;   // [T][blocks] the first entry from each 128 columns of the vocabulary on
+    int K, blocks;
+    float* dots;                // [T][K] <h_t, W_id>
     // CE_GRAD
     const float* lse;
     const float* dloss;
@@ -73,7 +79,7 @@ struct CeArgs {
 // that a store covers whole 128-byte lines: a thread a row writes 32 bytes here and there, which held dW of few tokens (all
 // epilogue) at 2.7 TB/s.
 constexpr int kCeStagePitch = 144;                     // bytes a row: 128 and 16, so that neither side meets a bank twice
-__host__ __device__ constexpr bool ce_staged(int mode) { return mode == CE_GRAD || mode == CE_DW; }
+__host__ __device__ constexpr bool ce_staged(int mode) { return mode == CE_GRAD || mode == CE_PATCH || mode == CE_DW; }
 __host__ __device__ constexpr int ce_stages(int mode) { return ce_staged(mode) ? kCeStages - 1 : kCeStages; }
 __host__ __device__ constexpr int ce_smem(int mode) {
     return ce_stages(mode) * kCeStage + (ce_staged(mode) ? kCeEpiWarps * 32 * kCeStagePitch : 0) + 256 + 1024;
@@ -188,6 +194,7 @@ template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCeThreads, 1)
 ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb, const CeArgs a) {
     constexpr bool A_MN = MODE == CE_DW, B_MN = MODE == CE_DH || MODE == CE_DW;
+    constexpr bool ENTRIES = MODE == CE_PICK || MODE == CE_PATCH, STATS = MODE == CE_STATS || MODE == CE_PICK;
     constexpr int STAGES = ce_stages(MODE);
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -290,21 +297,42 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
         }
     } else {
         const int quad = warp & 3, half = (warp - 2) >> 2, row = (int)rank * kCeHalf + quad * 32 + lane;
-        const float ref = MODE == CE_STATS ? 1.f : ce_ref(a.ref, a.refs);
+        const float ref = STATS ? 1.f : ce_ref(a.ref, a.refs);
         const uint32_t staging = smem_u32(smem + STAGES * kCeStage + 256) + (warp - 2) * (32 * kCeStagePitch);
         bool ok = true;
         int j = 0;
         for (int i = pair; i < tiles && ok; i += pairs, ++j) {
             const int buf = j & 1;
-            ok = ce_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            tc_fence_after();
             const int split = MODE == CE_DH ? i / per : 0;
             int m, n;
             ce_tile(i - split * per, a.group, mt, nt, m, n);
             const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
             const int n0 = n * kCeN + half * kCeHalf;           // this warp's 128 columns
+            // the row's next entries from this warp's first column on, fetched while the products run
+            const uint2* entry = nullptr;
+            const uint2* last = nullptr;
+            uint2 next[4];
+            if (ENTRIES) {
+                const uint2 none = make_uint2(0x7FFFFFFFu, 0);
+                next[0] = next[1] = next[2] = next[3] = none;
+                if (r < live) {
+                    const int64_t token = a.rows[r];
+                    last = a.entries + token * (a.K + 1) + a.K;
+                    entry = last - a.K + a.first_entry[token * a.blocks + (a.v0 + n0) / kCeHalf];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) next[e] = entry + e <= last ? entry[e] : none;
+                    entry += 4;
+                }
+            }
+            auto pop = [&] {
+                next[0] = next[1]; next[1] = next[2]; next[2] = next[3];
+                next[3] = entry <= last ? *entry : make_uint2(0x7FFFFFFFu, 0);
+                ++entry;
+            };
+            ok = ce_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
             const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + buf * kCeN + half * kCeHalf;
             // once the tile has been read from tensor memory, before what was read is written out
             auto hand_back = [&] {
@@ -312,20 +340,31 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(leader_addr(smem_u32(&ctl->acc_empty[buf])));
             };
-            if (MODE == CE_STATS || MODE == CE_GRAD) {
+            if (STATS || MODE == CE_GRAD || MODE == CE_PATCH) {
                 const bool in = r < live;
                 const int t = in ? a.rows[r] : 0;
-                const int tgt = in && a.target ? (int)(a.target[t] - a.v0) - n0 : -1;        // the target's column among them
+                const int tgt = !ENTRIES && in ? (int)(a.target[t] - a.v0) - n0 : -1;        // the target's column among them
                 const int cols = (int)(a.V - a.v0) - n0;                             // of the vocabulary (the rest is padding)
                 const float k2 = a.scale * kLog2e;
-                if (MODE == CE_STATS) {
+                if (STATS) {
                     float mx = -INFINITY, sum = 0.f;
+                    // the entries' logits, column by column (at most the 128 there are): one column for all rows that have it
+                    if (MODE == CE_PICK) {
+                        for (;;) {
+                            __syncwarp();
+                            const uint32_t c = __reduce_min_sync(0xffffffffu, next[0].x - (uint32_t)n0);
+                            if (c >= (uint32_t)kCeHalf) break;
+                            const float v = tc_ld1(acc + c);
+                            for (; next[0].x - (uint32_t)n0 == c; pop()) a.dots[(int64_t)t * a.K + next[0].y] = v;
+                        }
+                        __syncwarp();
+                    }
 #pragma unroll 1
                     for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                         if (c0 >= cols) break;
                         float v[32];
                         tc_ld32(acc + c0, v);
-                        if (__any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
+                        if (!ENTRIES && __any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
                                 if (tgt == c0 + e) a.tlogit[r] = v[e];
@@ -392,6 +431,11 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                             for (int e = 0; e < 32; e += 8) sts128(staging + lane * kCeStagePitch + (h + e) * 2, pack8(v + e));
                         }
                         if (c0 + 64 == kCeHalf) hand_back();
+                        // where the teacher has a share: formed with the logit that the forward left, not here
+                        if (MODE == CE_PATCH) {
+                            for (uint32_t at; (at = next[0].x - (uint32_t)(a.v0 + n0 + c0)) < 64u; pop())
+                                sts16(staging + lane * kCeStagePitch + at * 2, __bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(next[0].y) * f)));
+                        }
                         __syncwarp();
 #pragma unroll
                         for (int i8 = 0; i8 < 8; ++i8) {
@@ -478,7 +522,7 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
     __syncthreads();
     if (ctl->abort[0]) {
         for (int i = 0; i < 64; ++i) __nanosleep(2000);        // copies in flight land before the memory is given up
-        if (tid == 0) report_wait(a.status, MHCLITE_OP_LINEAR_CE + 100 * MODE, ctl->abort[1], (int)blockIdx.x, ctl->abort[2]);
+        if (tid == 0) report_wait(a.status, (ENTRIES ? MHCLITE_OP_LINEAR_DISTILL : MHCLITE_OP_LINEAR_CE) + 100 * MODE, ctl->abort[1], (int)blockIdx.x, ctl->abort[2]);
     }
     __syncthreads();
     pair_sync();                                               // the other CTA's products may read this one's memory until here
@@ -917,17 +961,17 @@ static int launch_ce_small(const mhclite_ctx* c, const SmallPlan& q, int64_t T, 
     launch_after(k, dim3(grid), dim3(kSmThreads), q.smem, s, (int)T, V, c->C, q.wk_log, (const uint4*)h, (const uint4*)W, target, scale, part, tlogit);
     return grid;
 }
-// The pairs of the rows that `listed` (the targets, or the like) has 0 to V - 1 for; what is picked on the way is the epilogue's.
-static bool launch_ce_stats(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const void* h, const void* W, const int64_t* listed,
-                            const int64_t* target, float scale, float* loss, float* lse, cudaStream_t s) {
+// The pairs of the rows that `listed` (the targets, or the like) has 0 to V - 1 for; `a` brings the mode's own arguments.
+template <int MODE>
+static bool launch_ce_stats(const mhclite_ctx* c, const CePlan& p, CeArgs a, int64_t T, int64_t V, const void* h, const void* W,
+                            const int64_t* listed, float scale, float* loss, float* lse, cudaStream_t s) {
     CUtensorMap mh, mw;
     if (!map_k(&mh, p.hl, p.Tpad, c->C, c->C, p.a_box) || !map_k(&mw, W, V, c->C, c->C, kCeHalf)) return false;
     launch_ce_rows(c, p, T, V, listed, h, loss, lse, nullptr, nullptr, s);
-    CeArgs a = {};
     a.live = p.live; a.rows = p.rows; a.V = V; a.C = c->C; a.v0 = 0; a.vn = (int)V;
     a.m_tiles = p.Tpad / kCeM; a.n_tiles = p.n_tiles; a.scale = scale;
-    a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.target = target; a.Tpad = p.Tpad; a.status = c->op_status;
-    launch_ce_gemm<CE_STATS>(c, mh, mw, a, s);
+    a.a_box = p.a_box; a.part = p.part; a.tlogit = p.tlogit; a.Tpad = p.Tpad; a.status = c->op_status;
+    launch_ce_gemm<MODE>(c, mh, mw, a, s);
     c->launches += 1;                                          // the join that follows
     return true;
 }
@@ -943,23 +987,24 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
         return true;
     }
     const CePlan p = plan_ce(T, V, c->C, 0, scratch);
-    if (!launch_ce_stats(c, p, T, V, h, W, target, target, scale, loss, lse, s)) return false;
+    CeArgs a = {};
+    a.target = target;
+    if (!launch_ce_stats<CE_STATS>(c, p, a, T, V, h, W, target, scale, loss, lse, s)) return false;
     launch_after(ce_join_k, dim3((unsigned)((T + 31) / 32)), dim3(1024), 0, s, p.live, p.rows, 2 * p.n_tiles, p.Tpad, p.part, p.tlogit, scale * kLog2e, loss, lse);
     return true;
 }
 
-// dh and dW of the rows that `listed` has 0 to V - 1 for; `fix(v0, vn)` is called between a piece's G and its products.
-template <typename F>
-static bool launch_ce_grads(const mhclite_ctx* c, const CePlan& p, int64_t T, int64_t V, const void* h, const void* W, const int64_t* listed,
-                            const int64_t* target, float scale, const float* lse, const float* dloss, void* dh, void* dW, cudaStream_t s, F fix) {
+// dh and dW of the rows that `listed` has 0 to V - 1 for; `a` brings the mode's own arguments.
+template <int MODE>
+static bool launch_ce_grads(const mhclite_ctx* c, const CePlan& p, CeArgs a, int64_t T, int64_t V, const void* h, const void* W,
+                            const int64_t* listed, float scale, const float* lse, const float* dloss, void* dh, void* dW, cudaStream_t s) {
     const int C = c->C;
     CUtensorMap mh, mw, mg, mwn, mgt, mhn;
     if (!map_k(&mh, p.hl, p.Tpad, C, C, p.a_box) || !map_k(&mw, W, V, C, C, kCeHalf) || !map_k(&mg, p.G, p.Tpad, p.piece, p.piece, p.a_box) ||
         !map_mn(&mwn, W, V, C, C) || !map_mn(&mgt, p.G, p.Tpad, p.piece, p.piece) || !map_mn(&mhn, p.hl, p.Tpad, C, C))
         return false;
     launch_ce_rows(c, p, T, V, listed, h, nullptr, nullptr, dh, dloss, s);
-    CeArgs a = {};
-    a.live = p.live; a.rows = p.rows; a.V = V; a.C = C; a.scale = scale; a.target = target; a.Tpad = p.Tpad;
+    a.live = p.live; a.rows = p.rows; a.V = V; a.C = C; a.scale = scale; a.Tpad = p.Tpad;
     a.lse = lse; a.dloss = dloss; a.G = p.G; a.pitch = p.piece; a.dh_acc = p.dh_acc; a.dh = (__nv_bfloat16*)dh;
     a.wide = C % 16 == 0 && ((uintptr_t)dh & 31) == 0;
     a.dW = (__nv_bfloat16*)dW; a.ref = p.ref; a.refs = p.row_blocks; a.a_box = p.a_box; a.splits = p.splits; a.status = c->op_status;
@@ -968,8 +1013,7 @@ static bool launch_ce_grads(const mhclite_ctx* c, const CePlan& p, int64_t T, in
         a.vn = (int)(V - a.v0 < p.piece ? V - a.v0 : p.piece);
         a.first = i == 0; a.last = i + 1 == p.pieces;
         a.m_tiles = p.Tpad / kCeM; a.n_tiles = (a.vn + kCeN - 1) / kCeN;
-        launch_ce_gemm<CE_GRAD>(c, mh, mw, a, s);
-        fix(a.v0, a.vn);
+        launch_ce_gemm<MODE>(c, mh, mw, a, s);
         a.m_tiles = (a.vn + kCeM - 1) / kCeM; a.n_tiles = (C + kCeN - 1) / kCeN;
         launch_ce_gemm<CE_DW>(c, mgt, mhn, a, s);
         a.m_tiles = p.Tpad / kCeM;
@@ -986,7 +1030,9 @@ static bool launch_ce_grads(const mhclite_ctx* c, const CePlan& p, int64_t T, in
 
 bool launch_linear_ce_bwd(const mhclite_ctx* c, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target, float scale,
                           const float* lse, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s) {
-    return launch_ce_grads(c, plan_ce(T, V, c->C, 1, scratch), T, V, h, W, target, target, scale, lse, dloss, dh, dW, s, [](int, int) {});
+    CeArgs a = {};
+    a.target = target;
+    return launch_ce_grads<CE_GRAD>(c, plan_ce(T, V, c->C, 1, scratch), a, T, V, h, W, target, scale, lse, dloss, dh, dW, s);
 }
 
 }  // namespace mhcl

@@ -6,74 +6,172 @@
 // or of weight 0 is left out before the products, as a row without a target is.
 #pragma once
 
+#include <type_traits>
+
 namespace mhcl {
 
-constexpr int kDsPer = kDistillMaxK / 32;                  // entries of a row that a lane holds
-
-// A row's entries over the lanes of a warp: entry i * 32 + lane in place i.
+// A row's entries over the lanes of a warp, PER (1, 2, 4 or 8) each: entry i * 32 + lane in place i.
+template <int PER>
 struct DsRow {
-    int id[kDsPer];             // -1 where absent
-    float z[kDsPer];
+    int id[PER];                // -1 where absent
+    float z[PER];
     bool live;                  // some entry has weight (or is NaN)
 };
-template <typename Z> __device__ __forceinline__ float ds_float(Z v);
-template <> __device__ __forceinline__ float ds_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float ds_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-template <typename Z>
-__device__ __forceinline__ DsRow ds_load(int64_t t, int K, int64_t V, const int64_t* ids, const Z* z, int* status) {
-    DsRow r;
-    bool any = false;
+template <int PER>
+__device__ __forceinline__ DsRow<PER> ds_load(int64_t t, int K, int64_t V, const int64_t* ids, const void* z, int z_f32, int* status) {
+    DsRow<PER> r;
     const int lane = threadIdx.x & 31;
+    int64_t id[PER];
+    float v[PER];
 #pragma unroll
-    for (int i = 0; i < kDsPer; ++i) {
-        r.id[i] = -1;
-        r.z[i] = -INFINITY;
+    for (int i = 0; i < PER; ++i) {                                     // all loads before the first use
         const int k = i * 32 + lane;
-        if (k < K) {
-            const int64_t id = ids[t * K + k];
-            if (id >= 0 && id < V) {
-                r.id[i] = (int)id;
-                r.z[i] = ds_float(z[t * K + k]);
-                any = any || r.z[i] != -INFINITY;
-            } else if (id >= V && status) {
-                report_index(status, MHCLITE_OP_LINEAR_DISTILL, t, id);
-            }
-        }
+        id[i] = k < K ? ids[t * K + k] : -1;
+        v[i] = k >= K ? 0.f : z_f32 ? ((const float*)z)[t * K + k] : __bfloat162float(((const __nv_bfloat16*)z)[t * K + k]);
+    }
+    bool any = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const bool in = id[i] >= 0 && id[i] < V;
+        r.id[i] = in ? (int)id[i] : -1;
+        r.z[i] = in ? v[i] : -INFINITY;
+        any = any || r.z[i] != -INFINITY;
+        if (id[i] >= V && status) report_index(status, MHCLITE_OP_LINEAR_DISTILL, t, id[i]);
     }
     r.live = __any_sync(0xffffffffu, any);
     return r;
 }
 // z becomes the logarithm of the entry's weight; -inf where there is none.
-__device__ __forceinline__ void ds_weights(DsRow& r, float inv_tau) {
+template <int PER>
+__device__ __forceinline__ void ds_weights(DsRow<PER>& r, float inv_tau) {
     float top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kDsPer; ++i) top = fmaxf(top, r.z[i]);
+    for (int i = 0; i < PER; ++i) top = fmaxf(top, r.z[i]);
     top = warp_max(top);
     if (top == -INFINITY) top = 0.f;
 #pragma unroll
-    for (int i = 0; i < kDsPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         r.z[i] = (r.z[i] - top) * inv_tau;
         sum += expf(r.z[i]);
     }
     const float b = logf(warp_sum(sum));
 #pragma unroll
-    for (int i = 0; i < kDsPer; ++i) r.z[i] -= b;
+    for (int i = 0; i < PER; ++i) r.z[i] -= b;
 }
 
-// Which rows have a teacher: target 0 or -1 for ce_rows_k; logp of the others is cleared.
-template <typename Z>
-__global__ void __launch_bounds__(256) ds_live_k(int64_t T, int K, int64_t V, const int64_t* ids, const Z* z, int64_t* target, float* logp,
+// A warp's 32 PER keys by rising value, key lane * PER + i in place i of a lane: Batcher's bitonic network, exchanges between
+// lanes where the distance reaches beyond one.
+template <int PER>
+__device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int size = 2; size <= 32 * PER; size *= 2)
+#pragma unroll
+        for (int apart = size / 2; apart > 0; apart /= 2) {
+            if (apart >= PER) {
+                const int other = apart / PER;
+                // within ascending runs the lower lane keeps the smaller key
+                const bool small = ((lane & other) == 0) == ((lane * PER & size) == 0);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const uint64_t y = __shfl_xor_sync(0xffffffffu, (unsigned long long)key[i], other);
+                    key[i] = (y < key[i]) == small ? y : key[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    if (i & apart) continue;
+                    const bool up = size < PER ? (i & size) == 0 : (lane * PER & size) == 0;
+                    const uint64_t x = key[i], y = key[i | apart];
+                    const bool swap = (y < x) == up;
+                    key[i] = swap ? y : x;
+                    key[i | apart] = swap ? x : y;
+                }
+            }
+        }
+}
+
+// A row's entries by rising id, for the tiles' epilogues: (id, k) for the forward, (id, bits of exp(logp) - the id's weights) for
+// the backward; absent ones and one more behind all ids.  With them, for every 128 columns, which entry is the first from there
+// on (`first`), so that an epilogue needs no search.  A warp a row.  Rows with a teacher get 0 in `target`, which ce_rows_k lists
+// them by, others -1 and, in the forward, logp 0.
+template <int PER, bool GRAD>
+__global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, const int64_t* ids, const void* z, int z_f32, float inv_tau,
+                                                 const float* logp_in, uint2* entries, uint16_t* first, int blocks, int64_t* target, float* logp,
                                                  int* status) {
+    __shared__ int id_s[8][32 * PER];
+    __shared__ float p_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1], w_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1];
     pdl_wait();
     pdl_launch();
-    const int lane = threadIdx.x & 31;
-    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ws = GRAD ? warp : 0;
+    const int64_t t = (int64_t)blockIdx.x * 8 + warp;
     if (t >= T) return;
-    const DsRow r = ds_load(t, K, V, ids, z, status);
+    DsRow<PER> r = ds_load<PER>(t, K, V, ids, z, z_f32, status);
     if (lane == 0) target[t] = r.live ? 0 : -1;
-    if (logp && !r.live)
-        for (int k = lane; k < K; k += 32) logp[t * K + k] = 0.f;
+    if (!r.live) {
+        if (!GRAD)
+            for (int k = lane; k < K; k += 32) logp[t * K + k] = 0.f;
+        return;
+    }
+    uint64_t key[PER];
+    if (GRAD) ds_weights(r, inv_tau);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int k = i * 32 + lane;
+        key[i] = (uint64_t)(uint32_t)(r.id[i] < 0 ? 0x7FFFFFFF : r.id[i]) << 32 | (uint32_t)k;       // as numbered where ids are equal
+        if (GRAD) p_s[ws][k] = expf(r.z[i]);
+    }
+    ds_sort(key);
+    bool twice = false;
+    const int before = __shfl_up_sync(0xffffffffu, (int)(key[PER - 1] >> 32), 1);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int id = (int)(key[i] >> 32), prior = i ? (int)(key[i ? i - 1 : 0] >> 32) : lane ? before : -1;
+        id_s[warp][lane * PER + i] = id;
+        twice = twice || (id == prior && id != 0x7FFFFFFF);
+    }
+    __syncwarp();
+    float value[PER];
+    if (GRAD) {
+        float p[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p[i] = p_s[ws][(int)(key[i] & 0xFFFFFFFFu)];
+        __syncwarp();
+        if (__any_sync(0xffffffffu, twice)) {                           // an id's entries, which lie side by side, all get their sum
+            for (int i = 0; i < PER; ++i) {
+                const int at = lane * PER + i, id = id_s[warp][at];
+                if (id == 0x7FFFFFFF) continue;
+                int from = at;
+                while (from > 0 && id_s[warp][from - 1] == id) --from;
+                float sum = 0.f;
+                for (; from < 32 * PER && id_s[warp][from] == id; ++from) sum += w_s[ws][from];
+                p_s[ws][(int)(key[i] & 0xFFFFFFFFu)] = sum;             // each entry its own place
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < PER; ++i) p[i] = p_s[ws][(int)(key[i] & 0xFFFFFFFFu)];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int k = (int)(key[i] & 0xFFFFFFFFu);
+            value[i] = (int)(key[i] >> 32) != 0x7FFFFFFF ? expf(logp_in[t * K + k]) - p[i] : 0.f;
+        }
+    }
+    uint2* out = entries + t * (K + 1);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int at = lane * PER + i;
+        if (at < K) out[at] = make_uint2((uint32_t)(key[i] >> 32), GRAD ? __float_as_uint(value[i]) : (uint32_t)key[i]);
+    }
+    if (lane == 0) out[K] = make_uint2(0x7FFFFFFFu, 0);
+    for (int b = lane; b < blocks; b += 32) {
+        int at = 0;
+#pragma unroll
+        for (int step = 16 * PER; step > 0; step /= 2)                  // how many entries lie below the block
+            if (id_s[warp][at + step - 1] < b * 128) at += step;
+        at += id_s[warp][at] < b * 128;
+        first[t * blocks + b] = (uint16_t)at;
+    }
 }
 
 // <h_t, W_id> of every present entry: a warp an entry.
@@ -101,15 +199,24 @@ __global__ void __launch_bounds__(256) ds_dot_k(int64_t entries, int K, int64_t 
 
 // Joins the (maximum, sum) pairs of 32 rows a block as ce_join_k does, then a warp a row forms loss, lse and logp.  live and
 // rows are null where every row is in the pairs (a handful of tokens).
-template <typename Z>
+template <int PER>
 __global__ void __launch_bounds__(1024) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
-                                                  const float2* part, const float* dots, const int64_t* ids, const Z* z, float k2,
+                                                  const float2* part, const float* dots, const int64_t* ids, const void* z, int z_f32, float k2,
                                                   float inv_tau, float* loss, float* lse, float* logp, int* status) {
     __shared__ float2 red[32][33];
-    __shared__ float2 joined[32];
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = live ? *live : (int)T;
     if (blockIdx.x * 32 >= n) return;
+    const int row = blockIdx.x * 32 + warp;                             // of the second half
+    DsRow<PER> e;
+    float x[PER];
+    int64_t t = 0;
+    if (row < n) {                                                      // its loads run beside the first half's
+        t = rows ? rows[row] : row;
+        e = ds_load<PER>(t, K, V, ids, z, z_f32, rows ? nullptr : status);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) x[i] = e.id[i] >= 0 ? dots[t * K + i * 32 + lane] : 0.f;
+    }
     float m = -INFINITY, s = 0.f;
     if (r < n) {
 #pragma unroll 8
@@ -122,26 +229,18 @@ __global__ void __launch_bounds__(1024) ds_join_k(int64_t T, int K, int64_t V, c
     }
     red[warp][lane] = make_float2(m, s);
     __syncthreads();
-    {                                                                   // lane: a range of tiles, warp: a row
-        const float2 p = red[lane][warp];
-        const float top = warp_max(p.x), base = top == -INFINITY ? 0.f : top;
-        const float sum = warp_sum(p.y * ex2(p.x - base));
-        if (lane == 0) joined[warp] = make_float2(top, sum);
-    }
-    __syncwarp();
-    const int row = blockIdx.x * 32 + warp;
     if (row >= n) return;
-    const int64_t t = rows ? rows[row] : row;
-    DsRow e = ds_load(t, K, V, ids, z, rows ? nullptr : status);
-    const float top = joined[warp].x, base = top == -INFINITY ? 0.f : top, b = log2f(joined[warp].y);
+    const float2 p = red[lane][warp];                                   // lane: a range of tiles, warp: a row
+    const float top = warp_max(p.x), base = top == -INFINITY ? 0.f : top;
+    const float b = log2f(warp_sum(p.y * ex2(p.x - base)));
     ds_weights(e, inv_tau);
     float l = 0.f;
 #pragma unroll
-    for (int i = 0; i < kDsPer; ++i) {
+    for (int i = 0; i < PER; ++i) {
         const int k = i * 32 + lane;
         if (k >= K) continue;
         // x - lse as a difference to the row's largest logit, so that a likely id keeps its digits
-        const float q = e.live && e.id[i] >= 0 ? (fmaf(dots[t * K + k], k2, -base) - b) * kLn2 : 0.f;
+        const float q = e.live && e.id[i] >= 0 ? (fmaf(x[i], k2, -base) - b) * kLn2 : 0.f;
         logp[t * K + k] = q;
         if (e.live && e.z[i] != -INFINITY) l += expf(e.z[i]) * (e.z[i] - q);
     }
@@ -152,111 +251,75 @@ __global__ void __launch_bounds__(1024) ds_join_k(int64_t T, int K, int64_t V, c
     }
 }
 
-// Entries of G that the teacher has a share in, over what the product's epilogue wrote there: a warp a row.  An id that occurs
-// twice has the sum of its weights, and both of its entries write the same.
-template <typename Z>
-__global__ void __launch_bounds__(256) ds_fix_k(int K, int64_t V, const int* live, const int* rows, int v0, int vn, const int64_t* ids,
-                                                const Z* z, float inv_tau, const float* logp, const float* dloss, const uint32_t* ref, int refs,
-                                                __nv_bfloat16* G, int64_t pitch) {
-    pdl_wait();
-    pdl_launch();
-    const int lane = threadIdx.x & 31, n = *live;
-    const int row = blockIdx.x * 8 + (threadIdx.x >> 5);
-    const float top = ce_ref(ref, refs);
-    if (row >= n) return;
-    const int64_t t = rows[row];
-    DsRow e = ds_load(t, K, V, ids, z, nullptr);
-    ds_weights(e, inv_tau);
-    float p[kDsPer], sum[kDsPer];
-#pragma unroll
-    for (int i = 0; i < kDsPer; ++i) { p[i] = expf(e.z[i]); sum[i] = 0.f; }
-#pragma unroll
-    for (int j = 0; j < kDsPer; ++j) {
-        if (j * 32 >= K) break;
-        for (int l = 0; l < 32; ++l) {
-            const int id = __shfl_sync(0xffffffffu, e.id[j], l);
-            const float w = __shfl_sync(0xffffffffu, p[j], l);
-#pragma unroll
-            for (int i = 0; i < kDsPer; ++i)
-                if (id == e.id[i]) sum[i] += w;
-        }
-    }
-    const float f = dloss[t] / top;
-#pragma unroll
-    for (int i = 0; i < kDsPer; ++i) {
-        const int at = e.id[i] - v0;
-        if (e.id[i] >= 0 && at >= 0 && at < vn) G[row * pitch + at] = __float2bfloat16_rn((expf(logp[t * K + i * 32 + lane]) - sum[i]) * f);
-    }
-}
-
 // ---- host side -------------------------------------------------------------------------------------------------------
-struct DsPlan { CePlan ce; int64_t* target; float* dots; size_t bytes; };
+struct DsPlan { CePlan ce; int64_t* target; float* dots; uint2* entries; uint16_t* first; int blocks; size_t bytes; };
 static DsPlan plan_ds(int64_t T, int64_t V, int K, int C, int grad, void* base) {
     DsPlan p;
     char* b = (char*)base;
     p.ce = plan_ce(T, V, C, grad, base);
-    size_t off = ce_scratch_bytes(T, V, C, grad);
-    off = (off + 255) & ~(size_t)255;
+    size_t off = (ce_scratch_bytes(T, V, C, grad) + 255) & ~(size_t)255;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     p.target = (int64_t*)take((size_t)T * 8);
     p.dots = grad ? nullptr : (float*)take((size_t)T * K * 4);
+    p.entries = (uint2*)take((size_t)T * (K + 1) * 8);
+    p.blocks = 2 * p.ce.n_tiles;
+    p.first = (uint16_t*)take((size_t)T * p.blocks * 2);
     p.bytes = off;
     return p;
 }
 size_t distill_scratch_bytes(int64_t T, int64_t V, int K, int C, int grad) { return plan_ds(T, V, K, C, grad, nullptr).bytes; }
 
-template <typename Z>
-static void launch_ds_live(const mhclite_ctx* c, int64_t T, int64_t V, int K, const int64_t* ids, const Z* z, int64_t* target, float* logp,
-                           int* status, cudaStream_t s) {
+// Calls f with the entries a lane holds, as a compile-time number.
+template <typename F>
+static auto ds_per(int K, F f) {
+    return K <= 32 ? f(std::integral_constant<int, 1>()) : K <= 64 ? f(std::integral_constant<int, 2>())
+           : K <= 128 ? f(std::integral_constant<int, 4>()) : f(std::integral_constant<int, 8>());
+}
+template <bool GRAD>
+static void launch_ds_sort(const mhclite_ctx* c, const DsPlan& p, int64_t T, int64_t V, int K, const int64_t* ids, const void* z, int z_f32,
+                           float inv_tau, const float* logp_in, float* logp, cudaStream_t s) {
     c->launches += 1;
-    launch_after(ds_live_k<Z>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, ids, z, target, logp, status);
+    ds_per(K, [&](auto per) {
+        launch_after(ds_sort_k<decltype(per)::value, GRAD>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, ids, z, z_f32, inv_tau, logp_in,
+                     p.entries, p.first, p.blocks, p.target, logp, c->op_status);
+    });
 }
 
-template <typename Z>
-static bool ds_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids, const Z* z, float scale,
-                   float inv_tau, float* loss, float* lse, float* logp, void* scratch, cudaStream_t s) {
-    const DsPlan p = plan_ds(T, V, K, c->C, 0, scratch);
-    const int64_t entries = T * K, blocks = (entries + 7) / 8, most = (int64_t)c->sm_count * 32;
-    const float k2 = scale * kLog2e;
-    c->launches += 2;
-    launch_after(ds_dot_k, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, entries, K, V, c->C, ids, (const uint4*)h,
-                 (const uint4*)W, p.dots);
-    const SmallPlan q = plan_small(T, c->C);
-    if (q.stages) {
-        const int grid = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
-        launch_after(ds_join_k<Z>, dim3(1), dim3(1024), 0, s, T, K, V, nullptr, nullptr, grid, kSmTokens, (const float2*)scratch, p.dots, ids, z,
-                     k2, inv_tau, loss, lse, logp, c->op_status);
-        return true;
-    }
-    launch_ds_live(c, T, V, K, ids, z, p.target, logp, c->op_status, s);
-    if (!launch_ce_stats(c, p.ce, T, V, h, W, p.target, nullptr, scale, loss, lse, s)) return false;
-    launch_after(ds_join_k<Z>, dim3((unsigned)((T + 31) / 32)), dim3(1024), 0, s, T, K, V, p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad,
-                 p.ce.part, p.dots, ids, z, k2, inv_tau, loss, lse, logp, c->op_status);
-    return true;
-}
 bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids,
                                const void* z, int z_f32, float scale, float inv_tau, float* loss, float* lse, float* logp, void* scratch,
                                cudaStream_t s) {
-    return z_f32 ? ds_fwd(c, T, V, K, h, W, ids, (const float*)z, scale, inv_tau, loss, lse, logp, scratch, s)
-                 : ds_fwd(c, T, V, K, h, W, ids, (const __nv_bfloat16*)z, scale, inv_tau, loss, lse, logp, scratch, s);
+    const DsPlan p = plan_ds(T, V, K, c->C, 0, scratch);
+    const SmallPlan q = plan_small(T, c->C);
+    auto join = [&](int blocks, const int* live, const int* rows, int n_parts, int pitch, const float2* part) {
+        ds_per(K, [&](auto per) {
+            launch_after(ds_join_k<decltype(per)::value>, dim3((unsigned)blocks), dim3(1024), 0, s, T, K, V, live, rows, n_parts, pitch, part, p.dots,
+                         ids, z, z_f32, scale * kLog2e, inv_tau, loss, lse, logp, c->op_status);
+        });
+    };
+    if (q.stages) {
+        const int64_t entries = T * K;
+        c->launches += 1;
+        launch_after(ds_dot_k, dim3((unsigned)((entries + 7) / 8)), dim3(256), 0, s, entries, K, V, c->C, ids, (const uint4*)h, (const uint4*)W, p.dots);
+        const int grid = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
+        join(1, nullptr, nullptr, grid, kSmTokens, (const float2*)scratch);
+        return true;
+    }
+    launch_ds_sort<false>(c, p, T, V, K, ids, z, z_f32, inv_tau, nullptr, logp, s);
+    CeArgs a = {};
+    a.entries = p.entries; a.first_entry = p.first; a.blocks = p.blocks; a.K = K; a.dots = p.dots;
+    if (!launch_ce_stats<CE_PICK>(c, p.ce, a, T, V, h, W, p.target, scale, loss, lse, s)) return false;
+    join((int)((T + 31) / 32), p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad, p.ce.part);
+    return true;
 }
 
-template <typename Z>
-static bool ds_bwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids, const Z* z, float scale,
-                   float inv_tau, const float* lse, const float* logp, const float* dloss, void* dh, void* dW, void* scratch, cudaStream_t s) {
-    const DsPlan p = plan_ds(T, V, K, c->C, 1, scratch);
-    launch_ds_live(c, T, V, K, ids, z, p.target, nullptr, c->op_status, s);
-    return launch_ce_grads(c, p.ce, T, V, h, W, p.target, nullptr, scale, lse, dloss, dh, dW, s, [&](int v0, int vn) {
-        c->launches += 1;
-        launch_after(ds_fix_k<Z>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, K, V, p.ce.live, p.ce.rows, v0, vn, ids, z, inv_tau, logp, dloss,
-                     p.ce.ref, p.ce.row_blocks, p.ce.G, p.ce.piece);
-    });
-}
 bool launch_linear_distill_bwd(const mhclite_ctx* c, int64_t T, int64_t V, int K, const void* h, const void* W, const int64_t* ids,
                                const void* z, int z_f32, float scale, float inv_tau, const float* lse, const float* logp, const float* dloss,
                                void* dh, void* dW, void* scratch, cudaStream_t s) {
-    return z_f32 ? ds_bwd(c, T, V, K, h, W, ids, (const float*)z, scale, inv_tau, lse, logp, dloss, dh, dW, scratch, s)
-                 : ds_bwd(c, T, V, K, h, W, ids, (const __nv_bfloat16*)z, scale, inv_tau, lse, logp, dloss, dh, dW, scratch, s);
+    const DsPlan p = plan_ds(T, V, K, c->C, 1, scratch);
+    launch_ds_sort<true>(c, p, T, V, K, ids, z, z_f32, inv_tau, logp, nullptr, s);
+    CeArgs a = {};
+    a.entries = p.entries; a.first_entry = p.first; a.blocks = p.blocks; a.K = K;
+    return launch_ce_grads<CE_PATCH>(c, p.ce, a, T, V, h, W, p.target, scale, lse, dloss, dh, dW, s);
 }
 
 }  // namespace mhcl
