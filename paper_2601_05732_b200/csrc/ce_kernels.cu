@@ -82,7 +82,7 @@ constexpr int kCeStagePitch = 144;                     // bytes a row: 128 and 1
 __host__ __device__ constexpr bool ce_staged(int mode) { return mode == CE_GRAD || mode == CE_PATCH || mode == CE_DW; }
 __host__ __device__ constexpr int ce_stages(int mode) { return ce_staged(mode) ? kCeStages - 1 : kCeStages; }
 __host__ __device__ constexpr int ce_smem(int mode) {
-    return ce_stages(mode) * kCeStage + (ce_staged(mode) ? kCeEpiWarps * 32 * kCeStagePitch : 0) + 256 + 1024;
+    return ce_stages(mode) * kCeStage + (ce_staged(mode) ? kCeEpiWarps * 32 * kCeStagePitch : mode == CE_PICK ? kCeEpiWarps * 32 * 128 : 0) + 256 + 1024;
 }
 
 struct CeCtl {
@@ -348,22 +348,22 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                 const float k2 = a.scale * kLog2e;
                 if (STATS) {
                     float mx = -INFINITY, sum = 0.f;
-                    // the entries' logits, column by column (at most the 128 there are): one column for all rows that have it
-                    if (MODE == CE_PICK) {
-                        for (;;) {
-                            __syncwarp();
-                            const uint32_t c = __reduce_min_sync(0xffffffffu, next[0].x - (uint32_t)n0);
-                            if (c >= (uint32_t)kCeHalf) break;
-                            const float v = tc_ld1(acc + c);
-                            for (; next[0].x - (uint32_t)n0 == c; pop()) a.dots[(int64_t)t * a.K + next[0].y] = v;
-                        }
-                        __syncwarp();
-                    }
 #pragma unroll 1
                     for (int c0 = 0; c0 < kCeHalf; c0 += 32) {
                         if (c0 >= cols) break;
                         float v[32];
                         tc_ld32(acc + c0, v);
+                        // the entries' logits: the columns go where a lane can index them, each lane its own row's
+                        if (MODE == CE_PICK && __any_sync(0xffffffffu, next[0].x - (uint32_t)(n0 + c0) < 32u)) {
+                            const uint32_t own = smem_u32(smem + STAGES * kCeStage + 256) + (warp - 2) * 4096 + lane * 128;
+#pragma unroll
+                            for (int e = 0; e < 32; e += 4)
+                                sts128(own + (((e >> 2) ^ (lane & 7)) << 4), make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]),
+                                                                                      __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])));
+                            for (uint32_t at; (at = next[0].x - (uint32_t)(n0 + c0)) < 32u; pop())
+                                a.dots[(int64_t)t * a.K + next[0].y] = lds32(own + (((at >> 2) ^ (lane & 7)) << 4) + (at & 3) * 4);
+                            __syncwarp();
+                        }
                         if (!ENTRIES && __any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e)

@@ -197,17 +197,17 @@ __global__ void __launch_bounds__(256) ds_dot_k(int64_t entries, int K, int64_t 
     }
 }
 
-// Joins the (maximum, sum) pairs of 32 rows a block as ce_join_k does, then a warp a row forms loss, lse and logp.  live and
+// Joins the (maximum, sum) pairs of 8 rows a block, 32 ranges of tiles side by side, then a warp a row forms loss, lse and logp.  live and
 // rows are null where every row is in the pairs (a handful of tokens).
 template <int PER>
-__global__ void __launch_bounds__(1024) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
+__global__ void __launch_bounds__(256) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
                                                   const float2* part, const float* dots, const int64_t* ids, const void* z, int z_f32, float k2,
                                                   float inv_tau, float* loss, float* lse, float* logp, int* status) {
-    __shared__ float2 red[32][33];
+    __shared__ float2 red[32][9];
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.x * 32 + lane, n = live ? *live : (int)T;
-    if (blockIdx.x * 32 >= n) return;
-    const int row = blockIdx.x * 32 + warp;                             // of the second half
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = live ? *live : (int)T;
+    if (blockIdx.x * 8 >= n) return;
+    const int r = blockIdx.x * 8 + (lane & 7), range = warp * 4 + (lane >> 3), row = blockIdx.x * 8 + warp;
     DsRow<PER> e;
     float x[PER];
     int64_t t = 0;
@@ -220,14 +220,14 @@ __global__ void __launch_bounds__(1024) ds_join_k(int64_t T, int K, int64_t V, c
     float m = -INFINITY, s = 0.f;
     if (r < n) {
 #pragma unroll 8
-        for (int k = warp; k < n_parts; k += 32) {
+        for (int k = range; k < n_parts; k += 32) {
             const float2 p = part[(int64_t)k * pitch + r];
             const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
             s = s * ex2(m - base) + p.y * ex2(p.x - base);
             m = top;
         }
     }
-    red[warp][lane] = make_float2(m, s);
+    red[range][lane & 7] = make_float2(m, s);
     __syncthreads();
     if (row >= n) return;
     const float2 p = red[lane][warp];                                   // lane: a range of tiles, warp: a row
@@ -290,9 +290,9 @@ bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
                                cudaStream_t s) {
     const DsPlan p = plan_ds(T, V, K, c->C, 0, scratch);
     const SmallPlan q = plan_small(T, c->C);
-    auto join = [&](int blocks, const int* live, const int* rows, int n_parts, int pitch, const float2* part) {
+    auto join = [&](const int* live, const int* rows, int n_parts, int pitch, const float2* part) {
         ds_per(K, [&](auto per) {
-            launch_after(ds_join_k<decltype(per)::value>, dim3((unsigned)blocks), dim3(1024), 0, s, T, K, V, live, rows, n_parts, pitch, part, p.dots,
+            launch_after(ds_join_k<decltype(per)::value>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, live, rows, n_parts, pitch, part, p.dots,
                          ids, z, z_f32, scale * kLog2e, inv_tau, loss, lse, logp, c->op_status);
         });
     };
@@ -301,14 +301,14 @@ bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
         c->launches += 1;
         launch_after(ds_dot_k, dim3((unsigned)((entries + 7) / 8)), dim3(256), 0, s, entries, K, V, c->C, ids, (const uint4*)h, (const uint4*)W, p.dots);
         const int grid = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
-        join(1, nullptr, nullptr, grid, kSmTokens, (const float2*)scratch);
+        join(nullptr, nullptr, grid, kSmTokens, (const float2*)scratch);
         return true;
     }
     launch_ds_sort<false>(c, p, T, V, K, ids, z, z_f32, inv_tau, nullptr, logp, s);
     CeArgs a = {};
     a.entries = p.entries; a.first_entry = p.first; a.blocks = p.blocks; a.K = K; a.dots = p.dots;
     if (!launch_ce_stats<CE_PICK>(c, p.ce, a, T, V, h, W, p.target, scale, loss, lse, s)) return false;
-    join((int)((T + 31) / 32), p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad, p.ce.part);
+    join(p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad, p.ce.part);
     return true;
 }
 
