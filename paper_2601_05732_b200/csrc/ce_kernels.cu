@@ -54,10 +54,10 @@ struct CeArgs {
     const int64_t* target;
     int Tpad;
     // CE_PICK, CE_PATCH
-    const uint2* entries;       // [T][K + 1] by rising id (ds_sort_k), the last of each row behind all ids
-    const uint16_t* first_entry;   // [T][blocks] the first entry from each 128 columns of the vocabulary on
-    int K, blocks;
-    float* dots;                // [T][K] <h_t, W_id>
+    const uint8_t* cols;        // [T][entries] a row's entries by rising id (ds_sort_k): the id's place in its 128 columns,
+    float* values;              // and <h_t, W_id> (out), or what the bracket is there (in)
+    const uint16_t* from;       // [T][blocks + 1] the first entry from each 128 columns of the vocabulary on
+    int entries, blocks;        // entries: a multiple of 8
     // CE_GRAD
     const float* lse;
     const float* dloss;
@@ -190,6 +190,32 @@ __device__ __forceinline__ void ce_tile(int i, int group, int mt, int nt, int& m
     m = g * group + (r - n * gm);
 }
 
+// A lane's walk along the entries of its row that lie in 128 columns.  Lanes are rows apart in memory, so a load costs the warp
+// the same for one byte or sixteen: columns come by eights, one fetch ahead.
+struct EntryWalk {
+    const uint2* cols;
+    int pos, end;
+    uint2 now, next;
+    __device__ __forceinline__ void start(const CeArgs& a, int64_t token, int block) {
+        const uint16_t* f = a.from + token * (a.blocks + 1) + block;
+        pos = f[0];
+        end = f[1];
+        cols = reinterpret_cast<const uint2*>(a.cols + token * a.entries);
+        now = pos < end ? cols[pos >> 3] : make_uint2(0, 0);
+        next = (pos | 7) + 1 < end ? cols[(pos >> 3) + 1] : now;
+    }
+    __device__ __forceinline__ uint32_t word() const { return (pos & 4) ? now.y : now.x; }          // of the four that pos is among
+    __device__ __forceinline__ uint32_t col() const { return pos < end ? word() >> ((pos & 3) * 8) & 255u : 255u; }     // 255 behind the last
+    __device__ __forceinline__ void move(int to) {                      // at most to the next four
+        const bool turn = (to ^ pos) & ~7;
+        pos = to;
+        if (turn) {
+            now = next;
+            if (pos + 8 < end) next = cols[(pos >> 3) + 1];
+        }
+    }
+};
+
 template <int MODE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kCeThreads, 1)
 ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUtensorMap tmb, const CeArgs a) {
@@ -308,27 +334,20 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
             ce_tile(i - split * per, a.group, mt, nt, m, n);
             const int r = m * kCeM + row;                       // row of the list, or of the piece (CE_DW)
             const int n0 = n * kCeN + half * kCeHalf;           // this warp's 128 columns
-            // the row's next entries from this warp's first column on, fetched while the products run
-            const uint2* entry = nullptr;
-            const uint2* last = nullptr;
-            uint2 next[4];
-            if (ENTRIES) {
-                const uint2 none = make_uint2(0x7FFFFFFFu, 0);
-                next[0] = next[1] = next[2] = next[3] = none;
+            EntryWalk walk;
+            float4 four = make_float4(0.f, 0.f, 0.f, 0.f);              // values of entries 4 i .. 4 i + 3
+            float* values = nullptr;
+            int from = 0;
+            if (ENTRIES) {                                              // fetched while the products run
+                walk.pos = walk.end = 0;
                 if (r < live) {
                     const int64_t token = a.rows[r];
-                    last = a.entries + token * (a.K + 1) + a.K;
-                    entry = last - a.K + a.first_entry[token * a.blocks + (a.v0 + n0) / kCeHalf];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) next[e] = entry + e <= last ? entry[e] : none;
-                    entry += 4;
+                    walk.start(a, token, (a.v0 + n0) / kCeHalf);
+                    from = walk.pos;
+                    values = a.values + token * a.entries;
+                    if (MODE == CE_PATCH && walk.pos < walk.end) four = *reinterpret_cast<const float4*>(values + (walk.pos & ~3));
                 }
             }
-            auto pop = [&] {
-                next[0] = next[1]; next[1] = next[2]; next[2] = next[3];
-                next[3] = entry <= last ? *entry : make_uint2(0x7FFFFFFFu, 0);
-                ++entry;
-            };
             ok = ce_wait(smem_u32(&ctl->acc_full[buf]), (j >> 1) & 1, abort, 4, j);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
@@ -354,14 +373,37 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         float v[32];
                         tc_ld32(acc + c0, v);
                         // the entries' logits: the columns go where a lane can index them, each lane its own row's
-                        if (MODE == CE_PICK && __any_sync(0xffffffffu, next[0].x - (uint32_t)(n0 + c0) < 32u)) {
+                        if (MODE == CE_PICK && __any_sync(0xffffffffu, walk.col() - c0 < 32u)) {
                             const uint32_t own = smem_u32(smem + STAGES * kCeStage + 256) + (warp - 2) * 4096 + lane * 128;
 #pragma unroll
                             for (int e = 0; e < 32; e += 4)
                                 sts128(own + (((e >> 2) ^ (lane & 7)) << 4), make_uint4(__float_as_uint(v[e]), __float_as_uint(v[e + 1]),
                                                                                       __float_as_uint(v[e + 2]), __float_as_uint(v[e + 3])));
-                            for (uint32_t at; (at = next[0].x - (uint32_t)(n0 + c0)) < 32u; pop())
-                                a.dots[(int64_t)t * a.K + next[0].y] = lds32(own + (((at >> 2) ^ (lane & 7)) << 4) + (at & 3) * 4);
+                            while (walk.col() - c0 < 32u) {              // as many of four as lie among these columns
+                                const uint32_t word = walk.word();
+                                const int q0 = walk.pos & ~3, of = walk.pos & 3;
+                                uint32_t at[4];
+                                bool in[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    at[e] = (word >> 8 * e & 255u) - c0;
+                                    in[e] = e >= of && q0 + e < walk.end && at[e] < 32u;
+                                }
+                                if (in[0]) four.x = lds32(own + (((at[0] >> 2) ^ (lane & 7)) << 4) + (at[0] & 3) * 4);
+                                if (in[1]) four.y = lds32(own + (((at[1] >> 2) ^ (lane & 7)) << 4) + (at[1] & 3) * 4);
+                                if (in[2]) four.z = lds32(own + (((at[2] >> 2) ^ (lane & 7)) << 4) + (at[2] & 3) * 4);
+                                if (in[3]) four.w = lds32(own + (((at[3] >> 2) ^ (lane & 7)) << 4) + (at[3] & 3) * 4);
+                                const int to = walk.pos + in[0] + in[1] + in[2] + in[3];
+                                if (to == q0 + 4 && q0 >= from) {
+                                    *reinterpret_cast<float4*>(values + q0) = four;
+                                } else if (to == q0 + 4 || to == walk.end) {
+                                    if (q0 >= from) values[q0] = four.x;
+                                    if (q0 + 1 >= from && q0 + 1 < to) values[q0 + 1] = four.y;
+                                    if (q0 + 2 >= from && q0 + 2 < to) values[q0 + 2] = four.z;
+                                    if (q0 + 3 >= from && q0 + 3 < to) values[q0 + 3] = four.w;
+                                }
+                                walk.move(to);
+                            }
                             __syncwarp();
                         }
                         if (!ENTRIES && __any_sync(0xffffffffu, tgt >= c0 && tgt < c0 + 32)) {
@@ -433,8 +475,13 @@ ce_gemm_k(const __grid_constant__ CUtensorMap tma, const __grid_constant__ CUten
                         if (c0 + 64 == kCeHalf) hand_back();
                         // where the teacher has a share: formed with the logit that the forward left, not here
                         if (MODE == CE_PATCH) {
-                            for (uint32_t at; (at = next[0].x - (uint32_t)(a.v0 + n0 + c0)) < 64u; pop())
-                                sts16(staging + lane * kCeStagePitch + at * 2, __bfloat16_as_ushort(__float2bfloat16_rn(__uint_as_float(next[0].y) * f)));
+                            for (uint32_t at; (at = walk.col() - c0) < 64u;) {
+                                const int of = walk.pos & 3;
+                                const float x = of == 0 ? four.x : of == 1 ? four.y : of == 2 ? four.z : four.w;
+                                sts16(staging + lane * kCeStagePitch + at * 2, __bfloat16_as_ushort(__float2bfloat16_rn(x * f)));
+                                walk.move(walk.pos + 1);
+                                if (of == 3 && walk.pos < walk.end) four = *reinterpret_cast<const float4*>(values + walk.pos);
+                            }
                         }
                         __syncwarp();
 #pragma unroll

@@ -91,16 +91,17 @@ __device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
         }
 }
 
-// A row's entries by rising id, for the tiles' epilogues: (id, k) for the forward, (id, bits of exp(logp) - the id's weights) for
-// the backward; absent ones and one more behind all ids.  With them, for every 128 columns, which entry is the first from there
-// on (`first`), so that an epilogue needs no search.  A warp a row.  Rows with a teacher get 0 in `target`, which ce_rows_k lists
-// them by, others -1 and, in the forward, logp 0.
+// A row's entries by rising id, absent ones last, for the tiles' epilogues: each one's place in its 128 columns (`cols`), and which
+// is the first from every 128 columns on (`first`), so that an epilogue needs no search.  With them, for the forward's join, their
+// numbers in the caller's order (`order`) and the logarithms of their weights (`weights`, +inf where absent), for the backward
+// what the bracket is there, exp(logp) - the id's weights (`weights` too).  A warp a row.  Rows with a teacher get 0 in `target`, which ce_rows_k lists them by, others -1 and, in the
+// forward, logp 0.
 template <int PER, bool GRAD>
 __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, const int64_t* ids, const void* z, int z_f32, float inv_tau,
-                                                 const float* logp_in, uint2* entries, uint16_t* first, int blocks, int64_t* target, float* logp,
-                                                 int* status) {
+                                                 const float* logp_in, int entries, uint8_t* cols, uint8_t* order, float* weights,
+                                                 uint16_t* first, int blocks, int64_t* target, float* logp, int* status) {
     __shared__ int id_s[8][32 * PER];
-    __shared__ float p_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1], w_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1];
+    __shared__ float p_s[8][32 * PER], w_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1];
     pdl_wait();
     pdl_launch();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, ws = GRAD ? warp : 0;
@@ -114,12 +115,12 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
         return;
     }
     uint64_t key[PER];
-    if (GRAD) ds_weights(r, inv_tau);
+    ds_weights(r, inv_tau);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int k = i * 32 + lane;
         key[i] = (uint64_t)(uint32_t)(r.id[i] < 0 ? 0x7FFFFFFF : r.id[i]) << 32 | (uint32_t)k;       // as numbered where ids are equal
-        if (GRAD) p_s[ws][k] = expf(r.z[i]);
+        p_s[warp][k] = GRAD ? expf(r.z[i]) : r.id[i] < 0 ? INFINITY : r.z[i];
     }
     ds_sort(key);
     bool twice = false;
@@ -131,11 +132,9 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
         twice = twice || (id == prior && id != 0x7FFFFFFF);
     }
     __syncwarp();
-    float value[PER];
     if (GRAD) {
-        float p[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p[i] = p_s[ws][(int)(key[i] & 0xFFFFFFFFu)];
+        for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p_s[warp][(int)(uint32_t)key[i]];
         __syncwarp();
         if (__any_sync(0xffffffffu, twice)) {                           // an id's entries, which lie side by side, all get their sum
             for (int i = 0; i < PER; ++i) {
@@ -145,32 +144,32 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
                 while (from > 0 && id_s[warp][from - 1] == id) --from;
                 float sum = 0.f;
                 for (; from < 32 * PER && id_s[warp][from] == id; ++from) sum += w_s[ws][from];
-                p_s[ws][(int)(key[i] & 0xFFFFFFFFu)] = sum;             // each entry its own place
+                p_s[warp][at] = sum;
             }
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < PER; ++i) p[i] = p_s[ws][(int)(key[i] & 0xFFFFFFFFu)];
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int k = (int)(key[i] & 0xFFFFFFFFu);
-            value[i] = (int)(key[i] >> 32) != 0x7FFFFFFF ? expf(logp_in[t * K + k]) - p[i] : 0.f;
+            for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p_s[warp][lane * PER + i];
         }
     }
-    uint2* out = entries + t * (K + 1);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int at = lane * PER + i;
-        if (at < K) out[at] = make_uint2((uint32_t)(key[i] >> 32), GRAD ? __float_as_uint(value[i]) : (uint32_t)key[i]);
+        const int at = lane * PER + i, id = (int)(key[i] >> 32), k = (int)(uint32_t)key[i];
+        if (at >= K) continue;
+        cols[t * entries + at] = (uint8_t)(id & 127);
+        if (GRAD) {
+            weights[t * entries + at] = id != 0x7FFFFFFF ? expf(logp_in[t * K + k]) - w_s[ws][at] : 0.f;
+        } else {
+            weights[t * entries + at] = p_s[warp][k];
+            order[t * entries + at] = (uint8_t)k;
+        }
     }
-    if (lane == 0) out[K] = make_uint2(0x7FFFFFFFu, 0);
-    for (int b = lane; b < blocks; b += 32) {
+    for (int b = lane; b <= blocks; b += 32) {
         int at = 0;
 #pragma unroll
         for (int step = 16 * PER; step > 0; step /= 2)                  // how many entries lie below the block
             if (id_s[warp][at + step - 1] < b * 128) at += step;
         at += id_s[warp][at] < b * 128;
-        first[t * blocks + b] = (uint16_t)at;
+        first[t * (blocks + 1) + b] = (uint16_t)at;
     }
 }
 
@@ -197,31 +196,45 @@ __global__ void __launch_bounds__(256) ds_dot_k(int64_t entries, int K, int64_t 
     }
 }
 
-// Joins the (maximum, sum) pairs of 8 rows a block, 32 ranges of tiles side by side, then a warp a row forms loss, lse and logp.  live and
-// rows are null where every row is in the pairs (a handful of tokens).
-template <int PER>
+// Joins the (maximum, sum) pairs of 8 rows a block, 32 ranges of tiles side by side, then a warp a row forms loss, lse and logp:
+// of the listed rows with their entries as ds_sort_k left them (LISTED), or of all rows with the entries as they came (a handful
+// of tokens, with ds_dot_k's products).
+template <int PER, bool LISTED>
 __global__ void __launch_bounds__(256) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
-                                                  const float2* part, const float* dots, const int64_t* ids, const void* z, int z_f32, float k2,
-                                                  float inv_tau, float* loss, float* lse, float* logp, int* status) {
+                                                 const float2* part, const float* dots, int entries, const uint8_t* order, const float* weights,
+                                                 const int64_t* ids, const void* z, int z_f32, float k2, float inv_tau, float* loss, float* lse,
+                                                 float* logp, int* status) {
     __shared__ float2 red[32][9];
     pdl_wait();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = live ? *live : (int)T;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = LISTED ? *live : (int)T;
     if (blockIdx.x * 8 >= n) return;
     const int r = blockIdx.x * 8 + (lane & 7), range = warp * 4 + (lane >> 3), row = blockIdx.x * 8 + warp;
-    DsRow<PER> e;
+    DsRow<PER> e;                                                       // z: log weights
     float x[PER];
+    int k[PER];
     int64_t t = 0;
-    if (row < n) {                                                      // its loads run beside the first half's
-        t = rows ? rows[row] : row;
-        e = ds_load<PER>(t, K, V, ids, z, z_f32, rows ? nullptr : status);
+    if (row < n) {                                                      // its loads run beside those of the pairs
+        t = LISTED ? rows[row] : row;
+        if (!LISTED) e = ds_load<PER>(t, K, V, ids, z, z_f32, status);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) x[i] = e.id[i] >= 0 ? dots[t * K + i * 32 + lane] : 0.f;
+        for (int i = 0; i < PER; ++i) {
+            const int at = i * 32 + lane;
+            k[i] = at;
+            if (LISTED) {
+                k[i] = at < K ? order[t * entries + at] : K;
+                e.z[i] = at < K ? weights[t * entries + at] : INFINITY;
+                e.id[i] = e.z[i] == INFINITY ? -1 : 0;
+                x[i] = at < K ? dots[t * entries + at] : 0.f;
+            } else {
+                x[i] = e.id[i] >= 0 ? dots[t * entries + at] : 0.f;
+            }
+        }
     }
     float m = -INFINITY, s = 0.f;
     if (r < n) {
 #pragma unroll 8
-        for (int k = range; k < n_parts; k += 32) {
-            const float2 p = part[(int64_t)k * pitch + r];
+        for (int i = range; i < n_parts; i += 32) {
+            const float2 p = part[(int64_t)i * pitch + r];
             const float top = fmaxf(m, p.x), base = top == -INFINITY ? 0.f : top;
             s = s * ex2(m - base) + p.y * ex2(p.x - base);
             m = top;
@@ -233,26 +246,27 @@ __global__ void __launch_bounds__(256) ds_join_k(int64_t T, int K, int64_t V, co
     const float2 p = red[lane][warp];                                   // lane: a range of tiles, warp: a row
     const float top = warp_max(p.x), base = top == -INFINITY ? 0.f : top;
     const float b = log2f(warp_sum(p.y * ex2(p.x - base)));
-    ds_weights(e, inv_tau);
+    if (!LISTED) ds_weights(e, inv_tau);
+    const bool alive = LISTED || e.live;
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int k = i * 32 + lane;
-        if (k >= K) continue;
+        if (k[i] >= K) continue;
         // x - lse as a difference to the row's largest logit, so that a likely id keeps its digits
-        const float q = e.live && e.id[i] >= 0 ? (fmaf(x[i], k2, -base) - b) * kLn2 : 0.f;
-        logp[t * K + k] = q;
-        if (e.live && e.z[i] != -INFINITY) l += expf(e.z[i]) * (e.z[i] - q);
+        const bool in = alive && e.id[i] >= 0;
+        const float q = in ? (fmaf(x[i], k2, -base) - b) * kLn2 : 0.f;
+        logp[t * K + k[i]] = q;
+        if (in && e.z[i] != -INFINITY) l += expf(e.z[i]) * (e.z[i] - q);
     }
     l = warp_sum(l);
     if (lane == 0) {
-        lse[t] = e.live ? (top + b) * kLn2 : 0.f;
+        lse[t] = alive ? (top + b) * kLn2 : 0.f;
         loss[t] = l;
     }
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
-struct DsPlan { CePlan ce; int64_t* target; float* dots; uint2* entries; uint16_t* first; int blocks; size_t bytes; };
+struct DsPlan { CePlan ce; int64_t* target; float *dots, *weights; uint8_t *cols, *order; uint16_t* first; int blocks, entries; size_t bytes; };
 static DsPlan plan_ds(int64_t T, int64_t V, int K, int C, int grad, void* base) {
     DsPlan p;
     char* b = (char*)base;
@@ -260,10 +274,13 @@ static DsPlan plan_ds(int64_t T, int64_t V, int K, int C, int grad, void* base) 
     size_t off = (ce_scratch_bytes(T, V, C, grad) + 255) & ~(size_t)255;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     p.target = (int64_t*)take((size_t)T * 8);
-    p.dots = grad ? nullptr : (float*)take((size_t)T * K * 4);
-    p.entries = (uint2*)take((size_t)T * (K + 1) * 8);
+    p.entries = (K + 7) / 8 * 8;
+    p.weights = (float*)take((size_t)T * p.entries * 4);
+    p.cols = (uint8_t*)take((size_t)T * p.entries);
+    p.dots = (float*)take(grad ? 0 : (size_t)T * p.entries * 4);
+    p.order = (uint8_t*)take(grad ? 0 : (size_t)T * p.entries);
     p.blocks = 2 * p.ce.n_tiles;
-    p.first = (uint16_t*)take((size_t)T * p.blocks * 2);
+    p.first = (uint16_t*)take((size_t)T * (p.blocks + 1) * 2);
     p.bytes = off;
     return p;
 }
@@ -281,7 +298,7 @@ static void launch_ds_sort(const mhclite_ctx* c, const DsPlan& p, int64_t T, int
     c->launches += 1;
     ds_per(K, [&](auto per) {
         launch_after(ds_sort_k<decltype(per)::value, GRAD>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, ids, z, z_f32, inv_tau, logp_in,
-                     p.entries, p.first, p.blocks, p.target, logp, c->op_status);
+                     p.entries, p.cols, p.order, p.weights, p.first, p.blocks, p.target, logp, c->op_status);
     });
 }
 
@@ -290,25 +307,28 @@ bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
                                cudaStream_t s) {
     const DsPlan p = plan_ds(T, V, K, c->C, 0, scratch);
     const SmallPlan q = plan_small(T, c->C);
-    auto join = [&](const int* live, const int* rows, int n_parts, int pitch, const float2* part) {
-        ds_per(K, [&](auto per) {
-            launch_after(ds_join_k<decltype(per)::value>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, live, rows, n_parts, pitch, part, p.dots,
-                         ids, z, z_f32, scale * kLog2e, inv_tau, loss, lse, logp, c->op_status);
-        });
-    };
+    const float k2 = scale * kLog2e;
+    const dim3 grid((unsigned)((T + 7) / 8)), block(256);
     if (q.stages) {
         const int64_t entries = T * K;
+        const float2* part = (const float2*)scratch;
         c->launches += 1;
-        launch_after(ds_dot_k, dim3((unsigned)((entries + 7) / 8)), dim3(256), 0, s, entries, K, V, c->C, ids, (const uint4*)h, (const uint4*)W, p.dots);
-        const int grid = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
-        join(nullptr, nullptr, grid, kSmTokens, (const float2*)scratch);
+        launch_after(ds_dot_k, dim3((unsigned)((entries + 7) / 8)), block, 0, s, entries, K, V, c->C, ids, (const uint4*)h, (const uint4*)W, p.dots);
+        const int parts = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
+        ds_per(K, [&](auto per) {
+            launch_after(ds_join_k<decltype(per)::value, false>, grid, block, 0, s, T, K, V, nullptr, nullptr, parts, kSmTokens, part, p.dots, K, nullptr,
+                         nullptr, ids, z, z_f32, k2, inv_tau, loss, lse, logp, c->op_status);
+        });
         return true;
     }
     launch_ds_sort<false>(c, p, T, V, K, ids, z, z_f32, inv_tau, nullptr, logp, s);
     CeArgs a = {};
-    a.entries = p.entries; a.first_entry = p.first; a.blocks = p.blocks; a.K = K; a.dots = p.dots;
+    a.cols = p.cols; a.values = p.dots; a.from = p.first; a.entries = p.entries; a.blocks = p.blocks;
     if (!launch_ce_stats<CE_PICK>(c, p.ce, a, T, V, h, W, p.target, scale, loss, lse, s)) return false;
-    join(p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad, p.ce.part);
+    ds_per(K, [&](auto per) {
+        launch_after(ds_join_k<decltype(per)::value, true>, grid, block, 0, s, T, K, V, p.ce.live, p.ce.rows, 2 * p.ce.n_tiles, p.ce.Tpad, p.ce.part, p.dots,
+                     p.entries, p.order, p.weights, nullptr, nullptr, 0, k2, inv_tau, loss, lse, logp, nullptr);
+    });
     return true;
 }
 
@@ -318,7 +338,7 @@ bool launch_linear_distill_bwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
     const DsPlan p = plan_ds(T, V, K, c->C, 1, scratch);
     launch_ds_sort<true>(c, p, T, V, K, ids, z, z_f32, inv_tau, logp, nullptr, s);
     CeArgs a = {};
-    a.entries = p.entries; a.first_entry = p.first; a.blocks = p.blocks; a.K = K;
+    a.cols = p.cols; a.values = p.weights; a.from = p.first; a.entries = p.entries; a.blocks = p.blocks;
     return launch_ce_grads<CE_PATCH>(c, p.ce, a, T, V, h, W, p.target, scale, lse, dloss, dh, dW, s);
 }
 
