@@ -30,10 +30,10 @@ struct SeqArgs {
     int T, S, W, range;                       // W ranges of `range` tokens, a multiple of kSeqStep
     const float *nll, *old, *ref, *adv, *dloss;
     const int64_t *target, *starts;
-    int token_adv, mean;
-    double log_lo, log_hi;                    // the borders of x
-    float lo0, lo1, hi0, hi1;                 // the fp32 numbers next to each, below (or at) and above
-    float held_lo, held_hi;                   // the borders of r
+    int mean;
+    double edge[2];                           // the borders of x under a positive advantage and of -x under a negative one,
+    float edge32[2], close[2];                // in fp32, and how close to it only 64 bits tell the side (below 0: never)
+    float held[2];                            // the borders of r
     double kl_weight, beta, margin, smoothing;
     float kl_slope;                           // kl_weight in fp32
     float *loss, *stats, *dnll;               // stats: [S][3], or the rewards [P][2]
@@ -91,15 +91,18 @@ struct SeqWalk {
     }
 };
 
-// Four fp32 of a lane; zeros behind the last token.
-__device__ __forceinline__ void seq_load(const float* p, int t, int T, float (&v)[4]) {
+// Four fp32 of a lane, as two pairs; zeros behind the last token.
+struct Quad { uint64_t lo, hi; };
+__device__ __forceinline__ Quad seq_load(const float* p, int t, int T, uint64_t policy) {
+    float v[4];
     if (t + 4 <= T) {
-        const uint4 q = ld_dep_stream(p + t);
-        v[0] = __uint_as_float(q.x); v[1] = __uint_as_float(q.y); v[2] = __uint_as_float(q.z); v[3] = __uint_as_float(q.w);
+        asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.f32 {%0, %1, %2, %3}, [%4], %5;"
+                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "l"(p + t), "l"(policy));
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = t + i < T ? p[t + i] : 0.f;
     }
+    return {pack2f(v[0], v[1]), pack2f(v[2], v[3])};
 }
 __device__ __forceinline__ void seq_store(float* p, int t, int T, const float (&v)[4]) {
     if (t + 4 <= T) {
@@ -110,46 +113,84 @@ __device__ __forceinline__ void seq_store(float* p, int t, int T, const float (&
             if (t + i < T) p[t + i] = v[i];
     }
 }
-// Which of a lane's four tokens have a target: the lanes read side by side (targets need not lie on 16 bytes) and vote.
-__device__ __forceinline__ uint4 seq_votes(const int64_t* target, int base, int T) {
-    uint32_t b[4];
-    const int lane = threadIdx.x & 31;
+__device__ __forceinline__ void seq_unpack(const Quad& q, float (&v)[4]) { unpack2f(q.lo, v[0], v[1]); unpack2f(q.hi, v[2], v[3]); }
+__device__ __forceinline__ Quad operator-(const Quad& a, const Quad& b) {      // rounded once
+    const uint64_t m = pack2f(-1.f, -1.f);
+    return {fma2(b.lo, m, a.lo), fma2(b.hi, m, a.hi)};
+}
+// What is read once leaves L2 first: a gradient that is scaled at the end should still be there.
+__device__ __forceinline__ uint64_t seq_once() {
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+// Which of a step's tokens have a target.  The lanes read side by side (targets need not lie on 16 bytes), and of each target only
+// the half that has the sign, and vote.
+struct Targets { int sign[4]; };
+__device__ __forceinline__ Targets seq_targets(const int64_t* target, int base, int T) {
+    Targets v;
+    const int t = base + (threadIdx.x & 31);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int t = base + i * 32 + lane;
-        b[i] = __ballot_sync(0xffffffffu, t < T && target[t] >= 0);
-    }
-    return make_uint4(b[0], b[1], b[2], b[3]);
+    for (int i = 0; i < 4; ++i) v.sign[i] = t + i * 32 < T ? reinterpret_cast<const int*>(target + t + i * 32)[1] : -1;
+    return v;
+}
+__device__ __forceinline__ uint4 seq_votes(const Targets& v) {
+    return make_uint4(__ballot_sync(0xffffffffu, v.sign[0] >= 0), __ballot_sync(0xffffffffu, v.sign[1] >= 0),
+                      __ballot_sync(0xffffffffu, v.sign[2] >= 0), __ballot_sync(0xffffffffu, v.sign[3] >= 0));
 }
 __device__ __forceinline__ uint32_t seq_mine(const uint4& b) {
     const int lane = threadIdx.x & 31;
     const uint32_t lo = lane & 8 ? b.y : b.x, hi = lane & 8 ? b.w : b.z;
     return (lane & 16 ? hi : lo) >> ((lane & 7) * 4) & 15u;
 }
-
-// e^d - 1 and e^d - 1 - d.  Below 1/2 the second is its series, whose terms from d^10 / 10! on are below 2^-28 of it; above, the
-// difference loses three bits at most.
-__device__ __forceinline__ void exp_terms(float d, float& e1, float& e2) {
-    const float p = fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, fmaf(d, 1.f / 9.f, 1.f) * (1.f / 8.f), 1.f) * (1.f / 7.f), 1.f) * (1.f / 6.f), 1.f) *
-                           (1.f / 5.f), 1.f) * (1.f / 4.f), 1.f) * (1.f / 3.f), 1.f);
-    const float small = d * d * 0.5f * p, e = expf(d) - 1.f;
-    const bool near = fabsf(d) < 0.5f;
-    e2 = near ? small : e - d;
-    e1 = near ? d + small : e;
+// Those of a lane's four tokens that lie in cur .. end.
+__device__ __forceinline__ uint32_t seq_within(int t, int cur, int end) {
+    const int lo = max(cur - t, 0), hi = min(end - t, 4);
+    return hi > lo ? (1u << hi) - (1u << lo) : 0u;
 }
 
-template <int OP>
+// e^q: q log2 e with the part of it that fp32 leaves out, so that only ex2's 2^-22 and two roundings are left of the error.
+__device__ __forceinline__ uint64_t exp_pair(uint64_t q) {
+    const float low = (float)(1.4426950408889634 - (double)kLog2e);
+    const uint64_t l = pack2f(kLog2e, kLog2e), n = pack2f(kLn2, kLn2), one = pack2f(1.f, 1.f);
+    const uint64_t t = mul2(q, l), minus = mul2(t, pack2f(-1.f, -1.f));
+    float a, b;
+    unpack2f(mul2(fma2(q, pack2f(low, low), fma2(q, l, minus)), n), a, b);
+    return mul2(ex2_pair(t), add2(one, pack2f(fminf(a, 0.01f), fminf(b, 0.01f))));      // of an infinite q the rest is NaN: it goes
+}
+// e^d - 1 - d by its series: for |d| < 1 the terms from d^12 / 12! on are below 2^-28 of it.
+__device__ __forceinline__ uint64_t exp_series(uint64_t d) {
+    const float c[10] = {1.f / 39916800, 1.f / 3628800, 1.f / 362880, 1.f / 40320, 1.f / 5040, 1.f / 720, 1.f / 120, 1.f / 24, 1.f / 6, 1.f / 2};
+    uint64_t h = pack2f(c[0], c[0]);
+#pragma unroll
+    for (int i = 1; i < 10; ++i) h = fma2(h, d, pack2f(c[i], c[i]));
+    return mul2(mul2(d, d), h);
+}
+
+template <int OP, bool REF, bool EACH>                       // EACH: an advantage for each token
 __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w) {
     const int lane = threadIdx.x & 31, lo = w * a.range, hi = a.T - lo < a.range ? a.T : lo + a.range;
-    const float* p0 = OP == SEQ_POLICY && !a.token_adv ? a.adv : nullptr;
+    const float* p0 = OP == SEQ_POLICY && !EACH ? a.adv : nullptr;
     const float* p1 = OP == SEQ_POLICY && a.dnll && !a.mean ? a.dloss : nullptr;       // a gradient that needs nothing else
+    const uint64_t once = seq_once();
+    Targets target;
+    Quad nll, old = {0, 0}, ref = {0, 0}, adv = {0, 0};
+    auto fetch = [&](int base) {
+        const int t = base + lane * 4;
+        target = seq_targets(a.target, base, a.T);
+        nll = seq_load(a.nll, t, a.T, once);
+        if (OP == SEQ_POLICY) old = seq_load(a.old, t, a.T, once);
+        if (REF) ref = seq_load(a.ref, t, a.T, once);
+        if (EACH) adv = seq_load(a.adv, t, a.T, once);
+    };
+    fetch(lo);
     SeqWalk k;
     k.locate(a, lo, p0, p1);
     bool began = k.s >= 0 && seq_start(a, k.s) >= lo;
     double sa = 0, sb = 0;
     int sn = 0, sc = 0;
     auto flush = [&](SeqSum* to) {
-        const double x = warp_sum(sa), y = OP == SEQ_POLICY ? warp_sum(sb) : 0.0;
+        const double x = warp_sum(sa), y = REF && OP == SEQ_POLICY ? warp_sum(sb) : 0.0;
         const int n = __reduce_add_sync(0xffffffffu, sn), c = OP == SEQ_POLICY ? __reduce_add_sync(0xffffffffu, sc) : 0;
         if (lane == 0) { to->a = x; to->b = y; to->n = n; to->c = c; }
         sa = sb = 0;
@@ -158,65 +199,84 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w) {
     bool open = true;
     for (int base = lo; base < hi; base += kSeqStep) {
         const int t = base + lane * 4, stop = min(base + kSeqStep, hi);
-        const uint4 votes = seq_votes(a.target, base, a.T);
+        const uint4 votes = seq_votes(target);
         const uint32_t mine = seq_mine(votes);
-        float nll[4], x[4], r[4], e1[4], e2[4], adv[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-        seq_load(a.nll, t, a.T, nll);
-        uint32_t over = 0, under = 0;
+        float q[4], r[4], e1[4], e2[4], A[4], g[4] = {0.f, 0.f, 0.f, 0.f};
+        const Quad n0 = nll, o0 = old;
         if (OP == SEQ_POLICY) {
-            seq_load(a.old, t, a.T, x);
-            if (a.token_adv) seq_load(a.adv, t, a.T, adv);
+            const Quad x = old - nll;
+            seq_unpack(x, q);
+            seq_unpack({exp_pair(x.lo), exp_pair(x.hi)}, r);
+            if (REF) {
+                const Quad d = nll - ref, y = {exp_series(d.lo), exp_series(d.hi)};
+                seq_unpack({add2(d.lo, y.lo), add2(d.hi, y.hi)}, e1);
+                seq_unpack(y, e2);
+                float f[4];
+                seq_unpack(d, f);
+                if (!(fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))) < 1.f)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float q = x[i] - nll[i];                    // rounded once: only next to a border may that move it across
-                bool up = q > a.hi1, down = q < a.lo0;
-                if (q >= a.hi0 && q <= a.hi1) up = (double)x[i] - (double)nll[i] > a.log_hi;
-                if (q >= a.lo0 && q <= a.lo1) down = (double)x[i] - (double)nll[i] < a.log_lo;
-                over |= (uint32_t)up << i;
-                under |= (uint32_t)down << i;
-                r[i] = expf(q);
+                    for (int i = 0; i < 4; ++i)
+                        if (!(fabsf(f[i]) < 1.f)) { e1[i] = expf(f[i]) - 1.f; e2[i] = e1[i] == INFINITY ? e1[i] : e1[i] - f[i]; }
+                }
             }
-            if (a.ref) {
-                seq_load(a.ref, t, a.T, x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) exp_terms(nll[i] - x[i], e1[i], e2[i]);
-            }
+            if (EACH) seq_unpack(adv, A);
         } else {
             if (a.bits && lane == 0) a.bits[base / kSeqStep] = votes;
-            if (a.ref) {
-                seq_load(a.ref, t, a.T, x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] -= nll[i];
+            if (REF) {
+                seq_unpack(ref - nll, q);
             } else {
+                seq_unpack(nll, q);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = -nll[i];
+                for (int i = 0; i < 4; ++i) q[i] = -q[i];
             }
         }
+        if (base + kSeqStep < hi) fetch(base + kSeqStep);
         for (int cur = base; cur < stop;) {
             const int end = min(k.next, stop);
             if (k.s >= 0 && k.s < a.S) {
+                const uint32_t in = mine & seq_within(t, cur, end);
+                sn += __popc(in);
                 float pa = 0.f, pb = 0.f;
+                if (OP == SEQ_POLICY) {
+                    const float slope = a.mean ? 1.f : k.v1, kl_slope = a.kl_slope * slope;
+                    float held = 0.f, edge = 0.f, close = 0.f, sign = 1.f, adv_i = k.v0;
+                    int side = 0;
+                    auto choose = [&](float x) {                  // 0: no border
+                        adv_i = x;
+                        side = x < 0.f;
+                        sign = x < 0.f ? -1.f : 1.f;
+                        held = a.held[side];
+                        edge = x != 0.f ? a.edge32[side] : INFINITY;
+                        close = x != 0.f ? a.close[side] : -1.f;
+                    };
+                    if (!EACH) choose(k.v0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (!(mine >> i & 1u) || t + i < cur || t + i >= end) continue;
-                    ++sn;
-                    if (OP == SEQ_POLICY) {
-                        const float A = a.token_adv ? adv[i] : k.v0;
-                        const bool up = (over >> i & 1u) && A > 0.f, cut = up || ((under >> i & 1u) && A < 0.f);
-                        sc += cut;
-                        pa -= A * (cut ? (up ? a.held_hi : a.held_lo) : r[i]);
-                        float slope = cut ? 0.f : A * r[i];
-                        if (a.ref) {
-                            pb += e2[i];
-                            slope = fmaf(a.kl_slope, e1[i], slope);
+                    for (int i = 0; i < 4; ++i) {
+                        if (EACH) choose(A[i]);
+                        const float x = q[i] * sign;
+                        bool cut = x > edge;
+                        if (fabsf(x - edge) <= close) {           // q is rounded; next to a border that may move it across
+                            float on[4], ox[4];
+                            seq_unpack(n0, on);
+                            seq_unpack(o0, ox);
+                            cut = ((double)ox[i] - (double)on[i]) * (double)sign > a.edge[side];
                         }
-                        g[i] = a.mean ? slope : slope * k.v1;
-                    } else {
-                        pa += x[i];
+                        const bool there = in >> i & 1u;
+                        sc += cut && there;
+                        pa -= there ? adv_i * (cut ? held : r[i]) : 0.f;
+                        float grad = cut ? 0.f : adv_i * slope * r[i];
+                        if (REF) {
+                            pb += there ? e2[i] : 0.f;
+                            grad = fmaf(kl_slope, e1[i], grad);
+                        }
+                        if (there) g[i] = grad;
                     }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pa += in >> i & 1u ? q[i] : 0.f;
                 }
                 sa += (double)pa;
-                if (OP == SEQ_POLICY) sb += (double)pb;
+                if (REF && OP == SEQ_POLICY) sb += (double)pb;
             }
             if (k.next <= stop) {                                 // the sequence ends here
                 if (k.s >= 0 && k.s < a.S) flush(began ? a.whole + k.s : a.head + w);
@@ -287,26 +347,39 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         }
     }
 }
-// The last pass over the gradient: a range's tokens times what their sequences give.
+// The last pass over the gradient: four steps of tokens times what their sequences give, all of them fetched first.
+constexpr int kScaleSteps = 4, kScaleRange = kScaleSteps * kSeqStep;
 template <int OP>
 __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
-    const int lane = threadIdx.x & 31, lo = w * a.range, hi = a.T - lo < a.range ? a.T : lo + a.range;
+    const int lane = threadIdx.x & 31, lo = w * kScaleRange, hi = a.T - lo < kScaleRange ? a.T : lo + kScaleRange;
+    Quad v[kScaleSteps];
+    uint32_t mine[kScaleSteps];
+    const uint64_t once = seq_once();
+#pragma unroll
+    for (int i = 0; i < kScaleSteps; ++i) {
+        const int base = lo + i * kSeqStep;
+        if (base >= hi) break;
+        if (OP == SEQ_POLICY) v[i] = seq_load(a.dnll, base + lane * 4, a.T, once);
+        else mine[i] = seq_mine(a.bits[base / kSeqStep]);
+    }
     SeqWalk k;
     k.locate(a, lo, a.coef, nullptr);
-    for (int base = lo; base < hi; base += kSeqStep) {
+#pragma unroll
+    for (int i = 0; i < kScaleSteps; ++i) {
+        const int base = lo + i * kSeqStep;
+        if (base >= hi) break;
         const int t = base + lane * 4, stop = min(base + kSeqStep, hi);
-        float v[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t mine = 0;
-        if (OP == SEQ_POLICY) seq_load(a.dnll, t, a.T, v);
-        else mine = seq_mine(a.bits[base / kSeqStep]);
+        float x[4], g[4] = {0.f, 0.f, 0.f, 0.f};
+        if (OP == SEQ_POLICY) seq_unpack(v[i], x);
         for (int cur = base; cur < stop;) {
             const int end = min(k.next, stop);
             if (k.s >= 0 && k.s < a.S) {
+                const uint32_t in = seq_within(t, cur, end);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (t + i < cur || t + i >= end) continue;
-                    if (OP == SEQ_POLICY) g[i] = v[i] == 0.f ? 0.f : v[i] * k.v0;          // tokens that do not count stay 0
-                    else g[i] = mine >> i & 1u ? k.v0 : 0.f;
+                for (int e = 0; e < 4; ++e) {
+                    if (!(in >> e & 1u)) continue;
+                    if (OP == SEQ_POLICY) g[e] = x[e] == 0.f ? 0.f : x[e] * k.v0;          // tokens that do not count stay 0
+                    else g[e] = mine[i] >> e & 1u ? k.v0 : 0.f;
                 }
             }
             if (k.next <= stop && end < hi) k.advance(a, end, a.coef, nullptr);
@@ -315,13 +388,15 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
         seq_store(a.dnll, t, a.T, g);
     }
 }
+__device__ __forceinline__ int seq_scale_warps(const SeqArgs& a) { return (a.T - 1) / kScaleRange + 1; }      // T > 0
 
-template <int OP>
-__global__ void __launch_bounds__(kSeqBlock) seq_sum_k(const SeqArgs a) {
+// Four blocks an SM: as many ranges as are under way at once.
+template <int OP, bool REF, bool EACH>
+__global__ void __launch_bounds__(kSeqBlock, 4) seq_sum_k(const SeqArgs a) {
     pdl_wait();
     pdl_launch();
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < a.W) seq_sums<OP>(a, w);
+    if (w < a.W) seq_sums<OP, REF, EACH>(a, w);
 }
 template <int OP, int TEAM>
 __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
@@ -335,20 +410,20 @@ __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
     pdl_wait();
     pdl_launch();
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < a.W) seq_scale<OP>(a, w);
+    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w);
 }
 // A handful of tokens: the three one after another in one block.
-template <int OP>
+template <int OP, bool REF, bool EACH>
 __global__ void __launch_bounds__(1024) seq_one_k(const SeqArgs a) {
     pdl_wait();
     pdl_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, items = OP == SEQ_PAIR ? a.S / 2 : a.S;
-    if (warp < a.W) seq_sums<OP>(a, warp);
+    if (warp < a.W) seq_sums<OP, REF, EACH>(a, warp);
     __syncthreads();
     for (int i = warp; i < items; i += 32) seq_item<OP, 32>(a, i, lane);
     if (!a.dnll || (OP == SEQ_POLICY && !a.mean)) return;
     __syncthreads();
-    if (warp < a.W) seq_scale<OP>(a, warp);
+    if (warp < seq_scale_warps(a)) seq_scale<OP>(a, warp);
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
@@ -374,7 +449,7 @@ size_t seq_scratch_bytes(int64_t T, int64_t S) {
     return plan_seq(a, nullptr);
 }
 
-template <int OP>
+template <int OP, bool REF, bool EACH>
 static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStream_t s) {
     plan_seq(a, scratch);
     a.status = c->op_status;
@@ -382,37 +457,39 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
     if (a.T <= kSeqOne) {
         c->launches += 1;
-        launch_after(seq_one_k<OP>, dim3(1), dim3(1024), 0, s, a);
+        launch_after(seq_one_k<OP, REF, EACH>, dim3(1), dim3(1024), 0, s, a);
         return;
     }
     c->launches += 2;
-    launch_after(seq_sum_k<OP>, dim3(blocks), dim3(kSeqBlock), 0, s, a);
-    // few sequences are long ones, of many pieces each
-    if (items <= most) launch_after(seq_join_k<OP, kSeqBlock>, dim3(items), dim3(kSeqBlock), 0, s, a);
-    else launch_after(seq_join_k<OP, 32>, dim3(most), dim3(kSeqBlock), 0, s, a);
+    launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), 0, s, a);
+    // a warp adds up 32 pieces at a time: a block where sequences have more of them on average
+    const int warps = (items + kSeqBlock / 32 - 1) / (kSeqBlock / 32);
+    if (a.W > (int64_t)items * 32) launch_after(seq_join_k<OP, kSeqBlock>, dim3(items), dim3(kSeqBlock), 0, s, a);
+    else launch_after(seq_join_k<OP, 32>, dim3(warps < most ? warps : most), dim3(kSeqBlock), 0, s, a);
     if (!a.dnll || (OP == SEQ_POLICY && !a.mean)) return;
     c->launches += 1;
-    launch_after(seq_scale_k<OP>, dim3(blocks), dim3(kSeqBlock), 0, s, a);
+    const int scale = (a.T - 1) / kScaleRange + 1;
+    launch_after(seq_scale_k<OP>, dim3((scale + kSeqBlock / 32 - 1) / (kSeqBlock / 32)), dim3(kSeqBlock), 0, s, a);
 }
 
-// The fp32 numbers next to a border: the largest not above it and the one after.
-static void seq_border(double v, float& below, float& above) {
-    float f = (float)v;
-    if ((double)f > v) f = nextafterf(f, -INFINITY);
-    below = f;
-    above = nextafterf(f, INFINITY);
+// A border of x: its value, in fp32, and how close to that a log ratio rounded to fp32 has to be for its side to be in doubt
+// (a few units in the last place; where there is no border, never).
+static void seq_border(SeqArgs& a, int side, double edge, double held) {
+    a.edge[side] = edge;
+    a.edge32[side] = (float)edge;
+    a.close[side] = isinf(edge) ? -1.f : fabsf((float)edge) * 2.4e-7f + 1e-40f;
+    a.held[side] = (float)held;
 }
 void launch_policy_loss(const mhclite_ctx* c, int64_t T, int64_t S, const float* nll, const float* nll_old, const float* nll_ref,
                         const int64_t* target, const int64_t* starts, const float* adv, int token_adv, double clip_low, double clip_high,
                         double kl_weight, int mean, const float* dloss, float* loss, float* stats, float* dnll, void* scratch, cudaStream_t s) {
     SeqArgs a = {};
     a.T = (int)T; a.S = (int)S; a.nll = nll; a.old = nll_old; a.ref = nll_ref; a.adv = adv; a.dloss = dloss; a.target = target; a.starts = starts;
-    a.token_adv = token_adv; a.mean = mean; a.kl_weight = kl_weight; a.kl_slope = (float)kl_weight; a.loss = loss; a.stats = stats; a.dnll = dnll;
-    a.log_lo = log1p(-clip_low); a.log_hi = log1p(clip_high);
-    a.held_lo = (float)(1.0 - clip_low); a.held_hi = (float)(1.0 + clip_high);
-    seq_border(a.log_lo, a.lo0, a.lo1);
-    seq_border(a.log_hi, a.hi0, a.hi1);
-    launch_seq<SEQ_POLICY>(c, a, scratch, s);
+    a.mean = mean; a.kl_weight = kl_weight; a.kl_slope = (float)kl_weight; a.loss = loss; a.stats = stats; a.dnll = dnll;
+    seq_border(a, 0, log1p(clip_high), 1.0 + clip_high);
+    seq_border(a, 1, -log1p(-clip_low), 1.0 - clip_low);
+    if (nll_ref) token_adv ? launch_seq<SEQ_POLICY, true, true>(c, a, scratch, s) : launch_seq<SEQ_POLICY, true, false>(c, a, scratch, s);
+    else token_adv ? launch_seq<SEQ_POLICY, false, true>(c, a, scratch, s) : launch_seq<SEQ_POLICY, false, false>(c, a, scratch, s);
 }
 void launch_preference_loss(const mhclite_ctx* c, int64_t T, int64_t P, const float* nll, const float* nll_ref, const int64_t* target,
                             const int64_t* starts, double beta, double margin, double smoothing, int mean, const float* dloss, float* loss,
@@ -420,7 +497,8 @@ void launch_preference_loss(const mhclite_ctx* c, int64_t T, int64_t P, const fl
     SeqArgs a = {};
     a.T = (int)T; a.S = (int)(2 * P); a.nll = nll; a.ref = nll_ref; a.dloss = dloss; a.target = target; a.starts = starts; a.mean = mean;
     a.beta = beta; a.margin = margin; a.smoothing = smoothing; a.loss = loss; a.stats = reward; a.dnll = dnll;
-    launch_seq<SEQ_PAIR>(c, a, scratch, s);
+    if (nll_ref) launch_seq<SEQ_PAIR, true, false>(c, a, scratch, s);
+    else launch_seq<SEQ_PAIR, false, false>(c, a, scratch, s);
 }
 
 }  // namespace mhcl
