@@ -20,8 +20,13 @@ namespace mhcl {
 
 enum SeqOp { SEQ_POLICY = 0, SEQ_PAIR = 1 };
 constexpr int kSeqStep = 128;                 // tokens of a warp's step
-constexpr int kSeqWarps = 148 * 32;           // ranges at most (the plan gives the scratch's size, so it does not look at the device)
+constexpr int kScaleSteps = 4, kScaleRange = kScaleSteps * kSeqStep;      // of the last pass
 constexpr int kSeqBlock = 256;
+// Blocks an SM and steps in a warp's ring, and with them ranges at most: as many as are under way at once (of a B200's 148 SMs:
+// the plan gives the scratch's size, so it does not look at the device).
+__host__ __device__ constexpr int seq_blocks(int op) { return op == SEQ_POLICY ? 2 : 4; }
+__host__ __device__ constexpr int seq_stages(int op) { return op == SEQ_POLICY ? 4 : 3; }
+constexpr int seq_ranges(int op) { return 148 * seq_blocks(op) * (kSeqBlock / 32); }
 constexpr int kSeqOne = 32 * kSeqStep;        // up to here one block does it all in one launch
 
 struct SeqSum { double a, b; int n, c; };     // policy: pg, kl, tokens, clipped ones; preference: log ratio, -, tokens, -
@@ -39,7 +44,9 @@ struct SeqArgs {
     float *loss, *stats, *dnll;               // stats: [S][3], or the rewards [P][2]
     SeqSum *whole, *head, *tail;              // [S] complete ones; [W] the pieces at the ranges' begins and ends
     float* coef;                              // [S] what a gradient takes from its whole sequence
-    uint4* bits;                              // [steps] which tokens have a target (preference)
+    float* raw;                               // [T] the gradient without that (policy)
+    int* hint;                                // the sequence at every kScaleRange-th token
+    uint8_t* bits;                            // which of four tokens each have a target (preference)
     int* status;
 };
 
@@ -67,22 +74,32 @@ struct SeqWalk {
         v0 = __shfl_sync(0xffffffffu, c0, j);
         v1 = __shfl_sync(0xffffffffu, c1, j);
     }
-    __device__ __forceinline__ void locate(const SeqArgs& a, int cur, const float* p0, const float* p1) {
-        const int lane = threadIdx.x & 31;
-        int at = 0, n = a.S + 1;                              // starts <= cur: all before `at`, none from at + n on
-        while (n > 32) {
-            const int step = (n + 31) / 32, i = (lane + 1) * step - 1;
-            const int k = __popc(__ballot_sync(0xffffffffu, i < n && seq_start(a, at + i) <= cur));
-            at += k * step;
-            n = min(step, n - k * step);
-        }
-        base = at + __popc(__ballot_sync(0xffffffffu, lane < n && seq_start(a, at + lane) <= cur)) - 1;
-        bound = seq_start(a, base + 1 + lane);
-        const int i = base + lane;
+    // the sequence `to` is known, or found: eight probes a lane and round
+    __device__ __forceinline__ void enter(const SeqArgs& a, int to, int cur, const float* p0, const float* p1) {
+        const int lane = threadIdx.x & 31, i = to + lane;
         const bool in = i >= 0 && i < a.S;
+        base = to;
+        bound = seq_start(a, to + 1 + lane);
         c0 = p0 && in ? p0[i] : 0.f;
         c1 = p1 && in ? p1[i] : 0.f;
         take(0, cur);
+    }
+    __device__ __forceinline__ void locate(const SeqArgs& a, int cur, const float* p0, const float* p1) {
+        const int lane = threadIdx.x & 31;
+        int at = 0, n = a.S + 1;                              // starts <= cur: all before `at`, none from at + n on
+        while (n > 0) {
+            const int step = (n + 255) >> 8;
+            int k = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = (e * 32 + lane + 1) * step - 1;
+                k += i < n && seq_start(a, at + i) <= cur;
+            }
+            k = __reduce_add_sync(0xffffffffu, k);
+            at += k * step;
+            n = step == 1 ? 0 : min(step - 1, n - k * step);
+        }
+        enter(a, at - 1, cur, p0, p1);
     }
     __device__ __forceinline__ void advance(const SeqArgs& a, int cur, const float* p0, const float* p1) {
         const int j = __popc(__ballot_sync(0xffffffffu, bound <= cur));
@@ -91,19 +108,8 @@ struct SeqWalk {
     }
 };
 
-// Four fp32 of a lane, as two pairs; zeros behind the last token.
+// Four fp32 of a lane, as two pairs.
 struct Quad { uint64_t lo, hi; };
-__device__ __forceinline__ Quad seq_load(const float* p, int t, int T, uint64_t policy) {
-    float v[4];
-    if (t + 4 <= T) {
-        asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.f32 {%0, %1, %2, %3}, [%4], %5;"
-                     : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "l"(p + t), "l"(policy));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = t + i < T ? p[t + i] : 0.f;
-    }
-    return {pack2f(v[0], v[1]), pack2f(v[2], v[3])};
-}
 __device__ __forceinline__ void seq_store(float* p, int t, int T, const float (&v)[4]) {
     if (t + 4 <= T) {
         *reinterpret_cast<float4*>(p + t) = make_float4(v[0], v[1], v[2], v[3]);
@@ -124,25 +130,22 @@ __device__ __forceinline__ uint64_t seq_once() {
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
-// Which of a step's tokens have a target.  The lanes read side by side (targets need not lie on 16 bytes), and of each target only
-// the half that has the sign, and vote.
-struct Targets { int sign[4]; };
-__device__ __forceinline__ Targets seq_targets(const int64_t* target, int base, int T) {
-    Targets v;
-    const int t = base + (threadIdx.x & 31);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v.sign[i] = t + i * 32 < T ? reinterpret_cast<const int*>(target + t + i * 32)[1] : -1;
-    return v;
+// The steps of a warp come through a ring of its own in shared memory, STAGES - 1 of them under way: registers for a step ahead
+// spilled, and a spilled load is waited for.  A lane copies just what it will read, so that nothing is waited for between lanes.
+__device__ __forceinline__ void seq_copy16(uint32_t to, const void* p, int bytes, uint64_t policy) {       // zeros behind `bytes`
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(to), "l"(p), "r"(bytes), "l"(policy) : "memory");
 }
-__device__ __forceinline__ uint4 seq_votes(const Targets& v) {
-    return make_uint4(__ballot_sync(0xffffffffu, v.sign[0] >= 0), __ballot_sync(0xffffffffu, v.sign[1] >= 0),
-                      __ballot_sync(0xffffffffu, v.sign[2] >= 0), __ballot_sync(0xffffffffu, v.sign[3] >= 0));
+__device__ __forceinline__ void seq_copy8(uint32_t to, const int64_t* p, int bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ uint32_t seq_mine(const uint4& b) {
-    const int lane = threadIdx.x & 31;
-    const uint32_t lo = lane & 8 ? b.y : b.x, hi = lane & 8 ? b.w : b.z;
-    return (lane & 16 ? hi : lo) >> ((lane & 7) * 4) & 15u;
+__device__ __forceinline__ Quad seq_read(uint32_t at) {
+    Quad q;
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(q.lo), "=l"(q.hi) : "r"(at) : "memory");
+    return q;
 }
+// Bytes of a step: four targets a lane, and four fp32 a lane of each tensor.
+__host__ __device__ constexpr int seq_tensors(int op, bool ref, bool each) { return 1 + (op == SEQ_POLICY) + ref + each; }
+__host__ __device__ constexpr int seq_stage(int op, bool ref, bool each) { return 512 * (2 + seq_tensors(op, ref, each)); }
 // Those of a lane's four tokens that lie in cur .. end.
 __device__ __forceinline__ uint32_t seq_within(int t, int cur, int end) {
     const int lo = max(cur - t, 0), hi = min(end - t, 4);
@@ -167,25 +170,58 @@ __device__ __forceinline__ uint64_t exp_series(uint64_t d) {
     return mul2(mul2(d, d), h);
 }
 
-template <int OP, bool REF, bool EACH>                       // EACH: an advantage for each token
-__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w) {
+// What the border on an advantage's side asks for (none where it is 0).
+struct SeqSide {
+    float adv, sign, held, edge, close;
+    int side;
+    __device__ __forceinline__ void choose(const SeqArgs& a, float x) {
+        adv = x;
+        side = x < 0.f;
+        sign = side ? -1.f : 1.f;
+        held = side ? a.held[1] : a.held[0];
+        edge = x != 0.f ? (side ? a.edge32[1] : a.edge32[0]) : INFINITY;
+        close = x != 0.f ? (side ? a.close[1] : a.close[0]) : -1.f;
+    }
+};
+template <int OP, bool REF, bool EACH, int STAGES>           // EACH: an advantage for each token
+__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring) {
     const int lane = threadIdx.x & 31, lo = w * a.range, hi = a.T - lo < a.range ? a.T : lo + a.range;
     const float* p0 = OP == SEQ_POLICY && !EACH ? a.adv : nullptr;
     const float* p1 = OP == SEQ_POLICY && a.dnll && !a.mean ? a.dloss : nullptr;       // a gradient that needs nothing else
     const uint64_t once = seq_once();
-    Targets target;
-    Quad nll, old = {0, 0}, ref = {0, 0}, adv = {0, 0};
-    auto fetch = [&](int base) {
-        const int t = base + lane * 4;
-        target = seq_targets(a.target, base, a.T);
-        nll = seq_load(a.nll, t, a.T, once);
-        if (OP == SEQ_POLICY) old = seq_load(a.old, t, a.T, once);
-        if (REF) ref = seq_load(a.ref, t, a.T, once);
-        if (EACH) adv = seq_load(a.adv, t, a.T, once);
+    constexpr int STAGE = seq_stage(OP, REF, EACH);
+    const bool pairs = ((uintptr_t)a.target & 15) == 0;           // targets need not lie on 16 bytes
+    auto fetch = [&](int base, int slot) {
+        if (base < hi) {
+            const uint32_t to = ring + slot * STAGE + lane * 16;
+            const int t = base + lane * 4, left = a.T - t, bytes = left >= 4 ? 16 : left > 0 ? left * 4 : 0, from = left > 0 ? t : 0;
+            if (pairs && base + kSeqStep <= a.T) {
+                seq_copy16(to + lane * 16, a.target + t, 16, once);
+                seq_copy16(to + lane * 16 + 16, a.target + t + 2, 16, once);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) seq_copy8(to + lane * 16 + i * 8, i < left ? a.target + t + i : a.target, i < left ? 8 : 0);
+            }
+            seq_copy16(to + 1024, a.nll + from, bytes, once);
+            if (OP == SEQ_POLICY) seq_copy16(to + 1536, a.old + from, bytes, once);
+            if (REF) seq_copy16(to + 512 * (3 + (OP == SEQ_POLICY)), a.ref + from, bytes, once);
+            if (EACH) seq_copy16(to + STAGE - 512, a.adv + from, bytes, once);
+        }
+        cp_async_commit();
     };
-    fetch(lo);
+#pragma unroll
+    for (int i = 0; i < (STAGES > 1 ? STAGES - 1 : 1); ++i) fetch(lo + i * kSeqStep, i);
     SeqWalk k;
+    SeqSide z;
+    float slope = 0.f, kl_slope = 0.f;
+    auto arrive = [&] {                                           // at the next sequence
+        if (OP != SEQ_POLICY) return;
+        if (!EACH) z.choose(a, k.v0);
+        slope = a.mean ? 1.f : k.v1;
+        kl_slope = a.kl_slope * slope;
+    };
     k.locate(a, lo, p0, p1);
+    arrive();
     bool began = k.s >= 0 && seq_start(a, k.s) >= lo;
     double sa = 0, sb = 0;
     int sn = 0, sc = 0;
@@ -197,96 +233,122 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w) {
         sn = sc = 0;
     };
     bool open = true;
+    int slot = 0;
     for (int base = lo; base < hi; base += kSeqStep) {
         const int t = base + lane * 4, stop = min(base + kSeqStep, hi);
-        const uint4 votes = seq_votes(target);
-        const uint32_t mine = seq_mine(votes);
-        float q[4], r[4], e1[4], e2[4], A[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-        const Quad n0 = nll, o0 = old;
-        if (OP == SEQ_POLICY) {
+        cp_async_wait<(STAGES > 1 ? STAGES - 2 : 0)>();
+        const uint32_t at = ring + slot * STAGE;
+        const uint4 u = lds128(at + lane * 32), v = lds128(at + lane * 32 + 16);         // the halves with the sign
+        uint32_t mine = ~(u.y >> 31 | u.w >> 31 << 1 | v.y >> 31 << 2 | v.w >> 31 << 3) & 15u;
+        if (base + kSeqStep > a.T) mine &= seq_within(t, 0, a.T);
+        Quad nll = {0, 0}, old = {0, 0}, ref = {0, 0}, adv = {0, 0};
+        nll = seq_read(at + 1024 + lane * 16);
+        if (OP == SEQ_POLICY) old = seq_read(at + 1536 + lane * 16);
+        if (REF) ref = seq_read(at + 512 * (3 + (OP == SEQ_POLICY)) + lane * 16);
+        if (EACH) adv = seq_read(at + STAGE - 512 + lane * 16);
+        if (STAGES > 1) {                                         // into the slot of the step before
+            fetch(base + (STAGES - 1) * kSeqStep, slot == 0 ? STAGES - 1 : slot - 1);
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+        }
+        const bool none = !__any_sync(0xffffffffu, mine), whole = __all_sync(0xffffffffu, mine == 15u);
+        uint64_t q[2] = {0, 0}, r[2] = {0, 0}, e1[2] = {0, 0}, e2[2] = {0, 0};
+        float A[4], g[4] = {0.f, 0.f, 0.f, 0.f};
+        if (a.hint && lane == 0 && base % kScaleRange == 0) a.hint[base / kScaleRange] = k.s;
+        if (OP == SEQ_PAIR && a.bits) a.bits[t / 4] = (uint8_t)mine;
+        if (none) {
+        } else if (OP == SEQ_POLICY) {
             const Quad x = old - nll;
-            seq_unpack(x, q);
-            seq_unpack({exp_pair(x.lo), exp_pair(x.hi)}, r);
+            q[0] = x.lo; q[1] = x.hi;
+            r[0] = exp_pair(x.lo); r[1] = exp_pair(x.hi);
             if (REF) {
-                const Quad d = nll - ref, y = {exp_series(d.lo), exp_series(d.hi)};
-                seq_unpack({add2(d.lo, y.lo), add2(d.hi, y.hi)}, e1);
-                seq_unpack(y, e2);
+                const Quad d = nll - ref;
+                e2[0] = exp_series(d.lo); e2[1] = exp_series(d.hi);
+                e1[0] = add2(d.lo, e2[0]); e1[1] = add2(d.hi, e2[1]);
                 float f[4];
                 seq_unpack(d, f);
                 if (!(fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3]))) < 1.f)) {
+                    float u[4], v[4];
+                    seq_unpack({e1[0], e1[1]}, u);
+                    seq_unpack({e2[0], e2[1]}, v);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!(fabsf(f[i]) < 1.f)) { e1[i] = expf(f[i]) - 1.f; e2[i] = e1[i] == INFINITY ? e1[i] : e1[i] - f[i]; }
+                        if (!(fabsf(f[i]) < 1.f)) { u[i] = expf(f[i]) - 1.f; v[i] = u[i] == INFINITY ? u[i] : u[i] - f[i]; }
+                    e1[0] = pack2f(u[0], u[1]); e1[1] = pack2f(u[2], u[3]);
+                    e2[0] = pack2f(v[0], v[1]); e2[1] = pack2f(v[2], v[3]);
                 }
             }
             if (EACH) seq_unpack(adv, A);
+        } else if (REF) {
+            const Quad x = ref - nll;
+            q[0] = x.lo; q[1] = x.hi;
         } else {
-            if (a.bits && lane == 0) a.bits[base / kSeqStep] = votes;
-            if (REF) {
-                seq_unpack(ref - nll, q);
-            } else {
-                seq_unpack(nll, q);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = -q[i];
-            }
+            q[0] = mul2(nll.lo, pack2f(-1.f, -1.f)); q[1] = mul2(nll.hi, pack2f(-1.f, -1.f));
         }
-        if (base + kSeqStep < hi) fetch(base + kSeqStep);
-        for (int cur = base; cur < stop;) {
-            const int end = min(k.next, stop);
-            if (k.s >= 0 && k.s < a.S) {
-                const uint32_t in = mine & seq_within(t, cur, end);
-                sn += __popc(in);
-                float pa = 0.f, pb = 0.f;
-                if (OP == SEQ_POLICY) {
-                    const float slope = a.mean ? 1.f : k.v1, kl_slope = a.kl_slope * slope;
-                    float held = 0.f, edge = 0.f, close = 0.f, sign = 1.f, adv_i = k.v0;
-                    int side = 0;
-                    auto choose = [&](float x) {                  // 0: no border
-                        adv_i = x;
-                        side = x < 0.f;
-                        sign = x < 0.f ? -1.f : 1.f;
-                        held = a.held[side];
-                        edge = x != 0.f ? a.edge32[side] : INFINITY;
-                        close = x != 0.f ? a.close[side] : -1.f;
-                    };
-                    if (!EACH) choose(k.v0);
+        // adds up the tokens of `in`; ALL: every token of the step
+        auto tokens = [&](uint32_t in, auto ALL) {
+            constexpr bool all = decltype(ALL)::value;
+            sn += all ? 4 : __popc(in);
+            float x[4], v[4], y[4], d[4];
+            seq_unpack({q[0], q[1]}, x);
+            float pa = 0.f, pb = 0.f;
+            if (OP == SEQ_POLICY) {
+                seq_unpack({r[0], r[1]}, v);
+                seq_unpack({e1[0], e1[1]}, d);
+                seq_unpack({e2[0], e2[1]}, y);
+                bool cut[4];
+                float nearest = INFINITY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (EACH) z.choose(a, A[i]);
+                    const float o = x[i] * z.sign - z.edge;
+                    cut[i] = o > 0.f;
+                    nearest = EACH ? fminf(nearest, fabsf(o) - z.close) : fminf(nearest, fabsf(o));
+                }
+                if (nearest <= (EACH ? 0.f : z.close)) {          // x is rounded; next to a border that may move it across
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (EACH) choose(A[i]);
-                        const float x = q[i] * sign;
-                        bool cut = x > edge;
-                        if (fabsf(x - edge) <= close) {           // q is rounded; next to a border that may move it across
-                            float on[4], ox[4];
-                            seq_unpack(n0, on);
-                            seq_unpack(o0, ox);
-                            cut = ((double)ox[i] - (double)on[i]) * (double)sign > a.edge[side];
-                        }
-                        const bool there = in >> i & 1u;
-                        sc += cut && there;
-                        pa -= there ? adv_i * (cut ? held : r[i]) : 0.f;
-                        float grad = cut ? 0.f : adv_i * slope * r[i];
-                        if (REF) {
-                            pb += there ? e2[i] : 0.f;
-                            grad = fmaf(kl_slope, e1[i], grad);
-                        }
-                        if (there) g[i] = grad;
+                        if (EACH) z.choose(a, A[i]);
+                        if (!(fabsf(x[i] * z.sign - z.edge) <= z.close) || t + i >= a.T) continue;
+                        cut[i] = ((double)a.old[t + i] - (double)a.nll[t + i]) * (double)z.sign > (z.side ? a.edge[1] : a.edge[0]);
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) pa += in >> i & 1u ? q[i] : 0.f;
                 }
-                sa += (double)pa;
-                if (REF && OP == SEQ_POLICY) sb += (double)pb;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (EACH) z.choose(a, A[i]);
+                    const bool there = all || (in >> i & 1u);
+                    const float term = EACH ? z.adv * (cut[i] ? z.held : v[i]) : cut[i] ? z.held : v[i];
+                    if (cut[i] && there) ++sc;
+                    pa += there ? term : 0.f;
+                    float grad = (cut[i] ? 0.f : v[i]) * (z.adv * slope);
+                    if (REF) {
+                        pb += there ? y[i] : 0.f;
+                        grad = fmaf(kl_slope, d[i], grad);
+                    }
+                    g[i] = there ? grad : g[i];
+                }
+                pa *= EACH ? -1.f : -z.adv;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pa += all || (in >> i & 1u) ? x[i] : 0.f;
+            }
+            sa += (double)pa;
+            if (REF && OP == SEQ_POLICY) sb += (double)pb;
+        };
+        for (int cur = base; cur < stop;) {
+            const int end = min(k.next, stop);
+            if (!none && k.s >= 0 && k.s < a.S) {
+                if (whole && end - cur == kSeqStep) tokens(15u, std::true_type());
+                else tokens(mine & seq_within(t, cur, end), std::false_type());
             }
             if (k.next <= stop) {                                 // the sequence ends here
                 if (k.s >= 0 && k.s < a.S) flush(began ? a.whole + k.s : a.head + w);
                 open = end < hi;
-                if (open) k.advance(a, end, p0, p1);
+                if (open) { k.advance(a, end, p0, p1); arrive(); }
                 began = true;
             }
             cur = end;
         }
-        if (OP == SEQ_POLICY && a.dnll) seq_store(a.dnll, t, a.T, g);
+        if (OP == SEQ_POLICY && a.dnll) seq_store(a.raw, t, a.T, g);
     }
     if (open && k.s >= 0 && k.s < a.S) flush(began ? a.tail + w : a.head + w);
 }
@@ -348,29 +410,34 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
     }
 }
 // The last pass over the gradient: four steps of tokens times what their sequences give, all of them fetched first.
-constexpr int kScaleSteps = 4, kScaleRange = kScaleSteps * kSeqStep;
 template <int OP>
 __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
     const int lane = threadIdx.x & 31, lo = w * kScaleRange, hi = a.T - lo < kScaleRange ? a.T : lo + kScaleRange;
-    Quad v[kScaleSteps];
+    float4 v[kScaleSteps];
     uint32_t mine[kScaleSteps];
-    const uint64_t once = seq_once();
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i) {
         const int base = lo + i * kSeqStep;
         if (base >= hi) break;
-        if (OP == SEQ_POLICY) v[i] = seq_load(a.dnll, base + lane * 4, a.T, once);
-        else mine[i] = seq_mine(a.bits[base / kSeqStep]);
+        const int t = base + lane * 4;
+        if (OP == SEQ_PAIR) {
+            mine[i] = a.bits[t / 4];
+        } else if (base + kSeqStep <= a.T) {
+            v[i] = *reinterpret_cast<const float4*>(a.raw + t);
+        } else {
+            v[i] = make_float4(t < a.T ? a.raw[t] : 0.f, t + 1 < a.T ? a.raw[t + 1] : 0.f, t + 2 < a.T ? a.raw[t + 2] : 0.f, 0.f);
+            if (t + 3 < a.T) v[i].w = a.raw[t + 3];
+        }
     }
     SeqWalk k;
-    k.locate(a, lo, a.coef, nullptr);
+    k.enter(a, a.hint[w], lo, a.coef, nullptr);
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i) {
         const int base = lo + i * kSeqStep;
         if (base >= hi) break;
         const int t = base + lane * 4, stop = min(base + kSeqStep, hi);
         float x[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-        if (OP == SEQ_POLICY) seq_unpack(v[i], x);
+        if (OP == SEQ_POLICY) { x[0] = v[i].x; x[1] = v[i].y; x[2] = v[i].z; x[3] = v[i].w; }
         for (int cur = base; cur < stop;) {
             const int end = min(k.next, stop);
             if (k.s >= 0 && k.s < a.S) {
@@ -390,13 +457,13 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
 }
 __device__ __forceinline__ int seq_scale_warps(const SeqArgs& a) { return (a.T - 1) / kScaleRange + 1; }      // T > 0
 
-// Four blocks an SM: as many ranges as are under way at once.
 template <int OP, bool REF, bool EACH>
-__global__ void __launch_bounds__(kSeqBlock, 4) seq_sum_k(const SeqArgs a) {
+__global__ void __launch_bounds__(kSeqBlock, seq_blocks(OP)) seq_sum_k(const SeqArgs a) {
+    extern __shared__ __align__(16) unsigned char sm_raw[];
     pdl_wait();
     pdl_launch();
-    const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < a.W) seq_sums<OP, REF, EACH>(a, w);
+    const int warp = threadIdx.x >> 5, w = blockIdx.x * (kSeqBlock / 32) + warp;
+    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH));
 }
 template <int OP, int TEAM>
 __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
@@ -415,10 +482,11 @@ __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
 // A handful of tokens: the three one after another in one block.
 template <int OP, bool REF, bool EACH>
 __global__ void __launch_bounds__(1024) seq_one_k(const SeqArgs a) {
+    extern __shared__ __align__(16) unsigned char sm_raw[];
     pdl_wait();
     pdl_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, items = OP == SEQ_PAIR ? a.S / 2 : a.S;
-    if (warp < a.W) seq_sums<OP, REF, EACH>(a, warp);
+    if (warp < a.W) seq_sums<OP, REF, EACH, 1>(a, warp, smem_u32(sm_raw) + warp * seq_stage(OP, REF, EACH));
     __syncthreads();
     for (int i = warp; i < items; i += 32) seq_item<OP, 32>(a, i, lane);
     if (!a.dnll || (OP == SEQ_POLICY && !a.mean)) return;
@@ -427,46 +495,57 @@ __global__ void __launch_bounds__(1024) seq_one_k(const SeqArgs a) {
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
-static size_t plan_seq(SeqArgs& a, void* base) {
+static size_t plan_seq(int op, SeqArgs& a, void* base) {
     char* b = (char*)base;
     size_t off = 0;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     const int steps = (a.T + kSeqStep - 1) / kSeqStep;
-    a.range = (int)((steps + (int64_t)kSeqWarps - 1) / kSeqWarps) * kSeqStep;
+    a.range = (steps + seq_ranges(op) - 1) / seq_ranges(op) * kSeqStep;
     if (a.range == 0) a.range = kSeqStep;
     a.W = (int)(((int64_t)a.T + a.range - 1) / a.range);
     a.whole = (SeqSum*)take((size_t)a.S * sizeof(SeqSum));
     a.head = (SeqSum*)take((size_t)a.W * sizeof(SeqSum));
     a.tail = (SeqSum*)take((size_t)a.W * sizeof(SeqSum));
     a.coef = (float*)take((size_t)a.S * 4);
-    a.bits = (uint4*)take((size_t)steps * 16);
+    a.bits = (uint8_t*)take((size_t)steps * 32);
+    a.hint = (int*)take((size_t)(steps + kScaleSteps - 1) / kScaleSteps * 4);
+    a.raw = a.dnll;
     return off;
 }
 size_t seq_scratch_bytes(int64_t T, int64_t S) {
     SeqArgs a = {};
     a.T = (int)T;
     a.S = (int)S;
-    return plan_seq(a, nullptr);
+    const size_t p = plan_seq(SEQ_POLICY, a, nullptr), q = plan_seq(SEQ_PAIR, a, nullptr);
+    return p > q ? p : q;
 }
 
 template <int OP, bool REF, bool EACH>
 static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStream_t s) {
-    plan_seq(a, scratch);
+    plan_seq(OP, a, scratch);
     a.status = c->op_status;
-    if (OP == SEQ_POLICY || !a.dnll) a.bits = nullptr;
+    const bool scaled = a.dnll && !(OP == SEQ_POLICY && !a.mean);
+    if (!scaled) a.hint = nullptr;
+    if (OP == SEQ_POLICY || !scaled) a.bits = nullptr;
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
     if (a.T <= kSeqOne) {
         c->launches += 1;
-        launch_after(seq_one_k<OP, REF, EACH>, dim3(1), dim3(1024), 0, s, a);
+        constexpr int bytes = 32 * seq_stage(OP, REF, EACH);
+        static SmemOnce once;
+        smem_limit(once, seq_one_k<OP, REF, EACH>, c->device, bytes);
+        launch_after(seq_one_k<OP, REF, EACH>, dim3(1), dim3(1024), bytes, s, a);
         return;
     }
     c->launches += 2;
-    launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), 0, s, a);
+    constexpr int ring = kSeqBlock / 32 * seq_stages(OP) * seq_stage(OP, REF, EACH);
+    static SmemOnce once;
+    smem_limit(once, seq_sum_k<OP, REF, EACH>, c->device, ring);
+    launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), ring, s, a);
     // a warp adds up 32 pieces at a time: a block where sequences have more of them on average
     const int warps = (items + kSeqBlock / 32 - 1) / (kSeqBlock / 32);
     if (a.W > (int64_t)items * 32) launch_after(seq_join_k<OP, kSeqBlock>, dim3(items), dim3(kSeqBlock), 0, s, a);
     else launch_after(seq_join_k<OP, 32>, dim3(warps < most ? warps : most), dim3(kSeqBlock), 0, s, a);
-    if (!a.dnll || (OP == SEQ_POLICY && !a.mean)) return;
+    if (!scaled) return;
     c->launches += 1;
     const int scale = (a.T - 1) / kScaleRange + 1;
     launch_after(seq_scale_k<OP>, dim3((scale + kSeqBlock / 32 - 1) / (kSeqBlock / 32)), dim3(kSeqBlock), 0, s, a);
