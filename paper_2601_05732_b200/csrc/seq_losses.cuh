@@ -16,6 +16,8 @@
 // Sums: four tokens in fp32, from there in 64 bits.
 #pragma once
 
+#include <stddef.h>
+
 namespace mhcl {
 
 enum SeqOp { SEQ_POLICY = 0, SEQ_PAIR = 1 };
@@ -27,7 +29,10 @@ constexpr int kSeqBlock = 256;
 __host__ __device__ constexpr int seq_blocks(int op) { return op == SEQ_POLICY ? 2 : 4; }
 __host__ __device__ constexpr int seq_stages(int op) { return op == SEQ_POLICY ? 4 : 3; }
 constexpr int seq_ranges(int op) { return 148 * seq_blocks(op) * (kSeqBlock / 32); }
-constexpr int kSeqOne = 32 * kSeqStep;        // up to here one block does it all in one launch
+constexpr int kSeqOne = 16 * kSeqStep;        // up to here one block does it all in one launch,
+constexpr int kSeqOneS = 511;                 // (with up to that many sequences all in shared memory)
+constexpr int kSeqCluster = 32768;            // up to here one cluster of eight
+constexpr int kSeqClusterWarps = 8 * 16;
 
 struct SeqSum { double a, b; int n, c; };     // policy: pg, kl, tokens, clipped ones; preference: log ratio, -, tokens, -
 
@@ -183,8 +188,9 @@ struct SeqSide {
         close = x != 0.f ? (side ? a.close[1] : a.close[0]) : -1.f;
     }
 };
-template <int OP, bool REF, bool EACH, int STAGES>           // EACH: an advantage for each token
-__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring) {
+// `ready` is called between the first copies and the first look at the starts.
+template <int OP, bool REF, bool EACH, int STAGES, typename F>          // EACH: an advantage for each token
+__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring, F ready) {
     const int lane = threadIdx.x & 31, lo = w * a.range, hi = a.T - lo < a.range ? a.T : lo + a.range;
     const float* p0 = OP == SEQ_POLICY && !EACH ? a.adv : nullptr;
     const float* p1 = OP == SEQ_POLICY && a.dnll && !a.mean ? a.dloss : nullptr;       // a gradient that needs nothing else
@@ -220,6 +226,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring)
         slope = a.mean ? 1.f : k.v1;
         kl_slope = a.kl_slope * slope;
     };
+    ready();
     k.locate(a, lo, p0, p1);
     arrive();
     bool began = k.s >= 0 && seq_start(a, k.s) >= lo;
@@ -353,25 +360,33 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring)
     if (open && k.s >= 0 && k.s < a.S) flush(began ? a.tail + w : a.head + w);
 }
 
-// The sums of sequence s over a team of threads (a warp or a block of 256): all threads of the team get them.
+// The sums of sequence s over a team of threads (half a warp, a warp or a block of 256): all threads of the team get them.
 template <int TEAM>
 __device__ __forceinline__ SeqSum seq_total(const SeqArgs& a, int s, int member) {
+    const int64_t from = a.starts[s], to = a.starts[s + 1];
     const int b = seq_start(a, s), e = seq_start(a, s + 1);
     SeqSum t = {0.0, 0.0, 0, 0};
-    if (member == 0 && (a.starts[s] < 0 || a.starts[s] > a.starts[s + 1] || a.starts[s + 1] > a.T))
-        report_index(a.status, MHCLITE_OP_SEQUENCES, s, a.starts[s]);
-    if (b >= e) return t;
-    const int w0 = b / a.range, w1 = (e - 1) / a.range;
-    if (w0 == w1) return a.whole[s];
+    if (member == 0 && (from < 0 || from > to || to > a.T)) report_index(a.status, MHCLITE_OP_SEQUENCES, s, from);
+    const int w0 = b / a.range, w1 = b < e ? (e - 1) / a.range : w0 - 1;
+    if (w0 == w1) {
+        if (member == 0) t = a.whole[s];
+    } else {
 #pragma unroll 4
-    for (int w = w0 + member; w <= w1; w += TEAM) {
-        const SeqSum p = w == w0 ? a.tail[w] : a.head[w];
-        t.a += p.a; t.b += p.b; t.n += p.n; t.c += p.c;
+        for (int w = w0 + member; w <= w1; w += TEAM) {
+            const SeqSum p = w == w0 ? a.tail[w] : a.head[w];
+            t.a += p.a; t.b += p.b; t.n += p.n; t.c += p.c;
+        }
     }
-    t.a = warp_sum(t.a); t.b = warp_sum(t.b);
-    t.n = __reduce_add_sync(0xffffffffu, t.n); t.c = __reduce_add_sync(0xffffffffu, t.c);
+    __syncwarp();
+#pragma unroll
+    for (int o = TEAM < 32 ? TEAM / 2 : 16; o > 0; o >>= 1) {
+        t.a += __shfl_xor_sync(0xffffffffu, t.a, o);
+        t.b += __shfl_xor_sync(0xffffffffu, t.b, o);
+        t.n += __shfl_xor_sync(0xffffffffu, t.n, o);
+        t.c += __shfl_xor_sync(0xffffffffu, t.c, o);
+    }
     if (TEAM > 32) {
-        __shared__ SeqSum part[TEAM / 32];
+        __shared__ SeqSum part[TEAM > 32 ? TEAM / 32 : 1];
         __syncthreads();                                          // from the sequence before
         if ((member & 31) == 0) part[member >> 5] = t;
         __syncthreads();
@@ -393,7 +408,15 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         a.stats[3 * i + 2] = (float)(w * t.b);
         if (a.dnll && a.mean) a.coef[i] = (float)(w * a.dloss[i]);
     } else {
-        const SeqSum c = seq_total<TEAM>(a, 2 * i, member), r = seq_total<TEAM>(a, 2 * i + 1, member);
+        SeqSum c, r;
+        if (TEAM == 32) {                                         // both sequences side by side, half a warp each
+            c = seq_total<16>(a, 2 * i + (member >> 4), member & 15);
+            r.a = __shfl_down_sync(0xffffffffu, c.a, 16);
+            r.n = __shfl_down_sync(0xffffffffu, c.n, 16);
+        } else {
+            c = seq_total<TEAM>(a, 2 * i, member);
+            r = seq_total<TEAM>(a, 2 * i + 1, member);
+        }
         if (member != 0) return;
         const double wc = a.mean ? (c.n ? 1.0 / c.n : 0.0) : 1.0, wr = a.mean ? (r.n ? 1.0 / r.n : 0.0) : 1.0;
         const double rc = a.beta * wc * c.a, rr = a.beta * wr * r.a, x = rc - rr - a.margin;
@@ -409,12 +432,14 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         }
     }
 }
-// The last pass over the gradient: four steps of tokens times what their sequences give, all of them fetched first.
-template <int OP>
-__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
+// The last pass over the gradient: four steps of tokens times what their sequences give.  All that seq_sums left is fetched
+// before `wait`, behind which the join's results are there.
+template <int OP, typename F>
+__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, F wait) {
     const int lane = threadIdx.x & 31, lo = w * kScaleRange, hi = a.T - lo < kScaleRange ? a.T : lo + kScaleRange;
     float4 v[kScaleSteps];
     uint32_t mine[kScaleSteps];
+    const int first = a.hint[w];
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i) {
         const int base = lo + i * kSeqStep;
@@ -429,8 +454,9 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
             if (t + 3 < a.T) v[i].w = a.raw[t + 3];
         }
     }
+    wait();
     SeqWalk k;
-    k.enter(a, a.hint[w], lo, a.coef, nullptr);
+    k.enter(a, first, lo, a.coef, nullptr);
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i) {
         const int base = lo + i * kSeqStep;
@@ -463,7 +489,7 @@ __global__ void __launch_bounds__(kSeqBlock, seq_blocks(OP)) seq_sum_k(const Seq
     pdl_wait();
     pdl_launch();
     const int warp = threadIdx.x >> 5, w = blockIdx.x * (kSeqBlock / 32) + warp;
-    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH));
+    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH), [] {});
 }
 template <int OP, int TEAM>
 __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
@@ -472,26 +498,58 @@ __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, member = threadIdx.x % TEAM;
     for (int i = blockIdx.x * (kSeqBlock / TEAM) + threadIdx.x / TEAM; i < items; i += gridDim.x * (kSeqBlock / TEAM)) seq_item<OP, TEAM>(a, i, member);
 }
+// The join's blocks let this kernel begin behind their own wait for seq_sum_k, so what that left may be read before the wait for
+// the join.
 template <int OP>
 __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
-    pdl_wait();
-    pdl_launch();
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w);
+    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w, [] { pdl_wait(); });
 }
-// A handful of tokens: the three one after another in one block.
-template <int OP, bool REF, bool EACH>
-__global__ void __launch_bounds__(1024) seq_one_k(const SeqArgs a) {
+// Few tokens: the three one after another in one launch, of one block or (CLUSTER) of eight.  One block keeps what its warps
+// exchange, and the starts, in shared memory, unless there are too many sequences.
+struct SeqShared {
+    alignas(16) float raw[kSeqOne];                               // stored by fours
+    int64_t starts[kSeqOneS + 1];
+    SeqSum whole[kSeqOneS], head[16], tail[16];
+    float coef[kSeqOneS];
+    uint8_t bits[kSeqOne / 4];
+    int hint[kSeqOne / kScaleRange];
+};
+constexpr int kSeqShared = sizeof(SeqShared);
+static_assert(alignof(SeqShared) == 16 && kSeqShared % 16 == 0 && offsetof(SeqShared, raw) % 16 == 0, "16-byte accesses");
+template <int OP, bool REF, bool EACH, bool CLUSTER>
+__global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
     extern __shared__ __align__(16) unsigned char sm_raw[];
+    constexpr int STAGES = CLUSTER ? 4 : 1;
+    SeqArgs a = args;
+    const int warps = gridDim.x * (blockDim.x >> 5), in = threadIdx.x >> 5, warp = in * gridDim.x + blockIdx.x, lane = threadIdx.x & 31;
+    const int items = OP == SEQ_PAIR ? a.S / 2 : a.S;
+    const uint32_t ring = smem_u32(sm_raw) + (CLUSTER ? 0 : kSeqShared) + in * STAGES * seq_stage(OP, REF, EACH);
+    const bool scaled = a.dnll && !(OP == SEQ_POLICY && !a.mean);
     pdl_wait();
     pdl_launch();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, items = OP == SEQ_PAIR ? a.S / 2 : a.S;
-    if (warp < a.W) seq_sums<OP, REF, EACH, 1>(a, warp, smem_u32(sm_raw) + warp * seq_stage(OP, REF, EACH));
-    __syncthreads();
-    for (int i = warp; i < items; i += 32) seq_item<OP, 32>(a, i, lane);
-    if (!a.dnll || (OP == SEQ_POLICY && !a.mean)) return;
-    __syncthreads();
-    if (warp < seq_scale_warps(a)) seq_scale<OP>(a, warp);
+    auto together = [] {
+        __syncwarp();
+        if (CLUSTER) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        else __syncthreads();
+    };
+    const bool kept = !CLUSTER && a.S <= kSeqOneS;
+    SeqShared* sh = reinterpret_cast<SeqShared*>(sm_raw);
+    auto ready = [&] {
+        if (!kept) return;
+        for (int i = threadIdx.x; i <= a.S; i += blockDim.x) sh->starts[i] = args.starts[i];
+        a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;
+        if (scaled) { a.raw = sh->raw; a.hint = sh->hint; }
+        if (a.bits) a.bits = sh->bits;
+        __syncthreads();
+    };
+    if (warp < a.W) seq_sums<OP, REF, EACH, STAGES>(a, warp, ring, ready);
+    else ready();
+    together();
+    for (int i = warp; i < items; i += warps) seq_item<OP, 32>(a, i, lane);
+    if (!scaled || a.T == 0) return;
+    together();
+    for (int w = warp; w < seq_scale_warps(a); w += warps) seq_scale<OP>(a, w, [] {});
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
@@ -500,7 +558,8 @@ static size_t plan_seq(int op, SeqArgs& a, void* base) {
     size_t off = 0;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     const int steps = (a.T + kSeqStep - 1) / kSeqStep;
-    a.range = (steps + seq_ranges(op) - 1) / seq_ranges(op) * kSeqStep;
+    const int most = a.T <= kSeqCluster ? kSeqClusterWarps : seq_ranges(op);
+    a.range = (steps + most - 1) / most * kSeqStep;
     if (a.range == 0) a.range = kSeqStep;
     a.W = (int)(((int64_t)a.T + a.range - 1) / a.range);
     a.whole = (SeqSum*)take((size_t)a.S * sizeof(SeqSum));
@@ -513,6 +572,7 @@ static size_t plan_seq(int op, SeqArgs& a, void* base) {
     return off;
 }
 size_t seq_scratch_bytes(int64_t T, int64_t S) {
+    if (T <= kSeqOne && S <= kSeqOneS) return 0;                  // one block has it all in shared memory
     SeqArgs a = {};
     a.T = (int)T;
     a.S = (int)S;
@@ -528,12 +588,18 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
     if (!scaled) a.hint = nullptr;
     if (OP == SEQ_POLICY || !scaled) a.bits = nullptr;
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
-    if (a.T <= kSeqOne) {
+    if (a.T <= kSeqCluster) {
         c->launches += 1;
-        constexpr int bytes = 32 * seq_stage(OP, REF, EACH);
-        static SmemOnce once;
-        smem_limit(once, seq_one_k<OP, REF, EACH>, c->device, bytes);
-        launch_after(seq_one_k<OP, REF, EACH>, dim3(1), dim3(1024), bytes, s, a);
+        constexpr int one = kSeqShared + 16 * seq_stage(OP, REF, EACH), eight = 16 * 4 * seq_stage(OP, REF, EACH);
+        if (a.T <= kSeqOne) {
+            static SmemOnce once;
+            smem_limit(once, seq_one_k<OP, REF, EACH, false>, c->device, one);
+            launch_after(seq_one_k<OP, REF, EACH, false>, dim3(1), dim3(512), one, s, a);
+        } else {
+            static SmemOnce once;
+            smem_limit(once, seq_one_k<OP, REF, EACH, true>, c->device, eight);
+            launch_cluster_after(seq_one_k<OP, REF, EACH, true>, dim3(8), dim3(512), 8, eight, s, a);
+        }
         return;
     }
     c->launches += 2;

@@ -149,7 +149,7 @@ def check_pair(c, k, mean, grad=True, beta=0.3, margin=0.2, e=0.1, t=None):
 
 
 SHAPES = [  # T, S, kind
-    (1, 2, "all"), (1, 2, "ones"), (2, 2, "ones"), (3, 4, "ones"), (127, 2, "even"), (128, 4, "even"), (129, 6, "empties"), (300, 300, "ones"),
+    (1, 2, "all"), (1, 2, "ones"), (2, 2, "ones"), (3, 4, "ones"), (127, 2, "even"), (128, 4, "even"), (129, 6, "empties"), (300, 300, "ones"), (600, 600, "ones"), (2048, 510, "even"), (2048, 512, "empties"), (2049, 20, "even"), (32768, 6, "even"), (32769, 100, "even"),
     (1000, 8, "even"), (4095, 40, "even"), (4096, 2, "all"), (4096, 32, "steps"), (4097, 10, "even"), (5000, 4000, "even"), (20000, 3000, "empties"),
     (33333, 2, "even"), (65536, 64, "steps"), (100001, 12, "even"), (700001, 6, "even"), (700001, 2, "all"), (1300000, 300, "empties"),
     (30000, 20000, "even"),
@@ -332,10 +332,11 @@ def test_refusals(ctx):
         ctx.preference_loss(t["nll"], t["ref"], t["target"], t["starts"], 0.1, 0.0, 0.0, False, loss[:2], reward, t["dpair"], t["ref"])
     with pytest.raises(bad):
         run_policy(ctx, k, {**t, "nll": torch.zeros(101, device=DEV)[1:]}, True)      # not on 16 bytes
-    need = ctx.lib.mhclite_policy_scratch_bytes(100, 4)
+    big = Case(5000, 4)
+    b, need = big.tensors(), ctx.lib.mhclite_policy_scratch_bytes(5000, 4)
     ws = torch.empty(need, dtype=torch.uint8, device=DEV)
-    args = [t[n].data_ptr() for n in ("nll", "old", "ref", "target", "starts", "adv")]
-    assert ctx.lib.mhclite_policy_loss(ctx._h, 100, 4, *args, 0, 0.2, 0.2, 0.1, 1, None, loss.data_ptr(), stats.data_ptr(), None, ws.data_ptr(),
+    args = [b[n].data_ptr() for n in ("nll", "old", "ref", "target", "starts", "adv")]
+    assert ctx.lib.mhclite_policy_loss(ctx._h, 5000, 4, *args, 0, 0.2, 0.2, 0.1, 1, None, loss.data_ptr(), stats.data_ptr(), None, ws.data_ptr(),
                                        need - 1, None) == binding.ERR_WORKSPACE
     check_policy(ctx, k, True)                                           # a refused call leaves the context usable
 

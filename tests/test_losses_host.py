@@ -27,12 +27,13 @@ def test_scratch_bytes_of_distillation():
 def test_scratch_bytes_of_sequences():
     lib = binding.load()
     p, q = lib.mhclite_policy_scratch_bytes, lib.mhclite_preference_scratch_bytes
-    assert p(1, 1) > 0 and p(0, 3) > 0 and q(1000, 4) == p(1000, 8) > 0
+    assert p(1, 1) == p(0, 3) == q(1000, 4) == 0                 # a handful of tokens needs none
+    assert p(10, 1000) > 0 and q(100000, 4) == p(100000, 8) > 0
     for bad in ((-1, 3), (10, -1), (2**31, 3), (2**62, 3), (10, 2**30), (10, 2**62)):
         assert p(*bad) == 0 and q(*bad) == 0, bad
-    assert q(10, 2**29) == 0 and p(2**31 - 257, 2**30 - 1) > 0
-    # a bit a token and 28 bytes a sequence; the pieces' number has a bound
-    assert p(2**24, 1000) < (2**24 // 8) + 64 * 1000 + (1 << 20)
+    assert q(100000, 2**29) == 0 and p(2**31 - 257, 2**30 - 1) > 0
+    # a byte for four tokens, 28 a sequence; the pieces' number has a bound
+    assert p(2**24, 1000) < (2**24 // 4) + 64 * 1000 + (1 << 20)
 
 
 def test_null_context_is_refused():
