@@ -61,8 +61,8 @@ __device__ __forceinline__ void ds_weights(DsRow<PER>& r, float inv_tau) {
 
 // A warp's 32 PER keys by rising value, key lane * PER + i in place i of a lane: Batcher's bitonic network, exchanges between
 // lanes where the distance reaches beyond one.
-template <int PER>
-__device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
+template <int PER, typename KEY>
+__device__ __forceinline__ void ds_sort(KEY (&key)[PER]) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int size = 2; size <= 32 * PER; size *= 2)
@@ -74,7 +74,7 @@ __device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
                 const bool small = ((lane & other) == 0) == ((lane * PER & size) == 0);
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
-                    const uint64_t y = __shfl_xor_sync(0xffffffffu, (unsigned long long)key[i], other);
+                    const KEY y = __shfl_xor_sync(0xffffffffu, key[i], other);
                     key[i] = (y < key[i]) == small ? y : key[i];
                 }
             } else {
@@ -82,7 +82,7 @@ __device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
                 for (int i = 0; i < PER; ++i) {
                     if (i & apart) continue;
                     const bool up = size < PER ? (i & size) == 0 : (lane * PER & size) == 0;
-                    const uint64_t x = key[i], y = key[i | apart];
+                    const KEY x = key[i], y = key[i | apart];
                     const bool swap = (y < x) == up;
                     key[i] = swap ? y : x;
                     key[i | apart] = swap ? x : y;
@@ -96,11 +96,17 @@ __device__ __forceinline__ void ds_sort(uint64_t (&key)[PER]) {
 // numbers in the caller's order (`order`) and the logarithms of their weights (`weights`, +inf where absent), for the backward
 // what the bracket is there, exp(logp) - the id's weights (`weights` too).  A warp a row.  Rows with a teacher get 0 in `target`, which ce_rows_k lists them by, others -1 and, in the
 // forward, logp 0.
-template <int PER, bool GRAD>
+// KEY holds id and number: 32 bits do for vocabularies below 2^23 (256 entries of 4099 rows: 24 -> 20 us).
+template <int PER, bool GRAD, typename KEY>
 __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, const int64_t* ids, const void* z, int z_f32, float inv_tau,
                                                  const float* logp_in, int entries, uint8_t* cols, uint8_t* order, float* weights,
                                                  uint16_t* first, int blocks, int64_t* target, float* logp, int* status) {
-    __shared__ int id_s[8][32 * PER];
+    constexpr int NUMBER = sizeof(KEY) == 4 ? 8 : 32;                   // bits of the number, below the id
+    constexpr KEY ABSENT = sizeof(KEY) == 4 ? 0x7FFFFF : 0x7FFFFFFF;
+    auto id_of = [](KEY k) { return (k >> NUMBER) == ABSENT ? 0x7FFFFFFF : (int)(k >> NUMBER); };
+    auto number_of = [](KEY k) { return (int)(k & (((KEY)1 << NUMBER) - 1)); };
+    auto place = [](int at) { return at + (at >> 3); };                 // lanes PER apart meet different banks
+    __shared__ int id_s[8][36 * PER];
     __shared__ float p_s[8][32 * PER], w_s[GRAD ? 8 : 1][GRAD ? 32 * PER : 1];
     pdl_wait();
     pdl_launch();
@@ -114,36 +120,36 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
             for (int k = lane; k < K; k += 32) logp[t * K + k] = 0.f;
         return;
     }
-    uint64_t key[PER];
+    KEY key[PER];
     ds_weights(r, inv_tau);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
         const int k = i * 32 + lane;
-        key[i] = (uint64_t)(uint32_t)(r.id[i] < 0 ? 0x7FFFFFFF : r.id[i]) << 32 | (uint32_t)k;       // as numbered where ids are equal
+        key[i] = (r.id[i] < 0 ? ABSENT : (KEY)r.id[i]) << NUMBER | (KEY)k;       // as numbered where ids are equal
         p_s[warp][k] = GRAD ? expf(r.z[i]) : r.id[i] < 0 ? INFINITY : r.z[i];
     }
     ds_sort(key);
     bool twice = false;
-    const int before = __shfl_up_sync(0xffffffffu, (int)(key[PER - 1] >> 32), 1);
+    const int before = __shfl_up_sync(0xffffffffu, id_of(key[PER - 1]), 1);
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int id = (int)(key[i] >> 32), prior = i ? (int)(key[i ? i - 1 : 0] >> 32) : lane ? before : -1;
-        id_s[warp][lane * PER + i] = id;
+        const int id = id_of(key[i]), prior = i ? id_of(key[i ? i - 1 : 0]) : lane ? before : -1;
+        id_s[warp][place(lane * PER + i)] = id;
         twice = twice || (id == prior && id != 0x7FFFFFFF);
     }
     __syncwarp();
     if (GRAD) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p_s[warp][(int)(uint32_t)key[i]];
+        for (int i = 0; i < PER; ++i) w_s[ws][lane * PER + i] = p_s[warp][number_of(key[i])];
         __syncwarp();
         if (__any_sync(0xffffffffu, twice)) {                           // an id's entries, which lie side by side, all get their sum
             for (int i = 0; i < PER; ++i) {
-                const int at = lane * PER + i, id = id_s[warp][at];
+                const int at = lane * PER + i, id = id_s[warp][place(at)];
                 if (id == 0x7FFFFFFF) continue;
                 int from = at;
-                while (from > 0 && id_s[warp][from - 1] == id) --from;
+                while (from > 0 && id_s[warp][place(from - 1)] == id) --from;
                 float sum = 0.f;
-                for (; from < 32 * PER && id_s[warp][from] == id; ++from) sum += w_s[ws][from];
+                for (; from < 32 * PER && id_s[warp][place(from)] == id; ++from) sum += w_s[ws][from];
                 p_s[warp][at] = sum;
             }
             __syncwarp();
@@ -153,7 +159,7 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
     }
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int at = lane * PER + i, id = (int)(key[i] >> 32), k = (int)(uint32_t)key[i];
+        const int at = lane * PER + i, id = id_of(key[i]), k = number_of(key[i]);
         if (at >= K) continue;
         cols[t * entries + at] = (uint8_t)(id & 127);
         if (GRAD) {
@@ -163,12 +169,13 @@ __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, co
             order[t * entries + at] = (uint8_t)k;
         }
     }
+#pragma unroll 4
     for (int b = lane; b <= blocks; b += 32) {
         int at = 0;
 #pragma unroll
         for (int step = 16 * PER; step > 0; step /= 2)                  // how many entries lie below the block
-            if (id_s[warp][at + step - 1] < b * 128) at += step;
-        at += id_s[warp][at] < b * 128;
+            if (id_s[warp][place(at + step - 1)] < b * 128) at += step;
+        at += id_s[warp][place(at)] < b * 128;
         first[t * (blocks + 1) + b] = (uint16_t)at;
     }
 }
@@ -200,7 +207,7 @@ __global__ void __launch_bounds__(256) ds_dot_k(int64_t entries, int K, int64_t 
 // of the listed rows with their entries as ds_sort_k left them (LISTED), or of all rows with the entries as they came (a handful
 // of tokens, with ds_dot_k's products).
 template <int PER, bool LISTED>
-__global__ void __launch_bounds__(256) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
+__global__ void __launch_bounds__(256, 4) ds_join_k(int64_t T, int K, int64_t V, const int* live, const int* rows, int n_parts, int pitch,
                                                  const float2* part, const float* dots, int entries, const uint8_t* order, const float* weights,
                                                  const int64_t* ids, const void* z, int z_f32, float k2, float inv_tau, float* loss, float* lse,
                                                  float* logp, int* status) {
@@ -297,7 +304,8 @@ static void launch_ds_sort(const mhclite_ctx* c, const DsPlan& p, int64_t T, int
                            float inv_tau, const float* logp_in, float* logp, cudaStream_t s) {
     c->launches += 1;
     ds_per(K, [&](auto per) {
-        launch_after(ds_sort_k<decltype(per)::value, GRAD>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, ids, z, z_f32, inv_tau, logp_in,
+        constexpr int PER = decltype(per)::value;
+        launch_after(V < (1 << 23) ? ds_sort_k<PER, GRAD, uint32_t> : ds_sort_k<PER, GRAD, unsigned long long>, dim3((unsigned)((T + 7) / 8)), dim3(256), 0, s, T, K, V, ids, z, z_f32, inv_tau, logp_in,
                      p.entries, p.cols, p.order, p.weights, p.first, p.blocks, p.target, logp, c->op_status);
     });
 }

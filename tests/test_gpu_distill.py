@@ -249,6 +249,29 @@ def test_offsets_beyond_32_bits(ctx_of):
         assert (lse - ref).abs().max() < 1e-4 and (logp - rq).abs().max() < 1e-4
 
 
+def test_vocabularies_beyond_23_bits(ctx_of):
+    """More rows than a row's entries are sorted by in 32 bits: ids near both ends, one of them twice, gradients with them."""
+    C, V, T = 8, (1 << 23) + 77, 40
+    c = ctx_of(C)
+    W = torch.empty(V, C, dtype=BF, device=DEV).normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    h, z, dloss = randn(7, T, C), randn(8, T, 5, dtype=F32), randn(9, T, dtype=F32)
+    ids = torch.tensor([V - 1, 5, (1 << 23) - 1, 5, V - 2], device=DEV).expand(T, 5).contiguous()
+    ids[3], ids[4, 2:] = -1, -1
+    loss, lse, logp, dh, dW = run(c, h, W, ids, z, 1.0, 1.0, dloss)
+    live, there = (ids >= 0).any(1), ids >= 0
+    hd, Wd = h.double() * live[:, None], W.double()
+    x = hd @ Wd.T
+    ref = torch.logsumexp(x, 1)
+    rq = torch.where(there, x.gather(1, ids.clamp(min=0)) - ref[:, None], 0.0)
+    # one step of 16 products, V / 256 sums of one sign in the longest chain: 2^-24 x V / 256 = 0.002 at most
+    assert ((lse - ref * live).abs() <= V / 256 * 2.0 ** -24).all() and ((logp - rq).abs() <= V / 256 * 2.0 ** -24).all()
+    p = torch.where(there, torch.softmax(torch.where(there, z.double(), -float("inf")), 1), 0.0)
+    G = torch.softmax(x, 1).scatter_add_(1, ids.clamp(min=0), -p) * (dloss.double() * live)[:, None]
+    for got, want, e in ((dh, G @ Wd, (G ** 2) @ (Wd ** 2)), (dW, G.T @ hd, (G ** 2).T @ (hd ** 2))):
+        assert (got.double() - want).norm() <= HALF * want.norm() + 4 * HALF * e.sum().sqrt() + V / 256 * 2.0 ** -24 * (G.abs() @ Wd.abs()).norm()
+    assert (dW[[5, V - 1]].double() - (G.T @ hd)[[5, V - 1]]).abs().max() <= HALF * 2 * (G.T @ hd)[[5, V - 1]].abs().max() + 1e-3
+
+
 def test_ids_beyond_the_table_are_reported():
     for T in (20, 50):
         c = binding.MhcLite(2, 64, 0)                             # a context of its own: the report stays
