@@ -29,10 +29,13 @@ constexpr int kSeqBlock = 256;
 __host__ __device__ constexpr int seq_blocks(int op) { return op == SEQ_POLICY ? 2 : 4; }
 __host__ __device__ constexpr int seq_stages(int op) { return op == SEQ_POLICY ? 4 : 3; }
 constexpr int seq_ranges(int op) { return 148 * seq_blocks(op) * (kSeqBlock / 32); }
-constexpr int kSeqOne = 16 * kSeqStep;        // up to here one block does it all in one launch,
-constexpr int kSeqOneS = 511;                 // (with up to that many sequences all in shared memory)
-constexpr int kSeqCluster = 32768;            // up to here one cluster of eight
-constexpr int kSeqClusterWarps = 8 * 16;
+// Up to so many tokens and sequences one block does it all in one launch, with what its warps exchange in shared memory, or one
+// cluster of eight (with the gradient, 1500 tokens 5.5 us on the device against 8 in three launches, 16384 8.1 against 8.2 of
+// which the host alone takes 7; at 65536 eight SMs take 11.7 against 8.4).
+constexpr int kSeqOne = 16 * kSeqStep, kSeqOneS = 511;
+constexpr int kSeqCluster = 32768, kSeqClusterS = 16384, kSeqClusterWarps = 8 * 16;
+inline bool seq_one(int64_t T, int64_t S) { return T <= kSeqOne && S <= kSeqOneS; }
+inline bool seq_cluster(int64_t T, int64_t S) { return T <= kSeqCluster && S <= kSeqClusterS; }
 
 struct SeqSum { double a, b; int n, c; };     // policy: pg, kl, tokens, clipped ones; preference: log ratio, -, tokens, -
 
@@ -137,11 +140,15 @@ __device__ __forceinline__ uint64_t seq_once() {
 }
 // The steps of a warp come through a ring of its own in shared memory, STAGES - 1 of them under way: registers for a step ahead
 // spilled, and a spilled load is waited for.  A lane copies just what it will read, so that nothing is waited for between lanes.
-__device__ __forceinline__ void seq_copy16(uint32_t to, const void* p, int bytes, uint64_t policy) {       // zeros behind `bytes`
-    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(to), "l"(p), "r"(bytes), "l"(policy) : "memory");
+__device__ __forceinline__ void seq_copy16(uint32_t to, const void* p, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(to), "l"(p), "l"(policy) : "memory");
 }
-__device__ __forceinline__ void seq_copy8(uint32_t to, const int64_t* p, int bytes) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(to), "l"(p), "r"(bytes) : "memory");
+// Element i of 4 or 8 bytes where one is left there.
+template <typename V>
+__device__ __forceinline__ void seq_copy(uint32_t to, const V* p, int i, int left) {
+    if (left <= 0) return;
+    if (sizeof(V) == 8) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(p + i) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(p + i) : "memory");
 }
 __device__ __forceinline__ Quad seq_read(uint32_t at) {
     Quad q;
@@ -200,18 +207,29 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
     auto fetch = [&](int base, int slot) {
         if (base < hi) {
             const uint32_t to = ring + slot * STAGE + lane * 16;
-            const int t = base + lane * 4, left = a.T - t, bytes = left >= 4 ? 16 : left > 0 ? left * 4 : 0, from = left > 0 ? t : 0;
-            if (pairs && base + kSeqStep <= a.T) {
-                seq_copy16(to + lane * 16, a.target + t, 16, once);
-                seq_copy16(to + lane * 16 + 16, a.target + t + 2, 16, once);
+            const int t = base + lane * 4;
+            if (base + kSeqStep <= a.T) {                         // the usual case
+                if (pairs) {
+                    seq_copy16(to + lane * 16, a.target + t, once);
+                    seq_copy16(to + lane * 16 + 16, a.target + t + 2, once);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) seq_copy(to + lane * 16 + i * 8, a.target + t, i, 1);
+                }
+                seq_copy16(to + 1024, a.nll + t, once);
+                if (OP == SEQ_POLICY) seq_copy16(to + 1536, a.old + t, once);
+                if (REF) seq_copy16(to + 512 * (3 + (OP == SEQ_POLICY)), a.ref + t, once);
+                if (EACH) seq_copy16(to + STAGE - 512, a.adv + t, once);
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) seq_copy8(to + lane * 16 + i * 8, i < left ? a.target + t + i : a.target, i < left ? 8 : 0);
+                for (int i = 0; i < 4; ++i) {
+                    seq_copy(to + lane * 16 + i * 8, a.target + t, i, a.T - t - i);
+                    seq_copy(to + 1024 + i * 4, a.nll + t, i, a.T - t - i);
+                    if (OP == SEQ_POLICY) seq_copy(to + 1536 + i * 4, a.old + t, i, a.T - t - i);
+                    if (REF) seq_copy(to + 512 * (3 + (OP == SEQ_POLICY)) + i * 4, a.ref + t, i, a.T - t - i);
+                    if (EACH) seq_copy(to + STAGE - 512 + i * 4, a.adv + t, i, a.T - t - i);
+                }
             }
-            seq_copy16(to + 1024, a.nll + from, bytes, once);
-            if (OP == SEQ_POLICY) seq_copy16(to + 1536, a.old + from, bytes, once);
-            if (REF) seq_copy16(to + 512 * (3 + (OP == SEQ_POLICY)), a.ref + from, bytes, once);
-            if (EACH) seq_copy16(to + STAGE - 512, a.adv + from, bytes, once);
         }
         cp_async_commit();
     };
@@ -247,7 +265,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
         const uint32_t at = ring + slot * STAGE;
         const uint4 u = lds128(at + lane * 32), v = lds128(at + lane * 32 + 16);         // the halves with the sign
         uint32_t mine = ~(u.y >> 31 | u.w >> 31 << 1 | v.y >> 31 << 2 | v.w >> 31 << 3) & 15u;
-        if (base + kSeqStep > a.T) mine &= seq_within(t, 0, a.T);
+        if (base + kSeqStep > a.T) mine &= seq_within(t, 0, a.T);       // behind the last token there is nothing
         Quad nll = {0, 0}, old = {0, 0}, ref = {0, 0}, adv = {0, 0};
         nll = seq_read(at + 1024 + lane * 16);
         if (OP == SEQ_POLICY) old = seq_read(at + 1536 + lane * 16);
@@ -403,9 +421,8 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         if (member != 0) return;
         const double w = a.mean ? (t.n ? 1.0 / t.n : 0.0) : 1.0;
         a.loss[i] = (float)(w * (t.a + a.kl_weight * t.b));
-        a.stats[3 * i] = (float)t.n;
-        a.stats[3 * i + 1] = (float)t.c;
-        a.stats[3 * i + 2] = (float)(w * t.b);
+        float* stats = a.stats + 3 * (int64_t)i;
+        stats[0] = (float)t.n; stats[1] = (float)t.c; stats[2] = (float)(w * t.b);
         if (a.dnll && a.mean) a.coef[i] = (float)(w * a.dloss[i]);
     } else {
         SeqSum c, r;
@@ -505,8 +522,8 @@ __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
     if (w < seq_scale_warps(a)) seq_scale<OP>(a, w, [] { pdl_wait(); });
 }
-// Few tokens: the three one after another in one launch, of one block or (CLUSTER) of eight.  One block keeps what its warps
-// exchange, and the starts, in shared memory, unless there are too many sequences.
+// Few tokens: the three one after another in one launch, of one block, which keeps what its warps exchange, and the starts, in
+// shared memory, or (CLUSTER) of eight.
 struct SeqShared {
     alignas(16) float raw[kSeqOne];                               // stored by fours
     int64_t starts[kSeqOneS + 1];
@@ -533,10 +550,9 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
         if (CLUSTER) asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
         else __syncthreads();
     };
-    const bool kept = !CLUSTER && a.S <= kSeqOneS;
     SeqShared* sh = reinterpret_cast<SeqShared*>(sm_raw);
     auto ready = [&] {
-        if (!kept) return;
+        if (CLUSTER) return;
         for (int i = threadIdx.x; i <= a.S; i += blockDim.x) sh->starts[i] = args.starts[i];
         a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;
         if (scaled) { a.raw = sh->raw; a.hint = sh->hint; }
@@ -558,7 +574,7 @@ static size_t plan_seq(int op, SeqArgs& a, void* base) {
     size_t off = 0;
     auto take = [&](size_t n) { char* at = b + off; off += (n + 255) & ~(size_t)255; return at; };
     const int steps = (a.T + kSeqStep - 1) / kSeqStep;
-    const int most = a.T <= kSeqCluster ? kSeqClusterWarps : seq_ranges(op);
+    const int most = seq_cluster(a.T, a.S) ? kSeqClusterWarps : seq_ranges(op);
     a.range = (steps + most - 1) / most * kSeqStep;
     if (a.range == 0) a.range = kSeqStep;
     a.W = (int)(((int64_t)a.T + a.range - 1) / a.range);
@@ -572,7 +588,7 @@ static size_t plan_seq(int op, SeqArgs& a, void* base) {
     return off;
 }
 size_t seq_scratch_bytes(int64_t T, int64_t S) {
-    if (T <= kSeqOne && S <= kSeqOneS) return 0;                  // one block has it all in shared memory
+    if (seq_one(T, S)) return 0;
     SeqArgs a = {};
     a.T = (int)T;
     a.S = (int)S;
@@ -588,10 +604,10 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
     if (!scaled) a.hint = nullptr;
     if (OP == SEQ_POLICY || !scaled) a.bits = nullptr;
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
-    if (a.T <= kSeqCluster) {
+    if (seq_cluster(a.T, a.S)) {                                  // every case of one block is one of these
         c->launches += 1;
         constexpr int one = kSeqShared + 16 * seq_stage(OP, REF, EACH), eight = 16 * 4 * seq_stage(OP, REF, EACH);
-        if (a.T <= kSeqOne) {
+        if (seq_one(a.T, a.S)) {
             static SmemOnce once;
             smem_limit(once, seq_one_k<OP, REF, EACH, false>, c->device, one);
             launch_after(seq_one_k<OP, REF, EACH, false>, dim3(1), dim3(512), one, s, a);

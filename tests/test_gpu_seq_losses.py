@@ -288,6 +288,33 @@ def test_bad_starts_are_reported_and_harmless():
         c.device_status()
 
 
+@pytest.mark.parametrize("T,S_", [(100, 600), (100, 40000), (40000, 90000)])
+def test_far_more_sequences_than_tokens(ctx, T, S_):
+    k = Case(T, S_, "even")
+    check_policy(ctx, k, True), check_pair(ctx, k, False)
+
+
+@pytest.mark.parametrize("T", [300, 20000, 50000])
+def test_impossible_tokens(ctx, T):
+    """A token of probability 0 under the model, or under the one that sampled it: infinities where the formula has them."""
+    k = Case(T, 6, dead=0.0, ref=False)
+    k.starts = np.linspace(0, T, 7).astype(np.int64)
+    k.adv = np.array([1.0, 1.0, -1.0, -1.0, 1.0, -1.0])
+    a = [int(v) + 3 for v in k.starts[:4]]
+    k.nll[[a[0], a[2]]], k.old[[a[1], a[3]]] = np.inf, np.inf          # ratios of 0, and infinite ones
+    loss, stats, dnll = run_policy(ctx, k, k.tensors(), False)
+    with np.errstate(invalid="ignore", over="ignore"):
+        rl, rs, rd = S.policy_loss(k.nll, k.old, None, k.target, k.starts, k.adv, False, 0.2, 0.3, 0.0, False, k.dloss)
+    assert np.array_equal(f64(stats)[:, 1], rs[:, 1]) and np.isinf(rl[3]) and np.isfinite(np.delete(rl, 3)).all()
+    assert np.array_equal(np.isinf(f64(loss)), np.isinf(rl)) and not np.isnan(f64(loss)).any()
+    for i in a[:3]:
+        assert rd[i] == 0 and dnll[i] == 0
+    k.ref = np.where(np.isinf(k.nll), 1.0, k.nll)                      # the divergence of such a token is infinite
+    k.nll[a[2]], k.old[[a[1], a[3]]] = 1.0, 1.0
+    loss, stats, _ = run_policy(ctx, k, k.tensors(), True)
+    assert torch.isposinf(loss[0]) and torch.isposinf(stats[0, 2]) and torch.isfinite(loss[1:]).all()
+
+
 def test_no_tokens_and_no_sequences(ctx):
     k = Case(0, 4)
     k.starts[:] = 0
