@@ -416,6 +416,7 @@ __device__ __forceinline__ SeqSum seq_total(const SeqArgs& a, int s, int member)
 // What item i (a sequence, or a pair of them) gives.
 template <int OP, int TEAM>
 __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
+    const float dloss = a.dnll && member == 0 ? a.dloss[i] : 0.f;       // fetched beside the sums
     if (OP == SEQ_POLICY) {
         const SeqSum t = seq_total<TEAM>(a, i, member);
         if (member != 0) return;
@@ -423,7 +424,7 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         a.loss[i] = (float)(w * (t.a + a.kl_weight * t.b));
         float* stats = a.stats + 3 * (int64_t)i;
         stats[0] = (float)t.n; stats[1] = (float)t.c; stats[2] = (float)(w * t.b);
-        if (a.dnll && a.mean) a.coef[i] = (float)(w * a.dloss[i]);
+        if (a.dnll && a.mean) a.coef[i] = (float)(w * dloss);
     } else {
         SeqSum c, r;
         if (TEAM == 32) {                                         // both sequences side by side, half a warp each
@@ -443,7 +444,7 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         a.stats[2 * i] = (float)rc;
         a.stats[2 * i + 1] = (float)rr;
         if (a.dnll) {
-            const double dx = a.dloss[i] * (a.smoothing - (x > 0 ? m : 1.0) / (1.0 + m));
+            const double dx = dloss * (a.smoothing - (x > 0 ? m : 1.0) / (1.0 + m));
             a.coef[2 * i] = (float)(-a.beta * wc * dx);
             a.coef[2 * i + 1] = (float)(a.beta * wr * dx);
         }
@@ -474,6 +475,15 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, F wait) {
     wait();
     SeqWalk k;
     k.enter(a, first, lo, a.coef, nullptr);
+    if (k.next >= hi && lo + kScaleRange <= a.T && k.v0 - k.v0 == 0.f) {               // the usual case: one sequence, or none (then v0 is 0)
+#pragma unroll
+        for (int i = 0; i < kScaleSteps; ++i) {
+            float4* to = reinterpret_cast<float4*>(a.dnll + lo + i * kSeqStep) + lane;
+            if (OP == SEQ_POLICY) *to = make_float4(v[i].x * k.v0, v[i].y * k.v0, v[i].z * k.v0, v[i].w * k.v0);
+            else *to = make_float4(mine[i] & 1u ? k.v0 : 0.f, mine[i] & 2u ? k.v0 : 0.f, mine[i] & 4u ? k.v0 : 0.f, mine[i] & 8u ? k.v0 : 0.f);
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i) {
         const int base = lo + i * kSeqStep;
