@@ -392,6 +392,11 @@ MHCLITE_API int mhclite_linear_ce_bwd(mhclite_ctx* ctx, int64_t T, int64_t V, co
                         const int64_t* target, float logit_scale, const float* lse, const float* dloss,
                         mhclite_bf16* dh, mhclite_bf16* dW, void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- behind a first training: distillation, policy and preference losses ------------------------------
+ *
+ * The same rules as around the stack: scratch as an argument, int64 tensors on 8 bytes and all others on 16, results the same bit
+ * for bit from run to run, indices that cannot be checked on the host reported through the status words. */
+
 /* Distillation from a teacher's top logits.  The student's distribution q = softmax(l / temperature) over the vocabulary, of
  * the logits l[t,v] = logit_scale <h[t,:], W[v,:]>, which are never stored, against the teacher's over its K entries of a row:
  *   lse[t] = log sum_v exp(l[t,v] / temperature)                                          [T] f32

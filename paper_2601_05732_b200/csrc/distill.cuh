@@ -4,6 +4,14 @@
 //   dx[t,v] = dloss_t (exp(x[t,v] - lse_t) - sum_{k: id_k = v} p_k).
 // An entry is present where its id is one of the table's; z = -inf makes its weight 0.  A row whose entries are all absent
 // or of weight 0 is left out before the products, as a row without a target is.
+//
+// Forward: ds_sort_k sorts each row's entries by id; the product's epilogue (CE_PICK) picks their logits from the tiles on the way,
+// where a dot product each would read T K C values again (4099 x 1536, 256 entries: 3.2 GB through L2, 925 us for the call
+// against 550); ds_join_k forms the loss.  Backward: the epilogue (CE_PATCH) writes the bracket at the entries, formed in
+// fp32 from the forward's logp, over what the tile has there, before the bf16 tile goes out.
+// What bounds it: the tensor cores, and behind them the power cap, as the cross entropy (16384 x 2048 x 50257, 64 entries, loss and
+// gradients 10.2 ms, the cross entropy 10.25); the small kernels
+// around the product take 45 us for 4099 rows of 256 entries.
 #pragma once
 
 #include <type_traits>
@@ -94,8 +102,8 @@ __device__ __forceinline__ void ds_sort(KEY (&key)[PER]) {
 // A row's entries by rising id, absent ones last, for the tiles' epilogues: each one's place in its 128 columns (`cols`), and which
 // is the first from every 128 columns on (`first`), so that an epilogue needs no search.  With them, for the forward's join, their
 // numbers in the caller's order (`order`) and the logarithms of their weights (`weights`, +inf where absent), for the backward
-// what the bracket is there, exp(logp) - the id's weights (`weights` too).  A warp a row.  Rows with a teacher get 0 in `target`, which ce_rows_k lists them by, others -1 and, in the
-// forward, logp 0.
+// what the bracket is there, exp(logp) - the id's weights (`weights` too).  A warp a row.  Rows with a teacher get 0 in
+// `target`, which ce_rows_k lists them by, others -1 and, in the forward, logp 0.
 // KEY holds id and number: 32 bits do for vocabularies below 2^23 (256 entries of 4099 rows: 24 -> 20 us).
 template <int PER, bool GRAD, typename KEY>
 __global__ void __launch_bounds__(256) ds_sort_k(int64_t T, int K, int64_t V, const int64_t* ids, const void* z, int z_f32, float inv_tau,

@@ -14,6 +14,10 @@
 // piece in each, which seq_join_k adds up in order: the same bits from run to run.  What a gradient takes from a whole sequence
 // (1 / n, the pair's slope) is put on by a last pass.
 // Sums: four tokens in fp32, from there in 64 bits.
+//
+// What bounds it: HBM for large batches, 24 bytes a token with reference and gradient (16.8 M tokens, 2048 sequences, on one B200: the
+// sums 73 us at 5.5 TB/s, the join 6, the last pass 18 within L2; 98 for the call), start and drain in between (8.4 M tokens
+// of 4096 pairs 37 us for 134 MB), and the latency of dependent phases below some 500 000 tokens (8 to 10 us).
 #pragma once
 
 #include <stddef.h>
@@ -25,13 +29,14 @@ constexpr int kSeqStep = 128;                 // tokens of a warp's step
 constexpr int kScaleSteps = 4, kScaleRange = kScaleSteps * kSeqStep;      // of the last pass
 constexpr int kSeqBlock = 256;
 // Blocks an SM and steps in a warp's ring, and with them ranges at most: as many as are under way at once (of a B200's 148 SMs:
-// the plan gives the scratch's size, so it does not look at the device).
+// the plan gives the scratch's size, so it does not look at the device).  The policy loss takes some 110 registers: two
+// blocks 100 us for 16.8 M tokens, four of 64 registers, which spill, 108.
 __host__ __device__ constexpr int seq_blocks(int op) { return op == SEQ_POLICY ? 2 : 4; }
 __host__ __device__ constexpr int seq_stages(int op) { return op == SEQ_POLICY ? 4 : 3; }
 constexpr int seq_ranges(int op) { return 148 * seq_blocks(op) * (kSeqBlock / 32); }
 // Up to so many tokens and sequences one block does it all in one launch, with what its warps exchange in shared memory, or one
-// cluster of eight (with the gradient, 1500 tokens 5.5 us on the device against 8 in three launches, 16384 8.1 against 8.2 of
-// which the host alone takes 7; at 65536 eight SMs take 11.7 against 8.4).
+// cluster of eight (with the gradient: 1000 tokens 5.5 us against 7.5 with the cluster, 16384 7.9 against 8.2 in three launches, or
+// 9.2 where the host launches them; at 65536 the cluster's eight SMs take 11.7 against 8.4).
 constexpr int kSeqOne = 16 * kSeqStep, kSeqOneS = 511;
 constexpr int kSeqCluster = 32768, kSeqClusterS = 16384, kSeqClusterWarps = 8 * 16;
 inline bool seq_one(int64_t T, int64_t S) { return T <= kSeqOne && S <= kSeqOneS; }
