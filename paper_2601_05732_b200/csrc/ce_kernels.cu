@@ -717,8 +717,8 @@ __global__ void __launch_bounds__(256) ce_dh_join_k(const int* live, const int* 
 constexpr int kSmWarps = 16, kSmThreads = kSmWarps * 32, kSmTokens = 32;
 
 // WK (4, 8 or 16) warps share the channels of a row, 64 of them each a step; WR = 16 / WK groups of 16 rows a unit; NB
-// blocks of 8 tokens.
-template <int NB, int STAGES>
+// blocks of 8 tokens.  TARGETS: the logits of the tokens' targets are kept (distillation has none).
+template <int NB, int STAGES, bool TARGETS>
 __global__ void __launch_bounds__(kSmThreads, 1)
 ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
            const int64_t* target, float scale, float2* part, float* tlogit) {
@@ -805,7 +805,7 @@ ce_small_k(int T, int64_t V, int C, int wk_log, const uint4* h, const uint4* W,
             const int64_t row = unit * rows + er * 16 + (l >> 2) + (e >> 1) * 8;
             const int tok = i * 8 + (l & 3) * 2 + (e & 1);
             if (row >= V) continue;
-            if (target && tok < T && row == target[tok]) tlogit[tok] = v;
+            if (TARGETS && tok < T && row == target[tok]) tlogit[tok] = v;
             const float top = fmaxf(mx[j], v * k2), base = top == -INFINITY ? 0.f : top;
             sum[j] = sum[j] * ex2(mx[j] - base) + ex2(fmaf(v, k2, -base));
             mx[j] = top;
@@ -996,12 +996,13 @@ static SmallPlan plan_small(int64_t T, int C) {
 }
 
 // The few-token forward's pairs; returns the CTAs that leave one each.
+template <bool TARGETS>
 static int launch_ce_small(const mhclite_ctx* c, const SmallPlan& q, int64_t T, int64_t V, const void* h, const void* W, const int64_t* target,
                            float scale, float2* part, float* tlogit, cudaStream_t s) {
     const int64_t units = (V + (256 >> q.wk_log) - 1) / (256 >> q.wk_log);
     const int grid = (int)(units < c->sm_count ? units : c->sm_count);
-    auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5> : q.nb == 2 ? ce_small_k<2, 5> : ce_small_k<4, 5>)
-                           : (q.nb == 1 ? ce_small_k<1, 3> : q.nb == 2 ? ce_small_k<2, 3> : ce_small_k<4, 3>);
+    auto k = q.stages == 5 ? (q.nb == 1 ? ce_small_k<1, 5, TARGETS> : q.nb == 2 ? ce_small_k<2, 5, TARGETS> : ce_small_k<4, 5, TARGETS>)
+                           : (q.nb == 1 ? ce_small_k<1, 3, TARGETS> : q.nb == 2 ? ce_small_k<2, 3, TARGETS> : ce_small_k<4, 3, TARGETS>);
     static SmemOnce once[3][2];
     smem_limit(once[q.nb >> 1][q.stages == 5], k, c->device, 226 * 1024);
     c->launches += 2;                                          // with the join that follows
@@ -1029,7 +1030,7 @@ bool launch_linear_ce_fwd(const mhclite_ctx* c, int64_t T, int64_t V, const void
     if (q.stages) {
         float2* part = (float2*)scratch;                       // [CTAs][32], then the targets' logits
         float* tlogit = (float*)(part + (size_t)c->sm_count * kSmTokens);
-        const int grid = launch_ce_small(c, q, T, V, h, W, target, scale, part, tlogit, s);
+        const int grid = launch_ce_small<true>(c, q, T, V, h, W, target, scale, part, tlogit, s);
         launch_after(ce_small_join_k, dim3(1), dim3(512), 0, s, (int)T, V, grid, part, tlogit, target, scale * kLog2e, loss, lse, c->op_status);
         return true;
     }

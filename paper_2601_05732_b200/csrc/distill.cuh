@@ -330,7 +330,7 @@ bool launch_linear_distill_fwd(const mhclite_ctx* c, int64_t T, int64_t V, int K
         const float2* part = (const float2*)scratch;
         c->launches += 1;
         launch_after(ds_dot_k, dim3((unsigned)((entries + 7) / 8)), block, 0, s, entries, K, V, c->C, ids, (const uint4*)h, (const uint4*)W, p.dots);
-        const int parts = launch_ce_small(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
+        const int parts = launch_ce_small<false>(c, q, T, V, h, W, nullptr, scale, (float2*)scratch, nullptr, s);
         ds_per(K, [&](auto per) {
             launch_after(ds_join_k<decltype(per)::value, false>, grid, block, 0, s, T, K, V, nullptr, nullptr, parts, kSmTokens, part, p.dots, K, nullptr,
                          nullptr, ids, z, z_f32, k2, inv_tau, loss, lse, logp, c->op_status);

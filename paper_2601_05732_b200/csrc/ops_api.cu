@@ -294,8 +294,11 @@ static int check_sequences(mhclite_ctx* ctx, int64_t T, int64_t S, const float* 
     if (S < 0 || S >= kMaxSequences) return fail(ctx, MHCLITE_ERR_BAD_ARG, "the number of sequences must be in [0, 2^30)");
     if (S > 0) {
         MHCL_PTR8(ctx, starts); MHCL_PTR(ctx, loss); MHCL_PTR(ctx, table);
-        MHCL_NO_ALIAS(ctx, loss, table);
-        if (T > 0) { MHCL_PTR(ctx, nll); MHCL_PTR8(ctx, target); }
+        MHCL_NO_ALIAS(ctx, loss, table); MHCL_NO_ALIAS(ctx, loss, dloss); MHCL_NO_ALIAS(ctx, table, dloss);
+        if (T > 0) {
+            MHCL_PTR(ctx, nll); MHCL_PTR8(ctx, target);
+            MHCL_NO_ALIAS(ctx, loss, nll); MHCL_NO_ALIAS(ctx, table, nll);
+        }
     }
     if (T > 0 && S > 0 && !dloss != !dnll) return fail(ctx, MHCLITE_ERR_BAD_ARG, "dloss and dnll are given both or neither");
     MHCL_OPT_PTR(ctx, dloss); MHCL_OPT_PTR(ctx, dnll);
@@ -324,6 +327,7 @@ int mhclite_policy_loss(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll
     if (S == 0) return no_sequences(ctx, T, dnll, stream);
     if (T > 0) {
         MHCL_PTR(ctx, nll_old); MHCL_OPT_PTR(ctx, nll_ref); MHCL_PTR(ctx, adv);
+        MHCL_NO_ALIAS(ctx, loss, adv); MHCL_NO_ALIAS(ctx, stats, adv);
         if (dnll) { MHCL_NO_ALIAS(ctx, dnll, nll_old); MHCL_NO_ALIAS(ctx, dnll, nll_ref); MHCL_NO_ALIAS(ctx, dnll, adv); }
     }
     if ((rc = check_scratch(ctx, scratch, scratch_bytes, seq_scratch_bytes(T, S)))) return rc;

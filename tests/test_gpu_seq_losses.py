@@ -355,6 +355,9 @@ def test_refusals(ctx):
     for out in (t["nll"], t["old"], t["ref"]):
         with pytest.raises(bad):
             ctx.policy_loss(*head, loss, stats, t["dloss"], out)         # the gradient in place of an input
+    for out in (t["adv"], t["dloss"]):
+        with pytest.raises(bad):
+            ctx.policy_loss(*head, out, stats, t["dloss"], dnll)
     with pytest.raises(bad):
         ctx.preference_loss(t["nll"], t["ref"], t["target"], t["starts"], 0.1, 0.0, 0.0, False, loss[:2], reward, t["dpair"], t["ref"])
     with pytest.raises(bad):
@@ -402,7 +405,7 @@ def test_rows_behind_the_last_token_stay(ctx, T):
 
 
 def test_two_streams_at_once_and_bitwise_repeats(ctx):
-    ks = [Case(2000, 12), Case(200001, 40)]
+    ks = [Case(2000, 12), Case(20001, 30), Case(200001, 40)]
     ts = [k.tensors() for k in ks]
     torch.cuda.synchronize()
     outs, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
@@ -416,7 +419,7 @@ def test_two_streams_at_once_and_bitwise_repeats(ctx):
 
 def test_captured_and_replayed_with_new_inputs(ctx):
     """Two graphs, each with scratch of its own; between replays the tokens, the masks and the starts change."""
-    ks = [Case(2000, 12), Case(50001, 40)]
+    ks = [Case(2000, 12), Case(20001, 30), Case(50001, 40)]
     ts = [k.tensors() for k in ks]
     step = lambda: [o for k, t in zip(ks, ts) for m in (False, True) for o in (*run_policy(ctx, k, t, m), *run_pair(ctx, k, t, m))]
     side, graphs = torch.cuda.Stream(), []
