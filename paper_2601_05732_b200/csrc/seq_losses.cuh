@@ -46,6 +46,7 @@ struct SeqSum { double a, b; int n, c; };     // policy: pg, kl, tokens, clipped
 
 struct SeqArgs {
     int T, S, W, range;                       // W ranges of `range` tokens, a multiple of kSeqStep
+    uint64_t per_range;                       // 2^40 over the steps of a range, rounded up: seq_range_of
     const float *nll, *old, *ref, *adv, *dloss;
     const int64_t *target, *starts;
     int mean;
@@ -200,9 +201,9 @@ struct SeqSide {
         close = x != 0.f ? (side ? a.close[1] : a.close[0]) : -1.f;
     }
 };
-// `ready` is called between the first copies and the first look at the starts.
+// `ready` is called between the first copies and the first look at the starts; `first` is where the walk begins.
 template <int OP, bool REF, bool EACH, int STAGES, typename F>          // EACH: an advantage for each token
-__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring, F ready) {
+__device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring, F ready, SeqWalk& first) {
     const int lane = threadIdx.x & 31, lo = w * a.range, hi = a.T - lo < a.range ? a.T : lo + a.range;
     const float* p0 = OP == SEQ_POLICY && !EACH ? a.adv : nullptr;
     const float* p1 = OP == SEQ_POLICY && a.dnll && !a.mean ? a.dloss : nullptr;       // a gradient that needs nothing else
@@ -251,6 +252,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
     };
     ready();
     k.locate(a, lo, p0, p1);
+    first = k;
     arrive();
     bool began = k.s >= 0 && seq_start(a, k.s) >= lo;
     double sa = 0, sb = 0;
@@ -383,30 +385,37 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
     if (open && k.s >= 0 && k.s < a.S) flush(began ? a.tail + w : a.head + w);
 }
 
-// The sums of sequence s over a team of threads (half a warp, a warp or a block of 256): all threads of the team get them.
+// The range of token t.  Steps are below 2^24 and those of a range below 2^13, so the quotient by 2^40 is exact.
+__device__ __forceinline__ int seq_range_of(const SeqArgs& a, int t) { return (int)((uint64_t)(t / kSeqStep) * a.per_range >> 40); }
+// 1 / n to 2^-46, in a few instructions (a division in 64 bits takes some 400 cycles, and a join little else).
+__device__ __forceinline__ double seq_share(int n) {
+    if (n == 0) return 0.0;
+    const double w = 1.f / (float)n;
+    return w * (2.0 - (double)n * w);
+}
+// The sums of sequence s over a team of threads: half a warp, a warp or a block of 256.  Member 0 gets them.
 template <int TEAM>
 __device__ __forceinline__ SeqSum seq_total(const SeqArgs& a, int s, int member) {
     const int64_t from = a.starts[s], to = a.starts[s + 1];
     const int b = seq_start(a, s), e = seq_start(a, s + 1);
     SeqSum t = {0.0, 0.0, 0, 0};
     if (member == 0 && (from < 0 || from > to || to > a.T)) report_index(a.status, MHCLITE_OP_SEQUENCES, s, from);
-    const int w0 = b / a.range, w1 = b < e ? (e - 1) / a.range : w0 - 1;
-    if (w0 == w1) {
-        if (member == 0) t = a.whole[s];
-    } else {
+    if (b >= e) return t;
+    const int w0 = seq_range_of(a, b), w1 = seq_range_of(a, e - 1);
+    if (w0 == w1) return a.whole[s];
 #pragma unroll 4
-        for (int w = w0 + member; w <= w1; w += TEAM) {
-            const SeqSum p = w == w0 ? a.tail[w] : a.head[w];
-            t.a += p.a; t.b += p.b; t.n += p.n; t.c += p.c;
-        }
+    for (int w = w0 + member; w <= w1; w += TEAM) {
+        const SeqSum p = w == w0 ? a.tail[w] : a.head[w];
+        t.a += p.a; t.b += p.b; t.n += p.n; t.c += p.c;
     }
-    __syncwarp();
+    const uint32_t team = TEAM == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffffffffu;
+    __syncwarp(team);
 #pragma unroll
     for (int o = TEAM < 32 ? TEAM / 2 : 16; o > 0; o >>= 1) {
-        t.a += __shfl_xor_sync(0xffffffffu, t.a, o);
-        t.b += __shfl_xor_sync(0xffffffffu, t.b, o);
-        t.n += __shfl_xor_sync(0xffffffffu, t.n, o);
-        t.c += __shfl_xor_sync(0xffffffffu, t.c, o);
+        t.a += __shfl_xor_sync(team, t.a, o);
+        t.b += __shfl_xor_sync(team, t.b, o);
+        t.n += __shfl_xor_sync(team, t.n, o);
+        t.c += __shfl_xor_sync(team, t.c, o);
     }
     if (TEAM > 32) {
         __shared__ SeqSum part[TEAM > 32 ? TEAM / 32 : 1];
@@ -425,7 +434,7 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
     if (OP == SEQ_POLICY) {
         const SeqSum t = seq_total<TEAM>(a, i, member);
         if (member != 0) return;
-        const double w = a.mean ? (t.n ? 1.0 / t.n : 0.0) : 1.0;
+        const double w = a.mean ? seq_share(t.n) : 1.0;
         a.loss[i] = (float)(w * (t.a + a.kl_weight * t.b));
         float* stats = a.stats + 3 * (int64_t)i;
         stats[0] = (float)t.n; stats[1] = (float)t.c; stats[2] = (float)(w * t.b);
@@ -434,6 +443,7 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         SeqSum c, r;
         if (TEAM == 32) {                                         // both sequences side by side, half a warp each
             c = seq_total<16>(a, 2 * i + (member >> 4), member & 15);
+            __syncwarp();
             r.a = __shfl_down_sync(0xffffffffu, c.a, 16);
             r.n = __shfl_down_sync(0xffffffffu, c.n, 16);
         } else {
@@ -441,7 +451,7 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
             r = seq_total<TEAM>(a, 2 * i + 1, member);
         }
         if (member != 0) return;
-        const double wc = a.mean ? (c.n ? 1.0 / c.n : 0.0) : 1.0, wr = a.mean ? (r.n ? 1.0 / r.n : 0.0) : 1.0;
+        const double wc = a.mean ? seq_share(c.n) : 1.0, wr = a.mean ? seq_share(r.n) : 1.0;
         const double rc = a.beta * wc * c.a, rr = a.beta * wr * r.a, x = rc - rr - a.margin;
         const double m = exp(-fabs(x)), soft = log1p(m);          // softplus(-|x|)
         const double share = x > 0 ? a.smoothing : a.smoothing - 1.0;
@@ -455,29 +465,52 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         }
     }
 }
-// The last pass over the gradient: four steps of tokens times what their sequences give.  All that seq_sums left is fetched
-// before `wait`, behind which the join's results are there.
-template <int OP, typename F>
-__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, F wait) {
+// A step of the last pass: the raw gradient x, or which tokens count (`mine`), times what the sequences give.
+template <int OP>
+__device__ __forceinline__ void seq_scale_step(const SeqArgs& a, SeqWalk& k, int base, int hi, const float4& raw, uint32_t mine) {
+    const int t = base + (threadIdx.x & 31) * 4, stop = min(base + kSeqStep, hi);
+    const float x[4] = {raw.x, raw.y, raw.z, raw.w};
+    float g[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int cur = base; cur < stop;) {
+        const int end = min(k.next, stop);
+        if (k.s >= 0 && k.s < a.S) {
+            const uint32_t in = seq_within(t, cur, end);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (!(in >> e & 1u)) continue;
+                if (OP == SEQ_POLICY) g[e] = x[e] == 0.f ? 0.f : x[e] * k.v0;              // tokens that do not count stay 0
+                else g[e] = mine >> e & 1u ? k.v0 : 0.f;
+            }
+        }
+        if (k.next <= stop && end < hi) k.advance(a, end, a.coef, nullptr);
+        cur = end;
+    }
+    seq_store(a.dnll, t, a.T, g);
+}
+template <int OP>
+__device__ __forceinline__ void seq_scale_load(const SeqArgs& a, int base, float4& raw, uint32_t& mine) {
+    const int t = base + (threadIdx.x & 31) * 4;
+    if (OP == SEQ_PAIR) {
+        mine = a.bits[t / 4];
+    } else if (base + kSeqStep <= a.T) {
+        raw = *reinterpret_cast<const float4*>(a.raw + t);
+    } else {
+        raw = make_float4(t < a.T ? a.raw[t] : 0.f, t + 1 < a.T ? a.raw[t + 1] : 0.f, t + 2 < a.T ? a.raw[t + 2] : 0.f, 0.f);
+        if (t + 3 < a.T) raw.w = a.raw[t + 3];
+    }
+}
+// The last pass over the gradient, four steps a warp.  All that seq_sums left is fetched before the wait for the join, behind which
+// its results are there.
+template <int OP>
+__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
     const int lane = threadIdx.x & 31, lo = w * kScaleRange, hi = a.T - lo < kScaleRange ? a.T : lo + kScaleRange;
-    float4 v[kScaleSteps];
-    uint32_t mine[kScaleSteps];
+    float4 v[kScaleSteps] = {};
+    uint32_t mine[kScaleSteps] = {};
     const int first = a.hint[w];
 #pragma unroll
-    for (int i = 0; i < kScaleSteps; ++i) {
-        const int base = lo + i * kSeqStep;
-        if (base >= hi) break;
-        const int t = base + lane * 4;
-        if (OP == SEQ_PAIR) {
-            mine[i] = a.bits[t / 4];
-        } else if (base + kSeqStep <= a.T) {
-            v[i] = *reinterpret_cast<const float4*>(a.raw + t);
-        } else {
-            v[i] = make_float4(t < a.T ? a.raw[t] : 0.f, t + 1 < a.T ? a.raw[t + 1] : 0.f, t + 2 < a.T ? a.raw[t + 2] : 0.f, 0.f);
-            if (t + 3 < a.T) v[i].w = a.raw[t + 3];
-        }
-    }
-    wait();
+    for (int i = 0; i < kScaleSteps; ++i)
+        if (lo + i * kSeqStep < hi) seq_scale_load<OP>(a, lo + i * kSeqStep, v[i], mine[i]);
+    pdl_wait();
     SeqWalk k;
     k.enter(a, first, lo, a.coef, nullptr);
     if (k.next >= hi && lo + kScaleRange <= a.T && k.v0 - k.v0 == 0.f) {               // the usual case: one sequence, or none (then v0 is 0)
@@ -490,28 +523,8 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, F wait) {
         return;
     }
 #pragma unroll
-    for (int i = 0; i < kScaleSteps; ++i) {
-        const int base = lo + i * kSeqStep;
-        if (base >= hi) break;
-        const int t = base + lane * 4, stop = min(base + kSeqStep, hi);
-        float x[4], g[4] = {0.f, 0.f, 0.f, 0.f};
-        if (OP == SEQ_POLICY) { x[0] = v[i].x; x[1] = v[i].y; x[2] = v[i].z; x[3] = v[i].w; }
-        for (int cur = base; cur < stop;) {
-            const int end = min(k.next, stop);
-            if (k.s >= 0 && k.s < a.S) {
-                const uint32_t in = seq_within(t, cur, end);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (!(in >> e & 1u)) continue;
-                    if (OP == SEQ_POLICY) g[e] = x[e] == 0.f ? 0.f : x[e] * k.v0;          // tokens that do not count stay 0
-                    else g[e] = mine[i] >> e & 1u ? k.v0 : 0.f;
-                }
-            }
-            if (k.next <= stop && end < hi) k.advance(a, end, a.coef, nullptr);
-            cur = end;
-        }
-        seq_store(a.dnll, t, a.T, g);
-    }
+    for (int i = 0; i < kScaleSteps; ++i)
+        if (lo + i * kSeqStep < hi) seq_scale_step<OP>(a, k, lo + i * kSeqStep, hi, v[i], mine[i]);
 }
 __device__ __forceinline__ int seq_scale_warps(const SeqArgs& a) { return (a.T - 1) / kScaleRange + 1; }      // T > 0
 
@@ -521,7 +534,8 @@ __global__ void __launch_bounds__(kSeqBlock, seq_blocks(OP)) seq_sum_k(const Seq
     pdl_wait();
     pdl_launch();
     const int warp = threadIdx.x >> 5, w = blockIdx.x * (kSeqBlock / 32) + warp;
-    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH), [] {});
+    SeqWalk first;
+    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH), [] {}, first);
 }
 template <int OP, int TEAM>
 __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
@@ -535,7 +549,7 @@ __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
 template <int OP>
 __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w, [] { pdl_wait(); });
+    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w);
 }
 // Few tokens: the three one after another in one launch, of one block, which keeps what its warps exchange, and the starts, in
 // shared memory, or (CLUSTER) of eight.
@@ -543,9 +557,8 @@ struct SeqShared {
     alignas(16) float raw[kSeqOne];                               // stored by fours
     int64_t starts[kSeqOneS + 1];
     SeqSum whole[kSeqOneS], head[16], tail[16];
-    float coef[kSeqOneS];
+    float coef[kSeqOneS], adv[kSeqOneS], dloss[kSeqOneS];
     uint8_t bits[kSeqOne / 4];
-    int hint[kSeqOne / kScaleRange];
 };
 constexpr int kSeqShared = sizeof(SeqShared);
 static_assert(alignof(SeqShared) == 16 && kSeqShared % 16 == 0 && offsetof(SeqShared, raw) % 16 == 0, "16-byte accesses");
@@ -568,19 +581,35 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
     SeqShared* sh = reinterpret_cast<SeqShared*>(sm_raw);
     auto ready = [&] {
         if (CLUSTER) return;
-        for (int i = threadIdx.x; i <= a.S; i += blockDim.x) sh->starts[i] = args.starts[i];
+        const int losses = OP == SEQ_PAIR ? a.S / 2 : a.S;
+        for (int i = threadIdx.x; i <= a.S; i += blockDim.x) {
+            sh->starts[i] = args.starts[i];
+            if (OP == SEQ_POLICY && !EACH && i < a.S) sh->adv[i] = args.adv[i];
+            if (a.dnll && i < losses) sh->dloss[i] = args.dloss[i];
+        }
         a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;
-        if (scaled) { a.raw = sh->raw; a.hint = sh->hint; }
+        if (OP == SEQ_POLICY && !EACH) a.adv = sh->adv;
+        if (a.dnll) a.dloss = sh->dloss;
+        if (scaled) a.raw = sh->raw;
         if (a.bits) a.bits = sh->bits;
         __syncthreads();
     };
-    if (warp < a.W) seq_sums<OP, REF, EACH, STAGES>(a, warp, ring, ready);
+    SeqWalk k;
+    if (warp < a.W) seq_sums<OP, REF, EACH, STAGES>(a, warp, ring, ready, k);
     else ready();
     together();
     for (int i = warp; i < items; i += warps) seq_item<OP, 32>(a, i, lane);
     if (!scaled || a.T == 0) return;
     together();
-    for (int w = warp; w < seq_scale_warps(a); w += warps) seq_scale<OP>(a, w, [] {});
+    if (warp >= a.W) return;
+    const int lo = warp * a.range, hi = min(lo + a.range, a.T);       // each warp its own tokens again
+    k.enter(a, k.base, lo, a.coef, nullptr);
+    for (int base = lo; base < hi; base += kSeqStep) {
+        float4 raw = {};
+        uint32_t mine = 0;
+        seq_scale_load<OP>(a, base, raw, mine);
+        seq_scale_step<OP>(a, k, base, hi, raw, mine);
+    }
 }
 
 // ---- host side -------------------------------------------------------------------------------------------------------
@@ -593,6 +622,8 @@ static size_t plan_seq(int op, SeqArgs& a, void* base) {
     a.range = (steps + most - 1) / most * kSeqStep;
     if (a.range == 0) a.range = kSeqStep;
     a.W = (int)(((int64_t)a.T + a.range - 1) / a.range);
+    const int each = a.range / kSeqStep;
+    a.per_range = (((uint64_t)1 << 40) + each - 1) / each;
     a.whole = (SeqSum*)take((size_t)a.S * sizeof(SeqSum));
     a.head = (SeqSum*)take((size_t)a.W * sizeof(SeqSum));
     a.tail = (SeqSum*)take((size_t)a.W * sizeof(SeqSum));
@@ -616,7 +647,7 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
     plan_seq(OP, a, scratch);
     a.status = c->op_status;
     const bool scaled = a.dnll && !(OP == SEQ_POLICY && !a.mean);
-    if (!scaled) a.hint = nullptr;
+    if (!scaled || seq_cluster(a.T, a.S)) a.hint = nullptr;
     if (OP == SEQ_POLICY || !scaled) a.bits = nullptr;
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
     if (seq_cluster(a.T, a.S)) {                                  // every case of one block is one of these
