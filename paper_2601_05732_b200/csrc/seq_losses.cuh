@@ -101,7 +101,7 @@ struct SeqWalk {
     __device__ __forceinline__ void locate(const SeqArgs& a, int cur, const float* p0, const float* p1) {
         const int lane = threadIdx.x & 31;
         int at = 0, n = a.S + 1;                              // starts <= cur: all before `at`, none from at + n on
-        while (n > 0) {
+        while (n > 32) {
             const int step = (n + 255) >> 8;
             int k = 0;
 #pragma unroll
@@ -113,6 +113,7 @@ struct SeqWalk {
             at += k * step;
             n = step == 1 ? 0 : min(step - 1, n - k * step);
         }
+        at += __popc(__ballot_sync(0xffffffffu, lane < n && seq_start(a, at + lane) <= cur));
         enter(a, at - 1, cur, p0, p1);
     }
     __device__ __forceinline__ void advance(const SeqArgs& a, int cur, const float* p0, const float* p1) {
@@ -387,10 +388,12 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
 
 // The range of token t.  Steps are below 2^24 and those of a range below 2^13, so the quotient by 2^40 is exact.
 __device__ __forceinline__ int seq_range_of(const SeqArgs& a, int t) { return (int)((uint64_t)(t / kSeqStep) * a.per_range >> 40); }
-// 1 / n to 2^-46, in a few instructions (a division in 64 bits takes some 400 cycles, and a join little else).
+// 1 / n to 2^-44, in a few instructions (a division in 64 bits takes some 400 cycles, and a join little else).
 __device__ __forceinline__ double seq_share(int n) {
     if (n == 0) return 0.0;
-    const double w = 1.f / (float)n;
+    float f;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"((float)n));
+    const double w = f;                                           // to 2^-22: one step squares the error
     return w * (2.0 - (double)n * w);
 }
 // The sums of sequence s over a team of threads: half a warp, a warp or a block of 256.  Member 0 gets them.
@@ -553,6 +556,7 @@ __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
 }
 // Few tokens: the three one after another in one launch, of one block, which keeps what its warps exchange, and the starts, in
 // shared memory, or (CLUSTER) of eight.
+static_assert(kSeqOneS < 512, "a thread a start");
 struct SeqShared {
     alignas(16) float raw[kSeqOne];                               // stored by fours
     int64_t starts[kSeqOneS + 1];
@@ -581,12 +585,11 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
     SeqShared* sh = reinterpret_cast<SeqShared*>(sm_raw);
     auto ready = [&] {
         if (CLUSTER) return;
-        const int losses = OP == SEQ_PAIR ? a.S / 2 : a.S;
-        for (int i = threadIdx.x; i <= a.S; i += blockDim.x) {
-            sh->starts[i] = args.starts[i];
-            if (OP == SEQ_POLICY && !EACH && i < a.S) sh->adv[i] = args.adv[i];
-            if (a.dnll && i < losses) sh->dloss[i] = args.dloss[i];
-        }
+        const int i = threadIdx.x;                                // at most 511 sequences, 512 threads
+        const int64_t start = i <= a.S ? args.starts[i] : 0;
+        const float adv = OP == SEQ_POLICY && !EACH && i < a.S ? args.adv[i] : 0.f, dloss = a.dnll && i < items ? args.dloss[i] : 0.f;
+        if (i <= a.S) sh->starts[i] = start;
+        if (i < a.S) { sh->adv[i] = adv; sh->dloss[i] = dloss; }
         a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;
         if (OP == SEQ_POLICY && !EACH) a.adv = sh->adv;
         if (a.dnll) a.dloss = sh->dloss;
