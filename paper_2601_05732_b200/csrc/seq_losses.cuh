@@ -35,8 +35,8 @@ __host__ __device__ constexpr int seq_blocks(int op) { return op == SEQ_POLICY ?
 __host__ __device__ constexpr int seq_stages(int op) { return op == SEQ_POLICY ? 4 : 3; }
 constexpr int seq_ranges(int op) { return 148 * seq_blocks(op) * (kSeqBlock / 32); }
 // Up to so many tokens and sequences one block does it all in one launch, with what its warps exchange in shared memory, or one
-// cluster of eight (with the gradient: 1000 tokens 5.5 us against 7.5 with the cluster, 16384 7.9 against 8.2 in three launches, or
-// 9.2 where the host launches them; at 65536 the cluster's eight SMs take 11.7 against 8.4).
+// cluster of eight (with the gradient, on the device: 1000 tokens 4.1 us, 4096 with the cluster 6.4, 16384 6.9, 32768 8.3; three
+// launches 7.9 there, but the host takes 9 to 10 to make them; at 65536 the cluster's eight SMs take 11.7 against 8.4).
 constexpr int kSeqOne = 16 * kSeqStep, kSeqOneS = 511;
 constexpr int kSeqCluster = 32768, kSeqClusterS = 16384, kSeqClusterWarps = 8 * 16;
 inline bool seq_one(int64_t T, int64_t S) { return T <= kSeqOne && S <= kSeqOneS; }
