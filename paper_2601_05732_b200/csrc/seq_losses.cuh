@@ -12,7 +12,8 @@
 // Each warp walks a range of its own, 128 tokens a step (four a lane), with running sums of the sequence it is in: no exchange but
 // where a sequence ends, whatever the lengths.  A sequence inside one range is complete there; one that crosses ranges leaves a
 // piece in each, which seq_join_k adds up in order: the same bits from run to run.  What a gradient takes from a whole sequence
-// (1 / n, the pair's slope) is put on by a last pass.
+// (1 / n, the pair's slope) is put on by a last pass.  Steps in which several sequences end are added up by runs and a scan along
+// the lanes, all of their sequences at once (sequences of two tokens: 128 000 tokens 28 us against 135 one by one).
 // Sums: four tokens in fp32, from there in 64 bits.
 //
 // What bounds it: HBM for large batches, 24 bytes a token with reference and gradient (16.8 M tokens, 2048 sequences, on one B200: the
@@ -165,10 +166,51 @@ __device__ __forceinline__ Quad seq_read(uint32_t at) {
 // Bytes of a step: four targets a lane, and four fp32 a lane of each tensor.
 __host__ __device__ constexpr int seq_tensors(int op, bool ref, bool each) { return 1 + (op == SEQ_POLICY) + ref + each; }
 __host__ __device__ constexpr int seq_stage(int op, bool ref, bool each) { return 512 * (2 + seq_tensors(op, ref, each)); }
+// Bytes of a warp: the ring, and the 128 ints of seq_ids.
+__host__ __device__ constexpr int seq_bytes(int op, bool ref, bool each, int stages) { return stages * seq_stage(op, ref, each) + 512; }
 // Those of a lane's four tokens that lie in cur .. end.
 __device__ __forceinline__ uint32_t seq_within(int t, int cur, int end) {
     const int lo = max(cur - t, 0), hi = min(end - t, 4);
     return hi > lo ? (1u << hi) - (1u << lo) : 0u;
+}
+
+// Steps in which at least so many sequences end are added up all at once, by lanes, instead of sequence by sequence.
+constexpr int kSeqDense = 3;
+__device__ __forceinline__ bool seq_dense(const SeqWalk& k, int base, int stop) {
+    return __popc(__ballot_sync(0xffffffffu, k.bound > base && k.bound < stop)) >= kSeqDense;
+}
+// The sequence of each of a lane's four tokens (S behind the last): where one starts its number is put into `ids` (128 ints of the
+// warp's own), the largest where several do, and each token takes the largest up to it.  False where more than 256 start in the step.
+__device__ __forceinline__ bool seq_ids(const SeqArgs& a, int s, int base, int stop, uint32_t ids, int (&id)[4]) {
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+    sts128(ids + lane * 16, make_uint4(~0u, ~0u, ~0u, ~0u));
+    __syncwarp();
+    bool more = true;
+#pragma unroll 1
+    for (int c = 0; c < 8 && more; ++c) {
+        const int64_t i = (int64_t)s + 1 + c * 32 + lane;
+        const int at = i <= a.S ? seq_start(a, (int)i) : 0x7FFFFFFF;
+        if (at >= base && at < stop) asm volatile("red.shared.max.s32 [%0], %1;" ::"r"(ids + (at - base) * 4), "r"((int)i) : "memory");
+        more = __all_sync(0xffffffffu, at < stop);
+    }
+    __syncwarp();
+    const uint4 v = lds128(ids + lane * 16);
+    id[0] = (int)v.x;
+    id[1] = max(id[0], (int)v.y);
+    id[2] = max(id[1], (int)v.z);
+    id[3] = max(id[2], (int)v.w);
+    int top = id[3];
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, top, o);
+        if (lane >= o) top = max(top, y);
+    }
+    int before = __shfl_up_sync(0xffffffffu, top, 1);
+    before = lane ? max(before, s) : s;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) id[i] = max(id[i], before);
+    return !more;
 }
 
 // e^q: q log2 e with the part of it that fp32 leaves out, so that only ex2's 2^-22 and two roundings are left of the error.
@@ -367,7 +409,98 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
             sa += (double)pa;
             if (REF && OP == SEQ_POLICY) sb += (double)pb;
         };
-        for (int cur = base; cur < stop;) {
+        // Many sequences end here: a lane adds up runs of its own four tokens, a scan along the lanes joins what crosses them, and
+        // the lane of a sequence's last token has its sums.
+        auto dense = [&] {
+            int id[4];
+            if (!seq_ids(a, k.s, base, stop, ring + STAGES * STAGE, id)) return false;
+            const double ca = warp_sum(sa), cb = warp_sum(sb);    // what the first sequence brings along
+            const int cn = __reduce_add_sync(0xffffffffu, sn), cc = __reduce_add_sync(0xffffffffu, sc);
+            const int begin = k.s;
+            auto emit = [&](int s, double x, double y, int n) {   // n: tokens, and clipped ones from bit 16 on
+                if (s < 0 || s >= a.S) return;
+                const bool carried = s == begin;
+                SeqSum* to = carried && !began ? a.head + w : a.whole + s;
+                to->a = x + (carried ? ca : 0.0);
+                to->b = y + (carried ? cb : 0.0);
+                to->n = (n & 0xFFFF) + (carried ? cn : 0);
+                to->c = (n >> 16) + (carried ? cc : 0);
+            };
+            float x[4], v[4], y[4], d[4];
+            seq_unpack({q[0], q[1]}, x);
+            if (OP == SEQ_POLICY) {
+                seq_unpack({r[0], r[1]}, v);
+                seq_unpack({e1[0], e1[1]}, d);
+                seq_unpack({e2[0], e2[1]}, y);
+            }
+            float ra = 0.f, rb = 0.f, fa = 0.f, fb = 0.f;         // of the run, and of the lane's first if it is not the last
+            int rn = 0, fn = 0;
+            bool several = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool valid = id[i] >= 0 && id[i] < a.S, there = valid && (mine >> i & 1u);
+                if (i > 0 && id[i] != id[i - 1]) {
+                    if (several) { emit(id[i - 1], ra, rb, rn); } else { fa = ra; fb = rb; fn = rn; several = true; }
+                    ra = rb = 0.f;
+                    rn = 0;
+                }
+                if (OP == SEQ_POLICY) {
+                    z.choose(a, EACH ? A[i] : there ? a.adv[id[i]] : 0.f);
+                    const float by = a.mean ? 1.f : there && p1 ? p1[id[i]] : 0.f, o = x[i] * z.sign - z.edge;
+                    bool cut = o > 0.f;
+                    if (there && fabsf(o) <= z.close)
+                        cut = ((double)a.old[t + i] - (double)a.nll[t + i]) * (double)z.sign > (z.side ? a.edge[1] : a.edge[0]);
+                    float grad = (cut ? 0.f : v[i]) * (z.adv * by);
+                    if (REF) grad = fmaf(a.kl_slope * by, d[i], grad);
+                    if (there) {
+                        ra -= z.adv * (cut ? z.held : v[i]);
+                        if (REF) rb += y[i];
+                        rn += 1 + (cut ? 0x10000 : 0);
+                        g[i] = grad;
+                    }
+                } else if (there) {
+                    ra += x[i];
+                    rn += 1;
+                }
+            }
+            const int prior = __shfl_up_sync(0xffffffffu, id[3], 1);
+            bool head = several || lane == 0 || id[0] != prior;   // the lane's last run begins in it
+            double xa = ra, xb = rb;
+            int xn = rn;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const double ya = __shfl_up_sync(0xffffffffu, xa, o), yb = REF && OP == SEQ_POLICY ? __shfl_up_sync(0xffffffffu, xb, o) : 0.0;
+                const int yn = __shfl_up_sync(0xffffffffu, xn, o);
+                const bool yh = __shfl_up_sync(0xffffffffu, (int)head, o) != 0;
+                if (lane >= o && !head) { xa += ya; xb += yb; xn += yn; head = yh; }
+            }
+            const double pa = __shfl_up_sync(0xffffffffu, xa, 1), pb = __shfl_up_sync(0xffffffffu, xb, 1);
+            const int pn = __shfl_up_sync(0xffffffffu, xn, 1), after = __shfl_down_sync(0xffffffffu, id[0], 1);
+            if (several) {
+                const bool on = lane > 0 && id[0] == prior;
+                emit(id[0], fa + (on ? pa : 0.0), fb + (on ? pb : 0.0), fn + (on ? pn : 0));
+            }
+            if (lane < 31 && after != id[3]) emit(id[3], xa, xb, xn);
+            // the last sequence stays open, unless it ends with the step
+            const int last = __shfl_sync(0xffffffffu, id[3], 31);
+            const bool same = last == begin;
+            sa = lane == 31 ? xa + (same ? ca : 0.0) : 0.0;
+            sb = lane == 31 ? xb + (same ? cb : 0.0) : 0.0;
+            sn = lane == 31 ? (xn & 0xFFFF) + (same ? cn : 0) : 0;
+            sc = lane == 31 ? (xn >> 16) + (same ? cc : 0) : 0;
+            began = began || !same;
+            k.enter(a, last, stop, p0, p1);
+            if (__shfl_sync(0xffffffffu, k.bound, 0) <= stop) {
+                if (last >= 0 && last < a.S) flush(began ? a.whole + last : a.head + w);
+                open = stop < hi;
+                if (open) k.advance(a, stop, p0, p1);
+                began = true;
+            }
+            arrive();
+            return true;
+        };
+        const bool done = __builtin_expect(seq_dense(k, base, stop), 0) && dense();
+        for (int cur = done ? stop : base; cur < stop;) {
             const int end = min(k.next, stop);
             if (!none && k.s >= 0 && k.s < a.S) {
                 if (whole && end - cur == kSeqStep) tokens(15u, std::true_type());
@@ -430,30 +563,16 @@ __device__ __forceinline__ SeqSum seq_total(const SeqArgs& a, int s, int member)
     }
     return t;
 }
-// What item i (a sequence, or a pair of them) gives.
-template <int OP, int TEAM>
-__device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
-    const float dloss = a.dnll && member == 0 ? a.dloss[i] : 0.f;       // fetched beside the sums
+// What item i (a sequence, or a pair of them) gives from its sums.
+template <int OP>
+__device__ __forceinline__ void seq_give(const SeqArgs& a, int i, const SeqSum& c, const SeqSum& r, float dloss) {
     if (OP == SEQ_POLICY) {
-        const SeqSum t = seq_total<TEAM>(a, i, member);
-        if (member != 0) return;
-        const double w = a.mean ? seq_share(t.n) : 1.0;
-        a.loss[i] = (float)(w * (t.a + a.kl_weight * t.b));
+        const double w = a.mean ? seq_share(c.n) : 1.0;
+        a.loss[i] = (float)(w * (c.a + a.kl_weight * c.b));
         float* stats = a.stats + 3 * (int64_t)i;
-        stats[0] = (float)t.n; stats[1] = (float)t.c; stats[2] = (float)(w * t.b);
+        stats[0] = (float)c.n; stats[1] = (float)c.c; stats[2] = (float)(w * c.b);
         if (a.dnll && a.mean) a.coef[i] = (float)(w * dloss);
     } else {
-        SeqSum c, r;
-        if (TEAM == 32) {                                         // both sequences side by side, half a warp each
-            c = seq_total<16>(a, 2 * i + (member >> 4), member & 15);
-            __syncwarp();
-            r.a = __shfl_down_sync(0xffffffffu, c.a, 16);
-            r.n = __shfl_down_sync(0xffffffffu, c.n, 16);
-        } else {
-            c = seq_total<TEAM>(a, 2 * i, member);
-            r = seq_total<TEAM>(a, 2 * i + 1, member);
-        }
-        if (member != 0) return;
         const double wc = a.mean ? seq_share(c.n) : 1.0, wr = a.mean ? seq_share(r.n) : 1.0;
         const double rc = a.beta * wc * c.a, rr = a.beta * wr * r.a, x = rc - rr - a.margin;
         const double m = exp(-fabs(x)), soft = log1p(m);          // softplus(-|x|)
@@ -468,13 +587,79 @@ __device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
         }
     }
 }
-// A step of the last pass: the raw gradient x, or which tokens count (`mine`), times what the sequences give.
+template <int OP, int TEAM>
+__device__ __forceinline__ void seq_item(const SeqArgs& a, int i, int member) {
+    const float dloss = a.dnll && member == 0 ? a.dloss[i] : 0.f;       // fetched beside the sums
+    SeqSum c, r = {0.0, 0.0, 0, 0};
+    if (OP == SEQ_POLICY) {
+        c = seq_total<TEAM>(a, i, member);
+    } else if (TEAM == 32) {                                      // both sequences side by side, half a warp each
+        c = seq_total<16>(a, 2 * i + (member >> 4), member & 15);
+        __syncwarp();
+        r.a = __shfl_down_sync(0xffffffffu, c.a, 16);
+        r.n = __shfl_down_sync(0xffffffffu, c.n, 16);
+    } else {
+        c = seq_total<TEAM>(a, 2 * i, member);
+        r = seq_total<TEAM>(a, 2 * i + 1, member);
+    }
+    if (member == 0) seq_give<OP>(a, i, c, r, dloss);
+}
+// The sums of a sequence that lies in one range (or is empty); false where there are pieces to add up.
+__device__ __forceinline__ bool seq_complete(const SeqArgs& a, int s, SeqSum& t) {
+    const int64_t from = a.starts[s], to = a.starts[s + 1];
+    const int b = seq_start(a, s), e = seq_start(a, s + 1);
+    if (from < 0 || from > to || to > a.T) report_index(a.status, MHCLITE_OP_SEQUENCES, s, from);
+    t = {0.0, 0.0, 0, 0};
+    if (b >= e) return true;
+    if (seq_range_of(a, b) != seq_range_of(a, e - 1)) return false;
+    t = a.whole[s];
+    return true;
+}
+// All items, spread over `warps` warps; where there are more, over their lanes too: a lane alone where a sequence is complete, the
+// warp where there are pieces.
 template <int OP>
-__device__ __forceinline__ void seq_scale_step(const SeqArgs& a, SeqWalk& k, int base, int hi, const float4& raw, uint32_t mine) {
+__device__ __forceinline__ void seq_items(const SeqArgs& a, int warp, int warps) {
+    const int lane = threadIdx.x & 31, items = OP == SEQ_PAIR ? a.S / 2 : a.S;
+    if (items <= warps) {
+        if (warp < items) seq_item<OP, 32>(a, warp, lane);
+        return;
+    }
+    for (int64_t first = warp; first < items; first += (int64_t)warps * 32) {
+        const int64_t i = first + (int64_t)lane * warps;
+        bool left = i < items;
+        if (left) {
+            SeqSum c, r = {0.0, 0.0, 0, 0};
+            const float dloss = a.dnll ? a.dloss[i] : 0.f;
+            if (OP == SEQ_POLICY ? seq_complete(a, (int)i, c) : seq_complete(a, 2 * (int)i, c) && seq_complete(a, 2 * (int)i + 1, r)) {
+                seq_give<OP>(a, (int)i, c, r, dloss);
+                left = false;
+            }
+        }
+        for (uint32_t todo = __ballot_sync(0xffffffffu, left); todo; todo &= todo - 1)
+            seq_item<OP, 32>(a, (int)(first + (int64_t)(__ffs(todo) - 1) * warps), lane);
+    }
+}
+// A step of the last pass: the raw gradient x, or which tokens count (`mine`), times what the sequences give.
+template <int OP, bool DENSE>
+__device__ __forceinline__ void seq_scale_step(const SeqArgs& a, SeqWalk& k, int base, int hi, const float4& raw, uint32_t mine, uint32_t ids) {
     const int t = base + (threadIdx.x & 31) * 4, stop = min(base + kSeqStep, hi);
     const float x[4] = {raw.x, raw.y, raw.z, raw.w};
     float g[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int cur = base; cur < stop;) {
+    int id[4];
+    const bool done = DENSE && seq_dense(k, base, stop) && seq_ids(a, k.s, base, stop, ids, id);
+    if (done) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float by = id[e] >= 0 && id[e] < a.S ? a.coef[id[e]] : 0.f;
+            if (OP == SEQ_POLICY) g[e] = x[e] == 0.f ? 0.f : x[e] * by;
+            else g[e] = mine >> e & 1u ? by : 0.f;
+        }
+        if (stop < hi) {
+            k.enter(a, __shfl_sync(0xffffffffu, id[3], 31), stop, a.coef, nullptr);
+            if (__shfl_sync(0xffffffffu, k.bound, 0) <= stop) k.advance(a, stop, a.coef, nullptr);
+        }
+    }
+    for (int cur = done ? stop : base; cur < stop;) {
         const int end = min(k.next, stop);
         if (k.s >= 0 && k.s < a.S) {
             const uint32_t in = seq_within(t, cur, end);
@@ -505,7 +690,7 @@ __device__ __forceinline__ void seq_scale_load(const SeqArgs& a, int base, float
 // The last pass over the gradient, four steps a warp.  All that seq_sums left is fetched before the wait for the join, behind which
 // its results are there.
 template <int OP>
-__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
+__device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, uint32_t ids) {
     const int lane = threadIdx.x & 31, lo = w * kScaleRange, hi = a.T - lo < kScaleRange ? a.T : lo + kScaleRange;
     float4 v[kScaleSteps] = {};
     uint32_t mine[kScaleSteps] = {};
@@ -525,9 +710,15 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w) {
         }
         return;
     }
+    if (seq_dense(k, lo, hi)) {
+#pragma unroll
+        for (int i = 0; i < kScaleSteps; ++i)
+            if (lo + i * kSeqStep < hi) seq_scale_step<OP, true>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i)
-        if (lo + i * kSeqStep < hi) seq_scale_step<OP>(a, k, lo + i * kSeqStep, hi, v[i], mine[i]);
+        if (lo + i * kSeqStep < hi) seq_scale_step<OP, false>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
 }
 __device__ __forceinline__ int seq_scale_warps(const SeqArgs& a) { return (a.T - 1) / kScaleRange + 1; }      // T > 0
 
@@ -538,21 +729,24 @@ __global__ void __launch_bounds__(kSeqBlock, seq_blocks(OP)) seq_sum_k(const Seq
     pdl_launch();
     const int warp = threadIdx.x >> 5, w = blockIdx.x * (kSeqBlock / 32) + warp;
     SeqWalk first;
-    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_stages(OP) * seq_stage(OP, REF, EACH), [] {}, first);
+    if (w < a.W) seq_sums<OP, REF, EACH, seq_stages(OP)>(a, w, smem_u32(sm_raw) + warp * seq_bytes(OP, REF, EACH, seq_stages(OP)), [] {}, first);
 }
 template <int OP, int TEAM>
 __global__ void __launch_bounds__(kSeqBlock) seq_join_k(const SeqArgs a) {
     pdl_wait();
     pdl_launch();
-    const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, member = threadIdx.x % TEAM;
-    for (int i = blockIdx.x * (kSeqBlock / TEAM) + threadIdx.x / TEAM; i < items; i += gridDim.x * (kSeqBlock / TEAM)) seq_item<OP, TEAM>(a, i, member);
+    const int items = OP == SEQ_PAIR ? a.S / 2 : a.S;
+    if (TEAM == 1) seq_items<OP>(a, blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5), gridDim.x * (kSeqBlock / 32));
+    else
+        for (int i = blockIdx.x * (kSeqBlock / TEAM) + threadIdx.x / TEAM; i < items; i += gridDim.x * (kSeqBlock / TEAM)) seq_item<OP, TEAM>(a, i, threadIdx.x % TEAM);
 }
 // The join's blocks let this kernel begin behind their own wait for seq_sum_k, so what that left may be read before the wait for
 // the join.
 template <int OP>
 __global__ void __launch_bounds__(kSeqBlock) seq_scale_k(const SeqArgs a) {
+    __shared__ alignas(16) int ids[kSeqBlock / 32][kSeqStep];
     const int w = blockIdx.x * (kSeqBlock / 32) + (threadIdx.x >> 5);
-    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w);
+    if (w < seq_scale_warps(a)) seq_scale<OP>(a, w, smem_u32(ids[threadIdx.x >> 5]));
 }
 // Few tokens: the three one after another in one launch, of one block, which keeps what its warps exchange, and the starts, in
 // shared memory, or (CLUSTER) of eight.
@@ -573,7 +767,7 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
     SeqArgs a = args;
     const int warps = gridDim.x * (blockDim.x >> 5), in = threadIdx.x >> 5, warp = in * gridDim.x + blockIdx.x, lane = threadIdx.x & 31;
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S;
-    const uint32_t ring = smem_u32(sm_raw) + (CLUSTER ? 0 : kSeqShared) + in * STAGES * seq_stage(OP, REF, EACH);
+    const uint32_t ring = smem_u32(sm_raw) + (CLUSTER ? 0 : kSeqShared) + in * seq_bytes(OP, REF, EACH, STAGES);
     const bool scaled = a.dnll && !(OP == SEQ_POLICY && !a.mean);
     pdl_wait();
     pdl_launch();
@@ -601,7 +795,7 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
     if (warp < a.W) seq_sums<OP, REF, EACH, STAGES>(a, warp, ring, ready, k);
     else ready();
     together();
-    for (int i = warp; i < items; i += warps) seq_item<OP, 32>(a, i, lane);
+    seq_items<OP>(a, warp, warps);
     if (!scaled || a.T == 0) return;
     together();
     if (warp >= a.W) return;
@@ -611,7 +805,7 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
         float4 raw = {};
         uint32_t mine = 0;
         seq_scale_load<OP>(a, base, raw, mine);
-        seq_scale_step<OP>(a, k, base, hi, raw, mine);
+        seq_scale_step<OP, true>(a, k, base, hi, raw, mine, ring);
     }
 }
 
@@ -655,7 +849,7 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
     const int items = OP == SEQ_PAIR ? a.S / 2 : a.S, blocks = (a.W + kSeqBlock / 32 - 1) / (kSeqBlock / 32), most = c->sm_count * 16;
     if (seq_cluster(a.T, a.S)) {                                  // every case of one block is one of these
         c->launches += 1;
-        constexpr int one = kSeqShared + 16 * seq_stage(OP, REF, EACH), eight = 16 * 4 * seq_stage(OP, REF, EACH);
+        constexpr int one = kSeqShared + 16 * seq_bytes(OP, REF, EACH, 1), eight = 16 * seq_bytes(OP, REF, EACH, 4);
         if (seq_one(a.T, a.S)) {
             static SmemOnce once;
             smem_limit(once, seq_one_k<OP, REF, EACH, false>, c->device, one);
@@ -668,14 +862,15 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
         return;
     }
     c->launches += 2;
-    constexpr int ring = kSeqBlock / 32 * seq_stages(OP) * seq_stage(OP, REF, EACH);
+    constexpr int ring = kSeqBlock / 32 * seq_bytes(OP, REF, EACH, seq_stages(OP));
     static SmemOnce once;
     smem_limit(once, seq_sum_k<OP, REF, EACH>, c->device, ring);
     launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), ring, s, a);
-    // a warp adds up 32 pieces at a time: a block where sequences have more of them on average
-    const int warps = (items + kSeqBlock / 32 - 1) / (kSeqBlock / 32);
+    // a block where sequences have more pieces on average than a warp adds up at a time, a warp each as long as there are enough
+    // warps under way, then a lane each
     if (a.W > (int64_t)items * 32) launch_after(seq_join_k<OP, kSeqBlock>, dim3(items), dim3(kSeqBlock), 0, s, a);
-    else launch_after(seq_join_k<OP, 32>, dim3(warps < most ? warps : most), dim3(kSeqBlock), 0, s, a);
+    else if (items <= most * 8) launch_after(seq_join_k<OP, 32>, dim3((items + 7) / 8), dim3(kSeqBlock), 0, s, a);
+    else launch_after(seq_join_k<OP, 1>, dim3(most), dim3(kSeqBlock), 0, s, a);
     if (!scaled) return;
     c->launches += 1;
     const int scale = (a.T - 1) / kScaleRange + 1;

@@ -152,7 +152,7 @@ SHAPES = [  # T, S, kind
     (1, 2, "all"), (1, 2, "ones"), (2, 2, "ones"), (3, 4, "ones"), (127, 2, "even"), (128, 4, "even"), (129, 6, "empties"), (300, 300, "ones"), (600, 600, "ones"), (2048, 510, "even"), (2048, 512, "empties"), (2049, 20, "even"), (32768, 6, "even"), (32769, 100, "even"),
     (1000, 8, "even"), (4095, 40, "even"), (4096, 2, "all"), (4096, 32, "steps"), (4097, 10, "even"), (5000, 4000, "even"), (20000, 3000, "empties"),
     (33333, 2, "even"), (65536, 64, "steps"), (100001, 12, "even"), (700001, 6, "even"), (700001, 2, "all"), (1300000, 300, "empties"),
-    (30000, 20000, "even"),
+    (30000, 20000, "even"), (700001, 60000, "even"), (50000, 12000, "empties"), (1500, 400, "even"),
 ]
 
 
@@ -313,6 +313,29 @@ def test_impossible_tokens(ctx, T):
     k.nll[a[2]], k.old[[a[1], a[3]]] = 1.0, 1.0
     loss, stats, _ = run_policy(ctx, k, k.tensors(), True)
     assert torch.isposinf(loss[0]) and torch.isposinf(stats[0, 2]) and torch.isfinite(loss[1:]).all()
+
+
+@pytest.mark.parametrize("T", [1500, 9000, 60000])
+@pytest.mark.parametrize("token_adv", [False, True])
+def test_short_sequences_between_long_ones(ctx, T, token_adv):
+    """Runs of sequences of no, one and a few tokens, hundreds of empty ones at one place, long ones and gaps between: every way
+    of adding up a step, next to each other."""
+    k, r = Case(T, 2, token_adv=token_adv, dead=0.2), np.random.default_rng(T)
+    at, starts = 5, []
+    while at < T:
+        kind = r.integers(0, 5)
+        for _ in range([40, 300, 1, 3, 25][kind]):
+            starts.append(at)
+            at += int([r.integers(0, 4), 0, r.integers(100, 1000), r.integers(20, 60), r.integers(1, 12)][kind])
+    starts = np.minimum(np.array(starts + [T - 2]), T - 2)
+    k.starts = starts[: len(starts) // 2 * 2 - 1]                       # an even number of sequences
+    k.S = len(k.starts) - 1
+    k.dloss = r.normal(size=k.S).astype(np.float32).astype(np.float64)
+    k.dpair = k.dloss[: k.S // 2]
+    if not token_adv:
+        k.adv = r.normal(size=k.S).astype(np.float32).astype(np.float64)
+    for mean in (False, True):
+        check_policy(ctx, k, mean), check_pair(ctx, k, mean)
 
 
 def test_no_tokens_and_no_sequences(ctx):
