@@ -861,11 +861,11 @@ static void launch_seq(const mhclite_ctx* c, SeqArgs& a, void* scratch, cudaStre
         }
         return;
     }
-    c->launches += 2;
+    c->launches += blocks > 0 ? 2 : 1;
     constexpr int ring = kSeqBlock / 32 * seq_bytes(OP, REF, EACH, seq_stages(OP));
     static SmemOnce once;
     smem_limit(once, seq_sum_k<OP, REF, EACH>, c->device, ring);
-    launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), ring, s, a);
+    if (blocks > 0) launch_after(seq_sum_k<OP, REF, EACH>, dim3(blocks), dim3(kSeqBlock), ring, s, a);
     // a block where sequences have more pieces on average than a warp adds up at a time, a warp each as long as there are enough
     // warps under way, then a lane each
     if (a.W > (int64_t)items * 32) launch_after(seq_join_k<OP, kSeqBlock>, dim3(items), dim3(kSeqBlock), 0, s, a);

@@ -339,12 +339,13 @@ def test_short_sequences_between_long_ones(ctx, T, token_adv):
 
 
 def test_no_tokens_and_no_sequences(ctx):
-    k = Case(0, 4)
-    k.starts[:] = 0
-    loss, stats, _ = check_policy(ctx, k, True)
-    assert (loss == 0).all() and (stats == 0).all()
-    loss, reward, _ = check_pair(ctx, k, True, margin=0.5, e=0.0)
-    assert (reward == 0).all() and torch.allclose(loss, torch.full_like(loss, float(np.log1p(np.exp(0.5)))))
+    for n in (4, 3000, 40000):
+        k = Case(0, n)
+        k.starts[:] = 0
+        loss, stats, _ = check_policy(ctx, k, True)
+        assert (loss == 0).all() and (stats == 0).all()
+        loss, reward, _ = check_pair(ctx, k, True, margin=0.5, e=0.0)
+        assert (reward == 0).all() and torch.allclose(loss, torch.full_like(loss, float(np.log1p(np.exp(0.5)))))
     k = Case(50, 0)
     k.starts = np.array([0])
     t, before = k.tensors(), ctx.kernel_launches()
