@@ -268,6 +268,34 @@ def test_sure_pairs(ctx):
     assert loss[0] == 0 and loss[1] > 4000 and torch.isfinite(dnll).all() and (dnll[:4096] == 0).all() and (dnll[4096:] != 0).all()
 
 
+def test_offsets_beyond_32_bits(ctx):
+    """1.1 G tokens: 4.4 GB a tensor, 8.8 GB of targets.  The last sequences give what they give alone."""
+    T, m = 1_100_000_000, 5001
+    g = torch.Generator(device=DEV).manual_seed(1)
+    nll = torch.empty(T, device=DEV).exponential_(generator=g)
+    old, ref, dnll = nll * 1.01, nll * 0.98, torch.empty(T, device=DEV)
+    target = torch.ones(T, dtype=torch.int64, device=DEV)
+    target[-m::3] = -1
+    starts = torch.tensor([7, 1000, 900_000_000, T - m, T - m + 2000, T - 1, T - 1], device=DEV)
+    adv, dloss, few = torch.tensor([1.0, -1.0, 0.5, 2.0, -0.5, 1.0], device=DEV), torch.ones(6, device=DEV), slice(3, 6)
+    loss, pair, stats, reward = empty(6), empty(3), empty(6, 3), empty(3, 2)
+    own = lambda t: t[T - m:].clone()
+    small = [own(t) for t in (nll, old, ref, target)]
+    l2, s2, d2 = empty(4), empty(4, 3), empty(m)
+    at = torch.cat((torch.zeros(2, dtype=torch.int64, device=DEV), starts[4:] - (T - m)))
+    args = (0.2, 0.3, 0.1, True)
+    ctx.policy_loss(nll, old, ref, target, starts, adv, False, *args, loss, stats, dloss, dnll)
+    ctx.policy_loss(*small, at, adv[2:].clone(), False, *args, l2, s2, dloss[:4], d2)
+    assert torch.equal(stats[few][:, :2], s2[1:, :2]) and torch.allclose(loss[few], l2[1:], rtol=1e-5) and torch.allclose(stats[few], s2[1:], rtol=1e-5)
+    assert torch.equal(dnll[T - m:], d2) and torch.isfinite(loss).all() and abs(int(stats[2, 0]) - (T - m - 900_000_000)) <= 8      # half a step of fp32 there
+    assert (dnll[:7] == 0).all() and (dnll[7:T - m] != 0).any()
+    ctx.preference_loss(nll, ref, target, starts, 0.1, 0.0, 0.0, True, pair, reward, dloss[:3], dnll)
+    R = (small[2].double() - small[0].double()) * (small[3] >= 0)
+    n = (small[3][2000:m - 1] >= 0).sum()
+    assert reward[2, 0].item() == pytest.approx(0.1 * (R[2000:m - 1].sum() / n).item(), rel=1e-4, abs=1e-7) and reward[2, 1] == 0
+    assert (dnll[T - m + 2000:T - 1][small[3][2000:m - 1] < 0] == 0).all() and (dnll[T - m + 2000:T - 1][small[3][2000:m - 1] >= 0] != 0).all()
+
+
 def test_bad_starts_are_reported_and_harmless():
     r = np.random.default_rng(2)
     for T in (300, 30000):
