@@ -23,6 +23,8 @@
 
 #include <stddef.h>
 
+#include "seq_index.h"
+
 namespace mhcl {
 
 enum SeqOp { SEQ_POLICY = 0, SEQ_PAIR = 1 };
@@ -253,11 +255,12 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
     const uint64_t once = seq_once();
     constexpr int STAGE = seq_stage(OP, REF, EACH);
     const bool pairs = ((uintptr_t)a.target & 15) == 0;           // targets need not lie on 16 bytes
-    auto fetch = [&](int base, int slot) {
-        if (base < hi) {
+    auto fetch = [&](int from, int ahead, int slot) {
+        if (seq_before(from, ahead, hi)) {
+            const int base = from + ahead;
             const uint32_t to = ring + slot * STAGE + lane * 16;
             const int t = base + lane * 4;
-            if (base + kSeqStep <= a.T) {                         // the usual case
+            if (seq_whole(base, kSeqStep, a.T)) {                 // the usual case
                 if (pairs) {
                     seq_copy16(to + lane * 16, a.target + t, once);
                     seq_copy16(to + lane * 16 + 16, a.target + t + 2, once);
@@ -283,7 +286,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
         cp_async_commit();
     };
 #pragma unroll
-    for (int i = 0; i < (STAGES > 1 ? STAGES - 1 : 1); ++i) fetch(lo + i * kSeqStep, i);
+    for (int i = 0; i < (STAGES > 1 ? STAGES - 1 : 1); ++i) fetch(lo, i * kSeqStep, i);
     SeqWalk k;
     SeqSide z;
     float slope = 0.f, kl_slope = 0.f;
@@ -315,14 +318,14 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
         const uint32_t at = ring + slot * STAGE;
         const uint4 u = lds128(at + lane * 32), v = lds128(at + lane * 32 + 16);         // the halves with the sign
         uint32_t mine = ~(u.y >> 31 | u.w >> 31 << 1 | v.y >> 31 << 2 | v.w >> 31 << 3) & 15u;
-        if (base + kSeqStep > a.T) mine &= seq_within(t, 0, a.T);       // behind the last token there is nothing
+        if (!seq_whole(base, kSeqStep, a.T)) mine &= seq_within(t, 0, a.T);       // behind the last token there is nothing
         Quad nll = {0, 0}, old = {0, 0}, ref = {0, 0}, adv = {0, 0};
         nll = seq_read(at + 1024 + lane * 16);
         if (OP == SEQ_POLICY) old = seq_read(at + 1536 + lane * 16);
         if (REF) ref = seq_read(at + 512 * (3 + (OP == SEQ_POLICY)) + lane * 16);
         if (EACH) adv = seq_read(at + STAGE - 512 + lane * 16);
         if (STAGES > 1) {                                         // into the slot of the step before
-            fetch(base + (STAGES - 1) * kSeqStep, slot == 0 ? STAGES - 1 : slot - 1);
+            fetch(base, (STAGES - 1) * kSeqStep, slot == 0 ? STAGES - 1 : slot - 1);
             slot = slot + 1 == STAGES ? 0 : slot + 1;
         }
         const bool none = !__any_sync(0xffffffffu, mine), whole = __all_sync(0xffffffffu, mine == 15u);
@@ -680,7 +683,7 @@ __device__ __forceinline__ void seq_scale_load(const SeqArgs& a, int base, float
     const int t = base + (threadIdx.x & 31) * 4;
     if (OP == SEQ_PAIR) {
         mine = a.bits[t / 4];
-    } else if (base + kSeqStep <= a.T) {
+    } else if (seq_whole(base, kSeqStep, a.T)) {
         raw = *reinterpret_cast<const float4*>(a.raw + t);
     } else {
         raw = make_float4(t < a.T ? a.raw[t] : 0.f, t + 1 < a.T ? a.raw[t + 1] : 0.f, t + 2 < a.T ? a.raw[t + 2] : 0.f, 0.f);
@@ -697,11 +700,11 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, uint32_t ids)
     const int first = a.hint[w];
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i)
-        if (lo + i * kSeqStep < hi) seq_scale_load<OP>(a, lo + i * kSeqStep, v[i], mine[i]);
+        if (seq_before(lo, i * kSeqStep, hi)) seq_scale_load<OP>(a, lo + i * kSeqStep, v[i], mine[i]);
     pdl_wait();
     SeqWalk k;
     k.enter(a, first, lo, a.coef, nullptr);
-    if (k.next >= hi && lo + kScaleRange <= a.T && k.v0 - k.v0 == 0.f) {               // the usual case: one sequence, or none (then v0 is 0)
+    if (k.next >= hi && seq_whole(lo, kScaleRange, a.T) && k.v0 - k.v0 == 0.f) {               // the usual case: one sequence, or none (then v0 is 0)
 #pragma unroll
         for (int i = 0; i < kScaleSteps; ++i) {
             float4* to = reinterpret_cast<float4*>(a.dnll + lo + i * kSeqStep) + lane;
@@ -713,12 +716,12 @@ __device__ __forceinline__ void seq_scale(const SeqArgs& a, int w, uint32_t ids)
     if (seq_dense(k, lo, hi)) {
 #pragma unroll
         for (int i = 0; i < kScaleSteps; ++i)
-            if (lo + i * kSeqStep < hi) seq_scale_step<OP, true>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
+            if (seq_before(lo, i * kSeqStep, hi)) seq_scale_step<OP, true>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
         return;
     }
 #pragma unroll
     for (int i = 0; i < kScaleSteps; ++i)
-        if (lo + i * kSeqStep < hi) seq_scale_step<OP, false>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
+        if (seq_before(lo, i * kSeqStep, hi)) seq_scale_step<OP, false>(a, k, lo + i * kSeqStep, hi, v[i], mine[i], ids);
 }
 __device__ __forceinline__ int seq_scale_warps(const SeqArgs& a) { return (a.T - 1) / kScaleRange + 1; }      // T > 0
 

@@ -2,6 +2,7 @@
 import ctypes
 import os
 import re
+import subprocess
 
 import pytest
 import torch
@@ -78,3 +79,25 @@ def test_included_kernels_do_not_read_by_the_read_only_path():
             for word in ("__ldg", "__ldcg", ".nc.", "ld_stream(", "__restrict__"):
                 assert word not in src.replace("ld_dep_stream(", ""), (name, word)
     assert seen >= 1
+
+
+def test_token_indices_up_to_the_largest_count(tmp_path):
+    """T may be 2^31 - 257, so a walk looks for tokens whose index no 32-bit number holds.  In a constant expression a signed
+    overflow is an error of the compiler's: the questions asked of indices are asked here for the steps next to the end, with the
+    answers of Python's unbounded integers."""
+    csrc = os.path.join(os.path.dirname(binding.__file__), "csrc")
+    lines = []
+    for T in (1, 127, 128, 129, 2**31 - 641, 2**31 - 512, 2**31 - 511, 2**31 - 384, 2**31 - 383, 2**31 - 257):
+        for base in range((T - 1) // 128 * 128, -1, -128)[:6]:
+            for n in (0, 128, 256, 384, 512):
+                yes = ("!", "")
+                lines.append(f"static_assert({yes[base + n < T]}mhcl::seq_before({base}, {n}, {T}), \"\");")
+                lines.append(f"static_assert({yes[base + n <= T]}mhcl::seq_whole({base}, {n}, {T}), \"\");")
+    src = tmp_path / "index.cpp"
+    src.write_text('#include "seq_index.h"\n' + "\n".join(lines) + "\n")
+    r = subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-fsyntax-only", f"-I{csrc}", str(src)], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[:2000]
+    # and the kernels ask them so: no sum of an index and steps is compared with the end
+    kernels = re.sub(r"//[^\n]*", "", open(os.path.join(csrc, "seq_losses.cuh")).read())
+    assert not re.findall(r"\+ [\w *()-]*k(?:SeqStep|ScaleRange)\)* *[<>]=? *(?:a\.T|hi)\b", kernels)
+    assert kernels.count("seq_before(") >= 4 and kernels.count("seq_whole(") >= 4
