@@ -431,7 +431,7 @@ MHCLITE_API int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t 
  *     them (NaN included), and their dnll is 0.
  *   - mean != 0: the sum over a sequence's tokens that count is divided by their number (0 where there are none).
  *   - dloss (dL/dloss) and dnll [T] are given both or neither; one call gives losses and gradient.
- *   - T == 0: the losses are those of empty sequences.  S < 2^30.  All but target and starts are f32.
+ *   - T == 0: the losses are those of empty sequences; what there is one of for each token, and adv, may be NULL.  S < 2^30.  All but target and starts are f32.
  *
  * Clipped policy loss with a KL term.  x = nll_old - nll, r = exp(x), A = adv[s] (or adv[t] when token_adv != 0):
  *   pg[t] = max(-A r, -A min(max(r, 1 - clip_low), 1 + clip_high)),   d = nll - nll_ref,   kl[t] = exp(d) - d - 1

@@ -784,7 +784,8 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
         if (CLUSTER) return;
         const int i = threadIdx.x;                                // at most 511 sequences, 512 threads
         const int64_t start = i <= a.S ? args.starts[i] : 0;
-        const float adv = OP == SEQ_POLICY && !EACH && i < a.S ? args.adv[i] : 0.f, dloss = a.dnll && i < items ? args.dloss[i] : 0.f;
+        // without tokens the advantages are not looked at, and need not be there
+        const float adv = OP == SEQ_POLICY && !EACH && a.T > 0 && i < a.S ? args.adv[i] : 0.f, dloss = a.dnll && i < items ? args.dloss[i] : 0.f;
         if (i <= a.S) sh->starts[i] = start;
         if (i < a.S) { sh->adv[i] = adv; sh->dloss[i] = dloss; }
         a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;

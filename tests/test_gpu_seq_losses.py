@@ -381,6 +381,24 @@ def test_no_tokens_and_no_sequences(ctx):
     assert ctx.kernel_launches() == before
 
 
+@pytest.mark.parametrize("n", [1, 4, 510, 512, 40000])
+def test_no_tokens_and_none_of_their_tensors(ctx, n):
+    """Through the C entries, which take NULL for what no token asks for: one block, the cluster and the launches of many."""
+    lib, ws = ctx.lib, torch.empty(max(1, ctx.lib.mhclite_policy_scratch_bytes(0, n)), dtype=torch.uint8, device=DEV)
+    starts, loss, stats, reward = torch.zeros(n + 1, dtype=torch.int64, device=DEV), empty(n), empty(n, 3), empty(n // 2, 2)
+    torch.cuda.synchronize()
+    for each in (0, 1):
+        for ptr in (loss, stats):
+            ptr.fill_(float("nan"))
+        assert lib.mhclite_policy_loss(ctx._h, 0, n, None, None, None, None, starts.data_ptr(), None, each, 0.2, 0.2, 0.1, 1, None, loss.data_ptr(),
+                                       stats.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == binding.OK
+        assert (loss == 0).all() and (stats == 0).all()
+    if n > 1:
+        assert lib.mhclite_preference_loss(ctx._h, 0, n // 2, None, None, None, starts.data_ptr(), 0.1, 0.0, 0.0, 1, None, loss.data_ptr(),
+                                           reward.data_ptr(), None, ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream) == binding.OK
+        assert (reward == 0).all() and torch.allclose(loss[: n // 2], torch.full_like(loss[: n // 2], float(np.log(2.0))))
+
+
 def test_refusals(ctx):
     k = Case(100, 4)
     t = k.tensors()
