@@ -404,7 +404,9 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
                     }
                     g[i] = there ? grad : g[i];
                 }
-                pa *= EACH ? -1.f : -z.adv;
+                // a lane without tokens here takes no advantage either: it need not be finite
+                if (EACH) pa = -pa;
+                else pa = all || in ? pa * -z.adv : 0.f;
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pa += all || (in >> i & 1u) ? x[i] : 0.f;

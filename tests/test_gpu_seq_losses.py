@@ -219,6 +219,21 @@ def test_small_and_large_divergences(ctx, T):
     check_policy(ctx, k, True)
 
 
+@pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("T,S_", [(900, 12), (900, 200), (20000, 12), (20000, 3000), (50000, 12), (50000, 9000), (700001, 60)])
+def test_advantages_that_no_token_takes_may_be_anything(ctx, T, S_, value):
+    """A group of one answer normalised by its deviation has 0/0 for an advantage; an answer of which no token counts has no part
+    in anything.  At every way of adding up: one block, the cluster, many launches, with few and many ends in a step."""
+    k = Case(T, S_, dead=0.3)
+    for s in range(2, S_, 5):
+        k.target[k.starts[s]:k.starts[s + 1]] = -100
+        k.adv[s] = value
+    each = Case(T, S_, token_adv=True, dead=0.3)
+    each.adv[each.target < 0] = value
+    for mean in (False, True):
+        assert all(torch.isfinite(o).all() for c in (k, each) for o in check_policy(ctx, c, mean))
+
+
 @pytest.mark.parametrize("T,S_", [(900, 6), (50000, 20)])
 def test_tokens_that_do_not_count_may_hold_anything(ctx, T, S_):
     k = Case(T, S_, dead=0.5)
