@@ -397,7 +397,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
                     const float term = EACH ? z.adv * (cut[i] ? z.held : v[i]) : cut[i] ? z.held : v[i];
                     if (cut[i] && there) ++sc;
                     pa += there ? term : 0.f;
-                    float grad = (cut[i] ? 0.f : v[i]) * (z.adv * slope);
+                    float grad = cut[i] ? 0.f : v[i] * (z.adv * slope);
                     if (REF) {
                         pb += there ? y[i] : 0.f;
                         grad = fmaf(kl_slope, d[i], grad);
@@ -455,7 +455,7 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
                     bool cut = o > 0.f;
                     if (there && fabsf(o) <= z.close)
                         cut = ((double)a.old[t + i] - (double)a.nll[t + i]) * (double)z.sign > (z.side ? a.edge[1] : a.edge[0]);
-                    float grad = (cut ? 0.f : v[i]) * (z.adv * by);
+                    float grad = cut ? 0.f : v[i] * (z.adv * by);
                     if (REF) grad = fmaf(a.kl_slope * by, d[i], grad);
                     if (there) {
                         ra -= z.adv * (cut ? z.held : v[i]);

@@ -234,6 +234,42 @@ def test_advantages_that_no_token_takes_may_be_anything(ctx, T, S_, value):
         assert all(torch.isfinite(o).all() for c in (k, each) for o in check_policy(ctx, c, mean))
 
 
+def give_advantages(k, values):
+    """To single tokens, or to whole sequences; a quarter of the sequences and more stay as they are."""
+    for i, v in enumerate(values):
+        if k.token_adv:
+            k.adv[(np.searchsorted(k.starts, np.arange(k.T), side="right") % 4 == i) & (np.arange(k.T) % 5 == 0)] = v
+        else:
+            k.adv[i + 1::9] = v
+
+
+def same_where_not_finite(c, k, mean):
+    """Losses, counts and gradients as the oracle has them, infinities and NaN in the same places; returns the oracle's."""
+    loss, stats, dnll = (f64(o) for o in run_policy(c, k, k.tensors(), mean))
+    with np.errstate(invalid="ignore", over="ignore"):
+        rl, rs, rd = S.policy_loss(k.nll, k.old, k.ref, k.target, k.starts, k.adv, k.token_adv, 0.2, 0.3, 0.1, mean, k.dloss)
+    assert np.array_equal(stats[:, :2], rs[:, :2]) and np.isfinite(stats).all()
+    for got, ref in ((loss, rl), (dnll, rd)):
+        assert np.array_equal(np.isnan(got), np.isnan(ref))
+        assert np.array_equal(np.where(np.isinf(got), got, 0), np.where(np.isinf(ref), ref, 0))
+    return rl, rs, rd
+
+
+WAYS = [(900, 12), (900, 200), (20000, 12), (20000, 3000), (50000, 12), (50000, 9000), (700001, 60)]     # T, S: each way of adding up
+
+
+@pytest.mark.parametrize("T,S_", WAYS)
+@pytest.mark.parametrize("mean,token_adv", list(itertools.product([False, True], repeat=2)))
+def test_infinite_advantages(ctx, T, S_, mean, token_adv):
+    """Infinities where the formula has them and nowhere else, and no NaN: a clipped token's gradient is 0 under an infinite
+    advantage too."""
+    k = Case(T, S_, token_adv=token_adv, dead=0.3)
+    give_advantages(k, (np.inf, -np.inf))
+    rl, rs, rd = same_where_not_finite(ctx, k, mean)
+    live = (k.target >= 0) & np.isinf(k.adv if token_adv else k.adv[np.clip(np.searchsorted(k.starts, np.arange(T), side="right") - 1, 0, S_ - 1)])
+    assert np.isinf(rl).any() and np.isfinite(rl).any() and np.isinf(rd).any() and not np.isnan(rd).any() and np.isfinite(rd[live]).any()
+
+
 @pytest.mark.parametrize("T,S_", [(900, 6), (50000, 20)])
 def test_tokens_that_do_not_count_may_hold_anything(ctx, T, S_):
     k = Case(T, S_, dead=0.5)
