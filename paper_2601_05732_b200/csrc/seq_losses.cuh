@@ -233,7 +233,7 @@ __device__ __forceinline__ uint64_t exp_series(uint64_t d) {
     return mul2(mul2(d, d), h);
 }
 
-// What the border on an advantage's side asks for (none where it is 0).
+// What the border on an advantage's side asks for (none where it is 0 or NaN: then neither term is the larger).
 struct SeqSide {
     float adv, sign, held, edge, close;
     int side;
@@ -242,8 +242,9 @@ struct SeqSide {
         side = x < 0.f;
         sign = side ? -1.f : 1.f;
         held = side ? a.held[1] : a.held[0];
-        edge = x != 0.f ? (side ? a.edge32[1] : a.edge32[0]) : INFINITY;
-        close = x != 0.f ? (side ? a.close[1] : a.close[0]) : -1.f;
+        const bool there = fabsf(x) > 0.f;
+        edge = there ? (side ? a.edge32[1] : a.edge32[0]) : INFINITY;
+        close = there ? (side ? a.close[1] : a.close[0]) : -1.f;
     }
 };
 // `ready` is called between the first copies and the first look at the starts; `first` is where the walk begins.

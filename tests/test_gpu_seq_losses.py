@@ -270,6 +270,17 @@ def test_infinite_advantages(ctx, T, S_, mean, token_adv):
     assert np.isinf(rl).any() and np.isfinite(rl).any() and np.isinf(rd).any() and not np.isnan(rd).any() and np.isfinite(rd[live]).any()
 
 
+@pytest.mark.parametrize("T,S_", WAYS)
+@pytest.mark.parametrize("mean,token_adv", list(itertools.product([False, True], repeat=2)))
+def test_nan_advantages(ctx, T, S_, mean, token_adv):
+    """NaN stays with the tokens whose advantage it is, and their sequences; next to it no term is the larger, so no token of
+    theirs counts as clipped."""
+    k = Case(T, S_, token_adv=token_adv, dead=0.3)
+    give_advantages(k, (np.nan,))
+    rl, rs, rd = same_where_not_finite(ctx, k, mean)
+    assert np.isnan(rl).any() and np.isfinite(rl).any() and np.isnan(rd).any() and not np.isinf(rd).any()
+
+
 @pytest.mark.parametrize("T,S_", [(900, 6), (50000, 20)])
 def test_tokens_that_do_not_count_may_hold_anything(ctx, T, S_):
     k = Case(T, S_, dead=0.5)
