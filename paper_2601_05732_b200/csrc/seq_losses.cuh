@@ -215,14 +215,16 @@ __device__ __forceinline__ bool seq_ids(const SeqArgs& a, int s, int base, int s
     return !more;
 }
 
-// e^q: q log2 e with the part of it that fp32 leaves out, so that only ex2's 2^-22 and two roundings are left of the error.
+// e^q: q log2 e with the part of it that fp32 leaves out, so that only ex2's 2^-22 and two roundings are left of the error.  Where
+// the result is neither 0 nor infinite that part is below 2^-17; of a large q it is anything (of an infinite one NaN), and 1 + it
+// must stay above 0: it is held within 0.01.
 __device__ __forceinline__ uint64_t exp_pair(uint64_t q) {
     const float low = (float)(1.4426950408889634 - (double)kLog2e);
     const uint64_t l = pack2f(kLog2e, kLog2e), n = pack2f(kLn2, kLn2), one = pack2f(1.f, 1.f);
     const uint64_t t = mul2(q, l), minus = mul2(t, pack2f(-1.f, -1.f));
     float a, b;
     unpack2f(mul2(fma2(q, pack2f(low, low), fma2(q, l, minus)), n), a, b);
-    return mul2(ex2_pair(t), add2(one, pack2f(fminf(a, 0.01f), fminf(b, 0.01f))));      // of an infinite q the rest is NaN: it goes
+    return mul2(ex2_pair(t), add2(one, pack2f(fmaxf(fminf(a, 0.01f), -0.01f), fmaxf(fminf(b, 0.01f), -0.01f))));
 }
 // e^d - 1 - d by its series: for |d| < 1 the terms from d^12 / 12! on are below 2^-28 of it.
 __device__ __forceinline__ uint64_t exp_series(uint64_t d) {

@@ -281,6 +281,23 @@ def test_nan_advantages(ctx, T, S_, mean, token_adv):
     assert np.isnan(rl).any() and np.isfinite(rl).any() and np.isnan(rd).any() and not np.isinf(rd).any()
 
 
+@pytest.mark.parametrize("T,S_", WAYS)
+@pytest.mark.parametrize("mean,token_adv", list(itertools.product([False, True], repeat=2)))
+def test_log_ratios_of_any_size(ctx, T, S_, mean, token_adv):
+    """Finite log ratios from 1e7 to the largest fp32, as masked log probabilities of -1e9 or -1e30 make them: ratios of infinity
+    and 0, never below 0."""
+    k, r = Case(T, S_, token_adv=token_adv, dead=0.3), np.random.default_rng(T)
+    f = lambda a: a.astype(np.float32).astype(np.float64)
+    far = (np.searchsorted(k.starts, np.arange(T), side="right") % 3 == 0) & (r.random(T) < 0.1)
+    x = np.where(r.random(T) < 0.5, np.exp(r.uniform(np.log(1e7), np.log(1e11), T)), r.choice([1e8, 1e9, 1e10, 1e30, 3e38, np.finfo(np.float32).max], T))
+    up = far & (r.random(T) < 0.7)
+    k.old, k.nll = f(np.where(up, x, k.old)), f(np.where(far & ~up, x, k.nll))
+    k.old, k.ref = np.where(far & ~up, 1.0, k.old), np.where(far & ~up, k.nll, k.ref)
+    rl, rs, rd = same_where_not_finite(ctx, k, mean)
+    assert np.isposinf(rl).any() and not np.isneginf(rl).any() and np.isfinite(rl).any() and np.isinf(rd).any()
+    assert (run_policy(ctx, k, k.tensors(), mean)[2][torch.from_numpy(far & ~up).to(DEV)] == 0).all()
+
+
 @pytest.mark.parametrize("T,S_", [(900, 6), (50000, 20)])
 def test_tokens_that_do_not_count_may_hold_anything(ctx, T, S_):
     k = Case(T, S_, dead=0.5)
