@@ -298,6 +298,18 @@ def test_log_ratios_of_any_size(ctx, T, S_, mean, token_adv):
     assert (run_policy(ctx, k, k.tensors(), mean)[2][torch.from_numpy(far & ~up).to(DEV)] == 0).all()
 
 
+@pytest.mark.parametrize("T", [310_000, 700_003, 1_300_001])
+@pytest.mark.parametrize("ref,token_adv", [(False, False), (False, True), (True, True)])
+def test_several_steps_a_warp(ctx, T, ref, token_adv):
+    """Ranges of several steps, which go round the ring in shared memory: every set of tensors in it, targets on 16 bytes and on 8."""
+    k = Case(T, 46, "empties" if T == 700_003 else "even", ref=ref, token_adv=token_adv)
+    t = k.tensors()
+    shifted = {**t, "target": inside(t["target"])}
+    for mean in (False, True):
+        for check, run in ((check_policy, run_policy), (check_pair, run_pair)):
+            assert all(torch.equal(a, b) for a, b in zip(check(ctx, k, mean, t=t), run(ctx, k, shifted, mean)))
+
+
 @pytest.mark.parametrize("T,S_", [(900, 6), (50000, 20)])
 def test_tokens_that_do_not_count_may_hold_anything(ctx, T, S_):
     k = Case(T, S_, dead=0.5)
@@ -616,6 +628,42 @@ def test_inputs_that_another_stream_writes(ctx):
 
 
 # ---- model steps that end in these losses ---------------------------------------------------------------------------------
+def test_the_last_step_of_a_model_against_the_oracle():
+    """From the token losses that model_fwd leaves, policy_loss and preference_loss are the oracle's at the tolerances of fp32, and
+    so are the gradients that model_bwd takes; the token losses are those of a plain restatement of the head on the activations
+    that the library left."""
+    n, C, T, V = 4, 64, 150, 300
+    c, r = binding.MhcLite(n, C, 0), np.random.default_rng(3)
+    mk = lambda *s, std=1.0, mean=0.0: (r.normal(size=s) * std + mean).astype(np.float32)
+    Ps = [L.LayerParams(mk(n * C, 32, std=0.02), mk(32, std=0.1), np.full(3, 0.5, np.float32), mk(n * C, std=0.1, mean=1.0), DEV)]
+    Bs = [L.LayerBuffers(c, T)]
+    M = L.ModelEnds(c, T, dev(mk(V, C, std=0.5)), 1.3, dev(mk(C, std=0.1, mean=1.0)), dev(mk(V, C, std=0.3), BF), 1.0)
+    k = Case(T, 6)
+    k.starts = np.array([0, 40, 40, 77, 120, 131, 148])
+    target, ids = torch.from_numpy(np.where(k.target < 0, -100, k.target % V)).to(DEV), dev(r.integers(0, V, T), torch.int64)
+    k.target = target.cpu().numpy()
+    nll = L.model_fwd(c, M, Ps, Bs, ids, target, lambda l, u: torch.tanh(u.float()).to(BF))
+    # the logits from h as the library left it: 64 products, a sum over 300 words, a logarithm, each of fp32
+    x = M.h.double() @ M.W.double().T
+    want = (torch.logsumexp(x, 1) - x.gather(1, target.clamp(min=0)[:, None])[:, 0]) * (target >= 0)
+    size = (M.h.double().abs() @ M.W.double().abs().T).amax(1)
+    assert ((nll.double() - want).abs() <= 2 * (C / 16 + 4) * 2.0 ** -23 * size + (V / 256 + 64) * U + 2.0 ** -20 * (1 + want.abs())).all()
+    # and h from the streams: their mean, its norm, both rounded to bf16 (2^-8 each, and as much of the norm's sum)
+    top = M.x_top.double().mean(1)
+    h = top * torch.rsqrt(top.pow(2).mean(1, keepdim=True) + 1e-6) * M.w.double()
+    assert ((M.h.double() - h).abs() <= 3 * 2.0 ** -8 * (h.abs() + h.abs().mean())).all()
+    k.nll = f64(nll)
+    k.old, k.ref = ((k.nll + s * r.normal(size=T)).astype(np.float32).astype(np.float64) for s in (0.3, 0.4))
+    t = {**k.tensors(), "target": target}
+    A = L.Answers(t["starts"], T)
+    L.policy_loss(c, A, nll, t["old"], t["ref"], target, t["adv"], t["dloss"], clip_low=0.2, clip_high=0.3, kl_weight=0.1)
+    assert all(torch.equal(a, b) for a, b in zip((A.loss, A.stats, A.dnll), check_policy(c, k, True, t=t)))
+    B = L.Answers(t["starts"], T, pairs=True)
+    L.preference_loss(c, B, nll, t["ref"], target, t["dpair"], beta=0.3, margin=0.2, smoothing=0.1)
+    assert all(torch.equal(a, b) for a, b in zip((B.loss, B.reward, B.dnll), check_pair(c, k, False, t=t)))
+    c.device_status()
+
+
 @pytest.mark.parametrize("kind", ["distill", "policy", "preference"])
 def test_model_step_and_its_gradients_against_differences(kind):
     """ids -> loss through two mixing layers, and back.  The activations between the calls are bf16, so a difference of two
