@@ -148,6 +148,19 @@ def test_nan_in_a_present_entry_stays_in_its_row(ctx_of, T):
     assert torch.isfinite(lse).all() and torch.isfinite(logp).all()
 
 
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("bf,tau", [(False, 0.5), (False, 2.0), (True, 0.5)])
+def test_masks_of_the_lowest_value(ctx_of, T, bf, tau):
+    """Teacher logits masked with the type's lowest value instead of -inf: weights of 0, equal ones where a row has no others, and
+    a largest value next to which all others vanish."""
+    h, W, ids, z, dloss = case(T, 40, 64, 700, bf, absent=0.2)
+    lowest = torch.finfo(z.dtype).min
+    z[torch.rand(T, 40, generator=torch.Generator().manual_seed(1)).to(DEV) < 0.4] = lowest
+    z[3], z[5, 2:], z[6, 7] = lowest, lowest, -lowest
+    out = check(ctx_of(64), h, W, ids, z, 1.0, tau, dloss)
+    assert all(torch.isfinite(o).all() for o in out)
+
+
 @pytest.mark.parametrize("T", [1, 200])
 def test_no_row_has_a_teacher(ctx_of, T):
     h, W, ids, z, dloss = case(T, 5, 64, 300)
