@@ -328,6 +328,8 @@ int mhclite_policy_loss(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll
     if (T > 0) {
         MHCL_PTR(ctx, nll_old); MHCL_OPT_PTR(ctx, nll_ref); MHCL_PTR(ctx, adv);
         MHCL_NO_ALIAS(ctx, loss, adv); MHCL_NO_ALIAS(ctx, stats, adv);
+        MHCL_NO_ALIAS(ctx, loss, nll_old); MHCL_NO_ALIAS(ctx, stats, nll_old);
+        if (nll_ref) { MHCL_NO_ALIAS(ctx, loss, nll_ref); MHCL_NO_ALIAS(ctx, stats, nll_ref); }
         if (dnll) { MHCL_NO_ALIAS(ctx, dnll, nll_old); MHCL_NO_ALIAS(ctx, dnll, nll_ref); MHCL_NO_ALIAS(ctx, dnll, adv); }
     }
     if ((rc = check_scratch(ctx, scratch, scratch_bytes, seq_scratch_bytes(T, S)))) return rc;
@@ -350,6 +352,7 @@ int mhclite_preference_loss(mhclite_ctx* ctx, int64_t T, int64_t P, const float*
     if (P == 0) return no_sequences(ctx, T, dnll, stream);
     if (T > 0) {
         MHCL_OPT_PTR(ctx, nll_ref);
+        if (nll_ref) { MHCL_NO_ALIAS(ctx, loss, nll_ref); MHCL_NO_ALIAS(ctx, reward, nll_ref); }
         if (dnll) MHCL_NO_ALIAS(ctx, dnll, nll_ref);
     }
     if ((rc = check_scratch(ctx, scratch, scratch_bytes, seq_scratch_bytes(T, 2 * P)))) return rc;

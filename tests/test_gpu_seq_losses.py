@@ -532,6 +532,26 @@ def test_refusals(ctx):
     check_policy(ctx, k, True)                                           # a refused call leaves the context usable
 
 
+def test_losses_and_statistics_in_place_of_token_losses_are_refused(ctx):
+    k = Case(60, 60, "ones")                                             # as many sequences as tokens, so that the shapes fit
+    t, loss, stats, reward = k.tensors(), empty(60), empty(60, 3), empty(30, 2)
+    tail = (t["target"], t["starts"], t["adv"], False, 0.2, 0.2, 0.1, True)
+    for out in (t["nll"], t["old"], t["ref"]):
+        with pytest.raises(binding.MhcLiteError, match="alias"):
+            ctx.policy_loss(t["nll"], t["old"], t["ref"], *tail, out, stats)
+    long = torch.zeros(180, device=DEV)                                  # 180 floats: statistics, or the first tokens' losses
+    for i in range(3):
+        with pytest.raises(binding.MhcLiteError, match="alias"):
+            ctx.policy_loss(*(long[:60] if j == i else t[n] for j, n in enumerate(("nll", "old", "ref"))), *tail, loss, long.view(60, 3))
+    for out in (t["nll"][:30], t["ref"][:30]):
+        with pytest.raises(binding.MhcLiteError, match="alias"):
+            ctx.preference_loss(t["nll"], t["ref"], t["target"], t["starts"], 0.1, 0.0, 0.0, False, out, reward)
+    for out in (t["nll"].view(30, 2), t["ref"].view(30, 2)):
+        with pytest.raises(binding.MhcLiteError, match="alias"):
+            ctx.preference_loss(t["nll"], t["ref"], t["target"], t["starts"], 0.1, 0.0, 0.0, False, loss[:30], out)
+    check_policy(ctx, k, True), check_pair(ctx, k, True)
+
+
 def inside(t):
     """The same values in a view 16 bytes (one element, for int64: 8) into a buffer: the least alignment the calls allow."""
     if t is None:
