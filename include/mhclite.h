@@ -439,7 +439,8 @@ MHCLITE_API int mhclite_linear_distill_bwd(mhclite_ctx* ctx, int64_t T, int64_t 
  *   stats[s] = (tokens that count, those where the clipped term is the larger, sum (or mean) of kl)      [S,3]
  *   dnll[t] = dloss[s] (/ tokens) ((0 where the clipped term is the larger, else A r) + kl_weight (exp(d) - 1))
  * nll_ref may be NULL: no KL term.  0 <= clip_low <= 1, clip_high >= 0 (infinity: no upper border).  Which side of a border a
- * ratio is on is decided in 64 bits. */
+ * ratio is on is decided in 64 bits; ratios are fp32, infinite for log ratios above some 87, finite or not.  adv[s] of a sequence
+ * without a token that counts, and adv[t] of a token that does not, may be anything (NaN included). */
 MHCLITE_API size_t mhclite_policy_scratch_bytes(int64_t T, int64_t S);
 MHCLITE_API int mhclite_policy_loss(mhclite_ctx* ctx, int64_t T, int64_t S, const float* nll, const float* nll_old, const float* nll_ref,
                         const int64_t* target, const int64_t* starts, const float* adv, int token_adv, double clip_low, double clip_high,

@@ -17,8 +17,8 @@
 // Sums: four tokens in fp32, from there in 64 bits.
 //
 // What bounds it: HBM for large batches, 24 bytes a token with reference and gradient (16.8 M tokens, 2048 sequences, on one B200: the
-// sums 73 us at 5.5 TB/s, the join 6, the last pass 18 within L2; 98 for the call), start and drain in between (8.4 M tokens
-// of 4096 pairs 37 us for 134 MB), and the latency of dependent phases below some 500 000 tokens (8 to 10 us).
+// sums 73 us at 5.5 TB/s, the join 5, the last pass 18 within L2; 98 for the call), start and drain in between (8.4 M tokens
+// of 4096 pairs 37 us for 134 MB), and the latency of dependent phases below some 500 000 tokens (9 to 10 us).
 #pragma once
 
 #include <stddef.h>
@@ -226,7 +226,7 @@ __device__ __forceinline__ uint64_t exp_pair(uint64_t q) {
     unpack2f(mul2(fma2(q, pack2f(low, low), fma2(q, l, minus)), n), a, b);
     return mul2(ex2_pair(t), add2(one, pack2f(fmaxf(fminf(a, 0.01f), -0.01f), fmaxf(fminf(b, 0.01f), -0.01f))));
 }
-// e^d - 1 - d by its series: for |d| < 1 the terms from d^12 / 12! on are below 2^-28 of it.
+// e^d - 1 - d by its series: for |d| < 1 the terms from d^12 / 12! on are below 2^-27 of it (5.3e-9 towards d = -1).
 __device__ __forceinline__ uint64_t exp_series(uint64_t d) {
     const float c[10] = {1.f / 39916800, 1.f / 3628800, 1.f / 362880, 1.f / 40320, 1.f / 5040, 1.f / 720, 1.f / 120, 1.f / 24, 1.f / 6, 1.f / 2};
     uint64_t h = pack2f(c[0], c[0]);
@@ -529,12 +529,13 @@ __device__ __forceinline__ void seq_sums(const SeqArgs& a, int w, uint32_t ring,
 
 // The range of token t.  Steps are below 2^24 and those of a range below 2^13, so the quotient by 2^40 is exact.
 __device__ __forceinline__ int seq_range_of(const SeqArgs& a, int t) { return (int)((uint64_t)(t / kSeqStep) * a.per_range >> 40); }
-// 1 / n to 2^-44, in a few instructions (a division in 64 bits takes some 400 cycles, and a join little else).
+// 1 / n to 2^-44 by one step of Newton's method, in a few instructions (a division in 64 bits takes some 400 cycles, and a join
+// little else).
 __device__ __forceinline__ double seq_share(int n) {
     if (n == 0) return 0.0;
     float f;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(f) : "f"((float)n));
-    const double w = f;                                           // to 2^-22: one step squares the error
+    const double w = f;                                           // to 2^-22: a step squares the error
     return w * (2.0 - (double)n * w);
 }
 // The sums of sequence s over a team of threads: half a warp, a warp or a block of 256.  Member 0 gets them.
@@ -794,7 +795,7 @@ __global__ void __launch_bounds__(512) seq_one_k(const SeqArgs args) {
         if (i <= a.S) sh->starts[i] = start;
         if (i < a.S) { sh->adv[i] = adv; sh->dloss[i] = dloss; }
         a.starts = sh->starts; a.whole = sh->whole; a.head = sh->head; a.tail = sh->tail; a.coef = sh->coef;
-        if (OP == SEQ_POLICY && !EACH) a.adv = sh->adv;
+        if (OP == SEQ_POLICY && !EACH) a.adv = sh->adv;           // for steps in which many sequences end: the walk has taken args.adv
         if (a.dnll) a.dloss = sh->dloss;
         if (scaled) a.raw = sh->raw;
         if (a.bits) a.bits = sh->bits;
